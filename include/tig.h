@@ -380,7 +380,8 @@ TIG_API int tig_state_import(tig_ctx *ctx, const float *mem_in, const double *la
 TIG_API void tig_destroy(tig_ctx *ctx);
 
 /* Static text for a status code / detail of the last failure on this context ("" if none);
- * tig_last_error(NULL) gives the detail of the last failed tig_init on the calling thread. */
+ * tig_last_error(NULL) gives the detail of the last failed tig_init, or of the last failed call that
+ * takes no context (tig_linear_*, tig_softmax_ce_*, tig_adamw_*), on the calling thread. */
 TIG_API const char *tig_strerror(int status);
 TIG_API const char *tig_last_error(const tig_ctx *ctx);
 
@@ -522,6 +523,141 @@ TIG_API int tig_pac_epoch(tig_pac_part *parts, int32_t n_parts, int64_t *steps_o
  */
 TIG_API int tig_pac_sync_shared(tig_ctx *const *ctxs, int32_t n_parts, const int32_t *const *local_ids,
                                 int64_t n_shared, int32_t mode);
+
+/* ------------------------------------------------------------------------------------------
+ * Operators of a trained head over embeddings: a dense layer, softmax cross entropy over a large
+ * vocabulary of candidates, and an AdamW step over many tensors.  Independent of any tig_ctx.
+ *   - all tensors are device memory of the current device, row-major with a row stride in ELEMENTS
+ *     (>= the row's length); any element-aligned address and stride is taken (rows that are 16-byte
+ *     aligned, with strides and lengths of whole 16-byte pieces, are read where they lie, others are
+ *     copied into the workspace first);
+ *   - sums, softmax statistics and optimiser arithmetic are fp32 (norms and means fp64) whatever the
+ *     tensors' type; a result is rounded once, to nearest even;
+ *   - calls only enqueue on hip_stream, allocate nothing and can be captured into a graph.  A
+ *     workspace belongs to one call until that call has finished: calls on different streams, and
+ *     captured graphs that may run at the same time, need workspaces of their own;
+ *   - a call that fails with an argument error has enqueued nothing.  Detail: tig_last_error(NULL).
+ * ------------------------------------------------------------------------------------------ */
+typedef enum tig_dtype { TIG_F32 = 0, TIG_BF16 = 1, TIG_F16 = 2 } tig_dtype;
+typedef enum tig_activation {
+    TIG_ACT_NONE = 0,
+    TIG_ACT_RELU = 1, /* relu'(0) = 0 */
+    TIG_ACT_GELU = 2, /* z (1 + erf(z / sqrt 2)) / 2 */
+    TIG_ACT_SILU = 3  /* z / (1 + exp(-z)) */
+} tig_activation;
+
+/* Dense layer:  z = x W^T + b,  y = act(z) + residual.
+ *   forward   reads x, w, bias, residual; writes y and, if wanted, z (kept for the backward pass)
+ *   backward  dz = dy * act'(z);  dx = dz W,  dw = dz^T x,  dbias = sum over rows of dz.  (The
+ *             residual's gradient is dy itself.)  dz is rounded to `dtype` for the two products;
+ *             dbias is summed before that rounding.  z is not read for TIG_ACT_NONE.
+ * All tensors have the type `dtype`.  rows may be 0 (forward: nothing; backward: dw and dbias are
+ * zero).  y may be residual; no other output may overlap another tensor of the call.
+ * Rows of x, z, dy and so on lie ld* elements apart. */
+typedef struct tig_linear {
+    uint32_t struct_size;
+    int32_t dtype;          /* tig_dtype */
+    int32_t activation;     /* tig_activation */
+    int32_t reserved;
+    int64_t rows;           /* 0 .. 2^31 - 1 */
+    int64_t in_dim, out_dim; /* 1 .. 2^20 */
+    const void *x;          /* [rows x in_dim] */
+    const void *w;          /* [out_dim x in_dim] */
+    const void *bias;       /* [out_dim] or NULL */
+    const void *residual;   /* [rows x out_dim] or NULL (forward) */
+    void *y;                /* [rows x out_dim] (forward) */
+    void *z;                /* [rows x out_dim]; forward: written, or NULL; backward: read */
+    const void *dy;         /* [rows x out_dim] (backward) */
+    void *dx, *dw, *dbias;  /* [rows x in_dim], [out_dim x in_dim], [out_dim]; NULL = not wanted (backward) */
+    int64_t ldx, ldw, ldr, ldy, ldz, lddy, lddx, lddw; /* 1 .. 2^22 */
+} tig_linear;
+
+/* Device bytes that the call needs as its workspace (256-byte aligned; 0: none).  Depends on the
+ * sizes, strides and addresses in `p`; of the outputs only whether they are NULL. */
+TIG_API int tig_linear_workspace_bytes(const tig_linear *p, int32_t backward, size_t *bytes);
+TIG_API int tig_linear_forward(const tig_linear *p, void *workspace, size_t workspace_bytes, void *hip_stream);
+TIG_API int tig_linear_backward(const tig_linear *p, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Softmax cross entropy of rows over a vocabulary of candidates, in pieces of the vocabulary; the
+ * logits are never kept.
+ *   l_iv = <x_i, w_v> + bias_v;  lse_i = log sum_v exp l_iv;  loss_i = lse_i - l_{i, label_i}
+ *   a row whose label is outside 0 .. vocab - 1 is ignored: loss_i = 0, no gradient, whatever x_i holds
+ *   s_i = scale / (number of rows that count), or scale * row_scale[i] if row_scale is given
+ *   gradients of sum_i s_i loss_i:  P_iv = s_i (exp(l_iv - lse_i) - [v == label_i]),
+ *       dx = P W,  dw = P^T x,  dbias = sum_i P
+ *   mean = sum of the loss_i that count / their number (0 if none counts)
+ * A candidate is masked by bias_v = -infinity: it gets no probability and its gradient is zero
+ * (w_v must be finite).  A row whose label is masked has loss +infinity and, where nothing is left,
+ * lse = -infinity; its gradient is P with the probabilities that are left.
+ * P is rounded to the type `dtype` for the two products (fp16: after scaling by 2^14, so that small
+ * probabilities stay), relative to the largest |s_i|. */
+typedef struct tig_softmax_ce {
+    uint32_t struct_size;
+    int32_t dtype;           /* tig_dtype of x, w, bias, dx, dw, dbias */
+    int64_t rows;            /* 0 .. 2^24 */
+    int64_t vocab;           /* 1 .. 2^31 - 1 */
+    int64_t dim;             /* 1 .. 2^16 */
+    const void *x;           /* [rows x dim] */
+    const void *w;           /* [vocab x dim] */
+    const void *bias;        /* [vocab] or NULL */
+    const int32_t *labels;   /* [rows] */
+    const float *row_scale;  /* [rows] or NULL: the mean */
+    float scale;             /* e.g. 1, or a loss scale */
+    int32_t reserved;
+    float *loss, *lse;       /* [rows]; may be NULL */
+    float *mean;             /* [1] or NULL */
+    void *dx, *dw, *dbias;   /* [rows x dim], [vocab x dim], [vocab]; NULL = not wanted */
+    int64_t ldx, ldw, lddx, lddw;
+} tig_softmax_ce;
+
+TIG_API int tig_softmax_ce_workspace_bytes(const tig_softmax_ce *p, size_t *bytes);
+TIG_API int tig_softmax_ce_run(const tig_softmax_ce *p, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* One AdamW step over many tensors:
+ *   norm = sqrt(sum over all tensors of (grad_scale g)^2);  c = grad_scale * min(1, max_norm / norm)
+ *          (max_norm 0: c = grad_scale, and no norm is formed)
+ *   g' = c g;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2
+ *   p  = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32, t = *step + 1, which the call writes back to *step.  With max_norm > 0 a norm that is not
+ * finite makes the call change nothing but *norm_out.
+ * State in 32 bits: m, v are fp32.  In 8 bits: m and sqrt(v) are held as e4m3 values (OCP, no
+ * infinities) times one power of two for every 256 adjacent elements of a tensor, the one that puts
+ * the largest magnitude into [128, 256).  A value between two e4m3 values goes up if its fraction of
+ * the step plus u reaches 1, u = fraction of ((i mod 256) * 0x6A09E667 + t * 0x9E3779B9) / 2^32 (its
+ * upper 24 bits), half a turn further for sqrt(v): over the steps as often up as the fraction says, so
+ * that a slow average does not stop at a value.  sqrt(v) > 0 is never held as 0. */
+typedef struct tig_adamw_tensor {
+    void *param;          /* [n], dtype */
+    const void *grad;     /* [n], dtype */
+    float *master;        /* [n] or NULL: then this is stepped, and param receives its rounded copy */
+    void *m, *v;          /* [n]: fp32, or one byte each */
+    float *m_scale, *v_scale; /* 8 bits: [(n + 255) / 256] each; else NULL */
+    int64_t n;            /* >= 0 */
+    int32_t dtype;        /* tig_dtype of param and grad */
+    float weight_decay;   /* >= 0 */
+} tig_adamw_tensor;
+
+typedef struct tig_adamw_config {
+    uint32_t struct_size;
+    int32_t state_bits;   /* 32 or 8, for all tensors */
+    double beta1, beta2;  /* [0, 1) */
+    double eps;           /* > 0 */
+    int64_t *step;        /* device [1]: steps made so far */
+} tig_adamw_config;
+
+typedef struct tig_adamw tig_adamw;
+
+TIG_API int tig_adamw_workspace_bytes(const tig_adamw_config *cfg, const tig_adamw_tensor *tensors, int64_t n_tensors, size_t *bytes);
+/* Lays the list of tensors out in `workspace` (device, 256-byte aligned, the caller's until
+ * tig_adamw_destroy).  Synchronous.  The tensors and their states stay the caller's, at the addresses
+ * given here; v (sqrt(v) in 8 bits) must not be negative. */
+TIG_API int tig_adamw_create(const tig_adamw_config *cfg, const tig_adamw_tensor *tensors, int64_t n_tensors, void *workspace,
+                             size_t workspace_bytes, void *hip_stream, tig_adamw **out);
+/* Enqueues one step with learning rate lr >= 0, grad_scale finite, max_norm >= 0.  norm_out: device [1] or
+ * NULL (written only with max_norm > 0).  The steps of one optimiser follow each other (one stream, or the
+ * caller's events); a captured step is a step with every replay, its numbers as they were at capture. */
+TIG_API int tig_adamw_step(tig_adamw *opt, double lr, double grad_scale, double max_norm, float *norm_out, void *hip_stream);
+TIG_API void tig_adamw_destroy(tig_adamw *opt);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,422 @@
+// Dense layer y = act(x W^T + b) + residual and its backward pass (include/tig.h, tig_linear_*).  gfx950.
+//
+//   up to 64 rows     k_linear_rows: the matrix is read once, straight into matrix-core operands; bound by its bytes
+//   more rows         the tile product of gemm.h, bias, activation and residual in its epilogue
+//   backward          k_linear_dz: dz = dy act'(z), and its column sums before it is rounded; then two tile products
+#include <type_traits>
+
+#include "act.h"
+#include "gemm.h"
+
+namespace tig {
+
+namespace {
+
+// Bias, activation, residual; z kept.
+template <typename T, int ACT>
+struct EpiLinear {
+    static constexpr bool kWhole = false;
+    const T *bias, *res;
+    T *y, *z;
+    int64_t ldr, ldy, ldz;
+    bool bias_ok, res_ok, y_ok, z_ok;  // four elements at once
+    __device__ inline int row(int64_t) const { return 0; }
+    __device__ inline void operator()(int, int64_t m, int64_t n, floatx4 v, int left) const
+    {
+        if (bias)
+            v += load_four(bias + n, left, bias_ok);
+        if (z)
+            store_four(z + m * ldz + n, v, left, z_ok);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[e] = activate<ACT>(v[e]);
+        if (res)
+            v += load_four(res + m * ldr + n, left, res_ok);
+        store_four(y + m * ldy + n, v, left, y_ok);
+    }
+};
+
+// ------------------------------------------------------------------------------------------
+// Few rows.  A workgroup takes sixteen columns of y for all rows; its wavefronts take turns along k, every lane loads 16 bytes
+// of one row of W (and of x) as the matrix instructions want them, and the wavefronts' sums are added in LDS.
+template <typename T>
+__device__ inline intx4 load_piece(const T *row, int64_t k, int64_t K)
+{
+    constexpr int per = Mat<T>::kPer16;
+    struct __attribute__((packed, aligned(sizeof(T)))) Any {
+        T v[per];
+    };
+    union {
+        Any any;
+        intx4 q;
+    } u;
+    if (k + per <= K) {
+        u.any = *(const Any *)(row + k);
+    } else {
+#pragma unroll
+        for (int e = 0; e < per; ++e)
+            u.any.v[e] = k + e < K ? row[k + e] : (T)0.0f;
+    }
+    return u.q;
+}
+
+template <typename T, int MT, int WAVES, class Epi>
+__global__ void __launch_bounds__(64 * WAVES) k_linear_rows(const T *x, int64_t ldx, const T *w, int64_t ldw, int64_t M, int64_t N, int64_t K, Epi epi)
+{
+    constexpr int per = Mat<T>::kPer16, kBlock = 4 * per, kUnroll = MT <= 2 ? 4 : 2;
+    __shared__ floatx4 red[WAVES][MT][64];
+    const int lane = lane_id(), wave = wave_id_uniform(), i16 = lane % 16, g = lane / 16;
+    const int64_t n0 = (int64_t)blockIdx.x * 16, n = n0 + i16 < N ? n0 + i16 : N - 1;
+    const T *wr = w + n * ldw + g * per;
+    const T *xr[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int64_t m = i * 16 + i16;
+        xr[i] = x + (m < M ? m : M - 1) * ldx + g * per;
+    }
+    floatx4 acc[MT] = {};
+    const int64_t full = K / kBlock;  // blocks that are whole for every lane
+    int64_t b = wave;
+    for (; b + (kUnroll - 1) * WAVES < full; b += kUnroll * WAVES) {
+        intx4 wv[kUnroll], xv[kUnroll][MT];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t k = (b + u * WAVES) * kBlock;
+            wv[u] = load_piece<T>(wr, k, k + per);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                xv[u][i] = load_piece<T>(xr[i], k, k + per);
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                mma16(acc[i], wv[u], xv[u][i], T());
+    }
+    for (; b * kBlock < K; b += WAVES) {
+        const int64_t k = b * kBlock, left = K - g * per;
+        const intx4 wv = load_piece<T>(wr, k, left);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+            mma16(acc[i], wv, load_piece<T>(xr[i], k, left), T());
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+        red[wave][i][lane] = acc[i];
+    __syncthreads();
+    for (int i = wave; i < MT; i += WAVES) {
+        floatx4 v = red[0][i][lane];
+#pragma unroll
+        for (int u = 1; u < WAVES; ++u)
+            v += red[u][i][lane];
+        const int64_t m = i * 16 + i16, c = n0 + 4 * g;
+        if (m < M && c < N)
+            epi(epi.row(m), m, c, v, N - c < 4 ? (int)(N - c) : 4);
+    }
+}
+
+constexpr int64_t kFewRows = 64;
+
+template <typename T, int WAVES, class Epi>
+hipError_t launch_linear_rows(const tig_linear &p, const Epi &epi, hipStream_t s)
+{
+    const dim3 grid((unsigned)((p.out_dim + 15) / 16)), block(64 * WAVES);
+    const T *x = (const T *)p.x, *w = (const T *)p.w;
+    if (p.rows <= 16)
+        hipLaunchKernelGGL((k_linear_rows<T, 1, WAVES, Epi>), grid, block, 0, s, x, p.ldx, w, p.ldw, p.rows, p.out_dim, p.in_dim, epi);
+    else if (p.rows <= 32)
+        hipLaunchKernelGGL((k_linear_rows<T, 2, WAVES, Epi>), grid, block, 0, s, x, p.ldx, w, p.ldw, p.rows, p.out_dim, p.in_dim, epi);
+    else
+        hipLaunchKernelGGL((k_linear_rows<T, 4, WAVES, Epi>), grid, block, 0, s, x, p.ldx, w, p.ldw, p.rows, p.out_dim, p.in_dim, epi);
+    return hipGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------
+// dz = dy act'(z) for a block of rows, four columns per thread, and the block's column sums of dz before it is rounded.
+constexpr int kDzRows = 64, kDzThreads = 256;
+inline int64_t dz_rows(int64_t rows) { return rows <= (int64_t)kDzRows * 32768 ? kDzRows : (rows + 32767) / 32768; }  // (a grid has 65535 rows)
+
+template <typename T, int ACT>
+__global__ void __launch_bounds__(kDzThreads) k_linear_dz(const T *dy, int64_t lddy, const T *z, int64_t ldz, T *dz, int64_t lddz, float *sums,
+                                                         int64_t lds, int64_t M, int64_t N, int64_t per, bool dy_ok, bool z_ok)
+{
+    const int64_t n = ((int64_t)blockIdx.x * kDzThreads + threadIdx.x) * 4;
+    if (n >= (dz ? lddz : N))
+        return;
+    const int64_t m0 = (int64_t)blockIdx.y * per, m1 = m0 + per < M ? m0 + per : M;
+    const int left = N - n < 4 ? (N > n ? (int)(N - n) : 0) : 4;
+    floatx4 total = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int64_t m = m0; m < m1; ++m) {
+        floatx4 v = load_four(dy + m * lddy + n, left, dy_ok);
+        if constexpr (ACT != TIG_ACT_NONE) {
+            const floatx4 q = load_four(z + m * ldz + n, left, z_ok);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] *= slope<ACT>(q[e]);
+        }
+        total += v;
+        if (dz)
+            store_four(dz + m * lddz + n, v, (int)(lddz - n < 4 ? lddz - n : 4), true);
+    }
+    if (sums && left > 0)
+        *(floatx4 *)(sums + (int64_t)blockIdx.y * lds + n) = total;
+}
+
+}  // namespace
+
+// out[n] = scale * sum of the blocks' column sums, in double
+template <typename T>
+__global__ void __launch_bounds__(256) k_join_sums(const float *sums, int64_t lds, int64_t blocks, int64_t N, T *out, const float *scale, float alpha)
+{
+    __shared__ double part[4][64];
+    const int64_t n = (int64_t)blockIdx.x * 64 + threadIdx.x % 64;
+    const int w = threadIdx.x / 64;
+    double total = 0.0;
+    if (n < N)
+#pragma unroll 4
+        for (int64_t b = w; b < blocks; b += 4)
+            total += (double)sums[b * lds + n];
+    part[w][threadIdx.x % 64] = total;
+    __syncthreads();
+    if (w == 0 && n < N) {
+        total = (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
+        out[n] = (T)(float)(total * (double)alpha * (scale ? (double)*scale : 1.0));
+    }
+}
+
+template <typename T>
+hipError_t launch_join_sums(const float *sums, int64_t lds, int64_t blocks, int64_t N, T *out, const float *scale, float alpha, hipStream_t s)
+{
+    hipLaunchKernelGGL((k_join_sums<T>), dim3((unsigned)((N + 63) / 64)), dim3(256), 0, s, sums, lds, blocks, N, out, scale, alpha);
+    return hipGetLastError();
+}
+template hipError_t launch_join_sums<float>(const float *, int64_t, int64_t, int64_t, float *, const float *, float, hipStream_t);
+template hipError_t launch_join_sums<__bf16>(const float *, int64_t, int64_t, int64_t, __bf16 *, const float *, float, hipStream_t);
+template hipError_t launch_join_sums<_Float16>(const float *, int64_t, int64_t, int64_t, _Float16 *, const float *, float, hipStream_t);
+
+namespace {
+
+inline size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
+
+struct LinearPlan {
+    bool few;                      // forward: k_linear_rows
+    GemmPlan y, dx, dw;
+    bool pack_x, pack_w;           // operands whose rows are not 16-byte aligned
+    bool store_dz;                 // backward: dz is written (else dy serves)
+    int64_t ld_px, ld_pw, ld_dz, ld_sums, sum_blocks;
+    size_t px, pw, dz, sums, part;  // offsets into the workspace
+    size_t bytes;
+};
+
+LinearPlan linear_plan(const tig_linear &p, bool backward)
+{
+    LinearPlan L = {};
+    const int es = dtype_bytes(p.dtype);
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off += align_up(bytes);
+        return at;
+    };
+    L.ld_px = L.ld_pw = pack_ld(p.in_dim, es);
+    if (p.rows == 0) {
+        L.bytes = 0;
+        return L;
+    }
+    if (!backward) {
+        L.few = p.rows <= kFewRows;
+        if (L.few)
+            return L;
+        L.pack_x = !gemm_fits(p.x, p.ldx, p.in_dim, es);
+        L.pack_w = !gemm_fits(p.w, p.ldw, p.in_dim, es);
+        L.y = gemm_plan(p.rows, p.out_dim, p.in_dim, es, true);
+        L.part = take(L.y.part_bytes);
+    } else {
+        L.store_dz = (p.dx || p.dw) && (p.activation != TIG_ACT_NONE || !gemm_fits(p.dy, p.lddy, p.out_dim, es));
+        L.pack_x = p.dw && !gemm_fits(p.x, p.ldx, p.in_dim, es);
+        L.pack_w = p.dx && !gemm_fits(p.w, p.ldw, p.in_dim, es);
+        L.dx = gemm_plan(p.rows, p.in_dim, p.out_dim, es, true);
+        L.dw = gemm_plan(p.out_dim, p.in_dim, p.rows, es, true);
+        size_t part = p.dx ? L.dx.part_bytes : 0;
+        if (p.dw && L.dw.part_bytes > part)
+            part = L.dw.part_bytes;
+        L.part = take(part);
+        L.ld_dz = pack_ld(p.out_dim, es);
+        if (L.store_dz)
+            L.dz = take((size_t)p.rows * L.ld_dz * es);
+        L.sum_blocks = (p.rows + dz_rows(p.rows) - 1) / dz_rows(p.rows);
+        L.ld_sums = (p.out_dim + 3) / 4 * 4;
+        if (p.dbias)
+            L.sums = take((size_t)L.sum_blocks * L.ld_sums * 4);
+    }
+    if (L.pack_x)
+        L.px = take((size_t)p.rows * L.ld_px * es);
+    if (L.pack_w)
+        L.pw = take((size_t)p.out_dim * L.ld_pw * es);
+    L.bytes = off;
+    return L;
+}
+
+int check_linear(const tig_linear *p, bool backward)
+{
+    if (!p || p->struct_size != sizeof(tig_linear))
+        return fail_text(TIG_EINVAL, "tig_linear: NULL argument or wrong struct_size");
+    if (!dtype_ok(p->dtype) || p->activation < TIG_ACT_NONE || p->activation > TIG_ACT_SILU || p->reserved != 0)
+        return fail_text(TIG_EINVAL, "tig_linear: unknown dtype or activation, or reserved is not 0");
+    if (p->rows < 0 || p->rows > 0x7fffffff || p->in_dim < 1 || p->in_dim > kMaxDim || p->out_dim < 1 || p->out_dim > kMaxDim)
+        return fail_text(TIG_EINVAL, "tig_linear: rows or dimensions out of range");
+    auto ld_ok = [](int64_t ld, int64_t cols) { return ld >= cols && ld <= (1 << 22); };
+    auto aligned = [&](const void *q) { return (uintptr_t)q % (uintptr_t)dtype_bytes(p->dtype) == 0; };
+    const bool rows = p->rows > 0;
+    if (!backward) {
+        if (rows && (!p->x || !p->w || !p->y))
+            return fail_text(TIG_EINVAL, "tig_linear_forward: x, w or y is NULL");
+        if (!ld_ok(p->ldx, p->in_dim) || !ld_ok(p->ldw, p->in_dim) || !ld_ok(p->ldy, p->out_dim) || (p->residual && !ld_ok(p->ldr, p->out_dim)) ||
+            (p->z && !ld_ok(p->ldz, p->out_dim)))
+            return fail_text(TIG_EINVAL, "tig_linear_forward: a row stride is smaller than its row or above 2^22");
+        if (!aligned(p->x) || !aligned(p->w) || !aligned(p->y) || !aligned(p->bias) || !aligned(p->residual) || !aligned(p->z))
+            return fail_text(TIG_EINVAL, "tig_linear_forward: an address is not aligned to its element");
+        return TIG_OK;
+    }
+    if (rows && (!p->dy || (p->dw && !p->x) || (p->dx && !p->w) || (p->activation != TIG_ACT_NONE && !p->z)))
+        return fail_text(TIG_EINVAL, "tig_linear_backward: dy, z, or the x (w) that dw (dx) needs, is NULL");
+    if (!ld_ok(p->lddy, p->out_dim) || (p->dw && (!ld_ok(p->ldx, p->in_dim) || !ld_ok(p->lddw, p->in_dim))) ||
+        (p->dx && (!ld_ok(p->ldw, p->in_dim) || !ld_ok(p->lddx, p->in_dim))) || (p->activation != TIG_ACT_NONE && !ld_ok(p->ldz, p->out_dim)))
+        return fail_text(TIG_EINVAL, "tig_linear_backward: a row stride is smaller than its row or above 2^22");
+    if (!aligned(p->dy) || !aligned(p->x) || !aligned(p->w) || !aligned(p->z) || !aligned(p->dx) || !aligned(p->dw) || !aligned(p->dbias))
+        return fail_text(TIG_EINVAL, "tig_linear_backward: an address is not aligned to its element");
+    return TIG_OK;
+}
+
+int check_workspace(const void *workspace, size_t have, size_t need)
+{
+    if (need == 0)
+        return TIG_OK;
+    if (!workspace || ((uintptr_t)workspace & 255))
+        return fail_text(TIG_EINVAL, "workspace is NULL or not 256-byte aligned");
+    return have >= need ? TIG_OK : fail_text(TIG_ENOSPACE, "workspace too small");
+}
+
+template <typename T>
+hipError_t forward(const tig_linear &p, const LinearPlan &L, char *ws, hipStream_t s)
+{
+    return with_activation(p.activation, [&](auto act) -> hipError_t {
+        using Epi = EpiLinear<T, decltype(act)::value>;
+        const int es = sizeof(T);
+        const Epi epi = {(const T *)p.bias, (const T *)p.residual, (T *)p.y, (T *)p.z, p.ldr, p.ldy, p.ldz,
+                         four_aligned(p.bias, 4, es), four_aligned(p.residual, p.ldr, es), four_aligned(p.y, p.ldy, es), four_aligned(p.z, p.ldz, es)};
+        if (L.few)  // (more wavefronts along k where the columns alone do not fill the chip)
+            return (p.out_dim + 15) / 16 >= 512 ? launch_linear_rows<T, 4>(p, epi, s) : launch_linear_rows<T, 8>(p, epi, s);
+        const T *x = (const T *)p.x, *w = (const T *)p.w;
+        int64_t ldx = p.ldx, ldw = p.ldw;
+        hipError_t e = hipSuccess;
+        if (L.pack_x) {
+            e = launch_pack(x, ldx, ws + L.px, L.ld_px, p.rows, p.in_dim, es, nullptr, s);
+            x = (const T *)(ws + L.px), ldx = L.ld_px;
+        }
+        if (e == hipSuccess && L.pack_w) {
+            e = launch_pack(w, ldw, ws + L.pw, L.ld_pw, p.out_dim, p.in_dim, es, nullptr, s);
+            w = (const T *)(ws + L.pw), ldw = L.ld_pw;
+        }
+        return e != hipSuccess ? e : launch_gemm<T, kRow, kRow>(L.y, x, ldx, w, ldw, p.rows, p.out_dim, p.in_dim, ws + L.part, epi, s);
+    });
+}
+
+template <typename T>
+hipError_t backward(const tig_linear &p, const LinearPlan &L, char *ws, hipStream_t s)
+{
+    const int es = sizeof(T);
+    hipError_t e = hipSuccess;
+    if (p.rows == 0) {
+        if (p.dw)
+            e = launch_zero_rows(p.dw, p.lddw, p.out_dim, p.in_dim, es, s);
+        if (p.dbias && e == hipSuccess)
+            e = launch_zero_rows(p.dbias, p.out_dim, 1, p.out_dim, es, s);
+        return e;
+    }
+    const T *dz = (const T *)p.dy;
+    int64_t lddz = p.lddy;
+    if (L.store_dz || p.dbias) {
+        T *const out = L.store_dz ? (T *)(ws + L.dz) : nullptr;
+        float *const sums = p.dbias ? (float *)(ws + L.sums) : nullptr;
+        const dim3 grid((unsigned)((L.ld_dz / 4 + kDzThreads) / kDzThreads), (unsigned)L.sum_blocks);
+        with_activation(p.activation, [&](auto act) {
+            hipLaunchKernelGGL((k_linear_dz<T, decltype(act)::value>), grid, dim3(kDzThreads), 0, s, (const T *)p.dy, p.lddy, (const T *)p.z, p.ldz, out,
+                               L.ld_dz, sums, L.ld_sums, p.rows, p.out_dim, dz_rows(p.rows), four_aligned(p.dy, p.lddy, es), four_aligned(p.z, p.ldz, es));
+            return 0;
+        });
+        if ((e = hipGetLastError()) != hipSuccess)
+            return e;
+        if (out)
+            dz = out, lddz = L.ld_dz;
+        if (p.dbias && (e = launch_join_sums<T>(sums, L.ld_sums, L.sum_blocks, p.out_dim, (T *)p.dbias, nullptr, 1.0f, s)) != hipSuccess)
+            return e;
+    }
+    if (p.dx) {
+        const T *w = (const T *)p.w;
+        int64_t ldw = p.ldw;
+        if (L.pack_w) {
+            e = launch_pack(w, ldw, ws + L.pw, L.ld_pw, p.out_dim, p.in_dim, es, nullptr, s);
+            w = (const T *)(ws + L.pw), ldw = L.ld_pw;
+        }
+        const EpiStore<T> epi = {(T *)p.dx, p.lddx, nullptr, 1.0f, four_aligned(p.dx, p.lddx, es)};
+        if (e == hipSuccess)
+            e = launch_gemm<T, kRow, kCol>(L.dx, dz, lddz, w, ldw, p.rows, p.in_dim, p.out_dim, ws + L.part, epi, s);
+        if (e != hipSuccess)
+            return e;
+    }
+    if (p.dw) {
+        const T *x = (const T *)p.x;
+        int64_t ldx = p.ldx;
+        if (L.pack_x) {
+            e = launch_pack(x, ldx, ws + L.px, L.ld_px, p.rows, p.in_dim, es, nullptr, s);
+            x = (const T *)(ws + L.px), ldx = L.ld_px;
+        }
+        const EpiStore<T> epi = {(T *)p.dw, p.lddw, nullptr, 1.0f, four_aligned(p.dw, p.lddw, es)};
+        if (e == hipSuccess)
+            e = launch_gemm<T, kCol, kCol>(L.dw, dz, lddz, x, ldx, p.out_dim, p.in_dim, p.rows, ws + L.part, epi, s);
+    }
+    return e;
+}
+
+}  // namespace
+
+}  // namespace tig
+
+using namespace tig;
+
+int tig_linear_workspace_bytes(const tig_linear *p, int32_t backward, size_t *bytes)
+{
+    const int rc = check_linear(p, backward != 0);
+    if (rc != TIG_OK)
+        return rc;
+    if (!bytes)
+        return fail_text(TIG_EINVAL, "tig_linear_workspace_bytes: bytes is NULL");
+    *bytes = linear_plan(*p, backward != 0).bytes;
+    return TIG_OK;
+}
+
+int tig_linear_forward(const tig_linear *p, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    int rc = check_linear(p, false);
+    if (rc != TIG_OK || p->rows == 0)
+        return rc;
+    const LinearPlan L = linear_plan(*p, false);
+    if ((rc = check_workspace(workspace, workspace_bytes, L.bytes)) != TIG_OK)
+        return rc;
+    const hipError_t e = with_dtype(p->dtype, [&](auto t) { return forward<decltype(t)>(*p, L, (char *)workspace, (hipStream_t)hip_stream); });
+    return e == hipSuccess ? TIG_OK : fail_global("tig_linear_forward", e);
+}
+
+int tig_linear_backward(const tig_linear *p, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    int rc = check_linear(p, true);
+    if (rc != TIG_OK)
+        return rc;
+    const LinearPlan L = linear_plan(*p, true);
+    if ((rc = check_workspace(workspace, workspace_bytes, L.bytes)) != TIG_OK)
+        return rc;
+    const hipError_t e = with_dtype(p->dtype, [&](auto t) { return backward<decltype(t)>(*p, L, (char *)workspace, (hipStream_t)hip_stream); });
+    return e == hipSuccess ? TIG_OK : fail_global("tig_linear_backward", e);
+}

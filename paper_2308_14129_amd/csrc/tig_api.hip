@@ -459,6 +459,12 @@ int fail_global(const char *what, hipError_t e)
     snprintf(g_init_err, sizeof(g_init_err), "%s: %s", what, hipGetErrorString(e));
     return TIG_EHIP;
 }
+
+int fail_text(int status, const char *what)
+{
+    snprintf(g_init_err, sizeof(g_init_err), "%s", what);
+    return status;
+}
 }  // namespace tig
 
 extern "C" {

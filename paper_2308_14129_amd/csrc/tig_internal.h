@@ -389,5 +389,7 @@ struct PinnedStage {
 };
 // records a failed HIP call of a context-free entry point (read back with tig_last_error(NULL)); returns TIG_EHIP
 int fail_global(const char *what, hipError_t e);
+// the same for an argument error; returns `status`
+int fail_text(int status, const char *what);
 
 }  // namespace tig

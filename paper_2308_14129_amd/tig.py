@@ -77,7 +77,9 @@ class tig_out(Structure):
 EXPORTS = ("tig_workspace_bytes", "tig_init", "tig_step", "tig_step_static", "tig_step_profiled", "tig_reset", "tig_state_export",
            "tig_state_import", "tig_destroy", "tig_strerror", "tig_last_error", "tig_launch_info",
            "tig_train_workspace_bytes", "tig_train_attach", "tig_train_step", "tig_train_get",
-           "tig_modules_workspace_bytes", "tig_modules_attach")
+           "tig_modules_workspace_bytes", "tig_modules_attach",
+           "tig_linear_workspace_bytes", "tig_linear_forward", "tig_linear_backward", "tig_softmax_ce_workspace_bytes",
+           "tig_softmax_ce_run", "tig_adamw_workspace_bytes", "tig_adamw_create", "tig_adamw_step", "tig_adamw_destroy")
 
 _lib = None
 
