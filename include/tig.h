@@ -270,7 +270,9 @@ TIG_API int tig_train_attach(tig_ctx *ctx, const tig_weights *weights, void *wor
  * learning rate lr >= 0 (0: gradients only, weights untouched).  batch->neg_dst is required.
  * loss_out: device pointer to one float, or NULL.  Enqueued on the context's stream.  The call also prepares
  * the queries of the batch it expects next (the same number of events, continuing where this one ends), as tig_step
- * does; a following tig_step or tig_train_step on another batch prepares its own. */
+ * does; a following tig_step or tig_train_step on another batch prepares its own.  With a ranking head
+ * (tig_train_head_attach) the loss and the gradients are those of the sum of both losses, and the head's parameters are
+ * trained too; with tig_train_adamw_attach the update is AdamW's. */
 TIG_API int tig_train_step(tig_ctx *ctx, const tig_batch *batch, const tig_out *out, float lr, float *loss_out);
 
 /* Copies the master weights (what = 0) or the gradients of the last training step (what = 1) to
@@ -658,6 +660,51 @@ TIG_API int tig_adamw_create(const tig_adamw_config *cfg, const tig_adamw_tensor
  * caller's events); a captured step is a step with every replay, its numbers as they were at capture. */
 TIG_API int tig_adamw_step(tig_adamw *opt, double lr, double grad_scale, double max_norm, float *norm_out, void *hip_stream);
 TIG_API void tig_adamw_destroy(tig_adamw *opt);
+
+/* A ranking head of the training step: which node does an event's source turn to?  On top of the step's
+ * binary cross-entropy, its source embeddings e_b go through a dense layer with a residual and a softmax
+ * cross entropy over `num_items` candidate nodes first_node .. first_node + num_items - 1:
+ *   h_b = act(W e_b + c) + e_b,   L = weight * mean_b CE(items h_b + item_bias, dst_b - first_node)
+ * over the events whose destination is a candidate.  tig_train_step then trains the head's parameters
+ * with the model's, the loss it reports is the sum, and the gradient of e_b goes on into the model
+ * (gradients of events that share a query are added in fp64).  fp32. */
+typedef struct tig_train_head {
+    uint32_t struct_size;
+    int32_t activation;     /* tig_activation */
+    int64_t first_node;     /* first_node + num_items <= N */
+    int64_t num_items;      /* >= 1 */
+    float weight;           /* finite */
+    int32_t reserved;
+    const float *W, *c;             /* [E x E], [E]; host or device */
+    const float *items, *item_bias; /* [num_items x E], [num_items]; -infinity masks a candidate */
+} tig_train_head;
+
+/* Attaches a head to a context with a training workspace: its parameters are copied into `workspace`
+ * (device, 256-byte aligned, the caller's until tig_destroy; about 8 num_items (E + 1) bytes, the loss's
+ * pieces and max_batch (40 E) bytes).  Replaces an attached head; an attached optimiser has to be attached
+ * after the head (TIG_EINVAL otherwise).  tig_train_attach drops head and optimiser.  Synchronous. */
+TIG_API int tig_train_head_workspace_bytes(const tig_config *cfg, const tig_train_head *head, size_t *bytes);
+TIG_API int tig_train_head_attach(tig_ctx *ctx, const tig_train_head *head, void *workspace, size_t workspace_bytes);
+/* Copies the head's parameters (what = 0) or their gradients of the last training step (what = 1) to the
+ * non-NULL pointers of `dst` (its other fields are not read), host or device.  Synchronous. */
+TIG_API int tig_train_head_get(tig_ctx *ctx, int32_t what, const tig_train_head *dst);
+
+/* AdamW (tig_adamw_*) in place of SGD for a context's training steps: over the model's weights and an
+ * attached head's parameters, with weight decay for matrices (not for biases and the time encoding),
+ * clipped together to max_norm (0: not clipped).  tig_train_step's lr is its learning rate; lr = 0 makes
+ * no step.  States start at zero; they and the step counter lie in `workspace` (device, 256-byte aligned,
+ * the caller's until tig_destroy), which continues where it was if it is copied out and back.
+ * Synchronous. */
+typedef struct tig_train_adamw {
+    uint32_t struct_size;
+    int32_t state_bits;  /* 32 or 8 */
+    double beta1, beta2, eps;
+    float weight_decay;
+    float max_norm;
+} tig_train_adamw;
+
+TIG_API int tig_train_adamw_workspace_bytes(const tig_ctx *ctx, const tig_train_adamw *cfg, size_t *bytes);
+TIG_API int tig_train_adamw_attach(tig_ctx *ctx, const tig_train_adamw *cfg, void *workspace, size_t workspace_bytes);
 
 #ifdef __cplusplus
 }

@@ -45,13 +45,15 @@ def bce_loss(score_pos, score_neg):
 
 
 def train_step(state, src, dst, ts, edge_feat, W, first_eid, count, neg_dst, K, H, lr, index=None,
-               deferred=False, tie_eps=0.0, relu_flip=frozenset()):
+               deferred=False, tie_eps=0.0, relu_flip=frozenset(), head=None):
     """One training step.  Runs tig_oracle.step (state updated in place), then loss, gradients and
     the SGD update of W (in place).  Returns (the step's outputs, loss, grads: dict name -> float64).
     tie_eps > 0: the outputs carry "relu_ties", the ReLU units whose pre-activation is closer to zero
     than tie_eps, as (|pre-activation|, layer, row, unit) with layer "dec" (row = pair index: event b
     against its destination, count + b against its negative) or "merge" (row = query index).
-    relu_flip: units (layer, row, unit) whose gate is taken as the opposite of (pre-activation > 0)."""
+    relu_flip: units (layer, row, unit) whose gate is taken as the opposite of (pre-activation > 0).
+    head: a function of the embeddings (float64 [rows x E]) that returns another loss, which is added, and its gradient
+    with respect to them."""
     M = state.mem.shape[1]
     T = W["time_w"].shape[0]
     F = edge_feat.shape[1]
@@ -79,6 +81,10 @@ def train_step(state, src, dst, ts, edge_feat, W, first_eid, count, neg_dst, K, 
 
     # ---- decoder: d loss / d logit, back to the embeddings
     d_emb = np.zeros_like(emb)
+    if head is not None:
+        more, d_more = head(emb)
+        loss += more
+        d_emb += d_more
     pairs = [(b, B + b, out["score_pos"][b], -1.0) for b in range(B)] + \
             [(b, 2 * B + b, out["score_neg"][b], +1.0) for b in range(B)]
     ties = []

@@ -89,6 +89,7 @@ struct tig_ctx {
     void *static_scratch;  // this device's copy of g_static_scratch
     bool embed_stale;      // training steps have moved the master weights since the attention / merge / decoder weights were last folded
     void *train_ws;        // training workspace (master weights, gradients, the backward pass's buffers), or NULL
+    TrainExtra train_extra;  // ranking head and optimiser of training steps
     bool has_model;        // tig_init was given weights (the headline instance's prepared weights exist)
     void *mods_ws;         // workspace of an attached module selection, or NULL
     ModParams mods;        // ... and its parameters
@@ -874,6 +875,7 @@ static int step_impl(tig_ctx *ctx, const tig_batch *batch, const tig_out *out, h
         sp.train_ws = ctx->train_ws;
         sp.lr = train->lr;
         sp.loss_out = train->loss_out;
+        sp.train_extra = ctx->train_extra;
         train_step_args(d, ctx->train_ws, &a);
     }
     const hipError_t e = launch_step(d, ctx->plan, ctx->pw, a, sp, ctx->stream, marks);
@@ -973,6 +975,8 @@ int tig_train_attach(tig_ctx *ctx, const tig_weights *weights, void *workspace, 
     if (e != hipSuccess)
         return fail(ctx, TIG_EHIP, "tig_train_attach", e);
     ctx->train_ws = workspace;
+    tig_adamw_destroy(ctx->train_extra.opt);  // (head and optimiser went with the masters before)
+    ctx->train_extra = TrainExtra{};
     ctx->ahead_g_valid = false;  // staged rows of another set of weights
     return TIG_OK;
 }
@@ -1000,6 +1004,161 @@ int tig_train_get(tig_ctx *ctx, int32_t what, const tig_weights *dst)
     const hipError_t e = train_copy_out(ctx->d, ctx->train_ws, what == 1, *dst, ctx->stream);
     if (e != hipSuccess)
         return fail(ctx, TIG_EHIP, "tig_train_get", e);
+    return TIG_OK;
+}
+
+static int check_head(const Dims &d, const tig_train_head *h, int64_t num_nodes)
+{
+    if (!h || h->struct_size != sizeof(tig_train_head) || h->reserved != 0)
+        return TIG_EINVAL;
+    if (h->activation < TIG_ACT_NONE || h->activation > TIG_ACT_SILU || !(h->weight - h->weight == 0.0f))
+        return TIG_EINVAL;
+    if (h->first_node < 0 || h->num_items < 1 || h->num_items > num_nodes || h->first_node > num_nodes - h->num_items)
+        return TIG_EINVAL;
+    return train_supported(d) ? TIG_OK : TIG_EINVAL;
+}
+
+static TrainHead head_of(const Dims &d, const tig_train_head &h, void *ws)
+{
+    TrainHead t = {ws, h.first_node, h.num_items, h.weight, h.activation, 0};
+    t.ops_bytes = train_head_ops_bytes(d, t);
+    return t;
+}
+
+int tig_train_head_workspace_bytes(const tig_config *cfg, const tig_train_head *head, size_t *bytes)
+{
+    int rc = check_config(cfg);
+    if (rc == TIG_OK)
+        rc = check_head(make_dims(*cfg), head, 0x7FFFFFFF);
+    if (rc != TIG_OK)
+        return rc;
+    if (!bytes)
+        return TIG_EINVAL;
+    *bytes = train_head_bytes(make_dims(*cfg), head_of(make_dims(*cfg), *head, nullptr));
+    return TIG_OK;
+}
+
+int tig_train_head_attach(tig_ctx *ctx, const tig_train_head *head, void *workspace, size_t workspace_bytes)
+{
+    if (!ctx)
+        return TIG_EINVAL;
+    if (!ctx->train_ws)
+        return fail(ctx, TIG_EINVAL, "tig_train_head_attach: no training workspace attached (tig_train_attach)");
+    if (ctx->train_extra.opt)
+        return fail(ctx, TIG_EINVAL, "tig_train_head_attach: an optimiser is attached already (it goes after the head)");
+    if (check_head(ctx->d, head, ctx->num_nodes) != TIG_OK)
+        return fail(ctx, TIG_EINVAL, "tig_train_head_attach: NULL argument, wrong struct_size, unknown activation, weight not finite, or candidates "
+                                     "that are no nodes");
+    if (!head->W || !head->c || !head->items || !head->item_bias)
+        return fail(ctx, TIG_EINVAL, "tig_train_head_attach: a parameter is NULL");
+    if (!workspace || ((uintptr_t)workspace & 255))
+        return fail(ctx, TIG_EINVAL, "tig_train_head_attach: workspace is NULL or not 256-byte aligned");
+    const TrainHead h = head_of(ctx->d, *head, workspace);
+    if (workspace_bytes < train_head_bytes(ctx->d, h))
+        return fail(ctx, TIG_ENOSPACE, "tig_train_head_attach: workspace too small");
+    hipError_t e = train_head_attach(ctx->d, h, *head, ctx->stream);
+    if (e == hipSuccess)
+        e = hipStreamSynchronize(ctx->stream);
+    if (e != hipSuccess)
+        return fail(ctx, TIG_EHIP, "tig_train_head_attach", e);
+    ctx->train_extra.head = h;
+    return TIG_OK;
+}
+
+int tig_train_head_get(tig_ctx *ctx, int32_t what, const tig_train_head *dst)
+{
+    if (!ctx)
+        return TIG_EINVAL;
+    if (!ctx->train_extra.head.ws || !dst || dst->struct_size != sizeof(tig_train_head) || (what != 0 && what != 1))
+        return fail(ctx, TIG_EINVAL, "tig_train_head_get: no head attached, NULL destination or unknown selector");
+    hipError_t e = train_head_copy_out(ctx->d, ctx->train_extra.head, what == 1, *dst, ctx->stream);
+    if (e == hipSuccess)
+        e = hipStreamSynchronize(ctx->stream);
+    return e == hipSuccess ? TIG_OK : fail(ctx, TIG_EHIP, "tig_train_head_get", e);
+}
+
+// The optimiser's workspace: the step counter, its list of tensors, the states (all but the list start at zero).
+struct AdamPlace {
+    tig_adamw_tensor t[kMaxTrainTensors];
+    tig_adamw_config cfg;
+    int n;
+    size_t list, list_bytes, states, bytes;
+};
+
+static int adam_place(const tig_ctx *ctx, const tig_train_adamw &c, char *ws, AdamPlace *out)
+{
+    AdamPlace &A = *out;
+    A.n = train_tensors(ctx->d, ctx->train_ws, ctx->train_extra.head, c.weight_decay, A.t);
+    const bool eight = c.state_bits == 8;
+    // (addresses are taken from 256 on where there is no workspace yet, so that none is NULL)
+    char *const base = ws ? ws : (char *)256;
+    A.cfg = tig_adamw_config{(uint32_t)sizeof(tig_adamw_config), c.state_bits, c.beta1, c.beta2, c.eps, (int64_t *)base};
+    size_t off = 256;
+    auto take = [&](size_t bytes) {
+        char *const p = base + off;
+        off += align_up(bytes ? bytes : 1);
+        return p;
+    };
+    for (int i = 0; i < A.n; ++i) {
+        const size_t n = (size_t)A.t[i].n;
+        A.t[i].m = take(eight ? n : 4 * n);
+        A.t[i].v = take(eight ? n : 4 * n);
+        if (eight) {
+            A.t[i].m_scale = (float *)take((n + 255) / 256 * 4);
+            A.t[i].v_scale = (float *)take((n + 255) / 256 * 4);
+        }
+    }
+    A.states = off;
+    const int rc = tig_adamw_workspace_bytes(&A.cfg, A.t, A.n, &A.list_bytes);
+    A.list = off;
+    A.bytes = off + align_up(A.list_bytes);
+    return rc;
+}
+
+static int check_train_adamw(const tig_ctx *ctx, const tig_train_adamw *c)
+{
+    return c && c->struct_size == sizeof(tig_train_adamw) && ctx->train_ws && c->weight_decay >= 0.0f && c->weight_decay < 1e30f &&
+                   c->max_norm >= 0.0f && c->max_norm < 1e30f
+               ? TIG_OK
+               : TIG_EINVAL;
+}
+
+int tig_train_adamw_workspace_bytes(const tig_ctx *ctx, const tig_train_adamw *cfg, size_t *bytes)
+{
+    if (!ctx || !bytes || check_train_adamw(ctx, cfg) != TIG_OK)
+        return TIG_EINVAL;
+    AdamPlace A;
+    const int rc = adam_place(ctx, *cfg, nullptr, &A);
+    if (rc == TIG_OK)
+        *bytes = A.bytes;
+    return rc;
+}
+
+int tig_train_adamw_attach(tig_ctx *ctx, const tig_train_adamw *cfg, void *workspace, size_t workspace_bytes)
+{
+    if (!ctx)
+        return TIG_EINVAL;
+    if (check_train_adamw(ctx, cfg) != TIG_OK)
+        return fail(ctx, TIG_EINVAL, "tig_train_adamw_attach: no training workspace, NULL argument, wrong struct_size, or a negative number");
+    if (!workspace || ((uintptr_t)workspace & 255))
+        return fail(ctx, TIG_EINVAL, "tig_train_adamw_attach: workspace is NULL or not 256-byte aligned");
+    AdamPlace A;
+    int rc = adam_place(ctx, *cfg, (char *)workspace, &A);
+    if (rc != TIG_OK)
+        return fail(ctx, rc, "tig_train_adamw_attach: state_bits is 8 or 32, beta1 and beta2 in [0, 1), eps positive");
+    if (workspace_bytes < A.bytes)
+        return fail(ctx, TIG_ENOSPACE, "tig_train_adamw_attach: workspace too small");
+    hipError_t e = launch_fill_zero(workspace, A.states, ctx->stream);
+    if (e == hipSuccess)
+        e = hipStreamSynchronize(ctx->stream);
+    if (e != hipSuccess)
+        return fail(ctx, TIG_EHIP, "tig_train_adamw_attach", e);
+    tig_adamw *opt = nullptr;
+    if ((rc = tig_adamw_create(&A.cfg, A.t, A.n, (char *)workspace + A.list, A.list_bytes, ctx->stream, &opt)) != TIG_OK)
+        return fail(ctx, rc, "tig_train_adamw_attach: the optimiser could not be made");
+    tig_adamw_destroy(ctx->train_extra.opt);
+    ctx->train_extra.opt = opt;
+    ctx->train_extra.max_norm = cfg->max_norm;
     return TIG_OK;
 }
 
@@ -1310,6 +1469,7 @@ void tig_destroy(tig_ctx *ctx)
         for (int i = 0; i <= kNumStepKernels; ++i)
             (void)hipEventDestroy(ctx->marks[i]);
     hint_words_give(ctx->rows_seen_host);
+    tig_adamw_destroy(ctx->train_extra.opt);
     delete ctx;
 }
 

@@ -264,6 +264,19 @@ int embed_spare_workgroups(const Dims &d, const LaunchPlan &plan, int roles, int
 int prepare_workgroups(int count, bool shared);
 hipError_t prepare_kernels(const Dims &d, const LaunchPlan &plan);
 constexpr int kNumStepKernels = TIG_NUM_STEP_KERNELS;
+// What a training step has besides the model (train_head.hip): a ranking head (ws NULL: none) and an optimiser (NULL: SGD).
+struct TrainHead {
+    void *ws;
+    int64_t first_node, num_items;
+    float weight;
+    int32_t activation;
+    size_t ops_bytes;  // of the operators' workspace, whatever the batch (train_head_ops_bytes; 0: not known yet)
+};
+struct TrainExtra {
+    TrainHead head;
+    tig_adamw *opt;
+    double max_norm;
+};
 // What one step launches, in order: [scatter, select] (up-front selection of a batch above the
 // one-workgroup limit), [prepare] (selection and / or query preparation not done ahead),
 // [gru] (unless the previous step's closing launch ran it), embed, closing.
@@ -280,6 +293,7 @@ struct StepPlan {
     void *train_ws;
     float lr;
     float *loss_out;
+    TrainExtra train_extra;
     int32_t *clear_first;       // a counter to clear ahead of everything, or NULL
     GruAhead ahead;             // GRU workgroups of the closing launch
     const struct ModParams *mods;  // a context with a module selection, or NULL
@@ -317,7 +331,18 @@ hipError_t train_copy_out(const Dims &d, void *workspace, bool grads, const tig_
 // the arrays that a training step's GRU and embedding launches leave for its backward pass
 void train_step_args(const Dims &d, void *workspace, StepArgs *a);
 hipError_t launch_train(const Dims &d, const LaunchPlan &plan, const StepArgs &a, void *workspace, const PackedWeights &pw, float lr,
-                        float *loss_out, int *launches, hipStream_t s);
+                        float *loss_out, const TrainExtra &extra, int *launches, hipStream_t s);
+size_t train_head_ops_bytes(const Dims &d, const TrainHead &h);
+size_t train_head_bytes(const Dims &d, const TrainHead &h);
+hipError_t train_head_attach(const Dims &d, const TrainHead &h, const tig_train_head &from, hipStream_t s);
+hipError_t train_head_copy_out(const Dims &d, const TrainHead &h, bool grads, const tig_train_head &to, hipStream_t s);
+// forward and backward pass of the head over the step's embeddings; *demb: gradients of the query rows [2 * count x E]
+hipError_t launch_train_head(const Dims &d, const StepArgs &a, const TrainHead &h, const double **demb, const float **mean, int *launches, hipStream_t s);
+hipError_t launch_train_head_sgd(const Dims &d, const TrainHead &h, float lr, int *launches, hipStream_t s);
+// the optimiser's list of tensors: the masters and an attached head's parameters (their number is returned)
+constexpr int kMaxTrainTensors = 26;
+int train_head_tensors(const Dims &d, const TrainHead &h, float weight_decay, tig_adamw_tensor *out);
+int train_tensors(const Dims &d, void *train_ws, const TrainHead &h, float weight_decay, tig_adamw_tensor *out);
 // after training steps with lr != 0 the prepared weights follow the masters through fold_weights (products in double, two
 // intermediate matrices in single precision): this folds those of the inference kernels again, in double throughout
 hipError_t train_refold_embed(const Dims &d, void *workspace, void *packed, PackedWeights *pw, hipStream_t s);

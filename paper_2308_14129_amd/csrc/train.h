@@ -31,6 +31,7 @@ struct TrainArrays {
     float *PRT;                         // [K2 x Ek]    folded merge layer 1 | its state part
     float *A1T;                         // [Mq x N1]    folded query
     float *WiT;                         // [Tp x 3Mp]   message columns of the time encoding, all gates
+    const double *demb_x;               // [2B x E] gradients that a ranking head adds to the embeddings of query rows, or NULL
 };
 
 struct BackParams {
@@ -42,6 +43,17 @@ struct BackParams {
     int rpt;                  // rows a workgroup takes, 4 .. ROWS (the rest of its tile's rows stay empty)
     int slots;                // rows of the LDS table that collects the staged rows' gradients (0: none)
 };
+
+// the query row of an (event, role) entry
+__device__ inline int row_of_entry_tr(const QuerySet &qs, int i, int entries)
+{
+    int s = qs.slot[i];
+    if (s < 0) {
+        const int rep = -s - 1;
+        s = rep < entries ? qs.slot[rep] : 0;
+    }
+    return s >= 0 && s < entries ? s : 0;
+}
 
 hipError_t launch_train_decode(const Dims &d, const StepArgs &a, const PackedWeights &pw, const TrainArrays &t, hipStream_t s);
 hipError_t launch_train_back(const Dims &d, const LaunchPlan &plan, const StepArgs &a, const PackedWeights &pw,

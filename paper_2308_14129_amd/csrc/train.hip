@@ -572,6 +572,8 @@ struct UpdateJob {
     const float *terms;
     int n_terms;
     float *loss_out;
+    const float *head_mean;  // a ranking head's mean loss, or NULL
+    float head_weight;
     float *P, *G;
     size_t n_params;
     float lr;
@@ -647,7 +649,7 @@ __global__ void __launch_bounds__(256) k_tr_update(StepArgs a, UpdateJob u)
         __syncthreads();
     }
     if (threadIdx.x == 0)
-        *u.loss_out = red[0];
+        *u.loss_out = u.head_mean ? red[0] + u.head_weight * *u.head_mean : red[0];
 }
 
 __global__ void k_tr_phi0(const float *time_b, float *phi0, int T)
@@ -1043,14 +1045,18 @@ void train_step_args(const Dims &d, void *workspace, StepArgs *a)
 
 // Everything of a training step after the GRU launch.
 hipError_t launch_train(const Dims &d, const LaunchPlan &plan, const StepArgs &a, void *workspace, const PackedWeights &pw, float lr,
-                        float *loss_out, int *launches, hipStream_t s)
+                        float *loss_out, const TrainExtra &extra, int *launches, hipStream_t s)
 {
     const TrainLayout L = train_layout(d, workspace);
-    const TrainArrays &t = L.t;
+    TrainArrays t = L.t;
     const int M = d.M, E = d.E, da = d.da, D = d.Dmsg, ld_m1 = da + M;
+    const float *head_mean = nullptr;
     hipError_t e;
-    if ((e = launch_embed(d, plan, pw, a, s)) != hipSuccess || (e = launch_train_decode(d, a, pw, t, s)) != hipSuccess ||
-        (e = launch_train_back(d, plan, a, pw, t, s)) != hipSuccess)
+    if ((e = launch_embed(d, plan, pw, a, s)) != hipSuccess || (e = launch_train_decode(d, a, pw, t, s)) != hipSuccess)
+        return e;
+    if (extra.head.ws && (e = launch_train_head(d, a, extra.head, &t.demb_x, &head_mean, launches, s)) != hipSuccess)
+        return e;
+    if ((e = launch_train_back(d, plan, a, pw, t, s)) != hipSuccess)
         return e;
     if (a.msg_count > 0 && (e = launch_train_gru_back(d, plan, a, pw, t, s)) != hipSuccess)
         return e;
@@ -1106,14 +1112,41 @@ hipError_t launch_train(const Dims &d, const LaunchPlan &plan, const StepArgs &a
     u.M = M, u.T = d.T, u.E = E;
     u.commit_blocks = a.msg_count > 0 ? 32 : 0;  // (last: the GRU's backward read the memory as the step found it)
     u.terms = t.LOSS, u.n_terms = 2 * a.count, u.loss_out = loss_out;
-    u.P = L.P, u.G = L.G, u.n_params = L.n_params, u.lr = lr;
+    u.head_mean = head_mean, u.head_weight = extra.head.weight;
+    u.P = L.P, u.G = L.G, u.n_params = L.n_params, u.lr = extra.opt ? 0.0f : lr;
     u.TACC = t.TACC, u.WACC = t.WACC, u.phi0 = L.phi0, u.dphi0 = L.dphi0;
     const int blocks = u.commit_blocks + (loss_out ? 1 : 0) + (int)((L.n_params + 255) / 256);
     hipLaunchKernelGGL(k_tr_update, dim3(blocks), dim3(256), 0, s, a, u);
     if ((e = hipGetLastError()) != hipSuccess)
         return e;
     *launches += lr != 0.0f ? 6 : 4;  // contractions, two of k_tr_small, update; two of k_tr_small
+    if (lr != 0.0f && extra.opt) {
+        if (tig_adamw_step(extra.opt, lr, 1.0, extra.max_norm, nullptr, s) != TIG_OK)
+            return hipErrorUnknown;
+        hipLaunchKernelGGL(k_tr_phi0, dim3((d.T + 255) / 256), dim3(256), 0, s, L.w.time_b, L.phi0, d.T);
+        if ((e = hipGetLastError()) != hipSuccess)
+            return e;
+        *launches += extra.max_norm > 0.0 ? 4 : 3;
+    } else if (lr != 0.0f && extra.head.ws && (e = launch_train_head_sgd(d, extra.head, lr, launches, s)) != hipSuccess) {
+        return e;
+    }
     return lr != 0.0f ? fold_weights(d, L, pw, s) : hipSuccess;
+}
+
+// Masters, gradients and what decays: the arrays of tig_weights in order, then the head's.
+int train_tensors(const Dims &d, void *train_ws, const TrainHead &h, float weight_decay, tig_adamw_tensor *out)
+{
+    const TrainLayout L = train_layout(d, train_ws);
+    const float *const w[22] = {L.w.time_w, L.w.time_b, L.w.W_i, L.w.b_i, L.w.W_h, L.w.b_h, L.w.W_Q, L.w.b_Q, L.w.W_K, L.w.b_K, L.w.W_V,
+                                L.w.b_V, L.w.W_O, L.w.b_O, L.w.W_m1, L.w.b_m1, L.w.W_m2, L.w.b_m2, L.w.W_d1, L.w.b_d1, L.w.w_d2, L.w.b_d2};
+    for (int i = 0; i < 22; ++i) {
+        const size_t at = (size_t)(w[i] - L.P), n = (i + 1 < 22 ? (size_t)(w[i + 1] - L.P) : L.n_params) - at;
+        out[i] = tig_adamw_tensor{};
+        out[i].param = L.P + at, out[i].grad = L.G + at;
+        out[i].n = (int64_t)n;
+        out[i].weight_decay = i >= 2 && i % 2 == 0 ? weight_decay : 0.0f;  // (frequencies and phases; then matrix, bias, matrix, ...)
+    }
+    return 22 + (h.ws ? train_head_tensors(d, h, weight_decay, out + 22) : 0);
 }
 
 hipError_t train_refold_embed(const Dims &d, void *workspace, void *packed, PackedWeights *pw, hipStream_t s)

@@ -29,16 +29,6 @@ extern "C" __attribute__((visibility("default"))) int tig_debug_phase_clocks_bac
 
 namespace {
 
-__device__ inline int row_of_entry_tr(const QuerySet &qs, int i, int entries)
-{
-    int s = qs.slot[i];
-    if (s < 0) {
-        const int rep = -s - 1;
-        s = rep < entries ? qs.slot[rep] : 0;
-    }
-    return s >= 0 && s < entries ? s : 0;
-}
-
 // ------------------------------------------------------------------------------------------
 // One wavefront per event, sixteen consecutive events per workgroup.  y = W_a emb_src + W_b emb_other + b1 comes from
 // the per-row halves that the forward pass left; d y goes to the source's row of DA and the other's row
@@ -322,6 +312,8 @@ k_tr_back(StepArgs a, PackedWeights w, TrainArrays t, BackParams p)
 #pragma unroll
         for (int o = 0; o < TR::kOut; ++o) {
             const int row = TR::row(o), q = row_q[row];
+            if (t.demb_x && q >= 0 && q < neg_row0 && col < p.E)
+                d[o] += (float)t.demb_x[(size_t)q * p.E + col];
             ((float *)(X + (size_t)row * p.row_bytes))[2 * p.Ek + col] = d[o];
             if (q >= 0 && col < p.E)
                 t.DEMB[(size_t)q * p.E + col] = d[o];

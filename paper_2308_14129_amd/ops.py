@@ -9,7 +9,7 @@ from ctypes import POINTER, Structure, byref, c_double, c_float, c_int32, c_int6
 
 from . import tig
 
-ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+ACTIVATIONS = tig.ACTIVATIONS
 
 
 class tig_linear(Structure):

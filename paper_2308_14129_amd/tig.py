@@ -74,12 +74,27 @@ class tig_out(Structure):
                 ("is_winner", c_void_p)]
 
 
+class tig_train_head(Structure):
+    _fields_ = [("struct_size", c_uint32), ("activation", c_int32), ("first_node", c_int64), ("num_items", c_int64),
+                ("weight", c_float), ("reserved", c_int32), ("W", c_void_p), ("c", c_void_p), ("items", c_void_p),
+                ("item_bias", c_void_p)]
+
+
+class tig_train_adamw(Structure):
+    _fields_ = [("struct_size", c_uint32), ("state_bits", c_int32), ("beta1", c_double), ("beta2", c_double),
+                ("eps", c_double), ("weight_decay", c_float), ("max_norm", c_float)]
+
+
+HEAD_NAMES = ("W", "c", "items", "item_bias")
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+
 EXPORTS = ("tig_workspace_bytes", "tig_init", "tig_step", "tig_step_static", "tig_step_profiled", "tig_reset", "tig_state_export",
            "tig_state_import", "tig_destroy", "tig_strerror", "tig_last_error", "tig_launch_info",
            "tig_train_workspace_bytes", "tig_train_attach", "tig_train_step", "tig_train_get",
            "tig_modules_workspace_bytes", "tig_modules_attach",
            "tig_linear_workspace_bytes", "tig_linear_forward", "tig_linear_backward", "tig_softmax_ce_workspace_bytes",
-           "tig_softmax_ce_run", "tig_adamw_workspace_bytes", "tig_adamw_create", "tig_adamw_step", "tig_adamw_destroy")
+           "tig_train_head_workspace_bytes", "tig_train_head_attach", "tig_train_head_get", "tig_train_adamw_workspace_bytes",
+           "tig_train_adamw_attach", "tig_softmax_ce_run", "tig_adamw_workspace_bytes", "tig_adamw_create", "tig_adamw_step", "tig_adamw_destroy")
 
 _lib = None
 
@@ -126,8 +141,14 @@ def load_library() -> ctypes.CDLL:
     lib.tig_modules_attach.argtypes = [c_void_p, POINTER(tig_modules), POINTER(tig_weights), c_void_p, c_size_t]
     lib.tig_modules_workspace_bytes.restype = ctypes.c_int
     lib.tig_modules_attach.restype = ctypes.c_int
-    for n in ("tig_workspace_bytes", "tig_init", "tig_step", "tig_step_static", "tig_step_profiled", "tig_reset", "tig_state_export",
-              "tig_state_import", "tig_launch_info", "tig_train_workspace_bytes", "tig_train_attach", "tig_train_step",
+    lib.tig_train_head_workspace_bytes.argtypes = [POINTER(tig_config), POINTER(tig_train_head), POINTER(c_size_t)]
+    lib.tig_train_head_attach.argtypes = [c_void_p, POINTER(tig_train_head), c_void_p, c_size_t]
+    lib.tig_train_head_get.argtypes = [c_void_p, c_int32, POINTER(tig_train_head)]
+    lib.tig_train_adamw_workspace_bytes.argtypes = [c_void_p, POINTER(tig_train_adamw), POINTER(c_size_t)]
+    lib.tig_train_adamw_attach.argtypes = [c_void_p, POINTER(tig_train_adamw), c_void_p, c_size_t]
+    for n in ("tig_train_head_workspace_bytes", "tig_train_head_attach", "tig_train_head_get", "tig_train_adamw_workspace_bytes",
+              "tig_train_adamw_attach", "tig_workspace_bytes", "tig_init", "tig_step", "tig_step_static", "tig_step_profiled", "tig_reset",
+              "tig_state_export", "tig_state_import", "tig_launch_info", "tig_train_workspace_bytes", "tig_train_attach", "tig_train_step",
               "tig_train_get"):
         getattr(lib, n).restype = ctypes.c_int
     _lib = lib
@@ -303,6 +324,43 @@ class TigContext:
         w = tig_weights(ctypes.sizeof(tig_weights), 0, *[arrs[k].ctypes.data for k in WEIGHT_NAMES])
         self._check(self.lib.tig_train_get(self.handle, {"weights": 0, "grads": 1}[what], ctypes.byref(w)))
         return arrs
+
+    def train_head_attach(self, head: dict, first_node: int, activation="gelu", weight=1.0):
+        """Allocates the workspace of a ranking head over the candidates first_node .. (a row of head["items"] each) and
+        attaches it: head has W [E x E], c [E], items [num_items x E], item_bias [num_items]."""
+        torch = self._torch
+        if activation not in ACTIVATIONS:
+            raise TigError(TIG_EINVAL, f"activation {activation!r} is none of {', '.join(ACTIVATIONS)}")
+        want = {"W": (self.E, self.E), "c": (self.E,), "items": (head["items"].shape[0], self.E), "item_bias": (head["items"].shape[0],)}
+        for k, shape in want.items():
+            if tuple(head[k].shape) != shape or str(head[k].dtype).split(".")[-1] != "float32":
+                raise TigError(TIG_EINVAL, f"head[{k!r}] is not a float32 array of shape {shape}")
+        h = tig_train_head(ctypes.sizeof(tig_train_head), ACTIVATIONS[activation], first_node, want["items"][0], weight, 0,
+                           *[_addr(head[k]) for k in HEAD_NAMES])
+        n = c_size_t(0)
+        self._check(self.lib.tig_train_head_workspace_bytes(ctypes.byref(self.cfg), ctypes.byref(h), ctypes.byref(n)))
+        ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+        self._check(self.lib.tig_train_head_attach(self.handle, ctypes.byref(h), ws.data_ptr(), n.value))
+        self.head_ws, self._head_shapes = ws, want
+
+    def train_head_get(self, what: str) -> dict:
+        """The head's parameters ("weights") or the last step's gradients ("grads") as host arrays."""
+        if not getattr(self, "_head_shapes", None):
+            raise TigError(TIG_EINVAL, "no ranking head is attached")
+        arrs = {k: np.empty(self._head_shapes[k], dtype=np.float32) for k in HEAD_NAMES}
+        h = tig_train_head(ctypes.sizeof(tig_train_head), 0, 0, 0, 0.0, 0, *[arrs[k].ctypes.data for k in HEAD_NAMES])
+        self._check(self.lib.tig_train_head_get(self.handle, {"weights": 0, "grads": 1}[what], ctypes.byref(h)))
+        return arrs
+
+    def train_adamw_attach(self, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, max_norm=0.0, state_bits=32):
+        """AdamW in place of SGD for the training steps (the model's weights and an attached head's parameters)."""
+        torch = self._torch
+        c = tig_train_adamw(ctypes.sizeof(tig_train_adamw), state_bits, betas[0], betas[1], eps, weight_decay, max_norm)
+        n = c_size_t(0)
+        self._check(self.lib.tig_train_adamw_workspace_bytes(self.handle, ctypes.byref(c), ctypes.byref(n)))
+        ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+        self._check(self.lib.tig_train_adamw_attach(self.handle, ctypes.byref(c), ws.data_ptr(), n.value))
+        self.adamw_ws = ws
 
     def step_raw(self, batch: tig_batch, out: tig_out) -> int:
         return self.lib.tig_step(self.handle, ctypes.byref(batch), ctypes.byref(out))
