@@ -318,6 +318,14 @@ hipError_t launch_gemm_tile(const GemmPlan &plan, GemmArgs<T> g, const Epi &epi,
     return hipGetLastError();
 }
 
+template <class Epi>
+hipError_t launch_join(const float *part, int splits, int64_t M, int64_t N, int64_t ldp, const Epi &epi, hipStream_t s)
+{
+    const int64_t blocks = (M * ((N + 3) / 4) + 255) / 256;
+    hipLaunchKernelGGL((k_gemm_join<Epi>), dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, s, part, splits, M, N, ldp, epi);
+    return hipGetLastError();
+}
+
 // part: plan.part_bytes of device memory (16-byte aligned), if any
 template <typename T, Form FA, Form FB, class Epi>
 hipError_t launch_gemm(const GemmPlan &plan, const T *A, int64_t lda, const T *B, int64_t ldb, int64_t M, int64_t N, int64_t K, void *part,
@@ -331,19 +339,13 @@ hipError_t launch_gemm(const GemmPlan &plan, const T *A, int64_t lda, const T *B
                    : plan.tile == 128 ? launch_gemm_tile<T, FA, FB, Epi, 128, 128, 2, 2>(plan, g, epi, s)
                                       : launch_gemm_tile<T, FA, FB, Epi, 64, 64, 2, 2>(plan, g, epi, s);
     if constexpr (!Epi::kWhole)
-        if (e == hipSuccess && plan.splits > 1) {
-            const int64_t items = M * ((N + 3) / 4), blocks = (items + 255) / 256;
-            hipLaunchKernelGGL((k_gemm_join<Epi>), dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, s, (const float *)part,
-                               plan.splits, M, N, g.ldp, epi);
-            e = hipGetLastError();
-        }
+        if (e == hipSuccess && plan.splits > 1)
+            e = launch_join((const float *)part, plan.splits, M, N, g.ldp, epi, s);
     return e;
 }
 
-// dst[rows x ld_dst] = src, the columns from `cols` to ld_dst zero; rows with keep[2 * row] == 0 zero (keep may be NULL).
-// dst is 16-byte aligned and ld_dst whole 16-byte pieces.
-hipError_t launch_pack(const void *src, int64_t ld_src, void *dst, int64_t ld_dst, int64_t rows, int64_t cols, int elem, const float *keep,
-                       hipStream_t s);
+// dst[rows x ld_dst] = src, the columns from `cols` to ld_dst zero.  dst is 16-byte aligned and ld_dst whole 16-byte pieces.
+hipError_t launch_pack(const void *src, int64_t ld_src, void *dst, int64_t ld_dst, int64_t rows, int64_t cols, int elem, hipStream_t s);
 // rows of zeros
 hipError_t launch_zero_rows(void *dst, int64_t ld, int64_t rows, int64_t cols, int elem, hipStream_t s);
 // out[n] = alpha * scale (if not NULL) * sum over b < blocks of sums[b * lds + n], added in double

@@ -47,7 +47,7 @@ namespace {
 
 // A thread takes one 16-byte piece of dst.
 template <typename E>
-__global__ void __launch_bounds__(256) k_pack(const E *src, int64_t ld_src, E *dst, int64_t ld_dst, int64_t rows, int64_t cols, const float *keep)
+__global__ void __launch_bounds__(256) k_pack(const E *src, int64_t ld_src, E *dst, int64_t ld_dst, int64_t rows, int64_t cols)
 {
     constexpr int per = 16 / (int)sizeof(E);
     const int64_t pieces = ld_dst / per, items = rows * pieces;
@@ -56,11 +56,10 @@ __global__ void __launch_bounds__(256) k_pack(const E *src, int64_t ld_src, E *d
         struct alignas(16) Piece {
             E v[per];
         } q;
-        const bool on = !keep || keep[2 * r] != 0.0f;
         const E *p = src + r * ld_src + c;
 #pragma unroll
         for (int e = 0; e < per; ++e)
-            q.v[e] = on && c + e < cols ? p[e] : (E)0;
+            q.v[e] = c + e < cols ? p[e] : (E)0;
         *(Piece *)(dst + r * ld_dst + c) = q;
     }
 }
@@ -87,17 +86,16 @@ hipError_t launch_zero_rows(void *dst, int64_t ld, int64_t rows, int64_t cols, i
     return hipGetLastError();
 }
 
-hipError_t launch_pack(const void *src, int64_t ld_src, void *dst, int64_t ld_dst, int64_t rows, int64_t cols, int elem, const float *keep,
-                       hipStream_t s)
+hipError_t launch_pack(const void *src, int64_t ld_src, void *dst, int64_t ld_dst, int64_t rows, int64_t cols, int elem, hipStream_t s)
 {
     const int64_t items = rows * (ld_dst * elem / 16), blocks = (items + 255) / 256;
     if (items == 0)
         return hipSuccess;
     const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384));
     if (elem == 4)
-        hipLaunchKernelGGL((k_pack<uint32_t>), grid, dim3(256), 0, s, (const uint32_t *)src, ld_src, (uint32_t *)dst, ld_dst, rows, cols, keep);
+        hipLaunchKernelGGL((k_pack<uint32_t>), grid, dim3(256), 0, s, (const uint32_t *)src, ld_src, (uint32_t *)dst, ld_dst, rows, cols);
     else
-        hipLaunchKernelGGL((k_pack<uint16_t>), grid, dim3(256), 0, s, (const uint16_t *)src, ld_src, (uint16_t *)dst, ld_dst, rows, cols, keep);
+        hipLaunchKernelGGL((k_pack<uint16_t>), grid, dim3(256), 0, s, (const uint16_t *)src, ld_src, (uint16_t *)dst, ld_dst, rows, cols);
     return hipGetLastError();
 }
 

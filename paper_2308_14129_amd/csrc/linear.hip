@@ -312,11 +312,11 @@ hipError_t forward(const tig_linear &p, const LinearPlan &L, char *ws, hipStream
         int64_t ldx = p.ldx, ldw = p.ldw;
         hipError_t e = hipSuccess;
         if (L.pack_x) {
-            e = launch_pack(x, ldx, ws + L.px, L.ld_px, p.rows, p.in_dim, es, nullptr, s);
+            e = launch_pack(x, ldx, ws + L.px, L.ld_px, p.rows, p.in_dim, es, s);
             x = (const T *)(ws + L.px), ldx = L.ld_px;
         }
         if (e == hipSuccess && L.pack_w) {
-            e = launch_pack(w, ldw, ws + L.pw, L.ld_pw, p.out_dim, p.in_dim, es, nullptr, s);
+            e = launch_pack(w, ldw, ws + L.pw, L.ld_pw, p.out_dim, p.in_dim, es, s);
             w = (const T *)(ws + L.pw), ldw = L.ld_pw;
         }
         return e != hipSuccess ? e : launch_gemm<T, kRow, kRow>(L.y, x, ldx, w, ldw, p.rows, p.out_dim, p.in_dim, ws + L.part, epi, s);
@@ -357,7 +357,7 @@ hipError_t backward(const tig_linear &p, const LinearPlan &L, char *ws, hipStrea
         const T *w = (const T *)p.w;
         int64_t ldw = p.ldw;
         if (L.pack_w) {
-            e = launch_pack(w, ldw, ws + L.pw, L.ld_pw, p.out_dim, p.in_dim, es, nullptr, s);
+            e = launch_pack(w, ldw, ws + L.pw, L.ld_pw, p.out_dim, p.in_dim, es, s);
             w = (const T *)(ws + L.pw), ldw = L.ld_pw;
         }
         const EpiStore<T> epi = {(T *)p.dx, p.lddx, nullptr, 1.0f, four_aligned(p.dx, p.lddx, es)};
@@ -370,7 +370,7 @@ hipError_t backward(const tig_linear &p, const LinearPlan &L, char *ws, hipStrea
         const T *x = (const T *)p.x;
         int64_t ldx = p.ldx;
         if (L.pack_x) {
-            e = launch_pack(x, ldx, ws + L.px, L.ld_px, p.rows, p.in_dim, es, nullptr, s);
+            e = launch_pack(x, ldx, ws + L.px, L.ld_px, p.rows, p.in_dim, es, s);
             x = (const T *)(ws + L.px), ldx = L.ld_px;
         }
         const EpiStore<T> epi = {(T *)p.dw, p.lddw, nullptr, 1.0f, four_aligned(p.dw, p.lddw, es)};

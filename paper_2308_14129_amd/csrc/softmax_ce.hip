@@ -5,7 +5,9 @@
 //   gradient     for one piece of the vocabulary after the other: the logits once more, P = w_i (exp(l - lse) - [label]) in their
 //                epilogue, and two tile products, dX += P W and dW = P^T X.  A piece of P stays within the last-level cache.
 // s_i = S w_i with S the largest |s_i|: P holds values of at most 1, the products are scaled by S afterwards.
+// Rows of at most 128 columns in 16-bit types go the way of ce_narrow.h.
 #include "act.h"
+#include "ce_narrow.h"
 #include "gemm.h"
 
 namespace tig {
@@ -13,12 +15,12 @@ namespace tig {
 namespace {
 
 struct CeHead {
-    float S;         // largest |s_i|
-    int32_t counted; // rows that count
+    float S;  // largest |s_i|
 };
-// what the epilogue of P needs of a row: lse (+infinity: no probabilities) and w_i * P's scale
+// what the epilogue of P needs of a row: lse (+infinity: no probabilities), w_i * P's scale, the label (-1: ignored)
 struct CeRow {
     float lse, w;
+    int32_t label;
 };
 
 template <typename T>
@@ -35,35 +37,54 @@ __device__ inline float exp_of(float x)
         return __expf(x);
 }
 
-// number of rows that count and the largest |s_i|
-__global__ void __launch_bounds__(1024) k_ce_head(const int32_t *labels, const float *row_scale, float scale, int64_t rows, int64_t vocab, CeHead *head)
+// the largest |s_i| where rows have weights of their own
+__global__ void __launch_bounds__(1024) k_ce_top(const int32_t *labels, const float *row_scale, float scale, int64_t rows, int64_t vocab, CeHead *head)
 {
-    __shared__ int n_of[16];
     __shared__ float top_of[16];
-    int n = 0;
     float top = 0.0f;
-    for (int64_t i = threadIdx.x; i < rows; i += 1024) {
-        const int32_t label = labels[i];
-        if (label >= 0 && label < vocab) {
-            ++n;
-            if (row_scale)
-                top = fmaxf(top, fabsf(row_scale[i]));
-        }
-    }
-    for (int d = 32; d > 0; d >>= 1) {
-        n += __shfl_xor(n, d);
+    for (int64_t i = threadIdx.x; i < rows; i += 1024)
+        if (labels[i] >= 0 && labels[i] < vocab)
+            top = fmaxf(top, fabsf(row_scale[i]));
+    for (int d = 32; d > 0; d >>= 1)
         top = fmaxf(top, __shfl_xor(top, d));
-    }
     if (lane_id() == 0)
-        n_of[wave_id()] = n, top_of[wave_id()] = top;
+        top_of[wave_id()] = top;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < 16; ++w) {
-            n += n_of[w];
+        for (int w = 1; w < 16; ++w)
             top = fmaxf(top, top_of[w]);
+        head->S = top * fabsf(scale);
+    }
+}
+
+// number of rows that count; their mean loss, in double, always in the same order; S without weights
+__global__ void __launch_bounds__(1024) k_ce_mean(const float *loss, const int32_t *labels, int64_t rows, int64_t vocab, bool weighted, float scale,
+                                                  CeHead *head, float *mean)
+{
+    __shared__ double part[1024];
+    __shared__ int count[1024];
+    double total = 0.0;
+    int n = 0;
+    for (int64_t i = threadIdx.x; i < rows; i += 1024) {
+        total += (double)loss[i];
+        n += labels[i] >= 0 && labels[i] < vocab;
+    }
+    part[threadIdx.x] = total;
+    count[threadIdx.x] = n;
+    __syncthreads();
+    for (int d = 512; d > 0; d >>= 1) {
+        if ((int)threadIdx.x < d) {
+            part[threadIdx.x] += part[threadIdx.x + d];
+            count[threadIdx.x] += count[threadIdx.x + d];
         }
-        head->counted = n;
-        head->S = row_scale ? top * fabsf(scale) : fabsf(scale) / (float)(n > 0 ? n : 1);
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) {
+        n = count[0] > 0 ? count[0] : 1;
+        if (mean)
+            *mean = (float)(part[0] / (double)n);
+        if (!weighted)
+            head->S = fabsf(scale) / (float)n;
     }
 }
 
@@ -132,11 +153,22 @@ struct EpiStats {
     }
 };
 
-// Sixteen rows per workgroup, sixteen threads each: the tiles' parts joined, the label's logit, loss.
+// Sixteen rows per workgroup, sixteen threads each: the tiles' parts joined, the label's logit, loss; for the gradient the row's
+// record, or the tables that ce_narrow.h streams (whole tiles: rows behind the last take no part), and the row itself where it
+// counts, else zeros: whatever it holds, P^T X does not see it.
+template <typename T>
+struct CeRowsOut {
+    float *loss, *lse;
+    CeRow *rec;
+    float *lse2, *w;   // narrow
+    int32_t *label;
+    T *x0;
+    int64_t ld_x0;
+};
 template <typename T>
 __global__ void __launch_bounds__(256) k_ce_rows(const float2 *part, int64_t tiles, int64_t rows, const T *x, int64_t ldx, const T *w, int64_t ldw,
                                                  const T *bias, int64_t dim, int64_t vocab, const int32_t *labels, const float *row_scale, float scale,
-                                                 const CeHead *head, float *loss, float *lse_out, CeRow *rec, float *label_logit)
+                                                 const CeHead *head, CeRowsOut<T> out)
 {
     const int64_t i = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
     const int t = threadIdx.x % 16;
@@ -162,64 +194,115 @@ __global__ void __launch_bounds__(256) k_ce_rows(const float2 *part, int64_t til
         top = to;
         dot += __shfl_xor(dot, d);
     }
-    if (!on || t != 0)
+    if (on && out.x0)  // (rows of x are whole 16-byte pieces here)
+        for (int64_t c = t * Mat<T>::kPer16; c < out.ld_x0; c += 16 * Mat<T>::kPer16) {
+            const intx4 v = counts && c < dim ? *(const intx4 *)(xr + c) : intx4{0, 0, 0, 0};
+            *(intx4 *)(out.x0 + i * out.ld_x0 + c) = v;
+        }
+    if (t != 0)
         return;
     const float lse = top == -INFINITY && sum == 0.0f ? -INFINITY : top + logf(sum);
-    if (bias && counts)
-        dot += to_float(bias[label]);
-    if (lse_out)
-        lse_out[i] = lse;
-    if (loss)
-        loss[i] = !counts ? 0.0f : (dot == -INFINITY ? INFINITY : lse - dot);
-    if (rec) {
-        float wi = 0.0f;
-        if (counts)
-            wi = row_scale ? (head->S > 0.0f ? row_scale[i] * scale / head->S : 0.0f) : (scale < 0.0f ? -1.0f : 1.0f);
-        rec[i] = CeRow{wi != 0.0f && lse != -INFINITY ? lse : INFINITY, wi * kPScale<T>};
-        label_logit[i] = dot;
+    if (on) {
+        if (bias && counts)
+            dot += to_float(bias[label]);
+        if (out.lse)
+            out.lse[i] = lse;
+        if (out.loss)
+            out.loss[i] = !counts ? 0.0f : (dot == -INFINITY ? INFINITY : lse - dot);
+    }
+    if (!out.rec && !out.lse2)
+        return;
+    float wi = 0.0f;
+    if (on && counts)
+        wi = row_scale ? (head->S > 0.0f ? row_scale[i] * scale / head->S : 0.0f) : (scale < 0.0f ? -1.0f : 1.0f);
+    const bool none = wi == 0.0f || lse == -INFINITY;
+    if (out.rec) {
+        if (on)
+            out.rec[i] = CeRow{none ? INFINITY : lse, wi * kPScale<T>, wi != 0.0f ? label : -1};
+    } else {
+        constexpr float shift = sizeof(T) == 2 && kPScale<T> != 1.0f ? 14.0f : 0.0f;
+        out.lse2[i] = none ? INFINITY : lse * kLog2e - shift;
+        out.w[i] = wi;
+        out.label[i] = wi != 0.0f ? label : -1;
     }
 }
 
-// P of a piece of the vocabulary, columns up to a whole 16-byte piece zero (the label's place: k_ce_labels)
+// P of a piece of the vocabulary from v0 on, columns up to a whole 16-byte piece zero; sums: the column sums of P over the tile's
+// rows, before rounding (over a lane's rows, the sixteen lanes of a column, and the wavefronts on top of each other).
 template <typename T>
 struct EpiP {
-    static constexpr bool kWhole = false;
+    static constexpr bool kWhole = true;
     const T *bias;
     bool bias_ok;
     const CeRow *rec;
     T *P;
-    int64_t ldp;
-    __device__ inline CeRow row(int64_t m) const { return rec[m]; }
-    __device__ inline void operator()(const CeRow &r, int64_t m, int64_t n, floatx4 v, int left) const
+    int64_t ldp, v0;
+    float *sums;  // [tiles_m][ldp] or NULL
+    template <int BM, int BN, int WM, int WN, int FM, int FN>
+    __device__ inline void tile(const TileAt &at, floatx4 (&acc)[FM][FN], char *smem) const
     {
-        if (bias)
-            v += load_four(bias + n, left, bias_ok);
+        const int lane = lane_id(), i16 = lane % 16, g = lane / 16;
+        const int64_t end = (at.N + Mat<T>::kPer16 - 1) / Mat<T>::kPer16 * Mat<T>::kPer16;
+        floatx4 b[FN];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            v[e] = e < left && r.lse != INFINITY ? exp_of<T>(v[e] - r.lse) * r.w : 0.0f;
-        store_four(P + m * ldp + n, v, 4, true);
+        for (int j = 0; j < FN; ++j) {
+            const int64_t n = at.n0 + j * 16 + 4 * g;
+            const int left = at.N - n < 4 ? (at.N > n ? (int)(at.N - n) : 0) : 4;
+            b[j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (bias)
+                b[j] = load_four(bias + n, left, bias_ok);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                b[j][e] = e < left ? b[j][e] : -INFINITY;
+        }
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int64_t m = at.m0 + i * 16 + i16;
+            const bool on = m < at.M;
+            const CeRow r = rec[on ? m : 0];
+            const float lse = on ? r.lse : INFINITY;
+            const int64_t hot = on ? (int64_t)r.label - v0 - at.n0 - 4 * g : -1;  // (of this lane's columns 16 j + e)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float p = lse != INFINITY ? exp_of<T>(acc[i][j][e] + b[j][e] - lse) : 0.0f;
+                    p -= hot == 16 * j + e && r.label >= 0 ? 1.0f : 0.0f;
+                    acc[i][j][e] = p * r.w;
+                }
+                const int64_t n = at.n0 + j * 16 + 4 * g;
+                if (on && n < end)
+                    store_four(P + m * ldp + n, acc[i][j], 4, true);
+            }
+        }
+        if (!sums)
+            return;
+        float *const red = (float *)smem;  // [WM][BN]
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            floatx4 total = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+                if (at.m0 + i * 16 + i16 < at.M)
+                    total += acc[i][j];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                total[e] = row_sum_all(total[e]);
+            if (i16 == 0)
+                *(floatx4 *)(red + at.wm * BN + at.wn * (BN / WN) + j * 16 + 4 * g) = total;
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < BN; c += 64 * WM * WN) {
+            float total = red[c];
+#pragma unroll
+            for (int w = 1; w < WM; ++w)
+                total += red[w * BN + c];
+            const int64_t n = (int64_t)at.tn * BN + c;
+            if (n < at.N)
+                sums[(int64_t)at.tm * ldp + n] = total;
+        }
     }
 };
-
-// P at the labels of the piece [v0, v0 + vc), and the zeros behind its last column up to a whole 16-byte piece
-template <typename T>
-__global__ void __launch_bounds__(256) k_ce_labels(T *P, int64_t ldp, int64_t rows, int64_t v0, int64_t vc, const int32_t *labels, const CeRow *rec,
-                                                   const float *label_logit)
-{
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= rows)
-        return;
-    constexpr int64_t per = Mat<T>::kPer16;
-    for (int64_t c = (vc + 3) / 4 * 4; c < (vc + per - 1) / per * per; ++c)
-        P[i * ldp + c] = (T)0.0f;
-    const int64_t c = (int64_t)labels[i] - v0;
-    const CeRow r = rec[i];
-    if (c >= 0 && c < vc && r.w != 0.0f) {
-        const float l = label_logit[i];
-        const float p = r.lse == INFINITY || l == -INFINITY ? 0.0f : expf(l - r.lse);
-        P[i * ldp + c] = (T)((p - 1.0f) * r.w);
-    }
-}
 
 // a piece's share of dX: stored, or added to the pieces before it
 struct EpiAdd {
@@ -247,38 +330,29 @@ __global__ void __launch_bounds__(256) k_ce_dx(const float *acc, int64_t ld, int
     }
 }
 
-// column sums of a piece of P over blocks of rows, eight columns per thread
-constexpr int kSumRows = 64;
+// narrow rows: dX = S w_i (sum of P W over all ranges)
 template <typename T>
-__global__ void __launch_bounds__(256) k_ce_sums(const T *P, int64_t ldp, int64_t rows, int64_t vc, int64_t per, float *sums, int64_t lds)
+__global__ void __launch_bounds__(256) k_ce_narrow_dx(const float *grad, int splits, int64_t ld, int64_t rows, int64_t dim, const float *weight,
+                                                      const CeHead *head, float alpha, T *dx, int64_t lddx, bool aligned)
 {
-    const int64_t n = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (n >= vc)
-        return;
-    const int64_t m0 = (int64_t)blockIdx.y * per, m1 = m0 + per < rows ? m0 + per : rows;
-    floatx4 total = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int64_t per = (dim + 3) / 4;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * per; i += (int64_t)gridDim.x * 256) {
+        const int64_t m = i / per, n = i % per * 4;
+        floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 8
-    for (int64_t m = m0; m < m1; ++m)
-        total += load_four(P + m * ldp + n, 4, true);
-    *(floatx4 *)(sums + (int64_t)blockIdx.y * lds + n) = total;
+        for (int s = 0; s < splits; ++s)
+            v += *(const floatx4 *)(grad + ((int64_t)s * rows + m) * ld + n);
+        store_four(dx + m * lddx + n, v * (alpha * head->S * weight[m]), dim - n < 4 ? (int)(dim - n) : 4, aligned);
+    }
 }
 
-// mean of the rows that count, in double, always in the same order
-__global__ void __launch_bounds__(1024) k_ce_mean(const float *loss, int64_t rows, const CeHead *head, float *mean)
+// a bias in fp32, -infinity behind its last (whole tiles)
+template <typename T>
+__global__ void __launch_bounds__(256) k_ce_bias(const T *bias, int64_t vocab, float *out, int64_t all)
 {
-    __shared__ double part[1024];
-    double total = 0.0;
-    for (int64_t i = threadIdx.x; i < rows; i += 1024)
-        total += (double)loss[i];
-    part[threadIdx.x] = total;
-    __syncthreads();
-    for (int d = 512; d > 0; d >>= 1) {
-        if ((int)threadIdx.x < d)
-            part[threadIdx.x] += part[threadIdx.x + d];
-        __syncthreads();
-    }
-    if (threadIdx.x == 0)
-        *mean = (float)(part[0] / (double)(head && head->counted > 0 ? head->counted : 1));
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < all)
+        out[i] = i < vocab ? to_float(bias[i]) : -INFINITY;
 }
 
 inline size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
@@ -290,8 +364,14 @@ struct CePlan {
     GemmPlan stat;
     int64_t piece;           // candidates of a piece
     GemmPlan logits, dx, dw;
-    int64_t ldp, ld_acc, sum_per, sum_blocks;
+    int64_t ldp, ld_acc;
     bool acc;                // more than one piece: dX in fp32 first
+    // narrow rows
+    int kb;                  // 32-column blocks of a row (0: not narrow)
+    int64_t own_rows, own_cands;  // tiles of own rows
+    int s_stat, s_dx, s_dw;  // ranges of the streamed rows
+    int64_t row_tiles, cand_tiles;  // whole tiles of 64
+    size_t bias32, lse2, weight;
     size_t head, loss, rec, label, part, px, pw, px0, P, dxa, join, sums;
     size_t bytes;
 };
@@ -324,6 +404,34 @@ CePlan ce_plan(const tig_softmax_ce &p)
         L.px = take((size_t)n * L.ld_x * es);
     if (L.pack_w)
         L.pw = take((size_t)V * L.ld_w * es);
+    if (es == 2 && d <= 128) {
+        L.kb = d <= 64 ? 2 : 4;
+        const int64_t tile = L.kb == 2 ? kNarrowTile<2> : kNarrowTile<4>;
+        L.own_rows = (n + tile - 1) / tile, L.own_cands = (V + tile - 1) / tile;
+        L.row_tiles = (n + kNarrowStream - 1) / kNarrowStream, L.cand_tiles = (V + kNarrowStream - 1) / kNarrowStream;
+        L.s_stat = L.s_dx = narrow_splits(L.own_rows, V);
+        L.s_dw = narrow_splits(L.own_cands, n);
+        L.stat_rows = n;
+        L.part = take((size_t)L.s_stat * n * sizeof(float2));
+        if (p.bias)
+            L.bias32 = take((size_t)L.cand_tiles * kNarrowStream * 4);
+        if (L.grad) {
+            const size_t tab = (size_t)L.row_tiles * kNarrowStream * 4;
+            L.lse2 = take(tab);
+            L.weight = take(tab);
+            L.label = take(tab);
+            L.px0 = take((size_t)n * L.ld_x * es);
+            L.ld_acc = (d + 3) / 4 * 4;
+            if (p.dx)
+                L.dxa = take((size_t)L.s_dx * n * L.ld_acc * 4);
+            if (p.dw && L.s_dw > 1)
+                L.join = take((size_t)L.s_dw * V * L.ld_acc * 4);
+            if (p.dbias)
+                L.sums = take((size_t)L.s_dw * V * 4);
+        }
+        L.bytes = off;
+        return L;
+    }
     L.stat = gemm_plan(n, V, d, es, false);
     const int64_t tiles = (V + L.stat.tile - 1) / L.stat.tile;
     int64_t most = (int64_t)(kStatBytes / 8) / tiles / 256 * 256;
@@ -333,7 +441,6 @@ CePlan ce_plan(const tig_softmax_ce &p)
     L.part = take((size_t)L.stat_rows * tiles * sizeof(float2));
     if (L.grad) {
         L.rec = take(sizeof(CeRow) * (size_t)n);
-        L.label = take(4 * (size_t)n);
         int64_t piece = (int64_t)(kPieceBytes / es) / n / 256 * 256;
         if (piece < 256)
             piece = 256;
@@ -353,10 +460,8 @@ CePlan ce_plan(const tig_softmax_ce &p)
         if (p.dw && L.dw.part_bytes > join)
             join = L.dw.part_bytes;
         L.join = take(join);
-        L.sum_per = n <= (int64_t)kSumRows * 32768 ? kSumRows : (n + 32767) / 32768;
-        L.sum_blocks = (n + L.sum_per - 1) / L.sum_per;
         if (p.dbias)
-            L.sums = take((size_t)L.sum_blocks * L.ldp * 4);
+            L.sums = take((size_t)((n + L.logits.tile - 1) / L.logits.tile) * L.ldp * 4);
     }
     L.bytes = off;
     return L;
@@ -392,9 +497,94 @@ int check_ce(const tig_softmax_ce *p)
     } while (0)
 
 template <typename T>
+hipError_t launch_rows(const tig_softmax_ce &p, int64_t r, int64_t m, const float2 *part, int64_t tiles, const T *x, int64_t ldx, const T *w, int64_t ldw,
+                       const CeHead *head, const CeRowsOut<T> &out, hipStream_t s)
+{
+    const int64_t all = out.lse2 ? (m + kNarrowStream - 1) / kNarrowStream * kNarrowStream : m;
+    hipLaunchKernelGGL((k_ce_rows<T>), dim3((unsigned)((all + 15) / 16)), dim3(256), 0, s, part, tiles, m, x + r * ldx, ldx, w, ldw, (const T *)p.bias, p.dim,
+                       p.vocab, p.labels + r, p.row_scale ? p.row_scale + r : nullptr, p.scale, head, out);
+    return hipGetLastError();
+}
+
+hipError_t launch_mean(const tig_softmax_ce &p, const float *loss, CeHead *head, hipStream_t s)
+{
+    hipLaunchKernelGGL(k_ce_mean, dim3(1), dim3(1024), 0, s, loss, p.labels, p.rows, p.vocab, p.row_scale != nullptr, p.scale, head, p.mean);
+    return hipGetLastError();
+}
+
+// 16-bit rows of at most 32 KB columns; x and w are rows of whole 16-byte pieces
+template <typename T, int KB>
+hipError_t run_narrow(const tig_softmax_ce &p, const CePlan &L, char *ws, const T *x, int64_t ldx, const T *w, int64_t ldw, const CeRowsOut<T> &out,
+                      hipStream_t s)
+{
+    const int64_t n = p.rows, V = p.vocab;
+    CeHead *const head = (CeHead *)(ws + L.head);
+    const float alpha = 1.0f / kPScale<T>;
+    float *bias32 = nullptr;
+    if (p.bias) {
+        bias32 = (float *)(ws + L.bias32);
+        const int64_t all = L.cand_tiles * kNarrowStream;
+        hipLaunchKernelGGL((k_ce_bias<T>), dim3((unsigned)((all + 255) / 256)), dim3(256), 0, s, (const T *)p.bias, V, bias32, all);
+        CE_TRY(hipGetLastError());
+    }
+    const dim3 threads(64 * kNarrowWaves);
+    NarrowArgs<T> a = {};
+    a.own = x, a.ld_own = ldx, a.n_own = n;
+    a.stream = w, a.ld_stream = ldw, a.n_stream = V;
+    a.d = (int)p.dim;
+    a.stream_add = bias32;
+    a.splits = L.s_stat, a.per = (L.cand_tiles + L.s_stat - 1) / L.s_stat;
+    a.part = (float2 *)(ws + L.part);
+    hipLaunchKernelGGL((k_narrow_stats<T, KB>), dim3((unsigned)(L.own_rows * L.s_stat)), threads, 0, s, a);
+    CE_TRY(hipGetLastError());
+    CE_TRY(launch_rows(p, 0, n, a.part, L.s_stat, x, ldx, w, ldw, head, out, s));
+    CE_TRY(launch_mean(p, out.loss, head, s));
+    if (!L.grad)
+        return hipSuccess;
+    a.own = out.x0, a.ld_own = out.ld_x0;
+    a.ld_grad = L.ld_acc;
+    a.p_scale = kPScale<T>;
+    if (p.dx) {
+        a.splits = L.s_dx, a.per = (L.cand_tiles + L.s_dx - 1) / L.s_dx;
+        a.lse2_own = out.lse2;
+        a.labels = out.label;
+        a.grad = (float *)(ws + L.dxa);
+        hipLaunchKernelGGL((k_narrow_grad<T, KB, false, false>), dim3((unsigned)(L.own_rows * L.s_dx)), threads, 0, s, a);
+        CE_TRY(hipGetLastError());
+        const int64_t blocks = (n * ((p.dim + 3) / 4) + 255) / 256;
+        hipLaunchKernelGGL((k_ce_narrow_dx<T>), dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, s, a.grad, L.s_dx, a.ld_grad, n, p.dim,
+                           out.w, head, alpha, (T *)p.dx, p.lddx, four_aligned(p.dx, p.lddx, 2));
+        CE_TRY(hipGetLastError());
+    }
+    if (p.dw || p.dbias) {
+        a.own = w, a.ld_own = ldw, a.n_own = V;
+        a.stream = out.x0, a.ld_stream = out.ld_x0, a.n_stream = n;
+        a.own_add = bias32, a.stream_add = nullptr;
+        a.lse2_stream = out.lse2, a.w_stream = out.w, a.labels = out.label;
+        a.splits = L.s_dw, a.per = (L.row_tiles + L.s_dw - 1) / L.s_dw;
+        a.grad = p.dw && L.s_dw > 1 ? (float *)(ws + L.join) : nullptr;
+        a.sums = p.dbias ? (float *)(ws + L.sums) : nullptr;
+        const EpiStore<T> store = {(T *)p.dw, p.lddw, &head->S, alpha, four_aligned(p.dw, p.lddw, 2)};
+        if (p.dw && L.s_dw == 1)
+            a.direct = store;
+        const dim3 grid((unsigned)(L.own_cands * L.s_dw));
+        if (p.row_scale || p.scale < 0.0f)
+            hipLaunchKernelGGL((k_narrow_grad<T, KB, true, true>), grid, threads, 0, s, a);
+        else
+            hipLaunchKernelGGL((k_narrow_grad<T, KB, true, false>), grid, threads, 0, s, a);
+        CE_TRY(hipGetLastError());
+        if (p.dw && L.s_dw > 1)
+            CE_TRY(launch_join(a.grad, L.s_dw, V, p.dim, a.ld_grad, store, s));
+        if (p.dbias)
+            CE_TRY((launch_join_sums<T>(a.sums, V, L.s_dw, V, (T *)p.dbias, &head->S, alpha, s)));
+    }
+    return hipSuccess;
+}
+
+template <typename T>
 hipError_t run(const tig_softmax_ce &p, const CePlan &L, char *ws, hipStream_t s)
 {
-    const int es = sizeof(T);
+    constexpr int es = sizeof(T);
     const int64_t n = p.rows, V = p.vocab, d = p.dim;
     CeHead *const head = (CeHead *)(ws + L.head);
     if (n == 0) {
@@ -408,69 +598,69 @@ hipError_t run(const tig_softmax_ce &p, const CePlan &L, char *ws, hipStream_t s
     }
     const T *x = (const T *)p.x, *w = (const T *)p.w, *bias = (const T *)p.bias;
     int64_t ldx = p.ldx, ldw = p.ldw;
-    hipLaunchKernelGGL(k_ce_head, dim3(1), dim3(1024), 0, s, p.labels, p.row_scale, p.scale, n, V, head);
-    CE_TRY(hipGetLastError());
+    if (p.row_scale && L.grad) {
+        hipLaunchKernelGGL(k_ce_top, dim3(1), dim3(1024), 0, s, p.labels, p.row_scale, p.scale, n, V, head);
+        CE_TRY(hipGetLastError());
+    }
     if (L.pack_x) {
-        CE_TRY(launch_pack(x, ldx, ws + L.px, L.ld_x, n, d, es, nullptr, s));
+        CE_TRY(launch_pack(x, ldx, ws + L.px, L.ld_x, n, d, es, s));
         x = (const T *)(ws + L.px), ldx = L.ld_x;
     }
     if (L.pack_w) {
-        CE_TRY(launch_pack(w, ldw, ws + L.pw, L.ld_w, V, d, es, nullptr, s));
+        CE_TRY(launch_pack(w, ldw, ws + L.pw, L.ld_w, V, d, es, s));
         w = (const T *)(ws + L.pw), ldw = L.ld_w;
     }
-    const bool bias_ok = four_aligned(bias, 4, es);
     float *const loss = p.loss ? p.loss : (float *)(ws + L.loss);
-    CeRow *const rec = L.grad ? (CeRow *)(ws + L.rec) : nullptr;
-    float *const label = L.grad ? (float *)(ws + L.label) : nullptr;
+    CeRowsOut<T> out = {};
+    out.loss = loss, out.lse = p.lse;
+    if (L.grad && L.kb)
+        out.lse2 = (float *)(ws + L.lse2), out.w = (float *)(ws + L.weight), out.label = (int32_t *)(ws + L.label);
+    else if (L.grad)
+        out.rec = (CeRow *)(ws + L.rec);
+    if (L.grad && (L.kb || p.dw))
+        out.x0 = (T *)(ws + L.px0), out.ld_x0 = L.ld_x;
+    if constexpr (es == 2)
+        if (L.kb)
+            return L.kb == 2 ? run_narrow<T, 2>(p, L, ws, x, ldx, w, ldw, out, s) : run_narrow<T, 4>(p, L, ws, x, ldx, w, ldw, out, s);
+    const bool bias_ok = four_aligned(bias, 4, es);
     float2 *const part = (float2 *)(ws + L.part);
     const int64_t tiles = (V + L.stat.tile - 1) / L.stat.tile;
     for (int64_t r = 0; r < n; r += L.stat_rows) {
         const int64_t m = n - r < L.stat_rows ? n - r : L.stat_rows;
         const EpiStats<T> epi = {bias, bias_ok, part, m};
         CE_TRY((launch_gemm<T, kRow, kRow>(L.stat, x + r * ldx, ldx, w, ldw, m, V, d, nullptr, epi, s)));
-        hipLaunchKernelGGL((k_ce_rows<T>), dim3((unsigned)((m + 15) / 16)), dim3(256), 0, s, part, tiles, m, x + r * ldx, ldx, w, ldw, bias, d, V,
-                           p.labels + r, p.row_scale ? p.row_scale + r : nullptr, p.scale, head, loss + r, p.lse ? p.lse + r : nullptr,
-                           rec ? rec + r : nullptr, label ? label + r : nullptr);
-        CE_TRY(hipGetLastError());
+        CeRowsOut<T> o = out;
+        o.loss += r;
+        o.lse = o.lse ? o.lse + r : nullptr;
+        o.rec = o.rec ? o.rec + r : nullptr;
+        o.x0 = o.x0 ? o.x0 + r * o.ld_x0 : nullptr;
+        CE_TRY(launch_rows(p, r, m, part, tiles, x, ldx, w, ldw, head, o, s));
     }
-    if (p.mean) {
-        hipLaunchKernelGGL(k_ce_mean, dim3(1), dim3(1024), 0, s, loss, n, head, p.mean);
-        CE_TRY(hipGetLastError());
-    }
+    CE_TRY(launch_mean(p, loss, head, s));
     if (!L.grad)
         return hipSuccess;
     const float alpha = 1.0f / kPScale<T>;
     T *const P = (T *)(ws + L.P);
-    const T *x0 = nullptr;  // rows that do not count as zeros: whatever they hold, P^T X does not see it
-    if (p.dw) {
-        CE_TRY(launch_pack(x, ldx, ws + L.px0, L.ld_x, n, d, es, &rec->w, s));
-        x0 = (const T *)(ws + L.px0);
-    }
     for (int64_t v0 = 0; v0 < V; v0 += L.piece) {
         const int64_t vc = V - v0 < L.piece ? V - v0 : L.piece;
-        const EpiP<T> epi = {bias ? bias + v0 : nullptr, bias && four_aligned(bias + v0, 4, es), rec, P, L.ldp};
+        float *const sums = p.dbias ? (float *)(ws + L.sums) : nullptr;
+        const EpiP<T> epi = {bias ? bias + v0 : nullptr, bias && four_aligned(bias + v0, 4, es), out.rec, P, L.ldp, v0, sums};
         CE_TRY((launch_gemm<T, kRow, kRow>(L.logits, x, ldx, w + v0 * ldw, ldw, n, vc, d, nullptr, epi, s)));
-        hipLaunchKernelGGL((k_ce_labels<T>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, P, L.ldp, n, v0, vc, p.labels, rec, label);
-        CE_TRY(hipGetLastError());
-        if (p.dbias) {
-            hipLaunchKernelGGL((k_ce_sums<T>), dim3((unsigned)((vc + 1023) / 1024), (unsigned)L.sum_blocks), dim3(256), 0, s, P, L.ldp, n, vc, L.sum_per,
-                               (float *)(ws + L.sums), L.ldp);
-            CE_TRY(hipGetLastError());
-            CE_TRY((launch_join_sums<T>((const float *)(ws + L.sums), L.ldp, L.sum_blocks, vc, (T *)p.dbias + v0, &head->S, alpha, s)));
-        }
+        if (p.dbias)
+            CE_TRY((launch_join_sums<T>(sums, L.ldp, (n + L.logits.tile - 1) / L.logits.tile, vc, (T *)p.dbias + v0, &head->S, alpha, s)));
         if (p.dx) {
             if (L.acc) {
                 const EpiAdd add = {(float *)(ws + L.dxa), L.ld_acc, v0 == 0};
                 CE_TRY((launch_gemm<T, kRow, kCol>(L.dx, P, L.ldp, w + v0 * ldw, ldw, n, d, vc, ws + L.join, add, s)));
             } else {
-                const EpiStore<T> out = {(T *)p.dx, p.lddx, &head->S, alpha, four_aligned(p.dx, p.lddx, es)};
-                CE_TRY((launch_gemm<T, kRow, kCol>(L.dx, P, L.ldp, w, ldw, n, d, vc, ws + L.join, out, s)));
+                const EpiStore<T> store = {(T *)p.dx, p.lddx, &head->S, alpha, four_aligned(p.dx, p.lddx, es)};
+                CE_TRY((launch_gemm<T, kRow, kCol>(L.dx, P, L.ldp, w, ldw, n, d, vc, ws + L.join, store, s)));
             }
         }
         if (p.dw) {
             T *const dw = (T *)p.dw + v0 * p.lddw;
-            const EpiStore<T> out = {dw, p.lddw, &head->S, alpha, four_aligned(dw, p.lddw, es)};
-            CE_TRY((launch_gemm<T, kCol, kCol>(L.dw, P, L.ldp, x0, L.ld_x, vc, d, n, ws + L.join, out, s)));
+            const EpiStore<T> store = {dw, p.lddw, &head->S, alpha, four_aligned(dw, p.lddw, es)};
+            CE_TRY((launch_gemm<T, kCol, kCol>(L.dw, P, L.ldp, out.x0, L.ld_x, vc, d, n, ws + L.join, store, s)));
         }
     }
     if (p.dx && L.acc) {

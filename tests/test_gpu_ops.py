@@ -285,6 +285,45 @@ def test_softmax_ce_in_several_pieces(dtype):
     check_ce(20_000, 4000, 40, dtype, seed=13)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("weighted,scale", [(False, 1.0), (True, 1.0), (False, -2.0), (True, -0.5)])
+def test_softmax_ce_narrow_rows(dtype, weighted, scale):
+    # 16-bit rows of at most 128 columns: around their tiles of 64 streamed and 192 or 256 own rows, and ranges of several tiles
+    for i, shape in enumerate([(64, 64, 64), (65, 129, 65), (1000, 70, 128), (193, 4000, 127), (257, 900, 24), (2, 20_000, 100), (3000, 3, 8)]):
+        check_ce(*shape, dtype, bias=i % 2 == 0, weighted=weighted, scale=scale * (512 if dtype == "fp16" else 1), seed=60 + i, masked=0)
+
+
+def test_softmax_ce_wide_rows_in_several_pieces():
+    check_ce(20_000, 4000, 136, "bf16", seed=14)
+    check_ce(9000, 9000, 160, "fp16", seed=15, scale=1024.0, weighted=True)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_softmax_ce_only_some_gradients(dtype):
+    """Through the C entry: every subset of the gradients is what the whole set has."""
+    import ctypes
+    from ctypes import byref, c_size_t
+    gen = gen_of(23)
+    t = TYPES[dtype]
+    lib = ops._lib()
+    for n, V, d in ((90, 400, 100), (300, 130, 200), (2000, 300, 64)):
+        x, w, b = rnd(gen, n, d, dtype=t), rnd(gen, V, d, std=0.2, dtype=t), rnd(gen, V, dtype=t)
+        labels = torch.randint(0, V, (n,), device=DEV, generator=gen, dtype=torch.int32)
+        full = ops.softmax_ce(x, w, labels, b)
+        for which in range(1, 8):
+            out = [torch.full_like(q, 7.0) if which >> k & 1 else None for k, q in enumerate((x, w, b))]
+            p = ops.tig_softmax_ce(ctypes.sizeof(ops.tig_softmax_ce), {"fp32": 0, "bf16": 1, "fp16": 2}[dtype], n, V, d)
+            p.x, p.w, p.bias, p.labels, p.scale = x.data_ptr(), w.data_ptr(), b.data_ptr(), labels.data_ptr(), 1.0
+            p.ldx = p.ldw = p.lddx = p.lddw = d
+            p.dx, p.dw, p.dbias = [q.data_ptr() if q is not None else None for q in out]
+            need = c_size_t(0)
+            assert lib.tig_softmax_ce_workspace_bytes(byref(p), byref(need)) == 0
+            ws = torch.empty(need.value, dtype=torch.uint8, device=DEV)
+            assert lib.tig_softmax_ce_run(byref(p), ws.data_ptr(), need.value, torch.cuda.current_stream().cuda_stream) == 0
+            for q, want in zip(out, (full.dx, full.dw, full.dbias)):
+                assert q is None or torch.equal(q, want), (n, V, d, which)
+
+
 def test_softmax_ce_rows_left_out_take_no_part():
     gen = gen_of(17)
     for t in (torch.float32, torch.bfloat16):
