@@ -3,11 +3,12 @@
 // The tensors are cut into chunks of 4096 elements, one workgroup each, listed once in the workspace: one launch whatever their
 // number.  Bound by memory: every element's parameter and states are read and written once, its gradient read once, and once
 // more where the norm is wanted.
-//   k_adamw_norm    a chunk's sum of squares, in double
-//   k_adamw_begin   joins them; the step's numbers (clip coefficient, bias corrections), the counter
+//   k_adamw_norm    sums of squares, in double (only with clipping)
+//   k_adamw_begin   the step's numbers: clip coefficient, bias corrections, counter; for up to 1024 chunks the update's workgroups
+//                   form them themselves
 //   k_adamw_update  the step
-// 8-bit states: a wavefront takes 256 elements, four per lane, the block that shares a power of two: scales are exact, and
-// values that do not change keep their code whatever the rest of their block does.
+// 8-bit states: a wavefront takes the 256 elements that share a power of two, four per lane: scales are exact, and values that
+// do not change keep their code whatever the rest of their block does.
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -20,25 +21,26 @@ namespace tig {
 namespace {
 
 constexpr int kChunk = 4096, kStateBlock = 256, kAdamThreads = 256;
+constexpr int kAtOnce = 4 * kAdamThreads;     // elements of a workgroup, four of a lane
+constexpr int kRounds = kChunk / kAtOnce;     // of a chunk: all of its loads are on their way at once
+constexpr int kNormGroups = 2048;             // workgroups that form the norm, at most
+constexpr int64_t kFewChunks = 1024;          // up to here the update forms the step's numbers itself, the norm from at most
+constexpr int kFewGroups = 256;               // as many partial sums
 
-struct AdamTensor {
+// 4096 elements of a tensor: where they lie.  (All of it in one record: from it to the data is one round trip.)
+struct AdamChunk {
     void *param;
     const void *grad;
     float *master;
     void *m, *v;
     float *m_scale, *v_scale;
-    int64_t n;
+    int32_t n;
     int32_t dtype;
-    int32_t wide;  // four elements at once, of every array
     float decay;
-    int32_t pad;
+    int32_t wide;  // four elements at once, of every array
 };
 
-struct AdamChunk {
-    int32_t tensor, index;
-};
-
-// what k_adamw_begin leaves for the update
+// the step's numbers
 struct AdamNow {
     float c, step_size, root_scale, lr;
     uint32_t t;
@@ -46,26 +48,47 @@ struct AdamNow {
 };
 
 struct AdamParams {
-    const AdamTensor *tensors;
     const AdamChunk *chunks;
-    double *part;
+    double *part;       // [kNormGroups]
     AdamNow *now;
+    uint32_t *arrived;  // workgroups that are done with a launch; zero between launches
     int64_t *step;
     int64_t n_chunks;
+    int n_parts;        // of `part`
     double beta1, beta2, lr, grad_scale, max_norm;
     float b1, o1, b2, o2, eps;
     float *norm_out;
 };
 
+// The step's numbers: what follows from the norm (0 without clipping) ...
+__device__ inline void scale_by_norm(const AdamParams &p, double norm, AdamNow &now)
+{
+    now.skip = p.max_norm > 0.0 && !(norm < INFINITY);
+    double c = p.grad_scale;
+    if (p.max_norm > 0.0 && norm > p.max_norm)
+        c *= p.max_norm / norm;
+    now.c = (float)c;
+}
+// ... and from the number of the step.  (Half of a small update's time where each workgroup forms them after the norm.)
+__device__ inline AdamNow numbers(const AdamParams &p, int64_t t)
+{
+    AdamNow now = {};
+    now.lr = (float)p.lr;
+    now.step_size = (float)(p.lr / (1.0 - pow(p.beta1, (double)t)));
+    now.root_scale = (float)(1.0 / sqrt(1.0 - pow(p.beta2, (double)t)));
+    now.t = (uint32_t)t;
+    return now;
+}
+
 template <typename T>
-__device__ inline double squares(const T *g, int64_t n, bool wide)
+__device__ inline double squares(const T *g, int n, bool wide)
 {
     double total = 0.0;
 #pragma unroll
-    for (int u = 0; u < kChunk / (4 * kAdamThreads); ++u) {
-        const int64_t i = ((int64_t)u * kAdamThreads + threadIdx.x) * 4;
+    for (int u = 0; u < kChunk / kAtOnce; ++u) {
+        const int i = u * kAtOnce + (int)threadIdx.x * 4;
         if (i < n) {
-            const floatx4 v = load_four(g + i, n - i < 4 ? (int)(n - i) : 4, wide);
+            const floatx4 v = load_four(g + i, n - i < 4 ? n - i : 4, wide);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 total += (double)v[e] * (double)v[e];
@@ -74,54 +97,55 @@ __device__ inline double squares(const T *g, int64_t n, bool wide)
     return total;
 }
 
-__global__ void __launch_bounds__(kAdamThreads) k_adamw_norm(AdamParams p)
+// the workgroup's sum of its threads' values, for every thread
+__device__ inline double group_sum(double v)
 {
     __shared__ double part[kAdamThreads / kWave];
-    const AdamChunk ch = p.chunks[blockIdx.x];
-    const AdamTensor t = p.tensors[ch.tensor];
-    const int64_t at = (int64_t)ch.index * kChunk, n = t.n - at < kChunk ? t.n - at : kChunk;
-    double total = t.dtype == TIG_F32    ? squares((const float *)t.grad + at, n, t.wide)
-                   : t.dtype == TIG_BF16 ? squares((const __bf16 *)t.grad + at, n, t.wide)
-                                         : squares((const _Float16 *)t.grad + at, n, t.wide);
     for (int d = 32; d > 0; d >>= 1)
-        total += __shfl_xor(total, d);
+        v += __shfl_xor(v, d);
     if (lane_id() == 0)
-        part[wave_id()] = total;
+        part[wave_id()] = v;
     __syncthreads();
-    if (threadIdx.x == 0)
-        p.part[blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
+    return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-__global__ void __launch_bounds__(1024) k_adamw_begin(AdamParams p)
+// sums of squares in double, and the numbers that do not need them
+__global__ void __launch_bounds__(kAdamThreads) k_adamw_norm(AdamParams p)
 {
-    __shared__ double part[1024];
-    double norm = 0.0;
-    if (p.max_norm > 0.0) {
-        double total = 0.0;
-        for (int64_t i = threadIdx.x; i < p.n_chunks; i += 1024)
-            total += p.part[i];
-        part[threadIdx.x] = total;
-        __syncthreads();
-        for (int d = 512; d > 0; d >>= 1) {
-            if ((int)threadIdx.x < d)
-                part[threadIdx.x] += part[threadIdx.x + d];
-            __syncthreads();
-        }
-        norm = fabs(p.grad_scale) * sqrt(part[0]);
+    double total = 0.0;
+    if (blockIdx.x == 0 && threadIdx.x == 0)
+        *p.now = numbers(p, *p.step + 1);
+    AdamChunk next = p.chunks[blockIdx.x];
+    for (int64_t c = blockIdx.x; c < p.n_chunks; c += gridDim.x) {
+        const AdamChunk ch = next;
+        next = p.chunks[c + gridDim.x < p.n_chunks ? c + gridDim.x : c];
+        total += ch.dtype == TIG_F32    ? squares((const float *)ch.grad, ch.n, ch.wide)
+                 : ch.dtype == TIG_BF16 ? squares((const __bf16 *)ch.grad, ch.n, ch.wide)
+                                        : squares((const _Float16 *)ch.grad, ch.n, ch.wide);
     }
+    total = group_sum(total);
+    if (threadIdx.x == 0)
+        p.part[blockIdx.x] = total;
+}
+
+// the norm from the partial sums, always in the same order
+__device__ inline double norm_of(const AdamParams &p)
+{
+    double total = 0.0;
+    for (int i = threadIdx.x; i < p.n_parts; i += kAdamThreads)
+        total += p.part[i];
+    return fabs(p.grad_scale) * sqrt(group_sum(total));
+}
+
+// the step's numbers and the counter, ahead of an update of many chunks
+__global__ void __launch_bounds__(kAdamThreads) k_adamw_begin(AdamParams p)
+{
+    const double norm = p.max_norm > 0.0 ? norm_of(p) : 0.0;
     if (threadIdx.x != 0)
         return;
-    AdamNow now = {};
-    now.skip = p.max_norm > 0.0 && !(norm < INFINITY);
     const int64_t t = *p.step + 1;
-    double c = p.grad_scale;
-    if (p.max_norm > 0.0 && norm > p.max_norm)
-        c *= p.max_norm / norm;
-    now.c = (float)c;
-    now.lr = (float)p.lr;
-    now.step_size = (float)(p.lr / (1.0 - pow(p.beta1, (double)t)));
-    now.root_scale = (float)(1.0 / sqrt(1.0 - pow(p.beta2, (double)t)));
-    now.t = (uint32_t)t;
+    AdamNow now = numbers(p, t);
+    scale_by_norm(p, norm, now);
     *p.now = now;
     if (!now.skip)
         *p.step = t;
@@ -129,14 +153,18 @@ __global__ void __launch_bounds__(1024) k_adamw_begin(AdamParams p)
         *p.norm_out = (float)norm;
 }
 
+// the largest over the wavefront
 __device__ inline float wave_top(float v)
 {
-    for (int d = 32; d > 0; d >>= 1)
-        v = fmaxf(v, __shfl_xor(v, d));
-    return v;
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x121, 0xf, 0xf, true)));
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x122, 0xf, 0xf, true)));
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x124, 0xf, 0xf, true)));
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xf, 0xf, true)));
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
 }
 
-// four values as e4m3 times the block's power of two; u: the thresholds
+// four values as e4m3 times their block's power of two; u: the thresholds
 __device__ inline uint32_t to_8bit(const floatx4 &x, float top, const floatx4 &u, bool positive, float *scale)
 {
     const int e0 = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) - 8 : 0;
@@ -154,17 +182,13 @@ __device__ inline uint32_t to_8bit(const floatx4 &x, float top, const floatx4 &u
             r = copysignf(r, x[i]);
         q[i] = r;
     }
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
+    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w, true);
 }
 __device__ inline floatx4 from_8bit(uint32_t w, float scale)
 {
-    floatx4 v;
-    v[0] = __builtin_amdgcn_cvt_f32_fp8((int)w, 0) * scale;
-    v[1] = __builtin_amdgcn_cvt_f32_fp8((int)w, 1) * scale;
-    v[2] = __builtin_amdgcn_cvt_f32_fp8((int)w, 2) * scale;
-    v[3] = __builtin_amdgcn_cvt_f32_fp8((int)w, 3) * scale;
-    return v;
+    return floatx4{__builtin_amdgcn_cvt_f32_fp8((int)w, 0) * scale, __builtin_amdgcn_cvt_f32_fp8((int)w, 1) * scale,
+                   __builtin_amdgcn_cvt_f32_fp8((int)w, 2) * scale, __builtin_amdgcn_cvt_f32_fp8((int)w, 3) * scale};
 }
 __device__ inline uint32_t load_bytes(const uint8_t *p, int left, bool wide)
 {
@@ -188,103 +212,134 @@ __device__ inline void store_bytes(uint8_t *p, uint32_t w, int left, bool wide)
     }
 }
 
-// A wavefront's 256 elements from i on; products and sums in the order of the formulas, each rounded: a state's code does not
-// depend on what the compiler joins.
-template <typename T, int BITS>
-__device__ inline void update_block(const AdamParams &p, const AdamTensor &t, const AdamNow &now, int64_t block, float keep)
+// A lane's fours of a chunk; numbers(): the step's, once the loads are on their way.  Products and sums in the order of the formulas, each rounded: a state's code does not depend
+// on what the compiler joins.  A wavefront's four times 64 elements of a round are a block of 256.
+template <typename T, int BITS, bool WIDE, class F>
+__device__ inline void update_chunk(const AdamParams &p, const AdamChunk &ch, const F &numbers)
 {
 #pragma clang fp contract(off)
-    const int lane = lane_id();
-    const int64_t i = block * kStateBlock + lane * 4;
-    const int left = t.n - i < 4 ? (t.n > i ? (int)(t.n - i) : 0) : 4;
-    const bool wide = t.wide != 0;
-    const floatx4 g0 = load_four((const T *)t.grad + i, left, wide);
-    floatx4 x = t.master ? load_four(t.master + i, left, wide) : load_four((const T *)t.param + i, left, wide);
-    floatx4 m, v;
-    if constexpr (BITS == 32) {
-        m = load_four((const float *)t.m + i, left, wide);
-        v = load_four((const float *)t.v + i, left, wide);
-    } else {
-        m = from_8bit(load_bytes((const uint8_t *)t.m + i, left, wide), t.m_scale[block]);
-        v = from_8bit(load_bytes((const uint8_t *)t.v + i, left, wide), t.v_scale[block]);
+    floatx4 g[kRounds], x[kRounds], m[kRounds], v[kRounds];
+    uint32_t wm[kRounds], wv[kRounds];
+    float sm[kRounds], sv[kRounds];
+    const int i0 = (int)threadIdx.x * 4;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            v[e] = v[e] * v[e];
-    }
-    floatx4 root;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const float g = g0[e] * now.c;
-        const float ma = m[e] * p.b1, mb = g * p.o1;
-        m[e] = ma + mb;
-        const float gg = g * g;
-        const float va = v[e] * p.b2, vb = gg * p.o2;
-        v[e] = va + vb;
-        root[e] = sqrtf(v[e]);
-        x[e] = x[e] * keep - now.step_size * (m[e] / (root[e] * now.root_scale + p.eps));
-    }
-    if (t.master)
-        store_four(t.master + i, x, left, wide);
-    store_four((T *)t.param + i, x, left, wide);
-    if constexpr (BITS == 32) {
-        store_four((float *)t.m + i, m, left, wide);
-        store_four((float *)t.v + i, v, left, wide);
-    } else {
-        float top_m = 0.0f, top_r = 0.0f;
-        floatx4 um, ur;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            top_m = fmaxf(top_m, e < left ? fabsf(m[e]) : 0.0f);
-            top_r = fmaxf(top_r, e < left ? root[e] : 0.0f);
-            const uint32_t h = (uint32_t)(lane * 4 + e) * 0x6A09E667u + now.t * 0x9E3779B9u;
-            um[e] = (float)(h >> 8) * 0x1p-24f;
-            ur[e] = (float)((h + 0x80000000u) >> 8) * 0x1p-24f;
-        }
-        float sm, sv;
-        const uint32_t qm = to_8bit(m, wave_top(top_m), um, false, &sm), qr = to_8bit(root, wave_top(top_r), ur, true, &sv);
-        store_bytes((uint8_t *)t.m + i, qm, left, wide);
-        store_bytes((uint8_t *)t.v + i, qr, left, wide);
-        if (lane == 0) {
-            t.m_scale[block] = sm;
-            t.v_scale[block] = sv;
+    for (int r = 0; r < kRounds; ++r) {
+        const int i = i0 + r * kAtOnce, left = WIDE || ch.n - i >= 4 ? 4 : (ch.n > i ? ch.n - i : 0);
+        g[r] = load_four((const T *)ch.grad + i, left, WIDE);
+        x[r] = ch.master ? load_four(ch.master + i, left, WIDE) : load_four((const T *)ch.param + i, left, WIDE);
+        if constexpr (BITS == 32) {
+            m[r] = load_four((const float *)ch.m + i, left, WIDE);
+            v[r] = load_four((const float *)ch.v + i, left, WIDE);
+        } else {
+            const int block = left > 0 ? i / kStateBlock : 0;
+            wm[r] = load_bytes((const uint8_t *)ch.m + i, left, WIDE);
+            wv[r] = load_bytes((const uint8_t *)ch.v + i, left, WIDE);
+            sm[r] = ch.m_scale[block];
+            sv[r] = ch.v_scale[block];
         }
     }
-}
-
-template <typename T, int BITS>
-__device__ inline void update_chunk(const AdamParams &p, const AdamTensor &t, const AdamNow &now, int64_t chunk)
-{
-    const float keep = 1.0f - now.lr * t.decay;
-    const int64_t blocks = (t.n + kStateBlock - 1) / kStateBlock, first = chunk * (kChunk / kStateBlock);
-#pragma unroll 2
-    for (int u = 0; u < kChunk / kStateBlock / (kAdamThreads / kWave); ++u) {
-        const int64_t b = first + u * (kAdamThreads / kWave) + wave_id_uniform();
-        if (b < blocks)
-            update_block<T, BITS>(p, t, now, b, keep);
-    }
-}
-
-template <int BITS>
-__global__ void __launch_bounds__(kAdamThreads) k_adamw_update(AdamParams p)
-{
-    const AdamNow now = *p.now;
+    const AdamNow now = numbers();
     if (now.skip)
         return;
+    const float keep = 1.0f - now.lr * ch.decay;
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const int i = i0 + r * kAtOnce, left = WIDE || ch.n - i >= 4 ? 4 : (ch.n > i ? ch.n - i : 0);
+        if constexpr (BITS == 8) {
+            m[r] = from_8bit(wm[r], sm[r]);
+            v[r] = from_8bit(wv[r], sv[r]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[r][e] = v[r][e] * v[r][e];
+        }
+        floatx4 root;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float q = g[r][e] * now.c;
+            const float ma = m[r][e] * p.b1, mb = q * p.o1;
+            m[r][e] = ma + mb;
+            const float qq = q * q;
+            const float va = v[r][e] * p.b2, vb = qq * p.o2;
+            v[r][e] = va + vb;
+            root[e] = sqrtf(v[r][e]);
+            x[r][e] = x[r][e] * keep - now.step_size * (m[r][e] / (root[e] * now.root_scale + p.eps));
+        }
+        if (ch.master)
+            store_four(ch.master + i, x[r], left, WIDE);
+        store_four((T *)ch.param + i, x[r], left, WIDE);
+        if constexpr (BITS == 32) {
+            store_four((float *)ch.m + i, m[r], left, WIDE);
+            store_four((float *)ch.v + i, v[r], left, WIDE);
+        } else {
+            float top_m = 0.0f, top_r = 0.0f, a, b;
+            floatx4 um, ur;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                top_m = fmaxf(top_m, e < left ? fabsf(m[r][e]) : 0.0f);
+                top_r = fmaxf(top_r, e < left ? root[e] : 0.0f);
+                const uint32_t h = (uint32_t)(i % kStateBlock + e) * 0x6A09E667u + now.t * 0x9E3779B9u;
+                um[e] = (float)(h >> 8) * 0x1p-24f;
+                ur[e] = (float)((h + 0x80000000u) >> 8) * 0x1p-24f;
+            }
+            const uint32_t qm = to_8bit(m[r], wave_top(top_m), um, false, &a), qr = to_8bit(root, wave_top(top_r), ur, true, &b);
+            store_bytes((uint8_t *)ch.m + i, qm, left, WIDE);
+            store_bytes((uint8_t *)ch.v + i, qr, left, WIDE);
+            if (left > 0 && lane_id() == 0) {
+                ch.m_scale[i / kStateBlock] = a;
+                ch.v_scale[i / kStateBlock] = b;
+            }
+        }
+    }
+}
+
+// FEW: every workgroup forms the step's numbers, the last one to finish counts the step (the others have read the counter)
+template <int BITS, bool FEW>
+__global__ void __launch_bounds__(kAdamThreads) k_adamw_update(AdamParams p)
+{
     const AdamChunk ch = p.chunks[blockIdx.x];
-    const AdamTensor t = p.tensors[ch.tensor];
-    if (t.dtype == TIG_F32)
-        update_chunk<float, BITS>(p, t, now, ch.index);
-    else if (t.dtype == TIG_BF16)
-        update_chunk<__bf16, BITS>(p, t, now, ch.index);
+    AdamNow now;
+    int64_t t = 0;
+    auto form = [&]() -> AdamNow {
+        if constexpr (FEW) {
+            t = *p.step + 1;
+            now = p.max_norm > 0.0 ? *p.now : numbers(p, t);  // (uniform; of k_adamw_norm)
+            const double norm = p.max_norm > 0.0 ? norm_of(p) : 0.0;
+            scale_by_norm(p, norm, now);
+            if (p.norm_out && p.max_norm > 0.0 && blockIdx.x == 0 && threadIdx.x == 0)
+                *p.norm_out = (float)norm;
+        } else {
+            now = *p.now;
+        }
+        return now;
+    };
+    auto update = [&](auto type) {
+        using T = decltype(type);
+        if (ch.wide && ch.n == kChunk)  // (uniform)
+            update_chunk<T, BITS, true>(p, ch, form);
+        else
+            update_chunk<T, BITS, false>(p, ch, form);
+    };
+    if (ch.dtype == TIG_F32)
+        update(float());
+    else if (ch.dtype == TIG_BF16)
+        update(__bf16());
     else
-        update_chunk<_Float16, BITS>(p, t, now, ch.index);
+        update(_Float16());
+    if constexpr (FEW) {
+        __syncthreads();
+        if (threadIdx.x == 0 && atomicAdd(p.arrived, 1u) == gridDim.x - 1) {
+            *p.arrived = 0u;
+            if (!now.skip)
+                *p.step = t;
+        }
+    }
 }
 
 inline size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 
 struct AdamLayout {
     int64_t n_chunks;
-    size_t tensors, chunks, part, now, bytes;
+    size_t chunks, part, now, arrived, bytes;
 };
 
 AdamLayout adam_layout(const tig_adamw_tensor *t, int64_t n)
@@ -298,9 +353,9 @@ AdamLayout adam_layout(const tig_adamw_tensor *t, int64_t n)
         off += align_up(bytes);
         return at;
     };
-    L.tensors = take(sizeof(AdamTensor) * (size_t)n);
+    L.arrived = take(sizeof(uint32_t));
     L.chunks = take(sizeof(AdamChunk) * (size_t)L.n_chunks);
-    L.part = take(sizeof(double) * (size_t)L.n_chunks);
+    L.part = take(sizeof(double) * kNormGroups);  // (from here on nothing is laid out)
     L.now = take(sizeof(AdamNow));
     L.bytes = off;
     return L;
@@ -376,23 +431,24 @@ int tig_adamw_create(const tig_adamw_config *cfg, const tig_adamw_tensor *tensor
     if (workspace_bytes < L.bytes)
         return fail_text(TIG_ENOSPACE, "tig_adamw_create: workspace too small");
     tig_adamw *const opt = new (std::nothrow) tig_adamw;
-    char *const host = new (std::nothrow) char[L.part ? L.part : 1];  // tensors and chunks
+    char *const host = new (std::nothrow) char[L.part ? L.part : 1];  // the counter and the chunks
     if (!opt || !host) {
         delete opt;
         delete[] host;
         return fail_text(TIG_ENOMEM, "tig_adamw_create: out of host memory");
     }
     memset(host, 0, L.part);
-    AdamTensor *const dt = (AdamTensor *)(host + L.tensors);
     AdamChunk *ch = (AdamChunk *)(host + L.chunks);
     for (int64_t i = 0; i < n_tensors; ++i) {
         const tig_adamw_tensor &q = tensors[i];
         const int es = dtype_bytes(q.dtype), ss = cfg->state_bits == 32 ? 4 : 1;
-        dt[i] = AdamTensor{q.param, q.grad, q.master, q.m, q.v, q.m_scale, q.v_scale, q.n, q.dtype, 0, q.weight_decay, 0};
-        dt[i].wide = four_aligned(q.param, 4, es) && four_aligned(q.grad, 4, es) && four_aligned(q.master, 4, 4) && four_aligned(q.m, 4, ss) &&
-                     four_aligned(q.v, 4, ss);
-        for (int64_t c = 0; c < (q.n + kChunk - 1) / kChunk; ++c)
-            *ch++ = AdamChunk{(int32_t)i, (int32_t)c};
+        const bool wide = four_aligned(q.param, 4, es) && four_aligned(q.grad, 4, es) && four_aligned(q.master, 4, 4) && four_aligned(q.m, 4, ss) &&
+                          four_aligned(q.v, 4, ss);
+        auto at = [](const void *x, int64_t bytes) { return x ? (void *)((char *)x + bytes) : nullptr; };
+        for (int64_t c = 0; c < q.n; c += kChunk)
+            *ch++ = AdamChunk{at(q.param, c * es), at(q.grad, c * es), (float *)at(q.master, c * 4), at(q.m, c * ss), at(q.v, c * ss),
+                              (float *)at(q.m_scale, c / kStateBlock * 4), (float *)at(q.v_scale, c / kStateBlock * 4),
+                              (int32_t)(q.n - c < kChunk ? q.n - c : kChunk), q.dtype, q.weight_decay, wide ? 1 : 0};
     }
     hipStream_t s = (hipStream_t)hip_stream;
     hipError_t e = L.part ? hipMemcpyAsync(workspace, host, L.part, hipMemcpyHostToDevice, s) : hipSuccess;
@@ -406,7 +462,7 @@ int tig_adamw_create(const tig_adamw_config *cfg, const tig_adamw_tensor *tensor
     AdamParams &p = opt->p;
     memset(&p, 0, sizeof(p));
     char *const ws = (char *)workspace;
-    p.tensors = (const AdamTensor *)(ws + L.tensors);
+    p.arrived = (uint32_t *)(ws + L.arrived);
     p.chunks = (const AdamChunk *)(ws + L.chunks);
     p.part = (double *)(ws + L.part);
     p.now = (AdamNow *)(ws + L.now);
@@ -429,15 +485,24 @@ int tig_adamw_step(tig_adamw *opt, double lr, double grad_scale, double max_norm
     AdamParams p = opt->p;
     p.lr = lr, p.grad_scale = grad_scale, p.max_norm = max_norm, p.norm_out = norm_out;
     hipStream_t s = (hipStream_t)hip_stream;
-    const dim3 grid((unsigned)p.n_chunks);
-    if (max_norm > 0.0 && p.n_chunks > 0)
-        hipLaunchKernelGGL(k_adamw_norm, grid, dim3(kAdamThreads), 0, s, p);
-    hipLaunchKernelGGL(k_adamw_begin, dim3(1), dim3(max_norm > 0.0 ? 1024 : 64), 0, s, p);
-    if (p.n_chunks > 0) {
+    const dim3 grid((unsigned)p.n_chunks), threads(kAdamThreads);
+    const bool clip = max_norm > 0.0, few = p.n_chunks > 0 && p.n_chunks <= kFewChunks;
+    const int64_t most = few ? kFewGroups : kNormGroups;
+    p.n_parts = clip ? (int)(p.n_chunks < most ? p.n_chunks : most) : 0;
+    if (p.n_parts > 0)
+        hipLaunchKernelGGL(k_adamw_norm, dim3((unsigned)p.n_parts), threads, 0, s, p);
+    if (!few)
+        hipLaunchKernelGGL(k_adamw_begin, dim3(1), threads, 0, s, p);
+    if (few) {
         if (opt->bits == 8)
-            hipLaunchKernelGGL((k_adamw_update<8>), grid, dim3(kAdamThreads), 0, s, p);
+            hipLaunchKernelGGL((k_adamw_update<8, true>), grid, threads, 0, s, p);
         else
-            hipLaunchKernelGGL((k_adamw_update<32>), grid, dim3(kAdamThreads), 0, s, p);
+            hipLaunchKernelGGL((k_adamw_update<32, true>), grid, threads, 0, s, p);
+    } else if (p.n_chunks > 0) {
+        if (opt->bits == 8)
+            hipLaunchKernelGGL((k_adamw_update<8, false>), grid, threads, 0, s, p);
+        else
+            hipLaunchKernelGGL((k_adamw_update<32, false>), grid, threads, 0, s, p);
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? TIG_OK : fail_global("tig_adamw_step", e);

@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(64 * WAVES) k_linear_rows(const T *x, int64_t 
     }
 }
 
-constexpr int64_t kFewRows = 64;
+constexpr int64_t kFewRows = TIG_LINEAR_FEW_ROWS;
 
 template <typename T, int WAVES, class Epi>
 hipError_t launch_linear_rows(const tig_linear &p, const Epi &epi, hipStream_t s)

@@ -4,8 +4,11 @@ the current stream of its tensors' device and does not synchronise."""
 from __future__ import annotations
 
 import ctypes
+import struct
 from collections import namedtuple
 from ctypes import POINTER, Structure, byref, c_double, c_float, c_int32, c_int64, c_size_t, c_uint32, c_void_p
+
+import torch
 
 from . import tig
 
@@ -46,11 +49,12 @@ def _lib():
     global _ready
     if _ready is None:
         lib = tig.load_library()
-        lib.tig_linear_workspace_bytes.argtypes = [POINTER(tig_linear), c_int32, POINTER(c_size_t)]
-        lib.tig_linear_forward.argtypes = [POINTER(tig_linear), c_void_p, c_size_t, c_void_p]
-        lib.tig_linear_backward.argtypes = [POINTER(tig_linear), c_void_p, c_size_t, c_void_p]
-        lib.tig_softmax_ce_workspace_bytes.argtypes = [POINTER(tig_softmax_ce), POINTER(c_size_t)]
-        lib.tig_softmax_ce_run.argtypes = [POINTER(tig_softmax_ce), c_void_p, c_size_t, c_void_p]
+        assert ctypes.sizeof(tig_linear) == 184 and ctypes.sizeof(tig_softmax_ce) == 160  # (what linear() and softmax_ce() pack)
+        lib.tig_linear_workspace_bytes.argtypes = [c_void_p, c_int32, POINTER(c_size_t)]
+        lib.tig_linear_forward.argtypes = [c_void_p, c_void_p, c_size_t, c_void_p]
+        lib.tig_linear_backward.argtypes = [c_void_p, c_void_p, c_size_t, c_void_p]
+        lib.tig_softmax_ce_workspace_bytes.argtypes = [c_void_p, POINTER(c_size_t)]
+        lib.tig_softmax_ce_run.argtypes = [c_void_p, c_void_p, c_size_t, c_void_p]
         lib.tig_adamw_workspace_bytes.argtypes = [POINTER(tig_adamw_config), POINTER(tig_adamw_tensor), c_int64,
                                                   POINTER(c_size_t)]
         lib.tig_adamw_create.argtypes = [POINTER(tig_adamw_config), POINTER(tig_adamw_tensor), c_int64, c_void_p,
@@ -75,62 +79,59 @@ def _refuse(text):
     raise tig.TigError(tig.TIG_EINVAL, text)
 
 
-_codes = {}
+_codes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
 def _dtype_code(dtype):
-    if not _codes:
-        import torch
-        _codes.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
-    if dtype not in _codes:
+    code = _codes.get(dtype)
+    if code is None:
         _refuse(f"dtype {dtype} is none of float32, bfloat16, float16")
-    return _codes[dtype]
+    return code
 
 
-def _matrix(t, rows, cols, like, name):
+def _matrix(t, rows, cols, dtype, device, name):
     """Address and row stride of a [rows x cols] tensor whose columns are adjacent."""
     if t is None:
         return 0, 0
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.dtype != like.dtype or t.device != like.device:
-        _refuse(f"{name} is not a [{rows} x {cols}] tensor of {like.dtype} on {like.device}")
-    ld = t.stride(0) if rows > 1 else max(cols, t.stride(0))
-    if (cols > 1 and t.stride(1) != 1) or ld < cols:
+    if t.shape != (rows, cols) or t.dtype is not dtype or t.device != device:
+        _refuse(f"{name} is not a [{rows} x {cols}] tensor of {dtype} on {device}")
+    ld, step = t.stride()
+    if rows <= 1 and ld < cols:
+        ld = cols
+    if (step != 1 and cols > 1) or ld < cols:
         _refuse(f"{name}: columns have to be adjacent and rows may not overlap")
     return t.data_ptr(), ld
 
 
-def _vector(t, n, like, name, dtype=None):
+def _vector(t, n, dtype, device, name):
     if t is None:
         return 0
-    dtype = dtype or like.dtype
-    if t.dim() != 1 or t.shape[0] != n or t.dtype != dtype or t.device != like.device or (n > 1 and t.stride(0) != 1):
-        _refuse(f"{name} is not a contiguous [{n}] tensor of {dtype} on {like.device}")
+    if t.shape != (n,) or t.dtype is not dtype or t.device != device or (n > 1 and t.stride(0) != 1):
+        _refuse(f"{name} is not a contiguous [{n}] tensor of {dtype} on {device}")
     return t.data_ptr()
 
 
 class _On:
     """The device of a call's tensors made current where it is not, and its current stream."""
+    __slots__ = ("guard", "index")
 
     def __init__(self, device):
-        import torch
         if device.type != "cuda":
             _refuse(f"tensors are on {device}, not on a GPU")
-        self.guard = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
-        self.device = device
+        self.index = device.index
+        self.guard = None if device.index == torch._C._cuda_getDevice() else torch.cuda.device(device)
 
     def __enter__(self):
-        import torch
-        if self.guard:
+        if self.guard is not None:
             self.guard.__enter__()
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(self.index)
 
     def __exit__(self, *a):
-        if self.guard:
+        if self.guard is not None:
             self.guard.__exit__(*a)
 
 
 def _workspace(n, device):
-    import torch
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
 
@@ -140,60 +141,76 @@ def _activation(name):
     return ACTIVATIONS[name]
 
 
+# the structs as bytes: a small call is as long as its way to the launch
+_linear_bytes = struct.Struct("=Iiii3q10Q8q").pack
+_ce_bytes = struct.Struct("=Ii3q5Qfi6Q4q").pack
+_FEW_ROWS = 64  # TIG_LINEAR_FEW_ROWS
+
+
 def linear(x, w, bias=None, residual=None, activation="none", keep=False, out=None):
     """act(x w^T + bias) + residual for x [rows x in], w [out x in]; fp32, bf16 or fp16, sums in fp32.  With keep=True
     returns (y, z), z = x w^T + bias as linear_backward wants it.  out: where y goes (residual itself is fine)."""
-    import torch
     if x.dim() != 2 or w.dim() != 2:
         _refuse("x and w are matrices")
     rows, k = x.shape
     n = w.shape[0]
-    p = tig_linear(ctypes.sizeof(tig_linear), _dtype_code(x.dtype), _activation(activation), 0, rows, k, n)
-    p.x, p.ldx = _matrix(x, rows, k, x, "x")
-    p.w, p.ldw = _matrix(w, n, k, x, "w")
-    p.bias = _vector(bias, n, x, "bias")
-    p.residual, p.ldr = _matrix(residual, rows, n, x, "residual")
+    dtype, dev = x.dtype, x.device
+    code, act = _dtype_code(dtype), _activation(activation)
+    px, ldx = _matrix(x, rows, k, dtype, dev, "x")
+    pw, ldw = _matrix(w, n, k, dtype, dev, "w")
+    pb = _vector(bias, n, dtype, dev, "bias")
+    pr, ldr = _matrix(residual, rows, n, dtype, dev, "residual")
     lib = _lib()
-    with _On(x.device) as stream:
-        y = torch.empty((rows, n), dtype=x.dtype, device=x.device) if out is None else out
-        z = torch.empty((rows, n), dtype=x.dtype, device=x.device) if keep else None
-        p.y, p.ldy = _matrix(y, rows, n, x, "out")
-        p.z, p.ldz = _matrix(z, rows, n, x, "z")
-        need = c_size_t(0)
-        _check(lib.tig_linear_workspace_bytes(byref(p), 0, byref(need)))
-        ws = _workspace(need.value, x.device)
-        _check(lib.tig_linear_forward(byref(p), ws.data_ptr() if ws is not None else None, need.value, stream))
+    with _On(dev) as stream:
+        if out is None:
+            y = torch.empty((rows, n), dtype=dtype, device=dev)
+            py, ldy = y.data_ptr(), n
+        else:
+            y = out
+            py, ldy = _matrix(y, rows, n, dtype, dev, "out")
+        z, pz = None, 0
+        if keep:
+            z = torch.empty((rows, n), dtype=dtype, device=dev)
+            pz = z.data_ptr()
+        p = _linear_bytes(184, code, act, 0, rows, k, n, px, pw, pb, pr, py, pz, 0, 0, 0, 0, ldx, ldw, ldr, ldy, n, 0, 0, 0)
+        if rows <= _FEW_ROWS:
+            _check(lib.tig_linear_forward(p, None, 0, stream))
+        else:
+            need = c_size_t(0)
+            _check(lib.tig_linear_workspace_bytes(p, 0, byref(need)))
+            ws = _workspace(need.value, dev)
+            _check(lib.tig_linear_forward(p, ws.data_ptr() if ws is not None else None, need.value, stream))
     return (y, z) if keep else y
 
 
 def linear_backward(dy, x, w, z=None, activation="none", dx=True, dw=True, dbias=True):
     """Gradients (dx, dw, dbias) of linear() for dy [rows x out]; None in the place of one that is not wanted.  z: what
     linear(keep=True) returned (not needed without an activation).  The residual's gradient is dy."""
-    import torch
     if dy.dim() != 2 or x.dim() != 2 or w.dim() != 2:
         _refuse("dy, x and w are matrices")
     rows, n = dy.shape
     k = w.shape[1]
-    p = tig_linear(ctypes.sizeof(tig_linear), _dtype_code(dy.dtype), _activation(activation), 0, rows, k, n)
-    p.dy, p.lddy = _matrix(dy, rows, n, dy, "dy")
-    p.x, p.ldx = _matrix(x, rows, k, dy, "x")
-    p.w, p.ldw = _matrix(w, n, k, dy, "w")
-    if p.activation:
+    dtype, dev = dy.dtype, dy.device
+    code, act = _dtype_code(dtype), _activation(activation)
+    pd, lddy = _matrix(dy, rows, n, dtype, dev, "dy")
+    px, ldx = _matrix(x, rows, k, dtype, dev, "x")
+    pw, ldw = _matrix(w, n, k, dtype, dev, "w")
+    pz, ldz = 0, 0
+    if act:
         if z is None:
             _refuse("the backward pass of an activation needs z")
-        p.z, p.ldz = _matrix(z, rows, n, dy, "z")
+        pz, ldz = _matrix(z, rows, n, dtype, dev, "z")
     lib = _lib()
-    with _On(dy.device) as stream:
-        gx = torch.empty((rows, k), dtype=dy.dtype, device=dy.device) if dx else None
-        gw = torch.empty((n, k), dtype=dy.dtype, device=dy.device) if dw else None
-        gb = torch.empty(n, dtype=dy.dtype, device=dy.device) if dbias else None
-        p.dx, p.lddx = _matrix(gx, rows, k, dy, "dx")
-        p.dw, p.lddw = _matrix(gw, n, k, dy, "dw")
-        p.dbias = _vector(gb, n, dy, "dbias")
+    with _On(dev) as stream:
+        gx = torch.empty((rows, k), dtype=dtype, device=dev) if dx else None
+        gw = torch.empty((n, k), dtype=dtype, device=dev) if dw else None
+        gb = torch.empty(n, dtype=dtype, device=dev) if dbias else None
+        p = _linear_bytes(184, code, act, 0, rows, k, n, px, pw, 0, 0, 0, pz, pd, gx.data_ptr() if dx else 0, gw.data_ptr() if dw else 0,
+                          gb.data_ptr() if dbias else 0, ldx, ldw, 0, 0, ldz, lddy, k, k)
         need = c_size_t(0)
-        _check(lib.tig_linear_workspace_bytes(byref(p), 1, byref(need)))
-        ws = _workspace(need.value, dy.device)
-        _check(lib.tig_linear_backward(byref(p), ws.data_ptr() if ws is not None else None, need.value, stream))
+        _check(lib.tig_linear_workspace_bytes(p, 1, byref(need)))
+        ws = _workspace(need.value, dev)
+        _check(lib.tig_linear_backward(p, ws.data_ptr() if ws is not None else None, need.value, stream))
     return gx, gw, gb
 
 
@@ -205,34 +222,31 @@ def softmax_ce(x, w, labels, bias=None, row_scale=None, scale=1.0, grad=True):
     labels [rows]; a label outside the vocabulary (-1) leaves its row out.  Returns SoftmaxCE(loss [rows], lse [rows],
     mean [1], dx, dw, dbias): loss and lse in fp32, gradients of scale * mean (or of scale * sum of row_scale * loss) in
     x's type, None without `grad`."""
-    import torch
     if x.dim() != 2 or w.dim() != 2:
         _refuse("x and w are matrices")
     rows, d = x.shape
     vocab = w.shape[0]
-    p = tig_softmax_ce(ctypes.sizeof(tig_softmax_ce), _dtype_code(x.dtype), rows, vocab, d)
-    p.x, p.ldx = _matrix(x, rows, d, x, "x")
-    p.w, p.ldw = _matrix(w, vocab, d, x, "w")
-    p.bias = _vector(bias, vocab, x, "bias")
-    p.labels = _vector(labels, rows, x, "labels", torch.int32)
-    p.row_scale = _vector(row_scale, rows, x, "row_scale", torch.float32)
-    p.scale = scale
+    dtype, dev = x.dtype, x.device
+    code = _dtype_code(dtype)
+    px, ldx = _matrix(x, rows, d, dtype, dev, "x")
+    pw, ldw = _matrix(w, vocab, d, dtype, dev, "w")
+    pb = _vector(bias, vocab, dtype, dev, "bias")
+    pl = _vector(labels, rows, torch.int32, dev, "labels")
+    ps = _vector(row_scale, rows, torch.float32, dev, "row_scale")
     lib = _lib()
-    with _On(x.device) as stream:
-        dev = x.device
+    with _On(dev) as stream:
         stats = torch.empty(2 * rows + 1, dtype=torch.float32, device=dev)
         loss, lse, mean = stats[:rows], stats[rows : 2 * rows], stats[2 * rows :]
-        p.loss, p.lse, p.mean = loss.data_ptr(), lse.data_ptr(), mean.data_ptr()
-        dx = torch.empty((rows, d), dtype=x.dtype, device=dev) if grad else None
-        dw = torch.empty((vocab, d), dtype=x.dtype, device=dev) if grad else None
-        db = torch.empty(vocab, dtype=x.dtype, device=dev) if grad and bias is not None else None
-        p.dx, p.lddx = _matrix(dx, rows, d, x, "dx")
-        p.dw, p.lddw = _matrix(dw, vocab, d, x, "dw")
-        p.dbias = _vector(db, vocab, x, "dbias")
+        at = stats.data_ptr()
+        dx = torch.empty((rows, d), dtype=dtype, device=dev) if grad else None
+        dw = torch.empty((vocab, d), dtype=dtype, device=dev) if grad else None
+        db = torch.empty(vocab, dtype=dtype, device=dev) if grad and bias is not None else None
+        p = _ce_bytes(160, code, rows, vocab, d, px, pw, pb, pl, ps, scale, 0, at, at + 4 * rows, at + 8 * rows, dx.data_ptr() if grad else 0,
+                      dw.data_ptr() if grad else 0, db.data_ptr() if db is not None else 0, ldx, ldw, d, d)
         need = c_size_t(0)
-        _check(lib.tig_softmax_ce_workspace_bytes(byref(p), byref(need)))
+        _check(lib.tig_softmax_ce_workspace_bytes(p, byref(need)))
         ws = _workspace(need.value, dev)
-        _check(lib.tig_softmax_ce_run(byref(p), ws.data_ptr(), need.value, stream))
+        _check(lib.tig_softmax_ce_run(p, ws.data_ptr(), need.value, stream))
     return SoftmaxCE(loss, lse, mean, dx, dw, db)
 
 
@@ -244,7 +258,6 @@ class AdamW:
 
     def __init__(self, params, grads, m, v, step, masters=None, m_scales=None, v_scales=None, betas=(0.9, 0.999), eps=1e-8,
                  weight_decay=0.0):
-        import torch
         lists = dict(grads=grads, m=m, v=v)
         if masters is not None:
             lists["masters"] = masters
