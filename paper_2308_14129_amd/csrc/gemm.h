@@ -28,6 +28,9 @@ typedef int intx4 __attribute__((ext_vector_type(4)));
 
 enum Form { kRow = 0, kCol = 1 };
 
+#ifndef GEMM_WN
+#define GEMM_WN 4
+#endif
 constexpr int kTileBytes = 128;  // of k, per step
 
 template <typename T>
@@ -335,7 +338,7 @@ hipError_t launch_gemm(const GemmPlan &plan, const T *A, int64_t lda, const T *B
     g.A = A, g.B = B, g.lda = lda, g.ldb = ldb, g.M = M, g.N = N, g.K = K;
     g.splits = plan.splits, g.steps_per = plan.steps_per;
     g.part = (float *)part, g.ldp = gemm_part_ld(N);
-    hipError_t e = plan.tile == 256   ? launch_gemm_tile<T, FA, FB, Epi, 256, 256, 2, 4>(plan, g, epi, s)
+    hipError_t e = plan.tile == 256   ? launch_gemm_tile<T, FA, FB, Epi, 256, 256, 2, GEMM_WN>(plan, g, epi, s)
                    : plan.tile == 128 ? launch_gemm_tile<T, FA, FB, Epi, 128, 128, 2, 2>(plan, g, epi, s)
                                       : launch_gemm_tile<T, FA, FB, Epi, 64, 64, 2, 2>(plan, g, epi, s);
     if constexpr (!Epi::kWhole)

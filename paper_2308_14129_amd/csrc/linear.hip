@@ -132,35 +132,62 @@ hipError_t launch_linear_rows(const tig_linear &p, const Epi &epi, hipStream_t s
 }
 
 // ------------------------------------------------------------------------------------------
-// dz = dy act'(z) for a block of rows, four columns per thread, and the block's column sums of dz before it is rounded.
-constexpr int kDzRows = 64, kDzThreads = 256;
-inline int64_t dz_rows(int64_t rows) { return rows <= (int64_t)kDzRows * 32768 ? kDzRows : (rows + 32767) / 32768; }  // (a grid has 65535 rows)
+// dz = dy act'(z) for a block of rows and 64 pieces of 16 bytes (of dz) across, the wavefronts taking turns along the rows, and
+// the block's column sums of dz before it is rounded.
+constexpr int kDzWaves = 4;
 
 template <typename T, int ACT>
-__global__ void __launch_bounds__(kDzThreads) k_linear_dz(const T *dy, int64_t lddy, const T *z, int64_t ldz, T *dz, int64_t lddz, float *sums,
-                                                         int64_t lds, int64_t M, int64_t N, int64_t per, bool dy_ok, bool z_ok)
+__global__ void __launch_bounds__(64 * kDzWaves) k_linear_dz(const T *dy, int64_t lddy, const T *z, int64_t ldz, T *dz, int64_t lddz, float *sums,
+                                                            int64_t lds, int64_t M, int64_t N, int64_t per, bool dy_ok, bool z_ok)
 {
-    const int64_t n = ((int64_t)blockIdx.x * kDzThreads + threadIdx.x) * 4;
-    if (n >= (dz ? lddz : N))
-        return;
-    const int64_t m0 = (int64_t)blockIdx.y * per, m1 = m0 + per < M ? m0 + per : M;
-    const int left = N - n < 4 ? (N > n ? (int)(N - n) : 0) : 4;
-    floatx4 total = {0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int V = Mat<T>::kPer16 / 4;  // fours of a lane
+    __shared__ floatx4 part[kDzWaves][V][64];
+    const int lane = lane_id(), wave = wave_id_uniform();
+    const int64_t n0 = ((int64_t)blockIdx.x * 64 + lane) * (4 * V), m0 = (int64_t)blockIdx.y * per, m1 = m0 + per < M ? m0 + per : M;
+    floatx4 total[V] = {};
+    if (n0 < (dz ? lddz : N))
 #pragma unroll 4
-    for (int64_t m = m0; m < m1; ++m) {
-        floatx4 v = load_four(dy + m * lddy + n, left, dy_ok);
-        if constexpr (ACT != TIG_ACT_NONE) {
-            const floatx4 q = load_four(z + m * ldz + n, left, z_ok);
+        for (int64_t m = m0 + wave; m < m1; m += kDzWaves)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] *= slope<ACT>(q[e]);
-        }
-        total += v;
-        if (dz)
-            store_four(dz + m * lddz + n, v, (int)(lddz - n < 4 ? lddz - n : 4), true);
+            for (int u = 0; u < V; ++u) {
+                const int64_t n = n0 + 4 * u;
+                const int left = N - n < 4 ? (N > n ? (int)(N - n) : 0) : 4;
+                floatx4 v = load_four(dy + m * lddy + n, left, dy_ok);
+                if constexpr (ACT != TIG_ACT_NONE) {
+                    const floatx4 q = load_four(z + m * ldz + n, left, z_ok);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        v[e] *= slope<ACT>(q[e]);
+                }
+                total[u] += v;
+                if (dz)
+                    store_four(dz + m * lddz + n, v, 4, true);
+            }
+    if (!sums)
+        return;
+#pragma unroll
+    for (int u = 0; u < V; ++u)
+        part[wave][u][lane] = total[u];
+    __syncthreads();
+    for (int u = wave; u < V; u += kDzWaves) {
+        const int64_t n = n0 + 4 * u;
+        floatx4 v = part[0][u][lane];
+#pragma unroll
+        for (int w = 1; w < kDzWaves; ++w)
+            v += part[w][u][lane];
+        if (n < N)
+            *(floatx4 *)(sums + (int64_t)blockIdx.y * lds + n) = v;
     }
-    if (sums && left > 0)
-        *(floatx4 *)(sums + (int64_t)blockIdx.y * lds + n) = total;
+}
+
+// rows of a block: enough blocks to fill the chip, and no more than a grid's 65535
+inline int64_t dz_rows(int64_t rows, int64_t cols, int per_lane)
+{
+    const int64_t across = (cols + 64 * per_lane - 1) / (64 * per_lane);
+    int64_t per = 64;
+    while (per > 16 && (rows + per - 1) / per * across < 1024)
+        per /= 2;
+    return (rows + per - 1) / per <= 65535 ? per : (rows + 65534) / 65535;
 }
 
 }  // namespace
@@ -204,7 +231,7 @@ struct LinearPlan {
     GemmPlan y, dx, dw;
     bool pack_x, pack_w;           // operands whose rows are not 16-byte aligned
     bool store_dz;                 // backward: dz is written (else dy serves)
-    int64_t ld_px, ld_pw, ld_dz, ld_sums, sum_blocks;
+    int64_t ld_px, ld_pw, ld_dz, ld_sums, dz_per, sum_blocks;
     size_t px, pw, dz, sums, part;  // offsets into the workspace
     size_t bytes;
 };
@@ -245,7 +272,8 @@ LinearPlan linear_plan(const tig_linear &p, bool backward)
         L.ld_dz = pack_ld(p.out_dim, es);
         if (L.store_dz)
             L.dz = take((size_t)p.rows * L.ld_dz * es);
-        L.sum_blocks = (p.rows + dz_rows(p.rows) - 1) / dz_rows(p.rows);
+        L.dz_per = dz_rows(p.rows, L.ld_dz, 16 / es);
+        L.sum_blocks = (p.rows + L.dz_per - 1) / L.dz_per;
         L.ld_sums = (p.out_dim + 3) / 4 * 4;
         if (p.dbias)
             L.sums = take((size_t)L.sum_blocks * L.ld_sums * 4);
@@ -340,10 +368,11 @@ hipError_t backward(const tig_linear &p, const LinearPlan &L, char *ws, hipStrea
     if (L.store_dz || p.dbias) {
         T *const out = L.store_dz ? (T *)(ws + L.dz) : nullptr;
         float *const sums = p.dbias ? (float *)(ws + L.sums) : nullptr;
-        const dim3 grid((unsigned)((L.ld_dz / 4 + kDzThreads) / kDzThreads), (unsigned)L.sum_blocks);
+        const int64_t across = 64 * (16 / es);
+        const dim3 grid((unsigned)((L.ld_dz + across - 1) / across), (unsigned)L.sum_blocks);
         with_activation(p.activation, [&](auto act) {
-            hipLaunchKernelGGL((k_linear_dz<T, decltype(act)::value>), grid, dim3(kDzThreads), 0, s, (const T *)p.dy, p.lddy, (const T *)p.z, p.ldz, out,
-                               L.ld_dz, sums, L.ld_sums, p.rows, p.out_dim, dz_rows(p.rows), four_aligned(p.dy, p.lddy, es), four_aligned(p.z, p.ldz, es));
+            hipLaunchKernelGGL((k_linear_dz<T, decltype(act)::value>), grid, dim3(64 * kDzWaves), 0, s, (const T *)p.dy, p.lddy, (const T *)p.z, p.ldz, out,
+                               L.ld_dz, sums, L.ld_sums, p.rows, p.out_dim, L.dz_per, four_aligned(p.dy, p.lddy, es), four_aligned(p.z, p.ldz, es));
             return 0;
         });
         if ((e = hipGetLastError()) != hipSuccess)
