@@ -61,6 +61,7 @@ struct Operand {
     static constexpr int kLoads = kBytes / (64 * 16 * WAVES);  // loads of a wavefront per step
     static constexpr int kRowBytes = F == kRow ? kTileBytes : BX * (int)sizeof(T);
     static_assert(kLoads * 64 * 16 * WAVES == kBytes, "");
+    static constexpr int kReads = F == kRow ? 1 : (sizeof(T) == 4 ? 4 : 2);  // LDS loads of an operand
     uint32_t off[kLoads];   // byte offset of this lane's piece from the step's base, kBufferNone: outside of the operand's own range
     int at_k[kLoads];       // kRow: byte of k; kCol: k, within the step
 
@@ -223,36 +224,55 @@ __global__ void __launch_bounds__(64 * WM *WN) k_gemm(GemmArgs<T> g, Epi epi)
     int64_t left = g.K - s0 * Mat<T>::kStep;
     floatx4 acc[FM][FN] = {};
     const int n_steps = (int)(s1 - s0);
-    if (n_steps > 0) {
-        oa.load(pa, left, smem);
-        ob.load(pb, left, smem + OA::kBytes);
-    }
-    for (int s = 0; s < n_steps; ++s) {
-        char *const now = smem + (s & 1) * kStage;
-        __syncthreads();  // (waits for the loads into `now`, and for every wavefront's reads of the other buffer)
-        if (s + 1 < n_steps) {
-            pa += OA::step(g.lda);
-            pb += OB::step(g.ldb);
-            left -= Mat<T>::kStep;
-            char *const next = smem + ((s + 1) & 1) * kStage;
-            oa.load(pa, left, next);
-            ob.load(pb, left, next + OA::kBytes);
-        }
+    // Two halves of a step take turns: while one's operands are multiplied, the next one's are read from LDS, and between them
+    // the step after the next is asked for.  (Read and multiplied in turn, the matrix units waited a third of the time for LDS.)
+    intx4 a[2][FM], b[2][FN];
+    auto request = [&](int s) {  // (behind the last step: nothing is loaded, and no branch divides the instructions to be mixed)
+        char *const to = smem + (s & 1) * kStage;
+        oa.load(pa, s < n_steps ? left : 0, to);
+        ob.load(pb, s < n_steps ? left : 0, to + OA::kBytes);
+        pa += OA::step(g.lda);
+        pb += OB::step(g.ldb);
+        left -= Mat<T>::kStep;
+    };
+    auto multiply = [&](const intx4 (&x)[FM], const intx4 (&y)[FN], intx4 (&nx)[FM], intx4 (&ny)[FN], const char *from, int kk) {
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            intx4 a[FM], b[FN];
+        for (int j = 0; j < FN; ++j)
+            ny[j] = OB::frag(from + OA::kBytes, wn * (BN / WN) + j * 16, kk);
 #pragma unroll
-            for (int i = 0; i < FM; ++i)
-                a[i] = OA::frag(now, wm * (BM / WM) + i * 16, kk);
+        for (int i = 0; i < FM; ++i) {
+            nx[i] = OA::frag(from, wm * (BM / WM) + i * 16, kk);
 #pragma unroll
             for (int j = 0; j < FN; ++j)
-                b[j] = OB::frag(now + OA::kBytes, wn * (BN / WN) + j * 16, kk);
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int j = 0; j < FN; ++j)
-                    mma16(acc[i][j], b[j], a[i], T());
+                mma16(acc[i][j], y[j], x[i], T());
         }
+        // The reads go between the products, a few behind each but the last row's: left alone they are sunk to where they are
+        // waited for, and ahead of the first product they would be waited for with what it needs.
+        constexpr int kMma = FN * (sizeof(T) == 4 ? 4 : 1), kAll = FN * OB::kReads + FM * OA::kReads, kEach = (kAll + FM - 2) / (FM - 1);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, kMma, 0);
+            if (i + 1 < FM)
+                __builtin_amdgcn_sched_group_barrier(0x100, kEach, 0);
+        }
+    };
+    if (n_steps > 0) {
+        request(0);
+        __syncthreads();
+        request(1);
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+            a[0][i] = OA::frag(smem, wm * (BM / WM) + i * 16, 0);
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+            b[0][j] = OB::frag(smem + OA::kBytes, wn * (BN / WN) + j * 16, 0);
+    }
+    for (int s = 0; s < n_steps; ++s) {
+        multiply(a[0], b[0], a[1], b[1], smem + (s & 1) * kStage, 1);
+        __syncthreads();  // (step s + 1 is there, and nobody reads step s any more)
+        request(s + 2);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(a[1], b[1], a[0], b[0], smem + ((s + 1) & 1) * kStage, 0);  // (behind the last step: operands that nobody takes)
     }
     const TileAt at = {m0 + wm * (BM / WM), n0 + wn * (BN / WN), g.M, g.N, tm, tn, wm, wn};
     if constexpr (Epi::kWhole) {
