@@ -235,6 +235,9 @@ __global__ void __launch_bounds__(64 * WM *WN) k_gemm(GemmArgs<T> g, Epi epi)
         pb += OB::step(g.ldb);
         left -= Mat<T>::kStep;
     };
+#ifdef GEMM_PRIO
+    __builtin_amdgcn_s_setprio(1);
+#endif
     auto multiply = [&](const intx4 (&x)[FM], const intx4 (&y)[FN], intx4 (&nx)[FM], intx4 (&ny)[FN], const char *from, int kk) {
 #pragma unroll
         for (int j = 0; j < FN; ++j)
@@ -246,9 +249,9 @@ __global__ void __launch_bounds__(64 * WM *WN) k_gemm(GemmArgs<T> g, Epi epi)
             for (int j = 0; j < FN; ++j)
                 mma16(acc[i][j], y[j], x[i], T());
         }
-        // The reads go between the products, a few behind each but the last row's: left alone they are sunk to where they are
-        // waited for, and ahead of the first product they would be waited for with what it needs.
-        constexpr int kMma = FN * (sizeof(T) == 4 ? 4 : 1), kAll = FN * OB::kReads + FM * OA::kReads, kEach = (kAll + FM - 2) / (FM - 1);
+        // The reads go between the first rows' products: left alone they are sunk to where they are waited for, and ahead of the
+        // first product they would be waited for with what it needs.  (Two behind each row's: 3 - 8 % slower.)
+        constexpr int kMma = FN * (sizeof(T) == 4 ? 4 : 1), kEach = FA == kRow && FB == kRow ? 4 : 6;
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, kMma, 0);
