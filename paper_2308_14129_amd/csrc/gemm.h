@@ -28,9 +28,6 @@ typedef int intx4 __attribute__((ext_vector_type(4)));
 
 enum Form { kRow = 0, kCol = 1 };
 
-#ifndef GEMM_WN
-#define GEMM_WN 4
-#endif
 constexpr int kTileBytes = 128;  // of k, per step
 
 template <typename T>
@@ -235,9 +232,6 @@ __global__ void __launch_bounds__(64 * WM *WN) k_gemm(GemmArgs<T> g, Epi epi)
         pb += OB::step(g.ldb);
         left -= Mat<T>::kStep;
     };
-#ifdef GEMM_PRIO
-    __builtin_amdgcn_s_setprio(1);
-#endif
     auto multiply = [&](const intx4 (&x)[FM], const intx4 (&y)[FN], intx4 (&nx)[FM], intx4 (&ny)[FN], const char *from, int kk) {
 #pragma unroll
         for (int j = 0; j < FN; ++j)
@@ -277,6 +271,7 @@ __global__ void __launch_bounds__(64 * WM *WN) k_gemm(GemmArgs<T> g, Epi epi)
         __builtin_amdgcn_sched_barrier(0);
         multiply(a[1], b[1], a[0], b[0], smem + ((s + 1) & 1) * kStage, 0);  // (behind the last step: operands that nobody takes)
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nothing may reach LDS any more once the workgroup has given it back)
     const TileAt at = {m0 + wm * (BM / WM), n0 + wn * (BN / WN), g.M, g.N, tm, tn, wm, wn};
     if constexpr (Epi::kWhole) {
         __syncthreads();
@@ -361,7 +356,7 @@ hipError_t launch_gemm(const GemmPlan &plan, const T *A, int64_t lda, const T *B
     g.A = A, g.B = B, g.lda = lda, g.ldb = ldb, g.M = M, g.N = N, g.K = K;
     g.splits = plan.splits, g.steps_per = plan.steps_per;
     g.part = (float *)part, g.ldp = gemm_part_ld(N);
-    hipError_t e = plan.tile == 256   ? launch_gemm_tile<T, FA, FB, Epi, 256, 256, 2, GEMM_WN>(plan, g, epi, s)
+    hipError_t e = plan.tile == 256   ? launch_gemm_tile<T, FA, FB, Epi, 256, 256, 2, 4>(plan, g, epi, s)
                    : plan.tile == 128 ? launch_gemm_tile<T, FA, FB, Epi, 128, 128, 2, 2>(plan, g, epi, s)
                                       : launch_gemm_tile<T, FA, FB, Epi, 64, 64, 2, 2>(plan, g, epi, s);
     if constexpr (!Epi::kWhole)
