@@ -386,11 +386,11 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, 2) k_narrow_grad(NarrowArgs
                 a.sums[(int64_t)split * a.n_own + m] = total[i];
         }
         if (m < a.n_own && CANDS && a.direct.C) {
-            const float by = a.direct.row(m);
+            const auto by = a.direct.row(m);
 #pragma unroll
             for (int c = 0; c < DT; ++c)
                 if (c * 16 + 4 * g < a.d)
-                    a.direct(by, m, c * 16 + 4 * g, out[i][c], a.d - c * 16 - 4 * g < 4 ? a.d - c * 16 - 4 * g : 4);
+                    a.direct.template store<false>(by, Nothing(), Nothing(), c * 16 + 4 * g, out[i][c], a.d - c * 16 - 4 * g < 4 ? a.d - c * 16 - 4 * g : 4);
         } else if (m < a.n_own && a.grad) {
             float *const row = a.grad + ((int64_t)split * a.n_own + m) * a.ld_grad;
 #pragma unroll

@@ -18,6 +18,8 @@
 // The product is computed as B A^T, so that a lane ends with four adjacent columns of one row of C.
 #pragma once
 
+#include <type_traits>
+
 #include "kernels_common.h"
 
 namespace tig {
@@ -170,32 +172,67 @@ struct TileAt {
     int wm, wn;
 };
 
-// What an epilogue does element by element: epi(r, m, n, v, left) takes four adjacent columns of a row, of which `left` exist;
-// r = epi.row(m) is what it needs of the row.
+// What an epilogue does element by element, four adjacent columns of a row at a time, of which `left` exist:
+//   row(m), col(n, left)             what it needs of the row, of the columns
+//   load(row, n, left)               what it reads at the place
+//   store(row, col, read, n, v, left)
+// FULL: all four exist and lie as one access (epi.aligned()).  What the next row reads is on its way while this one is stored.
 template <int FM, int FN, class Epi>
 __device__ inline void each_four(const TileAt &at, const floatx4 (&acc)[FM][FN], const Epi &epi)
 {
     const int lane = lane_id(), i16 = lane % 16, g = lane / 16;
+    auto rows = [&](auto full) {
+        constexpr bool FULL = decltype(full)::value;
+        int left[FN];
+        decltype(epi.template col<FULL>(0, 0)) cols[FN];
+        decltype(epi.template load<FULL>(epi.row(0), 0, 0)) read[2][FN];
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        const int64_t m = at.m0 + i * 16 + i16;
-        if (m < at.M) {
-            const auto r = epi.row(m);
+        for (int j = 0; j < FN; ++j) {
+            const int64_t n = at.n0 + j * 16 + 4 * g, l = at.N - n;
+            left[j] = FULL ? 4 : (l < 4 ? (l > 0 ? (int)l : 0) : 4);
+            cols[j] = epi.template col<FULL>(n, left[j]);
+        }
+        auto fetch = [&](int i) {
+            const int64_t m = at.m0 + i * 16 + i16;
+            const auto r = epi.row(FULL || m < at.M ? m : at.M - 1);
 #pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const int64_t n = at.n0 + j * 16 + 4 * g, left = at.N - n;
-                if (left > 0)
-                    epi(r, m, n, acc[i][j], left < 4 ? (int)left : 4);
+            for (int j = 0; j < FN; ++j)
+                read[i & 1][j] = epi.template load<FULL>(r, at.n0 + j * 16 + 4 * g, left[j]);
+        };
+        fetch(0);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            if (i + 1 < FM)
+                fetch(i + 1);
+            const int64_t m = at.m0 + i * 16 + i16;
+            if (FULL || m < at.M) {
+                const auto r = epi.row(m);
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+                    if (FULL || left[j] > 0)
+                        epi.template store<FULL>(r, cols[j], read[i & 1][j], at.n0 + j * 16 + 4 * g, acc[i][j], left[j]);
             }
         }
-    }
+    };
+    if (at.m0 + FM * 16 <= at.M && at.n0 + FN * 16 <= at.N && epi.aligned())  // (uniform)
+        rows(std::true_type());
+    else
+        rows(std::false_type());
 }
+struct Nothing {
+};
 
 struct EpiPart {  // a range's partial sums
     float *part;
     int64_t ldp;
-    __device__ inline int row(int64_t) const { return 0; }
-    __device__ inline void operator()(int, int64_t m, int64_t n, const floatx4 &v, int) const { *(floatx4 *)(part + m * ldp + n) = v; }
+    __device__ inline bool aligned() const { return true; }
+    __device__ inline float *row(int64_t m) const { return part + m * ldp; }
+    template <bool FULL>
+    __device__ inline Nothing col(int64_t, int) const { return {}; }
+    template <bool FULL>
+    __device__ inline Nothing load(const float *, int64_t, int) const { return {}; }
+    template <bool FULL>
+    __device__ inline void store(float *r, Nothing, Nothing, int64_t n, const floatx4 &v, int) const { *(floatx4 *)(r + n) = v; }
 };
 
 template <typename T, Form FA, Form FB, int BM, int BN, int WM, int WN, class Epi>
@@ -232,7 +269,7 @@ __global__ void __launch_bounds__(64 * WM *WN) k_gemm(GemmArgs<T> g, Epi epi)
         pb += OB::step(g.ldb);
         left -= Mat<T>::kStep;
     };
-    auto multiply = [&](const intx4 (&x)[FM], const intx4 (&y)[FN], intx4 (&nx)[FM], intx4 (&ny)[FN], const char *from, int kk) {
+    auto multiply = [&](const intx4 (&x)[FM], const intx4 (&y)[FN], intx4 (&nx)[FM], intx4 (&ny)[FN], const char *from, int kk, auto loads) {
 #pragma unroll
         for (int j = 0; j < FN; ++j)
             ny[j] = OB::frag(from + OA::kBytes, wn * (BN / WN) + j * 16, kk);
@@ -244,11 +281,16 @@ __global__ void __launch_bounds__(64 * WM *WN) k_gemm(GemmArgs<T> g, Epi epi)
                 mma16(acc[i][j], y[j], x[i], T());
         }
         // The reads go between the first rows' products: left alone they are sunk to where they are waited for, and ahead of the
-        // first product they would be waited for with what it needs.  (Two behind each row's: 3 - 8 % slower.)
+        // first product they would be waited for with what it needs.  (Two behind each row's: 3 - 8 % slower.)  So do the next
+        // step's loads; the barrier comes as soon as the reads are done, and what is left of the products hides how far
+        // the wavefronts are apart (8192^3: with the loads ahead of all products and the barrier behind them 1070, 1030 and 1040
+        // instead of 1270, 1145 and 1147 TFLOP/s for the three forms).
         constexpr int kMma = FN * (sizeof(T) == 4 ? 4 : 1), kEach = FA == kRow && FB == kRow ? 4 : 6;
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, kMma, 0);
+            if (decltype(loads)::value && i < 4)
+                __builtin_amdgcn_sched_group_barrier(0x010, (OA::kLoads + OB::kLoads + 3) / 4, 0);
             if (i + 1 < FM)
                 __builtin_amdgcn_sched_group_barrier(0x100, kEach, 0);
         }
@@ -265,11 +307,10 @@ __global__ void __launch_bounds__(64 * WM *WN) k_gemm(GemmArgs<T> g, Epi epi)
             b[0][j] = OB::frag(smem + OA::kBytes, wn * (BN / WN) + j * 16, 0);
     }
     for (int s = 0; s < n_steps; ++s) {
-        multiply(a[0], b[0], a[1], b[1], smem + (s & 1) * kStage, 1);
+        multiply(a[0], b[0], a[1], b[1], smem + (s & 1) * kStage, 1, std::false_type());
         __syncthreads();  // (step s + 1 is there, and nobody reads step s any more)
         request(s + 2);
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(a[1], b[1], a[0], b[0], smem + ((s + 1) & 1) * kStage, 0);  // (behind the last step: operands that nobody takes)
+        multiply(a[1], b[1], a[0], b[0], smem + ((s + 1) & 1) * kStage, 0, std::true_type());  // (behind the last step: operands that nobody takes)
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nothing may reach LDS any more once the workgroup has given it back)
     const TileAt at = {m0 + wm * (BM / WM), n0 + wn * (BN / WN), g.M, g.N, tm, tn, wm, wn};
@@ -295,7 +336,9 @@ __global__ void __launch_bounds__(256) k_gemm_join(const float *part, int splits
 #pragma unroll 4
         for (int s = 0; s < splits; ++s)
             v += *(const floatx4 *)(p + (int64_t)s * M * ldp);
-        epi(epi.row(m), m, n, v, N - n < 4 ? (int)(N - n) : 4);
+        const int left = N - n < 4 ? (int)(N - n) : 4;
+        const auto r = epi.row(m);
+        epi.template store<false>(r, epi.template col<false>(n, left), epi.template load<false>(r, n, left), n, v, left);
     }
 }
 
@@ -429,12 +472,21 @@ struct EpiStore {
     int64_t ldc;
     const float *scale;
     float alpha;
-    bool aligned;
-    __device__ inline float row(int64_t) const { return scale ? alpha * *scale : alpha; }
-    __device__ inline void operator()(float by, int64_t m, int64_t n, floatx4 v, int left) const
+    bool ok;  // four elements at once
+    struct Row {
+        T *p;
+        float by;
+    };
+    __device__ inline bool aligned() const { return ok; }
+    __device__ inline Row row(int64_t m) const { return {C + m * ldc, scale ? alpha * *scale : alpha}; }
+    template <bool FULL>
+    __device__ inline Nothing col(int64_t, int) const { return {}; }
+    template <bool FULL>
+    __device__ inline Nothing load(const Row &, int64_t, int) const { return {}; }
+    template <bool FULL>
+    __device__ inline void store(const Row &r, Nothing, Nothing, int64_t n, const floatx4 &v, int left) const
     {
-        v *= by;
-        store_four(C + m * ldc + n, v, left, aligned);
+        store_four(r.p + n, v * r.by, left, FULL || ok);
     }
 };
 

@@ -20,19 +20,32 @@ struct EpiLinear {
     T *y, *z;
     int64_t ldr, ldy, ldz;
     bool bias_ok, res_ok, y_ok, z_ok;  // four elements at once
-    __device__ inline int row(int64_t) const { return 0; }
-    __device__ inline void operator()(int, int64_t m, int64_t n, floatx4 v, int left) const
+    struct Row {
+        const T *res;
+        T *y, *z;
+    };
+    __device__ inline bool aligned() const { return (bias_ok || !bias) && (res_ok || !res) && y_ok && (z_ok || !z); }
+    __device__ inline Row row(int64_t m) const { return {res + m * ldr, y + m * ldy, z + m * ldz}; }
+    template <bool FULL>
+    __device__ inline floatx4 col(int64_t n, int left) const
     {
-        if (bias)
-            v += load_four(bias + n, left, bias_ok);
+        return bias ? load_four(bias + n, left, FULL || bias_ok) : floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    template <bool FULL>
+    __device__ inline floatx4 load(const Row &r, int64_t n, int left) const
+    {
+        return res ? load_four(r.res + n, left, FULL || res_ok) : floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    template <bool FULL>
+    __device__ inline void store(const Row &r, const floatx4 &b, const floatx4 &more, int64_t n, floatx4 v, int left) const
+    {
+        v += b;
         if (z)
-            store_four(z + m * ldz + n, v, left, z_ok);
+            store_four(r.z + n, v, left, FULL || z_ok);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             v[e] = activate<ACT>(v[e]);
-        if (res)
-            v += load_four(res + m * ldr + n, left, res_ok);
-        store_four(y + m * ldy + n, v, left, y_ok);
+        store_four(r.y + n, v + more, left, FULL || y_ok);
     }
 };
 
@@ -110,8 +123,11 @@ __global__ void __launch_bounds__(64 * WAVES) k_linear_rows(const T *x, int64_t 
         for (int u = 1; u < WAVES; ++u)
             v += red[u][i][lane];
         const int64_t m = i * 16 + i16, c = n0 + 4 * g;
-        if (m < M && c < N)
-            epi(epi.row(m), m, c, v, N - c < 4 ? (int)(N - c) : 4);
+        if (m < M && c < N) {
+            const int left = N - c < 4 ? (int)(N - c) : 4;
+            const auto r = epi.row(m);
+            epi.template store<false>(r, epi.template col<false>(c, left), epi.template load<false>(r, c, left), c, v, left);
+        }
     }
 }
 

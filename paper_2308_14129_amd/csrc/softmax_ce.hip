@@ -310,12 +310,17 @@ struct EpiAdd {
     float *acc;
     int64_t ld;
     bool first;
-    __device__ inline int row(int64_t) const { return 0; }
-    __device__ inline void operator()(int, int64_t m, int64_t n, floatx4 v, int) const
+    __device__ inline bool aligned() const { return true; }
+    __device__ inline float *row(int64_t m) const { return acc + m * ld; }
+    template <bool FULL>
+    __device__ inline Nothing col(int64_t, int) const { return {}; }
+    template <bool FULL>
+    __device__ inline floatx4 load(const float *r, int64_t n, int left) const
     {
-        floatx4 *const p = (floatx4 *)(acc + m * ld + n);
-        *p = first ? v : *p + v;
+        return first || left == 0 ? floatx4{0.0f, 0.0f, 0.0f, 0.0f} : *(const floatx4 *)(r + n);
     }
+    template <bool FULL>
+    __device__ inline void store(float *r, Nothing, const floatx4 &before, int64_t n, const floatx4 &v, int) const { *(floatx4 *)(r + n) = before + v; }
 };
 
 template <typename T>
