@@ -17,9 +17,16 @@
 
 namespace tig {
 
+#ifndef NARROW_F4
+#define NARROW_F4 3
+#define NARROW_F2 4
+#define NARROW_W 2
+#define NARROW_SF 3
+#define NARROW_SW 2
+#endif
 constexpr int kNarrowWaves = 4, kNarrowStream = 64;
 template <int KB>
-constexpr int kNarrowOwn = KB <= 2 ? 4 : 3;  // sixteens of own rows of a wavefront (registers: two wavefronts on a SIMD)
+constexpr int kNarrowOwn = KB <= 2 ? NARROW_F2 : NARROW_F4;  // sixteens of own rows of a wavefront (registers: two wavefronts on a SIMD)
 template <int KB>
 constexpr int kNarrowTile = 16 * kNarrowOwn<KB> * kNarrowWaves;
 
@@ -150,7 +157,7 @@ __device__ inline floatx4 start_of(const NarrowArgs<T> &a, int64_t t, int r, con
 }
 
 template <typename T, int KB>
-__global__ void __launch_bounds__(64 * kNarrowWaves, 2) k_narrow_stats(NarrowArgs<T> a)
+__global__ void __launch_bounds__(64 * kNarrowWaves, NARROW_W) k_narrow_stats(NarrowArgs<T> a)
 {
     constexpr int FM = kNarrowOwn<KB>, FN = 4;
     using S = NarrowStream<T, KB>;
@@ -232,7 +239,7 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, 2) k_narrow_stats(NarrowArg
 
 // CANDS: own rows are candidates (dW), else rows of X (dX).  WEIGHTED: rows of X have weights of their own.
 template <typename T, int KB, bool CANDS, bool WEIGHTED>
-__global__ void __launch_bounds__(64 * kNarrowWaves, 2) k_narrow_grad(NarrowArgs<T> a)
+__global__ void __launch_bounds__(64 * kNarrowWaves, NARROW_W) k_narrow_grad(NarrowArgs<T> a)
 {
     constexpr int FM = kNarrowOwn<KB>, DT = 2 * KB;
     using S = NarrowStream<T, KB>;

@@ -462,6 +462,30 @@ __device__ inline floatx4 load_four(const T *p, int left, bool aligned)
     }
     return v;
 }
+// 16 bytes of elements
+template <typename T>
+__device__ inline void load_piece(const T *p, floatx4 (&v)[Mat<T>::kPer16 / 4])
+{
+    struct alignas(16) Piece {
+        T v[Mat<T>::kPer16];
+    };
+    const Piece q = *(const Piece *)p;
+#pragma unroll
+    for (int e = 0; e < Mat<T>::kPer16; ++e)
+        v[e / 4][e % 4] = to_float(q.v[e]);
+}
+template <typename T>
+__device__ inline void store_piece(T *p, const floatx4 (&v)[Mat<T>::kPer16 / 4])
+{
+    struct alignas(16) Piece {
+        T v[Mat<T>::kPer16];
+    } q;
+#pragma unroll
+    for (int e = 0; e < Mat<T>::kPer16; ++e)
+        q.v[e] = (T)v[e / 4][e % 4];
+    *(Piece *)p = q;
+}
+inline bool piece_aligned(const void *p, int64_t ld, int elem) { return ((uintptr_t)p & 15) == 0 && ld * elem % 16 == 0; }
 inline bool four_aligned(const void *p, int64_t ld, int elem) { return ((uintptr_t)p % (4 * elem)) == 0 && ld % 4 == 0; }
 
 // C = alpha * sum, alpha from the host times *scale (if not NULL)

@@ -53,7 +53,7 @@ struct EpiLinear {
 // Few rows.  A workgroup takes sixteen columns of y for all rows; its wavefronts take turns along k, every lane loads 16 bytes
 // of one row of W (and of x) as the matrix instructions want them, and the wavefronts' sums are added in LDS.
 template <typename T>
-__device__ inline intx4 load_piece(const T *row, int64_t k, int64_t K)
+__device__ inline intx4 operand_piece(const T *row, int64_t k, int64_t K)
 {
     constexpr int per = Mat<T>::kPer16;
     struct __attribute__((packed, aligned(sizeof(T)))) Any {
@@ -95,10 +95,10 @@ __global__ void __launch_bounds__(64 * WAVES) k_linear_rows(const T *x, int64_t 
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             const int64_t k = (b + u * WAVES) * kBlock;
-            wv[u] = load_piece<T>(wr, k, k + per);
+            wv[u] = operand_piece<T>(wr, k, k + per);
 #pragma unroll
             for (int i = 0; i < MT; ++i)
-                xv[u][i] = load_piece<T>(xr[i], k, k + per);
+                xv[u][i] = operand_piece<T>(xr[i], k, k + per);
         }
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
@@ -108,10 +108,10 @@ __global__ void __launch_bounds__(64 * WAVES) k_linear_rows(const T *x, int64_t 
     }
     for (; b * kBlock < K; b += WAVES) {
         const int64_t k = b * kBlock, left = K - g * per;
-        const intx4 wv = load_piece<T>(wr, k, left);
+        const intx4 wv = operand_piece<T>(wr, k, left);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
-            mma16(acc[i], wv, load_piece<T>(xr[i], k, left), T());
+            mma16(acc[i], wv, operand_piece<T>(xr[i], k, left), T());
     }
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -156,29 +156,58 @@ template <typename T, int ACT>
 __global__ void __launch_bounds__(64 * kDzWaves) k_linear_dz(const T *dy, int64_t lddy, const T *z, int64_t ldz, T *dz, int64_t lddz, float *sums,
                                                             int64_t lds, int64_t M, int64_t N, int64_t per, bool dy_ok, bool z_ok)
 {
-    constexpr int V = Mat<T>::kPer16 / 4;  // fours of a lane
+    constexpr int V = Mat<T>::kPer16 / 4, kDeep = 4;  // fours of a lane; rows on their way at a time
     __shared__ floatx4 part[kDzWaves][V][64];
     const int lane = lane_id(), wave = wave_id_uniform();
     const int64_t n0 = ((int64_t)blockIdx.x * 64 + lane) * (4 * V), m0 = (int64_t)blockIdx.y * per, m1 = m0 + per < M ? m0 + per : M;
     floatx4 total[V] = {};
-    if (n0 < (dz ? lddz : N))
-#pragma unroll 4
-        for (int64_t m = m0 + wave; m < m1; m += kDzWaves)
+    auto add = [&](int64_t m, floatx4 (&v)[V], const floatx4 (&q)[V]) {
+#pragma unroll
+        for (int u = 0; u < V; ++u) {
+            if constexpr (ACT != TIG_ACT_NONE)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[u][e] *= slope<ACT>(q[u][e]);
+            total[u] += v[u];
+        }
+        if (dz)
+            store_piece(dz + m * lddz + n0, v);
+    };
+    if (n0 + 4 * V <= N && dy_ok && z_ok) {
+        int64_t m = m0 + wave;
+        for (; m + (kDeep - 1) * kDzWaves < m1; m += kDeep * kDzWaves) {
+            floatx4 v[kDeep][V], q[kDeep][V];
+#pragma unroll
+            for (int r = 0; r < kDeep; ++r) {
+                load_piece(dy + (m + r * kDzWaves) * lddy + n0, v[r]);
+                if constexpr (ACT != TIG_ACT_NONE)
+                    load_piece(z + (m + r * kDzWaves) * ldz + n0, q[r]);
+            }
+#pragma unroll
+            for (int r = 0; r < kDeep; ++r)
+                add(m + r * kDzWaves, v[r], q[r]);
+        }
+        for (; m < m1; m += kDzWaves) {
+            floatx4 v[V], q[V];
+            load_piece(dy + m * lddy + n0, v);
+            if constexpr (ACT != TIG_ACT_NONE)
+                load_piece(z + m * ldz + n0, q);
+            add(m, v, q);
+        }
+    } else if (n0 < (dz ? lddz : N)) {
+        for (int64_t m = m0 + wave; m < m1; m += kDzWaves) {
+            floatx4 v[V], q[V];
 #pragma unroll
             for (int u = 0; u < V; ++u) {
                 const int64_t n = n0 + 4 * u;
                 const int left = N - n < 4 ? (N > n ? (int)(N - n) : 0) : 4;
-                floatx4 v = load_four(dy + m * lddy + n, left, dy_ok);
-                if constexpr (ACT != TIG_ACT_NONE) {
-                    const floatx4 q = load_four(z + m * ldz + n, left, z_ok);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        v[e] *= slope<ACT>(q[e]);
-                }
-                total[u] += v;
-                if (dz)
-                    store_four(dz + m * lddz + n, v, 4, true);
+                v[u] = load_four(dy + m * lddy + n, left, false);
+                if constexpr (ACT != TIG_ACT_NONE)
+                    q[u] = load_four(z + m * ldz + n, left, false);
             }
+            add(m, v, q);
+        }
+    }
     if (!sums)
         return;
 #pragma unroll
@@ -210,20 +239,21 @@ inline int64_t dz_rows(int64_t rows, int64_t cols, int per_lane)
 
 // out[n] = scale * sum of the blocks' column sums, in double
 template <typename T>
-__global__ void __launch_bounds__(256) k_join_sums(const float *sums, int64_t lds, int64_t blocks, int64_t N, T *out, const float *scale, float alpha)
+__global__ void __launch_bounds__(1024) k_join_sums(const float *sums, int64_t lds, int64_t blocks, int64_t N, T *out, const float *scale, float alpha)
 {
-    __shared__ double part[4][64];
-    const int64_t n = (int64_t)blockIdx.x * 64 + threadIdx.x % 64;
-    const int w = threadIdx.x / 64;
+    __shared__ double part[16][64];
+    const int c = threadIdx.x % 64, w = threadIdx.x / 64;
+    const int64_t n = (int64_t)blockIdx.x * 64 + c;
     double total = 0.0;
     if (n < N)
-#pragma unroll 4
-        for (int64_t b = w; b < blocks; b += 4)
+#pragma unroll 8
+        for (int64_t b = w; b < blocks; b += 16)
             total += (double)sums[b * lds + n];
-    part[w][threadIdx.x % 64] = total;
+    part[w][c] = total;
     __syncthreads();
     if (w == 0 && n < N) {
-        total = (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
+        for (int k = 1; k < 16; ++k)
+            total += part[k][c];
         out[n] = (T)(float)(total * (double)alpha * (scale ? (double)*scale : 1.0));
     }
 }
@@ -231,7 +261,7 @@ __global__ void __launch_bounds__(256) k_join_sums(const float *sums, int64_t ld
 template <typename T>
 hipError_t launch_join_sums(const float *sums, int64_t lds, int64_t blocks, int64_t N, T *out, const float *scale, float alpha, hipStream_t s)
 {
-    hipLaunchKernelGGL((k_join_sums<T>), dim3((unsigned)((N + 63) / 64)), dim3(256), 0, s, sums, lds, blocks, N, out, scale, alpha);
+    hipLaunchKernelGGL((k_join_sums<T>), dim3((unsigned)((N + 63) / 64)), dim3(1024), 0, s, sums, lds, blocks, N, out, scale, alpha);
     return hipGetLastError();
 }
 template hipError_t launch_join_sums<float>(const float *, int64_t, int64_t, int64_t, float *, const float *, float, hipStream_t);
@@ -388,7 +418,7 @@ hipError_t backward(const tig_linear &p, const LinearPlan &L, char *ws, hipStrea
         const dim3 grid((unsigned)((L.ld_dz + across - 1) / across), (unsigned)L.sum_blocks);
         with_activation(p.activation, [&](auto act) {
             hipLaunchKernelGGL((k_linear_dz<T, decltype(act)::value>), grid, dim3(64 * kDzWaves), 0, s, (const T *)p.dy, p.lddy, (const T *)p.z, p.ldz, out,
-                               L.ld_dz, sums, L.ld_sums, p.rows, p.out_dim, L.dz_per, four_aligned(p.dy, p.lddy, es), four_aligned(p.z, p.ldz, es));
+                               L.ld_dz, sums, L.ld_sums, p.rows, p.out_dim, L.dz_per, piece_aligned(p.dy, p.lddy, es), p.activation == TIG_ACT_NONE || piece_aligned(p.z, p.ldz, es));
             return 0;
         });
         if ((e = hipGetLastError()) != hipSuccess)

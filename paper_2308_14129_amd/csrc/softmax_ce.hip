@@ -255,26 +255,33 @@ struct EpiP {
             for (int e = 0; e < 4; ++e)
                 b[j][e] = e < left ? b[j][e] : -INFINITY;
         }
+        auto rows = [&](auto full) {
+            constexpr bool FULL = decltype(full)::value;
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            const int64_t m = at.m0 + i * 16 + i16;
-            const bool on = m < at.M;
-            const CeRow r = rec[on ? m : 0];
-            const float lse = on ? r.lse : INFINITY;
-            const int64_t hot = on ? (int64_t)r.label - v0 - at.n0 - 4 * g : -1;  // (of this lane's columns 16 j + e)
+            for (int i = 0; i < FM; ++i) {
+                const int64_t m = at.m0 + i * 16 + i16;
+                const bool on = FULL || m < at.M;
+                const CeRow r = rec[on ? m : 0];
+                const float lse = on ? r.lse : INFINITY;
+                T *const row = P + m * ldp + at.n0 + 4 * g;
+                const int64_t hot = on && r.label >= 0 ? (int64_t)r.label - v0 - at.n0 - 4 * g : -1;  // (of this lane's columns 16 j + e)
 #pragma unroll
-            for (int j = 0; j < FN; ++j) {
+                for (int j = 0; j < FN; ++j) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float p = lse != INFINITY ? exp_of<T>(acc[i][j][e] + b[j][e] - lse) : 0.0f;
-                    p -= hot == 16 * j + e && r.label >= 0 ? 1.0f : 0.0f;
-                    acc[i][j][e] = p * r.w;
+                    for (int e = 0; e < 4; ++e) {
+                        float p = lse != INFINITY ? exp_of<T>(acc[i][j][e] + b[j][e] - lse) : 0.0f;
+                        p -= hot == 16 * j + e ? 1.0f : 0.0f;
+                        acc[i][j][e] = p * r.w;
+                    }
+                    if (FULL || (on && at.n0 + j * 16 + 4 * g < end))
+                        store_four(row + j * 16, acc[i][j], 4, true);
                 }
-                const int64_t n = at.n0 + j * 16 + 4 * g;
-                if (on && n < end)
-                    store_four(P + m * ldp + n, acc[i][j], 4, true);
             }
-        }
+        };
+        if (at.m0 + FM * 16 <= at.M && at.n0 + FN * 16 <= at.N)  // (uniform)
+            rows(std::true_type());
+        else
+            rows(std::false_type());
         if (!sums)
             return;
         float *const red = (float *)smem;  // [WM][BN]
