@@ -11,22 +11,20 @@
 // values these eight are an operand of the second product as they lie, whose other operand (the streamed rows again, now
 // summed over) comes from the same LDS tile with the transposing load.  So each gradient forms the logits once more (10 n V d
 // operations instead of 8), and P is never in memory.
+//
+// BIASED: both matrices are copies with one column more: W's holds the candidate's bias (-infinity in the rows that fill its last
+// tile), X's ones, also in rows that do not count or fill the last tile.  The product adds the bias, and the column of dW that
+// belongs to the ones is the bias' gradient: the vector unit, which the exponentials keep busy as long as the products do the
+// matrix unit, has 10 of 16 instructions a logit less.
 #pragma once
 
 #include "gemm.h"
 
 namespace tig {
 
-#ifndef NARROW_F4
-#define NARROW_F4 3
-#define NARROW_F2 4
-#define NARROW_W 2
-#define NARROW_SF 3
-#define NARROW_SW 2
-#endif
 constexpr int kNarrowWaves = 4, kNarrowStream = 64;
 template <int KB>
-constexpr int kNarrowOwn = KB <= 2 ? NARROW_F2 : NARROW_F4;  // sixteens of own rows of a wavefront (registers: two wavefronts on a SIMD)
+constexpr int kNarrowOwn = KB <= 2 ? 4 : 3;  // sixteens of own rows of a wavefront (registers: two wavefronts on a SIMD)
 template <int KB>
 constexpr int kNarrowTile = 16 * kNarrowOwn<KB> * kNarrowWaves;
 
@@ -36,11 +34,11 @@ template <typename T>
 struct NarrowArgs {
     const T *own, *stream;
     int64_t ld_own, ld_stream, n_own, n_stream;
-    int d;
+    int d, k;                 // columns of a gradient, of the rows as they are read (BIASED: one more)
     int splits;               // ranges of the streamed rows
     int64_t per;              // tiles of a range
-    const float *own_add;     // [n_own] added to an own row's logits (a candidate's bias), or NULL
-    const float *stream_add;  // [whole tiles] added to a streamed row's logits, -infinity behind the last, or NULL
+    const float *own_add;     // not BIASED: [n_own] added to an own row's logits (a candidate's bias), or NULL
+    const float *stream_add;  // not BIASED: [whole tiles] added to a streamed row's logits, -infinity behind the last, or NULL
     const float *lse2_own;    // statistics: unused; dX: [n_own] lse log2 e - log2 of P's scale
     const float *lse2_stream; // dW: [whole tiles]
     const float *w_stream;    // dW, weighted rows: [whole tiles]
@@ -60,14 +58,14 @@ struct NarrowStream {
     static constexpr int kBytes = kNarrowStream * kRowBytes;
     uint32_t off[KB];
     int row[KB];
-    __device__ inline void init(int64_t ld, int d)
+    __device__ inline void init(int64_t ld, int k)
     {
 #pragma unroll
         for (int i = 0; i < KB; ++i) {
             const int o = ((wave_id_uniform() * KB + i) * 64 + lane_id()) * 16;
             row[i] = o / kRowBytes;
             const int c = (o % kRowBytes / 16) ^ (row[i] & kMask);
-            off[i] = c * 8 < d ? (uint32_t)(row[i] * ld * 2 + c * 16) : kBufferNone;
+            off[i] = c * 8 < k ? (uint32_t)(row[i] * ld * 2 + c * 16) : kBufferNone;
         }
     }
     __device__ inline void load(const T *base, int64_t left, char *lds) const
@@ -128,7 +126,7 @@ __device__ inline void load_own(const NarrowArgs<T> &a, int64_t m0, intx4 (&own)
 #pragma unroll
         for (int kk = 0; kk < KB; ++kk) {
             const int c = kk * 4 + g;
-            const uint32_t o = m < a.n_own && c * 8 < a.d ? (uint32_t)((i * 16 + i16) * a.ld_own * 2 + c * 16) : kBufferNone;
+            const uint32_t o = m < a.n_own && c * 8 < a.k ? (uint32_t)((i * 16 + i16) * a.ld_own * 2 + c * 16) : kBufferNone;
             own[i][kk] = __builtin_bit_cast(intx4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)o, 0, 0));
         }
     }
@@ -142,9 +140,11 @@ __device__ inline void load_with(const float *p, int64_t at, char *lds)
 }
 
 // what the logits of the four candidates from row r of tile t on start from: their bias, -infinity behind the last candidate
-template <typename T>
+template <bool BIASED, typename T>
 __device__ inline floatx4 start_of(const NarrowArgs<T> &a, int64_t t, int r, const char *with)
 {
+    if constexpr (BIASED)
+        return floatx4{0.0f, 0.0f, 0.0f, 0.0f};
     if (a.stream_add)  // (uniform; the table holds -infinity there)
         return *(const floatx4 *)(with + r * 4);
     floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -156,8 +156,8 @@ __device__ inline floatx4 start_of(const NarrowArgs<T> &a, int64_t t, int r, con
     return v;
 }
 
-template <typename T, int KB>
-__global__ void __launch_bounds__(64 * kNarrowWaves, NARROW_W) k_narrow_stats(NarrowArgs<T> a)
+template <typename T, int KB, bool BIASED>
+__global__ void __launch_bounds__(64 * kNarrowWaves, 2) k_narrow_stats(NarrowArgs<T> a)
 {
     constexpr int FM = kNarrowOwn<KB>, FN = 4;
     using S = NarrowStream<T, KB>;
@@ -168,10 +168,10 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, NARROW_W) k_narrow_stats(Na
     const int64_t m0 = (int64_t)tile * kNarrowTile<KB> + wave * 16 * FM;
     const int64_t t0 = split * a.per, all = (a.n_stream + kNarrowStream - 1) / kNarrowStream, t1 = t0 + a.per < all ? t0 + a.per : all;
     S st;
-    st.init(a.ld_stream, a.d);
+    st.init(a.ld_stream, a.k);
     auto request = [&](int64_t t, char *lds) {
         st.load(a.stream + t * kNarrowStream * a.ld_stream, a.n_stream - t * kNarrowStream, lds);
-        if (a.stream_add && wave == 0)
+        if (!BIASED && a.stream_add && wave == 0)
             load_with(a.stream_add, t * kNarrowStream, lds + S::kBytes);
     };
     intx4 own[FM][KB];
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, NARROW_W) k_narrow_stats(Na
         floatx4 acc[FM][FN];
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            const floatx4 from = start_of(a, t, 16 * j + 4 * g, now + S::kBytes);
+            const floatx4 from = start_of<BIASED>(a, t, 16 * j + 4 * g, now + S::kBytes);
 #pragma unroll
             for (int i = 0; i < FM; ++i)
                 acc[i][j] = from;
@@ -238,8 +238,8 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, NARROW_W) k_narrow_stats(Na
 }
 
 // CANDS: own rows are candidates (dW), else rows of X (dX).  WEIGHTED: rows of X have weights of their own.
-template <typename T, int KB, bool CANDS, bool WEIGHTED>
-__global__ void __launch_bounds__(64 * kNarrowWaves, NARROW_W) k_narrow_grad(NarrowArgs<T> a)
+template <typename T, int KB, bool BIASED, bool CANDS, bool WEIGHTED>
+__global__ void __launch_bounds__(64 * kNarrowWaves, 2) k_narrow_grad(NarrowArgs<T> a)
 {
     constexpr int FM = kNarrowOwn<KB>, DT = 2 * KB;
     using S = NarrowStream<T, KB>;
@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, NARROW_W) k_narrow_grad(Nar
     const int64_t m0 = (int64_t)tile * kNarrowTile<KB> + wave * 16 * FM;
     const int64_t t0 = split * a.per, all = (a.n_stream + kNarrowStream - 1) / kNarrowStream, t1 = t0 + a.per < all ? t0 + a.per : all;
     S st;
-    st.init(a.ld_stream, a.d);
+    st.init(a.ld_stream, a.k);
     auto request = [&](int64_t t, char *lds) {
         st.load(a.stream + t * kNarrowStream * a.ld_stream, a.n_stream - t * kNarrowStream, lds);
         if constexpr (CANDS) {
@@ -262,7 +262,7 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, NARROW_W) k_narrow_grad(Nar
             if (WEIGHTED && wave == 2)
                 load_with(a.w_stream, t * kNarrowStream, lds + S::kBytes + 512);
         } else {
-            if (a.stream_add && wave == 0)
+            if (!BIASED && a.stream_add && wave == 0)
                 load_with(a.stream_add, t * kNarrowStream, lds + S::kBytes);
         }
     };
@@ -290,8 +290,11 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, NARROW_W) k_narrow_grad(Nar
         if (t + 1 < t1)
             request(t + 1, smem[(t + 1 - t0) & 1]);
         const int base = (int)(t * kNarrowStream) + 4 * g;
-        bool hot = false;  // dX: the label of one of the wavefront's rows is in this tile
-        if constexpr (!CANDS) {
+        bool hot = false;  // a label of one of the rows is among the candidates of this wavefront and tile: seldom
+        if constexpr (CANDS) {
+            const int label = *(const int *)(now + S::kBytes + 256 + lane * 4);
+            hot = __ballot((uint32_t)(label - (int)m0) < (uint32_t)(16 * FM)) != 0ull;
+        } else {
 #pragma unroll
             for (int i = 0; i < FM; ++i)
                 hot |= (uint32_t)(mine_label[i] - (int)(t * kNarrowStream)) < (uint32_t)kNarrowStream;
@@ -306,7 +309,7 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, NARROW_W) k_narrow_grad(Nar
                 for (int j = 0; j < 2; ++j) {
                     floatx4 from = {0.0f, 0.0f, 0.0f, 0.0f};
                     if constexpr (!CANDS)
-                        from = start_of(a, t, x + 16 * j + 4 * g, now + S::kBytes);
+                        from = start_of<BIASED>(a, t, x + 16 * j + 4 * g, now + S::kBytes);
 #pragma unroll
                     for (int i = 0; i < FM; ++i)
                         acc[i][j] = from;
@@ -321,11 +324,9 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, NARROW_W) k_narrow_grad(Nar
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     floatx4 lse = {0.0f, 0.0f, 0.0f, 0.0f}, w = lse;
-                    intx4 label = {-1, -1, -1, -1};
+                    const char *const with = now + S::kBytes + (x + 16 * j + 4 * g) * 4;
                     if constexpr (CANDS) {
-                        const char *const with = now + S::kBytes + (x + 16 * j + 4 * g) * 4;
                         lse = *(const floatx4 *)with;
-                        label = *(const intx4 *)(with + 256);
                         if constexpr (WEIGHTED)
                             w = *(const floatx4 *)(with + 512);
                     }
@@ -333,7 +334,7 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, NARROW_W) k_narrow_grad(Nar
                     for (int i = 0; i < FM; ++i)
 #pragma unroll
                         for (int v = 0; v < 4; ++v)
-                            acc[i][j][v] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], kLog2e, CANDS ? mine[i] - lse[v] : mine[i]));
+                            acc[i][j][v] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], kLog2e, CANDS ? (BIASED ? -lse[v] : mine[i] - lse[v]) : mine[i]));
                     if constexpr (!CANDS)
                         if (hot)
 #pragma unroll
@@ -342,23 +343,19 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, NARROW_W) k_narrow_grad(Nar
                                 for (int i = 0; i < FM; ++i)
                                     acc[i][j][v] -= mine_label[i] == base + x + 16 * j + v ? a.p_scale : 0.0f;
                     if constexpr (CANDS) {
-                        // a label among this workgroup's candidates: seldom, and then for the whole wavefront
-                        const int64_t c0 = (int64_t)tile * kNarrowTile<KB>;
-                        bool any = false;
-#pragma unroll
-                        for (int v = 0; v < 4; ++v)
-                            any |= label[v] >= c0 && label[v] < c0 + kNarrowTile<KB>;
-                        if (__ballot(any) != 0ull)
+                        if (hot) {
+                            const intx4 label = *(const intx4 *)(with + 256);
 #pragma unroll
                             for (int v = 0; v < 4; ++v)
 #pragma unroll
                                 for (int i = 0; i < FM; ++i)
                                     acc[i][j][v] -= label[v] == (int)(m0 + i * 16 + i16) ? a.p_scale : 0.0f;
+                        }
 #pragma unroll
                         for (int i = 0; i < FM; ++i) {
                             if constexpr (WEIGHTED)
                                 acc[i][j] *= w;
-                            if (a.sums)
+                            if (!BIASED && a.sums)
                                 total[i] += (acc[i][j][0] + acc[i][j][1]) + (acc[i][j][2] + acc[i][j][3]);
                         }
                     }
@@ -375,7 +372,7 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, NARROW_W) k_narrow_grad(Nar
             }
 #pragma unroll
             for (int c = 0; c < DT; ++c)
-                if (c * 16 < a.d) {  // (uniform)
+                if (c * 16 < (CANDS ? a.k : a.d)) {  // (uniform)
                     const intx4 f = S::frag_t(now, x, c);
 #pragma unroll
                     for (int i = 0; i < FM; ++i)
@@ -386,7 +383,12 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, NARROW_W) k_narrow_grad(Nar
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
         const int64_t m = m0 + i * 16 + i16;
-        if (CANDS && a.sums) {
+        if (CANDS && BIASED && a.sums) {
+#pragma unroll
+            for (int c = 0; c < DT; ++c)
+                if (a.d / 4 == c * 4 + g && m < a.n_own)
+                    a.sums[(int64_t)split * a.n_own + m] = a.d % 4 == 0 ? out[i][c][0] : a.d % 4 == 1 ? out[i][c][1] : a.d % 4 == 2 ? out[i][c][2] : out[i][c][3];
+        } else if (CANDS && a.sums) {
             total[i] += __shfl_xor(total[i], 16);
             total[i] += __shfl_xor(total[i], 32);
             if (g == 0 && m < a.n_own)

@@ -164,6 +164,7 @@ struct CeRowsOut {
     int32_t *label;
     T *x0;
     int64_t ld_x0;
+    bool ones;         // a column of ones behind x0's last, also in rows that do not count and behind the last
 };
 template <typename T>
 __global__ void __launch_bounds__(256) k_ce_rows(const float2 *part, int64_t tiles, int64_t rows, const T *x, int64_t ldx, const T *w, int64_t ldw,
@@ -194,10 +195,17 @@ __global__ void __launch_bounds__(256) k_ce_rows(const float2 *part, int64_t til
         top = to;
         dot += __shfl_xor(dot, d);
     }
-    if (on && out.x0)  // (rows of x are whole 16-byte pieces here)
+    if (out.x0 && (on || out.ones))  // (rows of x are whole 16-byte pieces here)
         for (int64_t c = t * Mat<T>::kPer16; c < out.ld_x0; c += 16 * Mat<T>::kPer16) {
-            const intx4 v = counts && c < dim ? *(const intx4 *)(xr + c) : intx4{0, 0, 0, 0};
-            *(intx4 *)(out.x0 + i * out.ld_x0 + c) = v;
+            union {
+                intx4 q;
+                T v[Mat<T>::kPer16];
+            } u;
+            u.q = on && counts && c < dim ? *(const intx4 *)(xr + c) : intx4{0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < Mat<T>::kPer16; ++e)
+                u.v[e] = out.ones && c + e == dim ? (T)1.0f : u.v[e];
+            *(intx4 *)(out.x0 + i * out.ld_x0 + c) = u.q;
         }
     if (t != 0)
         return;
@@ -358,6 +366,27 @@ __global__ void __launch_bounds__(256) k_ce_narrow_dx(const float *grad, int spl
     }
 }
 
+// A copy with a column more (`extra`, or `fill` where that is NULL) and rows up to whole tiles: zeros and, in that column, `behind`.
+// A thread takes one 16-byte piece.
+template <typename T>
+__global__ void __launch_bounds__(256) k_ce_copy(const T *src, int64_t ld_src, int64_t rows, int64_t cols, const T *extra, float fill, float behind, T *dst,
+                                                 int64_t ld_dst, int64_t all)
+{
+    constexpr int per = Mat<T>::kPer16;
+    const int64_t pieces = ld_dst / per;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all * pieces; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / pieces, c = i % pieces * per;
+        struct alignas(16) Piece {
+            T v[per];
+        } q;
+        const T *p = src + r * ld_src + c;
+#pragma unroll
+        for (int e = 0; e < per; ++e)
+            q.v[e] = c + e < cols && r < rows ? p[e] : c + e != cols ? (T)0.0f : r >= rows ? (T)behind : extra ? extra[r] : (T)fill;
+        *(Piece *)(dst + r * ld_dst + c) = q;
+    }
+}
+
 // a bias in fp32, -infinity behind its last (whole tiles)
 template <typename T>
 __global__ void __launch_bounds__(256) k_ce_bias(const T *bias, int64_t vocab, float *out, int64_t all)
@@ -380,6 +409,7 @@ struct CePlan {
     bool acc;                // more than one piece: dX in fp32 first
     // narrow rows
     int kb;                  // 32-column blocks of a row (0: not narrow)
+    bool biased;             // copies with a column more (ce_narrow.h)
     int64_t own_rows, own_cands;  // tiles of own rows
     int s_stat, s_dx, s_dw;  // ranges of the streamed rows
     int64_t row_tiles, cand_tiles;  // whole tiles of 64
@@ -410,29 +440,34 @@ CePlan ce_plan(const tig_softmax_ce &p)
         L.bytes = off;
         return L;
     }
-    L.pack_x = !gemm_fits(p.x, p.ldx, d, es);
-    L.pack_w = !gemm_fits(p.w, p.ldw, d, es);
-    if (L.pack_x)
-        L.px = take((size_t)n * L.ld_x * es);
-    if (L.pack_w)
-        L.pw = take((size_t)V * L.ld_w * es);
     if (es == 2 && d <= 128) {
         L.kb = d <= 64 ? 2 : 4;
         const int64_t tile = L.kb == 2 ? kNarrowTile<2> : kNarrowTile<4>;
         L.own_rows = (n + tile - 1) / tile, L.own_cands = (V + tile - 1) / tile;
         L.row_tiles = (n + kNarrowStream - 1) / kNarrowStream, L.cand_tiles = (V + kNarrowStream - 1) / kNarrowStream;
+        // A column more, where the blocks have room for one.  The copy of W costs what about 80 rows do; where W is copied
+        // anyway, nothing.
+        const bool fits = gemm_fits(p.w, p.ldw, d, es);
+        L.biased = d < 32 * L.kb && (!fits || n >= 512);
+        L.pack_x = L.biased || !gemm_fits(p.x, p.ldx, d, es);
+        L.pack_w = L.biased || !fits;
+        L.ld_x = L.ld_w = pack_ld(L.biased ? d + 1 : d, es);
+        if (L.pack_x)
+            L.px = take((size_t)n * L.ld_x * es);
+        if (L.pack_w)
+            L.pw = take((size_t)L.cand_tiles * kNarrowStream * L.ld_w * es);
         L.s_stat = L.s_dx = narrow_splits(L.own_rows, V);
         L.s_dw = narrow_splits(L.own_cands, n);
         L.stat_rows = n;
         L.part = take((size_t)L.s_stat * n * sizeof(float2));
-        if (p.bias)
+        if (p.bias && !L.biased)
             L.bias32 = take((size_t)L.cand_tiles * kNarrowStream * 4);
         if (L.grad) {
             const size_t tab = (size_t)L.row_tiles * kNarrowStream * 4;
             L.lse2 = take(tab);
             L.weight = take(tab);
             L.label = take(tab);
-            L.px0 = take((size_t)n * L.ld_x * es);
+            L.px0 = take((size_t)L.row_tiles * kNarrowStream * L.ld_x * es);
             L.ld_acc = (d + 3) / 4 * 4;
             if (p.dx)
                 L.dxa = take((size_t)L.s_dx * n * L.ld_acc * 4);
@@ -444,6 +479,12 @@ CePlan ce_plan(const tig_softmax_ce &p)
         L.bytes = off;
         return L;
     }
+    L.pack_x = !gemm_fits(p.x, p.ldx, d, es);
+    L.pack_w = !gemm_fits(p.w, p.ldw, d, es);
+    if (L.pack_x)
+        L.px = take((size_t)n * L.ld_x * es);
+    if (L.pack_w)
+        L.pw = take((size_t)V * L.ld_w * es);
     L.stat = gemm_plan(n, V, d, es, false);
     const int64_t tiles = (V + L.stat.tile - 1) / L.stat.tile;
     int64_t most = (int64_t)(kStatBytes / 8) / tiles / 256 * 256;
@@ -524,8 +565,18 @@ hipError_t launch_mean(const tig_softmax_ce &p, const float *loss, CeHead *head,
     return hipGetLastError();
 }
 
+template <typename T>
+hipError_t launch_copy(const T *src, int64_t ld_src, int64_t rows, int64_t cols, const T *extra, float fill, float behind, T *dst, int64_t ld_dst,
+                       int64_t all, hipStream_t s)
+{
+    const int64_t blocks = (all * (ld_dst / Mat<T>::kPer16) + 255) / 256;
+    hipLaunchKernelGGL((k_ce_copy<T>), dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, s, src, ld_src, rows, cols, extra, fill, behind, dst,
+                       ld_dst, all);
+    return hipGetLastError();
+}
+
 // 16-bit rows of at most 32 KB columns; x and w are rows of whole 16-byte pieces
-template <typename T, int KB>
+template <typename T, int KB, bool BIASED>
 hipError_t run_narrow(const tig_softmax_ce &p, const CePlan &L, char *ws, const T *x, int64_t ldx, const T *w, int64_t ldw, const CeRowsOut<T> &out,
                       hipStream_t s)
 {
@@ -533,7 +584,7 @@ hipError_t run_narrow(const tig_softmax_ce &p, const CePlan &L, char *ws, const 
     CeHead *const head = (CeHead *)(ws + L.head);
     const float alpha = 1.0f / kPScale<T>;
     float *bias32 = nullptr;
-    if (p.bias) {
+    if (p.bias && !BIASED) {
         bias32 = (float *)(ws + L.bias32);
         const int64_t all = L.cand_tiles * kNarrowStream;
         hipLaunchKernelGGL((k_ce_bias<T>), dim3((unsigned)((all + 255) / 256)), dim3(256), 0, s, (const T *)p.bias, V, bias32, all);
@@ -542,12 +593,12 @@ hipError_t run_narrow(const tig_softmax_ce &p, const CePlan &L, char *ws, const 
     const dim3 threads(64 * kNarrowWaves);
     NarrowArgs<T> a = {};
     a.own = x, a.ld_own = ldx, a.n_own = n;
-    a.stream = w, a.ld_stream = ldw, a.n_stream = V;
-    a.d = (int)p.dim;
+    a.stream = w, a.ld_stream = ldw, a.n_stream = BIASED ? L.cand_tiles * kNarrowStream : V;
+    a.d = (int)p.dim, a.k = a.d + (BIASED ? 1 : 0);
     a.stream_add = bias32;
     a.splits = L.s_stat, a.per = (L.cand_tiles + L.s_stat - 1) / L.s_stat;
     a.part = (float2 *)(ws + L.part);
-    hipLaunchKernelGGL((k_narrow_stats<T, KB>), dim3((unsigned)(L.own_rows * L.s_stat)), threads, 0, s, a);
+    hipLaunchKernelGGL((k_narrow_stats<T, KB, BIASED>), dim3((unsigned)(L.own_rows * L.s_stat)), threads, 0, s, a);
     CE_TRY(hipGetLastError());
     CE_TRY(launch_rows(p, 0, n, a.part, L.s_stat, x, ldx, w, ldw, head, out, s));
     CE_TRY(launch_mean(p, out.loss, head, s));
@@ -561,7 +612,7 @@ hipError_t run_narrow(const tig_softmax_ce &p, const CePlan &L, char *ws, const 
         a.lse2_own = out.lse2;
         a.labels = out.label;
         a.grad = (float *)(ws + L.dxa);
-        hipLaunchKernelGGL((k_narrow_grad<T, KB, false, false>), dim3((unsigned)(L.own_rows * L.s_dx)), threads, 0, s, a);
+        hipLaunchKernelGGL((k_narrow_grad<T, KB, BIASED, false, false>), dim3((unsigned)(L.own_rows * L.s_dx)), threads, 0, s, a);
         CE_TRY(hipGetLastError());
         const int64_t blocks = (n * ((p.dim + 3) / 4) + 255) / 256;
         hipLaunchKernelGGL((k_ce_narrow_dx<T>), dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, s, a.grad, L.s_dx, a.ld_grad, n, p.dim,
@@ -570,7 +621,7 @@ hipError_t run_narrow(const tig_softmax_ce &p, const CePlan &L, char *ws, const 
     }
     if (p.dw || p.dbias) {
         a.own = w, a.ld_own = ldw, a.n_own = V;
-        a.stream = out.x0, a.ld_stream = out.ld_x0, a.n_stream = n;
+        a.stream = out.x0, a.ld_stream = out.ld_x0, a.n_stream = BIASED ? L.row_tiles * kNarrowStream : n;
         a.own_add = bias32, a.stream_add = nullptr;
         a.lse2_stream = out.lse2, a.w_stream = out.w, a.labels = out.label;
         a.splits = L.s_dw, a.per = (L.row_tiles + L.s_dw - 1) / L.s_dw;
@@ -581,9 +632,9 @@ hipError_t run_narrow(const tig_softmax_ce &p, const CePlan &L, char *ws, const 
             a.direct = store;
         const dim3 grid((unsigned)(L.own_cands * L.s_dw));
         if (p.row_scale || p.scale < 0.0f)
-            hipLaunchKernelGGL((k_narrow_grad<T, KB, true, true>), grid, threads, 0, s, a);
+            hipLaunchKernelGGL((k_narrow_grad<T, KB, BIASED, true, true>), grid, threads, 0, s, a);
         else
-            hipLaunchKernelGGL((k_narrow_grad<T, KB, true, false>), grid, threads, 0, s, a);
+            hipLaunchKernelGGL((k_narrow_grad<T, KB, BIASED, true, false>), grid, threads, 0, s, a);
         CE_TRY(hipGetLastError());
         if (p.dw && L.s_dw > 1)
             CE_TRY(launch_join(a.grad, L.s_dw, V, p.dim, a.ld_grad, store, s));
@@ -614,14 +665,19 @@ hipError_t run(const tig_softmax_ce &p, const CePlan &L, char *ws, hipStream_t s
         hipLaunchKernelGGL(k_ce_top, dim3(1), dim3(1024), 0, s, p.labels, p.row_scale, p.scale, n, V, head);
         CE_TRY(hipGetLastError());
     }
-    if (L.pack_x) {
-        CE_TRY(launch_pack(x, ldx, ws + L.px, L.ld_x, n, d, es, s));
+    if (L.biased) {
+        CE_TRY(launch_copy<T>(x, ldx, n, d, nullptr, 1.0f, 1.0f, (T *)(ws + L.px), L.ld_x, n, s));
+        CE_TRY(launch_copy<T>(w, ldw, V, d, bias, 0.0f, -INFINITY, (T *)(ws + L.pw), L.ld_w, L.cand_tiles * kNarrowStream, s));
+    } else {
+        if (L.pack_x)
+            CE_TRY(launch_pack(x, ldx, ws + L.px, L.ld_x, n, d, es, s));
+        if (L.pack_w)
+            CE_TRY(launch_pack(w, ldw, ws + L.pw, L.ld_w, V, d, es, s));
+    }
+    if (L.pack_x)
         x = (const T *)(ws + L.px), ldx = L.ld_x;
-    }
-    if (L.pack_w) {
-        CE_TRY(launch_pack(w, ldw, ws + L.pw, L.ld_w, V, d, es, s));
+    if (L.pack_w)
         w = (const T *)(ws + L.pw), ldw = L.ld_w;
-    }
     float *const loss = p.loss ? p.loss : (float *)(ws + L.loss);
     CeRowsOut<T> out = {};
     out.loss = loss, out.lse = p.lse;
@@ -630,10 +686,11 @@ hipError_t run(const tig_softmax_ce &p, const CePlan &L, char *ws, hipStream_t s
     else if (L.grad)
         out.rec = (CeRow *)(ws + L.rec);
     if (L.grad && (L.kb || p.dw))
-        out.x0 = (T *)(ws + L.px0), out.ld_x0 = L.ld_x;
+        out.x0 = (T *)(ws + L.px0), out.ld_x0 = L.ld_x, out.ones = L.biased;
     if constexpr (es == 2)
         if (L.kb)
-            return L.kb == 2 ? run_narrow<T, 2>(p, L, ws, x, ldx, w, ldw, out, s) : run_narrow<T, 4>(p, L, ws, x, ldx, w, ldw, out, s);
+            return L.kb == 2 ? (L.biased ? run_narrow<T, 2, true>(p, L, ws, x, ldx, w, ldw, out, s) : run_narrow<T, 2, false>(p, L, ws, x, ldx, w, ldw, out, s))
+                             : (L.biased ? run_narrow<T, 4, true>(p, L, ws, x, ldx, w, ldw, out, s) : run_narrow<T, 4, false>(p, L, ws, x, ldx, w, ldw, out, s));
     const bool bias_ok = four_aligned(bias, 4, es);
     float2 *const part = (float2 *)(ws + L.part);
     const int64_t tiles = (V + L.stat.tile - 1) / L.stat.tile;
