@@ -238,10 +238,11 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, 2) k_narrow_stats(NarrowArg
 }
 
 // CANDS: own rows are candidates (dW), else rows of X (dX).  WEIGHTED: rows of X have weights of their own.
-template <typename T, int KB, bool BIASED, bool CANDS, bool WEIGHTED>
+// DT: sixteens of columns of the gradient.
+template <typename T, int KB, int DT, bool BIASED, bool CANDS, bool WEIGHTED>
 __global__ void __launch_bounds__(64 * kNarrowWaves, 2) k_narrow_grad(NarrowArgs<T> a)
 {
-    constexpr int FM = kNarrowOwn<KB>, DT = 2 * KB;
+    constexpr int FM = kNarrowOwn<KB>;
     using S = NarrowStream<T, KB>;
     constexpr int kWith = 3 * 256;  // floats that go with a streamed tile: what its logits start from, or lse and weights, labels
     __shared__ __attribute__((aligned(1024))) char smem[2][S::kBytes + kWith];
@@ -371,13 +372,12 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, 2) k_narrow_grad(NarrowArgs
                 }
             }
 #pragma unroll
-            for (int c = 0; c < DT; ++c)
-                if (c * 16 < (CANDS ? a.k : a.d)) {  // (uniform)
-                    const intx4 f = S::frag_t(now, x, c);
+            for (int c = 0; c < DT; ++c) {
+                const intx4 f = S::frag_t(now, x, c);
 #pragma unroll
-                    for (int i = 0; i < FM; ++i)
-                        mma16(out[i][c], f, P[i], T());
-                }
+                for (int i = 0; i < FM; ++i)
+                    mma16(out[i][c], f, P[i], T());
+            }
         }
     }
 #pragma unroll

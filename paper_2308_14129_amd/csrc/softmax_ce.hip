@@ -441,7 +441,7 @@ CePlan ce_plan(const tig_softmax_ce &p)
         return L;
     }
     if (es == 2 && d <= 128) {
-        L.kb = d <= 64 ? 2 : 4;
+        L.kb = d <= 64 ? 2 : 4;  // (a column more does not change it, see run_narrow_of)
         const int64_t tile = L.kb == 2 ? kNarrowTile<2> : kNarrowTile<4>;
         L.own_rows = (n + tile - 1) / tile, L.own_cands = (V + tile - 1) / tile;
         L.row_tiles = (n + kNarrowStream - 1) / kNarrowStream, L.cand_tiles = (V + kNarrowStream - 1) / kNarrowStream;
@@ -576,7 +576,7 @@ hipError_t launch_copy(const T *src, int64_t ld_src, int64_t rows, int64_t cols,
 }
 
 // 16-bit rows of at most 32 KB columns; x and w are rows of whole 16-byte pieces
-template <typename T, int KB, bool BIASED>
+template <typename T, int KB, int DT, bool BIASED>
 hipError_t run_narrow(const tig_softmax_ce &p, const CePlan &L, char *ws, const T *x, int64_t ldx, const T *w, int64_t ldw, const CeRowsOut<T> &out,
                       hipStream_t s)
 {
@@ -612,7 +612,7 @@ hipError_t run_narrow(const tig_softmax_ce &p, const CePlan &L, char *ws, const 
         a.lse2_own = out.lse2;
         a.labels = out.label;
         a.grad = (float *)(ws + L.dxa);
-        hipLaunchKernelGGL((k_narrow_grad<T, KB, BIASED, false, false>), dim3((unsigned)(L.own_rows * L.s_dx)), threads, 0, s, a);
+        hipLaunchKernelGGL((k_narrow_grad<T, KB, DT, BIASED, false, false>), dim3((unsigned)(L.own_rows * L.s_dx)), threads, 0, s, a);
         CE_TRY(hipGetLastError());
         const int64_t blocks = (n * ((p.dim + 3) / 4) + 255) / 256;
         hipLaunchKernelGGL((k_ce_narrow_dx<T>), dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, s, a.grad, L.s_dx, a.ld_grad, n, p.dim,
@@ -632,9 +632,9 @@ hipError_t run_narrow(const tig_softmax_ce &p, const CePlan &L, char *ws, const 
             a.direct = store;
         const dim3 grid((unsigned)(L.own_cands * L.s_dw));
         if (p.row_scale || p.scale < 0.0f)
-            hipLaunchKernelGGL((k_narrow_grad<T, KB, BIASED, true, true>), grid, threads, 0, s, a);
+            hipLaunchKernelGGL((k_narrow_grad<T, KB, DT, BIASED, true, true>), grid, threads, 0, s, a);
         else
-            hipLaunchKernelGGL((k_narrow_grad<T, KB, BIASED, true, false>), grid, threads, 0, s, a);
+            hipLaunchKernelGGL((k_narrow_grad<T, KB, DT, BIASED, true, false>), grid, threads, 0, s, a);
         CE_TRY(hipGetLastError());
         if (p.dw && L.s_dw > 1)
             CE_TRY(launch_join(a.grad, L.s_dw, V, p.dim, a.ld_grad, store, s));
@@ -642,6 +642,22 @@ hipError_t run_narrow(const tig_softmax_ce &p, const CePlan &L, char *ws, const 
             CE_TRY((launch_join_sums<T>(a.sums, V, L.s_dw, V, (T *)p.dbias, &head->S, alpha, s)));
     }
     return hipSuccess;
+}
+
+template <typename T, bool BIASED>
+hipError_t run_narrow_of(const tig_softmax_ce &p, const CePlan &L, char *ws, const T *x, int64_t ldx, const T *w, int64_t ldw, const CeRowsOut<T> &out,
+                         hipStream_t s)
+{
+    const int64_t columns = p.dim + (BIASED ? 1 : 0);
+    if (columns <= 32)
+        return run_narrow<T, 2, 2, BIASED>(p, L, ws, x, ldx, w, ldw, out, s);
+    if (columns <= 64)
+        return run_narrow<T, 2, 4, BIASED>(p, L, ws, x, ldx, w, ldw, out, s);
+    if (columns <= 96)
+        return run_narrow<T, 4, 6, BIASED>(p, L, ws, x, ldx, w, ldw, out, s);
+    if (columns <= 112)
+        return run_narrow<T, 4, 7, BIASED>(p, L, ws, x, ldx, w, ldw, out, s);
+    return run_narrow<T, 4, 8, BIASED>(p, L, ws, x, ldx, w, ldw, out, s);
 }
 
 template <typename T>
@@ -689,8 +705,7 @@ hipError_t run(const tig_softmax_ce &p, const CePlan &L, char *ws, hipStream_t s
         out.x0 = (T *)(ws + L.px0), out.ld_x0 = L.ld_x, out.ones = L.biased;
     if constexpr (es == 2)
         if (L.kb)
-            return L.kb == 2 ? (L.biased ? run_narrow<T, 2, true>(p, L, ws, x, ldx, w, ldw, out, s) : run_narrow<T, 2, false>(p, L, ws, x, ldx, w, ldw, out, s))
-                             : (L.biased ? run_narrow<T, 4, true>(p, L, ws, x, ldx, w, ldw, out, s) : run_narrow<T, 4, false>(p, L, ws, x, ldx, w, ldw, out, s));
+            return L.biased ? run_narrow_of<T, true>(p, L, ws, x, ldx, w, ldw, out, s) : run_narrow_of<T, false>(p, L, ws, x, ldx, w, ldw, out, s);
     const bool bias_ok = four_aligned(bias, 4, es);
     float2 *const part = (float2 *)(ws + L.part);
     const int64_t tiles = (V + L.stat.tile - 1) / L.stat.tile;
