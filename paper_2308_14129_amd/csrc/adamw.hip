@@ -43,7 +43,7 @@ struct AdamChunk {
 // the step's numbers
 struct AdamNow {
     float c, step_size, root_scale, lr;
-    uint32_t t;
+    int64_t t;
     int32_t skip;
 };
 
@@ -76,7 +76,7 @@ __device__ inline AdamNow numbers(const AdamParams &p, int64_t t)
     now.lr = (float)p.lr;
     now.step_size = (float)(p.lr / (1.0 - pow(p.beta1, (double)t)));
     now.root_scale = (float)(1.0 / sqrt(1.0 - pow(p.beta2, (double)t)));
-    now.t = (uint32_t)t;
+    now.t = t;
     return now;
 }
 
@@ -277,7 +277,7 @@ __device__ inline void update_chunk(const AdamParams &p, const AdamChunk &ch, co
             for (int e = 0; e < 4; ++e) {
                 top_m = fmaxf(top_m, e < left ? fabsf(m[r][e]) : 0.0f);
                 top_r = fmaxf(top_r, e < left ? root[e] : 0.0f);
-                const uint32_t h = (uint32_t)(i % kStateBlock + e) * 0x6A09E667u + now.t * 0x9E3779B9u;
+                const uint32_t h = (uint32_t)(i % kStateBlock + e) * 0x6A09E667u + (uint32_t)now.t * 0x9E3779B9u;
                 um[e] = (float)(h >> 8) * 0x1p-24f;
                 ur[e] = (float)((h + 0x80000000u) >> 8) * 0x1p-24f;
             }
@@ -292,21 +292,25 @@ __device__ inline void update_chunk(const AdamParams &p, const AdamChunk &ch, co
     }
 }
 
-// FEW: every workgroup forms the step's numbers, the last one to finish counts the step (the others have read the counter)
+// FEW: every workgroup forms the step's numbers.  With clipping they start from what k_adamw_norm left, and nobody reads the
+// counter any more; without, the last workgroup to finish counts the step (the others have read the counter by then).
 template <int BITS, bool FEW>
 __global__ void __launch_bounds__(kAdamThreads) k_adamw_update(AdamParams p)
 {
     const AdamChunk ch = p.chunks[blockIdx.x];
     AdamNow now;
-    int64_t t = 0;
+    const bool clip = p.max_norm > 0.0;
     auto form = [&]() -> AdamNow {
         if constexpr (FEW) {
-            t = *p.step + 1;
-            now = p.max_norm > 0.0 ? *p.now : numbers(p, t);  // (uniform; of k_adamw_norm)
-            const double norm = p.max_norm > 0.0 ? norm_of(p) : 0.0;
+            now = clip ? *p.now : numbers(p, *p.step + 1);  // (uniform)
+            const double norm = clip ? norm_of(p) : 0.0;
             scale_by_norm(p, norm, now);
-            if (p.norm_out && p.max_norm > 0.0 && blockIdx.x == 0 && threadIdx.x == 0)
-                *p.norm_out = (float)norm;
+            if (clip && blockIdx.x == 0 && threadIdx.x == 0) {
+                if (p.norm_out)
+                    *p.norm_out = (float)norm;
+                if (!now.skip)
+                    *p.step = now.t;
+            }
         } else {
             now = *p.now;
         }
@@ -325,12 +329,11 @@ __global__ void __launch_bounds__(kAdamThreads) k_adamw_update(AdamParams p)
         update(__bf16());
     else
         update(_Float16());
-    if constexpr (FEW) {
+    if (FEW && !clip) {
         __syncthreads();
         if (threadIdx.x == 0 && atomicAdd(p.arrived, 1u) == gridDim.x - 1) {
             *p.arrived = 0u;
-            if (!now.skip)
-                *p.step = t;
+            *p.step = now.t;
         }
     }
 }
