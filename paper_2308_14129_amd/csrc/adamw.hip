@@ -1,11 +1,10 @@
 // One AdamW step over many tensors (include/tig.h, tig_adamw_*).  gfx950.
 //
-// The tensors are cut into chunks of 4096 elements, one workgroup each, listed once in the workspace: one launch whatever their
+// The tensors are cut into chunks, one workgroup each, listed once in the workspace: one launch whatever their
 // number.  Bound by memory: every element's parameter and states are read and written once, its gradient read once, and once
 // more where the norm is wanted.
 //   k_adamw_norm    sums of squares, in double (only with clipping)
-//   k_adamw_begin   the step's numbers: clip coefficient, bias corrections, counter; for up to 1024 chunks the update's workgroups
-//                   form them themselves
+//   k_adamw_begin   the step's numbers: clip coefficient, bias corrections, counter; few elements' update does that itself
 //   k_adamw_update  the step
 // 8-bit states: a wavefront takes the 256 elements that share a power of two, four per lane: scales are exact, and values that
 // do not change keep their code whatever the rest of their block does.
@@ -20,14 +19,16 @@ namespace tig {
 
 namespace {
 
-constexpr int kChunk = 4096, kStateBlock = 256, kAdamThreads = 256;
-constexpr int kAtOnce = 4 * kAdamThreads;     // elements of a workgroup, four of a lane
-constexpr int kRounds = kChunk / kAtOnce;     // of a chunk: all of its loads are on their way at once
-constexpr int kNormGroups = 2048;             // workgroups that form the norm, at most
-constexpr int64_t kFewChunks = 1024;          // up to here the update forms the step's numbers itself, the norm from at most
-constexpr int kFewGroups = 256;               // as many partial sums
+constexpr int kStateBlock = 256, kAdamThreads = 256;
+constexpr int kAtOnce = 4 * kAdamThreads;  // elements of a workgroup's round, four of a lane
+// A chunk has four rounds, all of whose loads are on their way at once, or, where the tensors have up to 2^22 elements together,
+// one: such a call is as long as a workgroup's chain of round trips.
+constexpr int kRoundsMany = 4, kRoundsFew = 1;
+constexpr int64_t kFewElements = 1 << 22;
+constexpr int kNormGroups = 8192;          // workgroups that form the norm, at most
+constexpr int kFewGroups = 256;            // the same for few elements: every workgroup of the update adds their sums up
 
-// 4096 elements of a tensor: where they lie.  (All of it in one record: from it to the data is one round trip.)
+// A chunk of a tensor: where it lies.  (All of it in one record: from it to the data is one round trip.)
 struct AdamChunk {
     void *param;
     const void *grad;
@@ -51,7 +52,6 @@ struct AdamParams {
     const AdamChunk *chunks;
     double *part;       // [kNormGroups]
     AdamNow *now;
-    uint32_t *arrived;  // workgroups that are done with a launch; zero between launches
     int64_t *step;
     int64_t n_chunks;
     int n_parts;        // of `part`
@@ -80,21 +80,20 @@ __device__ inline AdamNow numbers(const AdamParams &p, int64_t t)
     return now;
 }
 
-template <typename T>
-__device__ inline double squares(const T *g, int n, bool wide)
+template <int ROUNDS, typename T>
+__device__ inline void load_grads(const T *g, int n, bool wide, floatx4 (&v)[ROUNDS])
 {
-    double total = 0.0;
+    if (wide && n == ROUNDS * kAtOnce) {  // (uniform: a load in a lane's branch would be waited for at the branch's end)
 #pragma unroll
-    for (int u = 0; u < kChunk / kAtOnce; ++u) {
-        const int i = u * kAtOnce + (int)threadIdx.x * 4;
-        if (i < n) {
-            const floatx4 v = load_four(g + i, n - i < 4 ? n - i : 4, wide);
+        for (int r = 0; r < ROUNDS; ++r)
+            v[r] = load_four(g + r * kAtOnce + (int)threadIdx.x * 4, 4, true);
+    } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                total += (double)v[e] * (double)v[e];
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int i = r * kAtOnce + (int)threadIdx.x * 4;
+            v[r] = load_four(g + i, n - i < 4 ? (n > i ? n - i : 0) : 4, wide);
         }
     }
-    return total;
 }
 
 // the workgroup's sum of its threads' values, for every thread
@@ -110,18 +109,34 @@ __device__ inline double group_sum(double v)
 }
 
 // sums of squares in double, and the numbers that do not need them
+template <int ROUNDS>
 __global__ void __launch_bounds__(kAdamThreads) k_adamw_norm(AdamParams p)
 {
     double total = 0.0;
     if (blockIdx.x == 0 && threadIdx.x == 0)
         *p.now = numbers(p, *p.step + 1);
-    AdamChunk next = p.chunks[blockIdx.x];
-    for (int64_t c = blockIdx.x; c < p.n_chunks; c += gridDim.x) {
-        const AdamChunk ch = next;
-        next = p.chunks[c + gridDim.x < p.n_chunks ? c + gridDim.x : c];
-        total += ch.dtype == TIG_F32    ? squares((const float *)ch.grad, ch.n, ch.wide)
-                 : ch.dtype == TIG_BF16 ? squares((const __bf16 *)ch.grad, ch.n, ch.wide)
-                                        : squares((const _Float16 *)ch.grad, ch.n, ch.wide);
+    // two chunks' loads on their way at a time
+    for (int64_t c = blockIdx.x; c < p.n_chunks; c += 2 * (int64_t)gridDim.x) {
+        const bool both = c + gridDim.x < p.n_chunks;  // (uniform)
+        const AdamChunk ch[2] = {p.chunks[c], p.chunks[both ? c + gridDim.x : c]};
+        floatx4 v[2][ROUNDS];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int n = k == 0 || both ? ch[k].n : 0;
+            if (ch[k].dtype == TIG_F32)
+                load_grads<ROUNDS>((const float *)ch[k].grad, n, ch[k].wide, v[k]);
+            else if (ch[k].dtype == TIG_BF16)
+                load_grads<ROUNDS>((const __bf16 *)ch[k].grad, n, ch[k].wide, v[k]);
+            else
+                load_grads<ROUNDS>((const _Float16 *)ch[k].grad, n, ch[k].wide, v[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int r = 0; r < ROUNDS; ++r)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    total += (double)v[k][r][e] * (double)v[k][r][e];
     }
     total = group_sum(total);
     if (threadIdx.x == 0)
@@ -132,6 +147,7 @@ __global__ void __launch_bounds__(kAdamThreads) k_adamw_norm(AdamParams p)
 __device__ inline double norm_of(const AdamParams &p)
 {
     double total = 0.0;
+#pragma unroll 8
     for (int i = threadIdx.x; i < p.n_parts; i += kAdamThreads)
         total += p.part[i];
     return fabs(p.grad_scale) * sqrt(group_sum(total));
@@ -214,16 +230,16 @@ __device__ inline void store_bytes(uint8_t *p, uint32_t w, int left, bool wide)
 
 // A lane's fours of a chunk; numbers(): the step's, once the loads are on their way.  Products and sums in the order of the formulas, each rounded: a state's code does not depend
 // on what the compiler joins.  A wavefront's four times 64 elements of a round are a block of 256.
-template <typename T, int BITS, bool WIDE, class F>
+template <typename T, int BITS, int ROUNDS, bool WIDE, class F>
 __device__ inline void update_chunk(const AdamParams &p, const AdamChunk &ch, const F &numbers)
 {
 #pragma clang fp contract(off)
-    floatx4 g[kRounds], x[kRounds], m[kRounds], v[kRounds];
-    uint32_t wm[kRounds], wv[kRounds];
-    float sm[kRounds], sv[kRounds];
+    floatx4 g[ROUNDS], x[ROUNDS], m[ROUNDS], v[ROUNDS];
+    uint32_t wm[ROUNDS], wv[ROUNDS];
+    float sm[ROUNDS], sv[ROUNDS];
     const int i0 = (int)threadIdx.x * 4;
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         const int i = i0 + r * kAtOnce, left = WIDE || ch.n - i >= 4 ? 4 : (ch.n > i ? ch.n - i : 0);
         g[r] = load_four((const T *)ch.grad + i, left, WIDE);
         x[r] = ch.master ? load_four(ch.master + i, left, WIDE) : load_four((const T *)ch.param + i, left, WIDE);
@@ -243,7 +259,7 @@ __device__ inline void update_chunk(const AdamParams &p, const AdamChunk &ch, co
         return;
     const float keep = 1.0f - now.lr * ch.decay;
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
         const int i = i0 + r * kAtOnce, left = WIDE || ch.n - i >= 4 ? 4 : (ch.n > i ? ch.n - i : 0);
         if constexpr (BITS == 8) {
             m[r] = from_8bit(wm[r], sm[r]);
@@ -292,36 +308,31 @@ __device__ inline void update_chunk(const AdamParams &p, const AdamChunk &ch, co
     }
 }
 
-// FEW: every workgroup forms the step's numbers.  With clipping they start from what k_adamw_norm left, and nobody reads the
-// counter any more; without, the last workgroup to finish counts the step (the others have read the counter by then).
-template <int BITS, bool FEW>
+// SELF: every workgroup forms the norm from the partial sums (few elements), the first one counts the step
+template <int BITS, int ROUNDS, bool SELF>
 __global__ void __launch_bounds__(kAdamThreads) k_adamw_update(AdamParams p)
 {
     const AdamChunk ch = p.chunks[blockIdx.x];
-    AdamNow now;
-    const bool clip = p.max_norm > 0.0;
     auto form = [&]() -> AdamNow {
-        if constexpr (FEW) {
-            now = clip ? *p.now : numbers(p, *p.step + 1);  // (uniform)
-            const double norm = clip ? norm_of(p) : 0.0;
+        AdamNow now = *p.now;
+        if constexpr (SELF) {
+            const double norm = norm_of(p);
             scale_by_norm(p, norm, now);
-            if (clip && blockIdx.x == 0 && threadIdx.x == 0) {
+            if (blockIdx.x == 0 && threadIdx.x == 0) {
                 if (p.norm_out)
                     *p.norm_out = (float)norm;
                 if (!now.skip)
                     *p.step = now.t;
             }
-        } else {
-            now = *p.now;
         }
         return now;
     };
     auto update = [&](auto type) {
         using T = decltype(type);
-        if (ch.wide && ch.n == kChunk)  // (uniform)
-            update_chunk<T, BITS, true>(p, ch, form);
+        if (ch.wide && ch.n == ROUNDS * kAtOnce)  // (uniform)
+            update_chunk<T, BITS, ROUNDS, true>(p, ch, form);
         else
-            update_chunk<T, BITS, false>(p, ch, form);
+            update_chunk<T, BITS, ROUNDS, false>(p, ch, form);
     };
     if (ch.dtype == TIG_F32)
         update(float());
@@ -329,34 +340,32 @@ __global__ void __launch_bounds__(kAdamThreads) k_adamw_update(AdamParams p)
         update(__bf16());
     else
         update(_Float16());
-    if (FEW && !clip) {
-        __syncthreads();
-        if (threadIdx.x == 0 && atomicAdd(p.arrived, 1u) == gridDim.x - 1) {
-            *p.arrived = 0u;
-            *p.step = now.t;
-        }
-    }
 }
 
 inline size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 
 struct AdamLayout {
+    int rounds;
     int64_t n_chunks;
-    size_t chunks, part, now, arrived, bytes;
+    size_t chunks, part, now, bytes;
+    int64_t chunk() const { return (int64_t)rounds * kAtOnce; }
 };
 
 AdamLayout adam_layout(const tig_adamw_tensor *t, int64_t n)
 {
     AdamLayout L = {};
+    int64_t total = 0;
     for (int64_t i = 0; i < n; ++i)
-        L.n_chunks += (t[i].n + kChunk - 1) / kChunk;
+        total += t[i].n;
+    L.rounds = total <= kFewElements ? kRoundsFew : kRoundsMany;
+    for (int64_t i = 0; i < n; ++i)
+        L.n_chunks += (t[i].n + L.chunk() - 1) / L.chunk();
     size_t off = 0;
     auto take = [&](size_t bytes) {
         const size_t at = off;
         off += align_up(bytes);
         return at;
     };
-    L.arrived = take(sizeof(uint32_t));
     L.chunks = take(sizeof(AdamChunk) * (size_t)L.n_chunks);
     L.part = take(sizeof(double) * kNormGroups);  // (from here on nothing is laid out)
     L.now = take(sizeof(AdamNow));
@@ -390,7 +399,7 @@ int check_adamw(const tig_adamw_config *c, const tig_adamw_tensor *t, int64_t n)
         if ((uintptr_t)q.param % es || (uintptr_t)q.grad % es || ((uintptr_t)q.master & 3) || ((uintptr_t)q.m_scale & 3) || ((uintptr_t)q.v_scale & 3) ||
             (c->state_bits == 32 && (((uintptr_t)q.m | (uintptr_t)q.v) & 3)))
             return fail_text(TIG_EINVAL, "tig_adamw: an address is not aligned to its element");
-        chunks += (q.n + kChunk - 1) / kChunk;
+        chunks += (q.n + kRoundsMany * kAtOnce - 1) / (kRoundsMany * kAtOnce);
         if (chunks > 0x7fffffff)
             return fail_text(TIG_EINVAL, "tig_adamw: more than 2^31 chunks of 4096 elements");
     }
@@ -405,7 +414,7 @@ using namespace tig;
 
 struct tig_adamw {
     AdamParams p;
-    int32_t bits;
+    int32_t bits, rounds;
 };
 
 int tig_adamw_workspace_bytes(const tig_adamw_config *cfg, const tig_adamw_tensor *tensors, int64_t n_tensors, size_t *bytes)
@@ -434,7 +443,7 @@ int tig_adamw_create(const tig_adamw_config *cfg, const tig_adamw_tensor *tensor
     if (workspace_bytes < L.bytes)
         return fail_text(TIG_ENOSPACE, "tig_adamw_create: workspace too small");
     tig_adamw *const opt = new (std::nothrow) tig_adamw;
-    char *const host = new (std::nothrow) char[L.part ? L.part : 1];  // the counter and the chunks
+    char *const host = new (std::nothrow) char[L.part ? L.part : 1];  // the list of chunks
     if (!opt || !host) {
         delete opt;
         delete[] host;
@@ -448,10 +457,10 @@ int tig_adamw_create(const tig_adamw_config *cfg, const tig_adamw_tensor *tensor
         const bool wide = four_aligned(q.param, 4, es) && four_aligned(q.grad, 4, es) && four_aligned(q.master, 4, 4) && four_aligned(q.m, 4, ss) &&
                           four_aligned(q.v, 4, ss);
         auto at = [](const void *x, int64_t bytes) { return x ? (void *)((char *)x + bytes) : nullptr; };
-        for (int64_t c = 0; c < q.n; c += kChunk)
+        for (int64_t c = 0; c < q.n; c += L.chunk())
             *ch++ = AdamChunk{at(q.param, c * es), at(q.grad, c * es), (float *)at(q.master, c * 4), at(q.m, c * ss), at(q.v, c * ss),
                               (float *)at(q.m_scale, c / kStateBlock * 4), (float *)at(q.v_scale, c / kStateBlock * 4),
-                              (int32_t)(q.n - c < kChunk ? q.n - c : kChunk), q.dtype, q.weight_decay, wide ? 1 : 0};
+                              (int32_t)(q.n - c < L.chunk() ? q.n - c : L.chunk()), q.dtype, q.weight_decay, wide ? 1 : 0};
     }
     hipStream_t s = (hipStream_t)hip_stream;
     hipError_t e = L.part ? hipMemcpyAsync(workspace, host, L.part, hipMemcpyHostToDevice, s) : hipSuccess;
@@ -465,7 +474,6 @@ int tig_adamw_create(const tig_adamw_config *cfg, const tig_adamw_tensor *tensor
     AdamParams &p = opt->p;
     memset(&p, 0, sizeof(p));
     char *const ws = (char *)workspace;
-    p.arrived = (uint32_t *)(ws + L.arrived);
     p.chunks = (const AdamChunk *)(ws + L.chunks);
     p.part = (double *)(ws + L.part);
     p.now = (AdamNow *)(ws + L.now);
@@ -475,6 +483,7 @@ int tig_adamw_create(const tig_adamw_config *cfg, const tig_adamw_tensor *tensor
     p.b1 = (float)cfg->beta1, p.o1 = (float)(1.0 - cfg->beta1), p.b2 = (float)cfg->beta2, p.o2 = (float)(1.0 - cfg->beta2);
     p.eps = (float)cfg->eps;
     opt->bits = cfg->state_bits;
+    opt->rounds = L.rounds;
     *out = opt;
     return TIG_OK;
 }
@@ -488,25 +497,26 @@ int tig_adamw_step(tig_adamw *opt, double lr, double grad_scale, double max_norm
     AdamParams p = opt->p;
     p.lr = lr, p.grad_scale = grad_scale, p.max_norm = max_norm, p.norm_out = norm_out;
     hipStream_t s = (hipStream_t)hip_stream;
-    const dim3 grid((unsigned)p.n_chunks), threads(kAdamThreads);
-    const bool clip = max_norm > 0.0, few = p.n_chunks > 0 && p.n_chunks <= kFewChunks;
+    const bool clip = max_norm > 0.0, few = opt->rounds == kRoundsFew, self = clip && few && p.n_chunks > 0;
     const int64_t most = few ? kFewGroups : kNormGroups;
     p.n_parts = clip ? (int)(p.n_chunks < most ? p.n_chunks : most) : 0;
-    if (p.n_parts > 0)
-        hipLaunchKernelGGL(k_adamw_norm, dim3((unsigned)p.n_parts), threads, 0, s, p);
-    if (!few)
-        hipLaunchKernelGGL(k_adamw_begin, dim3(1), threads, 0, s, p);
-    if (few) {
-        if (opt->bits == 8)
-            hipLaunchKernelGGL((k_adamw_update<8, true>), grid, threads, 0, s, p);
-        else
-            hipLaunchKernelGGL((k_adamw_update<32, true>), grid, threads, 0, s, p);
-    } else if (p.n_chunks > 0) {
-        if (opt->bits == 8)
-            hipLaunchKernelGGL((k_adamw_update<8, false>), grid, threads, 0, s, p);
-        else
-            hipLaunchKernelGGL((k_adamw_update<32, false>), grid, threads, 0, s, p);
-    }
+    const dim3 grid((unsigned)p.n_chunks), parts((unsigned)p.n_parts), threads(kAdamThreads);
+    auto launch = [&](auto rounds) {
+        constexpr int R = decltype(rounds)::value;
+        if (p.n_parts > 0)
+            hipLaunchKernelGGL((k_adamw_norm<R>), parts, threads, 0, s, p);
+        if (!self)
+            hipLaunchKernelGGL(k_adamw_begin, dim3(1), threads, 0, s, p);
+        if (p.n_chunks == 0)
+            return;
+        auto *const update = opt->bits == 8 ? (self ? k_adamw_update<8, R, true> : k_adamw_update<8, R, false>)
+                                            : (self ? k_adamw_update<32, R, true> : k_adamw_update<32, R, false>);
+        hipLaunchKernelGGL(update, grid, threads, 0, s, p);
+    };
+    if (few)
+        launch(std::integral_constant<int, kRoundsFew>());
+    else
+        launch(std::integral_constant<int, kRoundsMany>());
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? TIG_OK : fail_global("tig_adamw_step", e);
 }
