@@ -87,7 +87,7 @@ hipError_t launch_step(const Dims &d, const LaunchPlan &plan, const PackedWeight
     if ((e = stamp()) != hipSuccess)
         return e;
     if (sp.train) {
-        if ((e = launch_train(d, plan, a, sp.train_ws, pw, sp.lr, sp.loss_out, sp.train_extra, sp.train_launches, s)) != hipSuccess || (e = stamp()) != hipSuccess)
+        if ((e = launch_train(d, plan, a, sp.train_ws, pw, sp.lr, sp.loss_out, sp.train_launches, s)) != hipSuccess || (e = stamp()) != hipSuccess)
             return e;
         // inspection outputs, if any are asked for (the training step has cleared its query set's counter)
         if (wants_inspection(a) && (e = launch_closing(d, plan, pw, a, GruAhead{}, s, false)) != hipSuccess)

@@ -872,10 +872,9 @@ static int step_impl(tig_ctx *ctx, const tig_batch *batch, const tig_out *out, h
     if (train) {
         sp.train = true;
         sp.train_launches = &launches;
-        sp.train_ws = ctx->train_ws;
+        sp.train_ws = TrainWork{ctx->train_ws, ctx->train_extra};
         sp.lr = train->lr;
         sp.loss_out = train->loss_out;
-        sp.train_extra = ctx->train_extra;
         train_step_args(d, ctx->train_ws, &a);
     }
     const hipError_t e = launch_step(d, ctx->plan, ctx->pw, a, sp, ctx->stream, marks);

@@ -277,6 +277,11 @@ struct TrainExtra {
     tig_adamw *opt;
     double max_norm;
 };
+// what a training step works on
+struct TrainWork {
+    void *ws;  // masters, gradients and the backward pass's buffers
+    TrainExtra extra;
+};
 // What one step launches, in order: [scatter, select] (up-front selection of a batch above the
 // one-workgroup limit), [prepare] (selection and / or query preparation not done ahead),
 // [gru] (unless the previous step's closing launch ran it), embed, closing.
@@ -290,10 +295,9 @@ struct StepPlan {
     // a training step: forward with its intermediates kept, loss, backward and SGD instead of embedding and closing
     bool train;
     int *train_launches;  // kernels of the training step, counted here
-    void *train_ws;
+    TrainWork train_ws;
     float lr;
     float *loss_out;
-    TrainExtra train_extra;
     int32_t *clear_first;       // a counter to clear ahead of everything, or NULL
     GruAhead ahead;             // GRU workgroups of the closing launch
     const struct ModParams *mods;  // a context with a module selection, or NULL
@@ -330,8 +334,8 @@ hipError_t train_attach(const Dims &d, const tig_weights &w, void *workspace, vo
 hipError_t train_copy_out(const Dims &d, void *workspace, bool grads, const tig_weights &out, hipStream_t s);
 // the arrays that a training step's GRU and embedding launches leave for its backward pass
 void train_step_args(const Dims &d, void *workspace, StepArgs *a);
-hipError_t launch_train(const Dims &d, const LaunchPlan &plan, const StepArgs &a, void *workspace, const PackedWeights &pw, float lr,
-                        float *loss_out, const TrainExtra &extra, int *launches, hipStream_t s);
+hipError_t launch_train(const Dims &d, const LaunchPlan &plan, const StepArgs &a, const TrainWork &work, const PackedWeights &pw, float lr,
+                        float *loss_out, int *launches, hipStream_t s);
 size_t train_head_ops_bytes(const Dims &d, const TrainHead &h);
 size_t train_head_bytes(const Dims &d, const TrainHead &h);
 hipError_t train_head_attach(const Dims &d, const TrainHead &h, const tig_train_head &from, hipStream_t s);

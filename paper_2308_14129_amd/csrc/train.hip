@@ -1044,10 +1044,11 @@ void train_step_args(const Dims &d, void *workspace, StepArgs *a)
 }
 
 // Everything of a training step after the GRU launch.
-hipError_t launch_train(const Dims &d, const LaunchPlan &plan, const StepArgs &a, void *workspace, const PackedWeights &pw, float lr,
-                        float *loss_out, const TrainExtra &extra, int *launches, hipStream_t s)
+hipError_t launch_train(const Dims &d, const LaunchPlan &plan, const StepArgs &a, const TrainWork &work, const PackedWeights &pw, float lr,
+                        float *loss_out, int *launches, hipStream_t s)
 {
-    const TrainLayout L = train_layout(d, workspace);
+    const TrainExtra &extra = work.extra;
+    const TrainLayout L = train_layout(d, work.ws);
     TrainArrays t = L.t;
     const int M = d.M, E = d.E, da = d.da, D = d.Dmsg, ld_m1 = da + M;
     const float *head_mean = nullptr;
