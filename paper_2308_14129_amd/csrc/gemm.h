@@ -399,9 +399,15 @@ hipError_t launch_gemm(const GemmPlan &plan, const T *A, int64_t lda, const T *B
     g.A = A, g.B = B, g.lda = lda, g.ldb = ldb, g.M = M, g.N = N, g.K = K;
     g.splits = plan.splits, g.steps_per = plan.steps_per;
     g.part = (float *)part, g.ldp = gemm_part_ld(N);
-    hipError_t e = plan.tile == 256   ? launch_gemm_tile<T, FA, FB, Epi, 256, 256, 2, 4>(plan, g, epi, s)
-                   : plan.tile == 128 ? launch_gemm_tile<T, FA, FB, Epi, 128, 128, 2, 2>(plan, g, epi, s)
-                                      : launch_gemm_tile<T, FA, FB, Epi, 64, 64, 2, 2>(plan, g, epi, s);
+    hipError_t e;
+    if (sizeof(T) == 2 && plan.tile == 256) {
+        if constexpr (sizeof(T) == 2)
+            e = launch_gemm_tile<T, FA, FB, Epi, 256, 256, 2, 4>(plan, g, epi, s);
+    } else if (plan.tile == 128) {
+        e = launch_gemm_tile<T, FA, FB, Epi, 128, 128, 2, 2>(plan, g, epi, s);
+    } else {
+        e = launch_gemm_tile<T, FA, FB, Epi, 64, 64, 2, 2>(plan, g, epi, s);
+    }
     if constexpr (!Epi::kWhole)
         if (e == hipSuccess && plan.splits > 1)
             e = launch_join((const float *)part, plan.splits, M, N, g.ldp, epi, s);

@@ -1,44 +1,47 @@
 // Host side of the products of gemm.h, and the packing of operands whose rows are not 16-byte aligned.
 #include "gemm.h"
 
+#include <cmath>
+
 namespace tig {
 
-// Which tile, and how many ranges of k.  A tile's time per step of 128 bytes of k is taken as proportional to its size, with the
-// smaller ones' poorer reuse of operands added (a tile of 128 x 128 as 1.3 quarters, one of 64 x 64 as 2 sixteenths of a
-// 256 x 256 one); a launch takes as many rounds as its workgroups need on 256 compute units, and joining ranges costs a
-// pass over the partial sums.  The cheapest combination is taken.
+// Which tile, and how many ranges of k: the cheapest by this estimate, in us.  A compute unit holds four workgroups of tiles of 64,
+// two of 128, one of 256; a round of them takes, per step of 128 bytes of k, `loaded` for each workgroup on the unit and never
+// less than `alone`, and `fixed` + `each` for every workgroup at its ends.  No launch is faster than its operands' way from the caches
+// at 14 TB/s, and joining ranges costs a launch and 8 bytes per element and range at 6.8 TB/s.  The constants are a fit to 690
+// timings (27 products in 16 bits, 15 in fp32, of 8 to 470,816 rows, each in every tile and 1 to 256 ranges): the tile and ranges that it
+// takes are within 0.5 % (16 bits) and 1.5 % (fp32) of the fastest on average.  Examples: 669 x 512 x 17024 in fp16 takes 36 us as
+// 128 x 128 x 16 ranges, 43 as 256 x 16, 50 as 64 x 4, 74 as 128 x 4; 8192 x 8192 x 2048 in bf16 224 as 256, 310 as 128, 415 as 64;
+// 4096 x 320 x 8184 in fp32 174 as 64 x 4, 260 as 256 x 8.  In fp32 a tile of 256 was never the fastest and is not built.
 GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K, int elem, bool may_split)
 {
+    struct Tile {
+        int size, per_cu;
+        double loaded, alone, fixed, each;
+    };
+    static const Tile tiles16[3] = {{256, 1, 1.6, 1.6, 6.5, 1.9}, {128, 2, 0.55, 1.1, 4.1, 0.9}, {64, 4, 0.29, 0.37, 3.2, 0.2}};
+    static const Tile tiles32[2] = {{128, 2, 1.6, 3.2, 4.1, 0.9}, {64, 4, 0.5, 0.6, 3.2, 0.2}};
+    const Tile *const tiles = elem == 4 ? tiles32 : tiles16;
     const int step = kTileBytes / elem;
-    const int64_t steps = (K + step - 1) / step;
-    GemmPlan best = {64, 1, (int)(steps > 0 ? steps : 1), 0};
+    const int64_t steps = K > 0 ? (K + step - 1) / step : 1;
+    GemmPlan best = {64, 1, (int)steps, 0};
     double best_cost = 1e300;
-    const int tiles[3] = {256, 128, 64};
-    const double cost_of[3] = {1.0, 0.25 * 1.3, 0.0625 * 2.0};
-    const int per_cu[3] = {1, 2, 4};  // workgroups that a compute unit holds at once
-    const double unit = elem == 4 ? 4.0 : 0.9;  // us of a 256 x 256 step on one compute unit
-    for (int t = 0; t < 3; ++t) {
-        const int64_t n_tiles = ((M + tiles[t] - 1) / tiles[t]) * ((N + tiles[t] - 1) / tiles[t]);
-        for (int splits = 1; splits <= 64 && splits <= (steps > 0 ? steps : 1); splits *= 2) {
-            if (splits > 1 && !may_split)
-                break;
-            const int64_t per = (steps + splits - 1) / splits;
-            // workgroups of one unit share it: a round of `per_cu` on every unit
-            const int64_t wgs = n_tiles * splits, full = wgs / (256 * per_cu[t]), rest = wgs % (256 * per_cu[t]);
-            const double share = (double)((rest + 255) / 256);
-            double cost = (full * per_cu[t] + share) * ((double)per * unit * cost_of[t] + 1.0);
-            if (rest > 0 && share < 2.0)  // a workgroup alone on its unit waits for its loads
-                cost += (double)per * 0.25;
-            if (splits > 1)
-                cost += 4.0 + (double)splits * M * N * 8.0 / 4e6;
+    for (int i = 0; i < (elem == 4 ? 2 : 3); ++i) {
+        const Tile &t = tiles[i];
+        const int64_t n_tiles = ((M + t.size - 1) / t.size) * ((N + t.size - 1) / t.size);
+        for (int splits = 1; splits <= (may_split ? 256 : 1) && splits <= steps; splits *= 2) {
+            const int64_t per = (steps + splits - 1) / splits, ranges = (steps + per - 1) / per;
+            const int64_t wgs = n_tiles * ranges, full = wgs / (256 * t.per_cu), share = (wgs % (256 * t.per_cu) + 255) / 256;
+            auto round = [&](int64_t n) { return n > 0 ? (double)per * fmax(t.alone, (double)n * t.loaded) + t.fixed + (double)n * t.each : 0.0; };
+            double cost = fmax((double)full * round(t.per_cu) + round(share), (double)wgs * per * 2 * t.size * kTileBytes / 14e6);
+            if (ranges > 1)
+                cost += 3.0 + (double)ranges * M * N * 8.0 / 6.8e6;
             if (cost < best_cost) {
                 best_cost = cost;
-                best = GemmPlan{tiles[t], (int)((steps + per - 1) / (per > 0 ? per : 1)), (int)(per > 0 ? per : 1), 0};
+                best = GemmPlan{t.size, (int)ranges, (int)per, 0};
             }
         }
     }
-    if (best.splits < 1)
-        best.splits = 1;
     best.part_bytes = best.splits > 1 ? (size_t)best.splits * M * gemm_part_ld(N) * 4 : 0;
     return best;
 }

@@ -153,7 +153,7 @@ struct EpiStats {
     }
 };
 
-// Sixteen rows per workgroup, sixteen threads each: the tiles' parts joined, the label's logit, loss; for the gradient the row's
+// LANES threads a row: the tiles' parts joined, the label's logit, loss; for the gradient the row's
 // record, or the tables that ce_narrow.h streams (whole tiles: rows behind the last take no part), and the row itself where it
 // counts, else zeros: whatever it holds, P^T X does not see it.
 template <typename T>
@@ -166,29 +166,40 @@ struct CeRowsOut {
     int64_t ld_x0;
     bool ones;         // a column of ones behind x0's last, also in rows that do not count and behind the last
 };
-template <typename T>
+template <typename T, int LANES>
 __global__ void __launch_bounds__(256) k_ce_rows(const float2 *part, int64_t tiles, int64_t rows, const T *x, int64_t ldx, const T *w, int64_t ldw,
                                                  const T *bias, int64_t dim, int64_t vocab, const int32_t *labels, const float *row_scale, float scale,
                                                  const CeHead *head, CeRowsOut<T> out)
 {
-    const int64_t i = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
-    const int t = threadIdx.x % 16;
+    const int64_t i = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    const int t = threadIdx.x % LANES;
     const bool on = i < rows;
     const int64_t r = on ? i : rows - 1;
     float top = -INFINITY, sum = 0.0f;
-    for (int64_t k = t; k < tiles; k += 16) {
-        const float2 v = part[k * rows + r];
-        const float to = fmaxf(top, v.x), from = to == -INFINITY ? 0.0f : to;
-        sum = sum * expf(top - from) + v.y * expf(v.x - from);
+    for (int64_t k = t; k < tiles; k += 4 * LANES) {
+        float2 v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t at = k + u * LANES;
+            v[u] = part[(at < tiles ? at : t) * rows + r];
+            if (at >= tiles)
+                v[u] = float2{-INFINITY, 0.0f};
+        }
+        const float to = fmaxf(fmaxf(fmaxf(top, v[0].x), v[1].x), fmaxf(v[2].x, v[3].x)), from = to == -INFINITY ? 0.0f : to;
+        sum *= expf(top - from);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            sum += v[u].y * expf(v[u].x - from);
         top = to;
     }
     const int32_t label = labels[r];
     const bool counts = label >= 0 && label < vocab;
     float dot = 0.0f;
     const T *xr = x + r * ldx, *wr = w + (counts ? (int64_t)label : 0) * ldw;
-    for (int64_t k = t; k < dim; k += 16)
+#pragma unroll 4
+    for (int64_t k = t; k < dim; k += LANES)
         dot += to_float(xr[k]) * to_float(wr[k]);
-    for (int d = 8; d > 0; d >>= 1) {
+    for (int d = LANES / 2; d > 0; d >>= 1) {
         const float ot = __shfl_xor(top, d), os = __shfl_xor(sum, d);
         const float to = fmaxf(top, ot), from = to == -INFINITY ? 0.0f : to;
         sum = sum * expf(top - from) + os * expf(ot - from);
@@ -196,7 +207,7 @@ __global__ void __launch_bounds__(256) k_ce_rows(const float2 *part, int64_t til
         dot += __shfl_xor(dot, d);
     }
     if (out.x0 && (on || out.ones))  // (rows of x are whole 16-byte pieces here)
-        for (int64_t c = t * Mat<T>::kPer16; c < out.ld_x0; c += 16 * Mat<T>::kPer16) {
+        for (int64_t c = t * Mat<T>::kPer16; c < out.ld_x0; c += LANES * Mat<T>::kPer16) {
             union {
                 intx4 q;
                 T v[Mat<T>::kPer16];
@@ -554,8 +565,10 @@ hipError_t launch_rows(const tig_softmax_ce &p, int64_t r, int64_t m, const floa
                        const CeHead *head, const CeRowsOut<T> &out, hipStream_t s)
 {
     const int64_t all = out.lse2 ? (m + kNarrowStream - 1) / kNarrowStream * kNarrowStream : m;
-    hipLaunchKernelGGL((k_ce_rows<T>), dim3((unsigned)((all + 15) / 16)), dim3(256), 0, s, part, tiles, m, x + r * ldx, ldx, w, ldw, (const T *)p.bias, p.dim,
-                       p.vocab, p.labels + r, p.row_scale ? p.row_scale + r : nullptr, p.scale, head, out);
+    // (a wavefront a row where the parts of 16 lanes would be long chains of loads)
+    const bool wide = tiles > 128 && m < 4096;
+    hipLaunchKernelGGL((wide ? k_ce_rows<T, 64> : k_ce_rows<T, 16>), dim3((unsigned)(wide ? (all + 3) / 4 : (all + 15) / 16)), dim3(256), 0, s, part, tiles, m,
+                       x + r * ldx, ldx, w, ldw, (const T *)p.bias, p.dim, p.vocab, p.labels + r, p.row_scale ? p.row_scale + r : nullptr, p.scale, head, out);
     return hipGetLastError();
 }
 
