@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, 2) k_narrow_stats(NarrowArg
         request(t0, smem[0]);
     for (int64_t t = t0; t < t1; ++t) {
         const char *const now = smem[(t - t0) & 1];
-        __syncthreads();
+        sync_with_loads();
         if (t + 1 < t1)
             request(t + 1, smem[(t + 1 - t0) & 1]);
         floatx4 acc[FM][FN];
@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, 2) k_narrow_grad(NarrowArgs
         request(t0, smem[0]);
     for (int64_t t = t0; t < t1; ++t) {
         const char *const now = smem[(t - t0) & 1];
-        __syncthreads();
+        sync_with_loads();
         if (t + 1 < t1)
             request(t + 1, smem[(t + 1 - t0) & 1]);
         const int base = (int)(t * kNarrowStream) + 4 * g;

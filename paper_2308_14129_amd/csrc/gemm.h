@@ -222,6 +222,16 @@ __device__ inline void each_four(const TileAt &at, const floatx4 (&acc)[FM][FN],
 struct Nothing {
 };
 
+// This wavefront's loads, into LDS among them, have arrived.
+__device__ inline void wait_for_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // vmcnt(0)
+// A barrier behind which every wavefront's loads into LDS can be read.  (__syncthreads() alone does not promise that: where a
+// loop carried the loads over its back edge the compiler waited for them ahead of the loop only.)
+__device__ inline void sync_with_loads()
+{
+    wait_for_loads();
+    __syncthreads();
+}
+
 struct EpiPart {  // a range's partial sums
     float *part;
     int64_t ldp;
@@ -297,7 +307,7 @@ __global__ void __launch_bounds__(64 * WM *WN) k_gemm(GemmArgs<T> g, Epi epi)
     };
     if (n_steps > 0) {
         request(0);
-        __syncthreads();
+        sync_with_loads();
         request(1);
 #pragma unroll
         for (int i = 0; i < FM; ++i)
@@ -308,11 +318,11 @@ __global__ void __launch_bounds__(64 * WM *WN) k_gemm(GemmArgs<T> g, Epi epi)
     }
     for (int s = 0; s < n_steps; ++s) {
         multiply(a[0], b[0], a[1], b[1], smem + (s & 1) * kStage, 1, std::false_type());
-        __syncthreads();  // (step s + 1 is there, and nobody reads step s any more)
+        sync_with_loads();  // (step s + 1 is there, and nobody reads step s any more)
         request(s + 2);
         multiply(a[1], b[1], a[0], b[0], smem + ((s + 1) & 1) * kStage, 0, std::true_type());  // (behind the last step: operands that nobody takes)
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nothing may reach LDS any more once the workgroup has given it back)
+    wait_for_loads();  // (nothing may reach LDS any more once the workgroup has given it back)
     const TileAt at = {m0 + wm * (BM / WM), n0 + wn * (BN / WN), g.M, g.N, tm, tn, wm, wn};
     if constexpr (Epi::kWhole) {
         __syncthreads();

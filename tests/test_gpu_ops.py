@@ -293,6 +293,13 @@ def test_softmax_ce_narrow_rows(dtype, weighted, scale):
         check_ce(*shape, dtype, bias=i % 2 == 0, weighted=weighted, scale=scale * (512 if dtype == "fp16" else 1), seed=60 + i, masked=0)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("n,V,d,bias", [(100, 200_003, 128, False), (100, 200_003, 128, True), (64, 150_001, 60, True), (700, 60_001, 100, True), (3, 300_000, 20, False)])
+def test_softmax_ce_narrow_rows_over_many_tiles(n, V, d, bias, dtype):
+    """Long ranges of streamed tiles: every tile has to be there before it is read."""
+    check_ce(n, V, d, dtype, bias=bias, seed=n)
+
+
 def test_softmax_ce_wide_rows_in_several_pieces():
     check_ce(20_000, 4000, 136, "bf16", seed=14)
     check_ce(9000, 9000, 160, "fp16", seed=15, scale=1024.0, weighted=True)
