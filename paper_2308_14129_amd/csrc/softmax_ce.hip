@@ -274,27 +274,38 @@ struct EpiP {
             for (int e = 0; e < 4; ++e)
                 b[j][e] = e < left ? b[j][e] : -INFINITY;
         }
+        // the rows' records, by way of LDS: behind a store to P each would wait for memory by itself
+        CeRow *const of_row = (CeRow *)(smem + WM * BN * sizeof(float));
+        for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) {
+            const int64_t m = (int64_t)at.tm * BM + r;
+            of_row[r] = m < at.M ? rec[m] : CeRow{INFINITY, 0.0f, -1};
+        }
+        __syncthreads();
+        floatx4 total[FN] = {};
         auto rows = [&](auto full) {
             constexpr bool FULL = decltype(full)::value;
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
                 const int64_t m = at.m0 + i * 16 + i16;
                 const bool on = FULL || m < at.M;
-                const CeRow r = rec[on ? m : 0];
-                const float lse = on ? r.lse : INFINITY;
+                const CeRow r = of_row[at.wm * (BM / WM) + i * 16 + i16];
+                const float lse = r.lse;
                 T *const row = P + m * ldp + at.n0 + 4 * g;
-                const int64_t hot = on && r.label >= 0 ? (int64_t)r.label - v0 - at.n0 - 4 * g : -1;  // (of this lane's columns 16 j + e)
+                const int64_t from = (int64_t)r.label - v0 - at.n0 - 4 * g;
+                const int hot = r.label >= 0 && from >= 0 && from < 16 * FN ? (int)from : -1;  // (of this lane's columns 16 j + e)
 #pragma unroll
                 for (int j = 0; j < FN; ++j) {
+                    floatx4 p;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float p = lse != INFINITY ? exp_of<T>(acc[i][j][e] + b[j][e] - lse) : 0.0f;
-                        p -= hot == 16 * j + e ? 1.0f : 0.0f;
-                        acc[i][j][e] = p * r.w;
+                        p[e] = lse != INFINITY ? exp_of<T>(acc[i][j][e] + b[j][e] - lse) : 0.0f;
+                        p[e] = (p[e] - (hot == 16 * j + e ? 1.0f : 0.0f)) * r.w;
                     }
+                    total[j] += p;
                     if (FULL || (on && at.n0 + j * 16 + 4 * g < end))
-                        store_four(row + j * 16, acc[i][j], 4, true);
+                        store_four(row + j * 16, p, 4, true);
                 }
+                __builtin_amdgcn_sched_barrier(0);  // (a row after the other: their values at once do not fit the registers)
             }
         };
         if (at.m0 + FM * 16 <= at.M && at.n0 + FN * 16 <= at.N)  // (uniform)
@@ -306,16 +317,11 @@ struct EpiP {
         float *const red = (float *)smem;  // [WM][BN]
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            floatx4 total = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-                if (at.m0 + i * 16 + i16 < at.M)
-                    total += acc[i][j];
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                total[e] = row_sum_all(total[e]);
+                total[j][e] = row_sum_all(total[j][e]);
             if (i16 == 0)
-                *(floatx4 *)(red + at.wm * BN + at.wn * (BN / WN) + j * 16 + 4 * g) = total;
+                *(floatx4 *)(red + at.wm * BN + at.wn * (BN / WN) + j * 16 + 4 * g) = total[j];
         }
         __syncthreads();
         for (int c = threadIdx.x; c < BN; c += 64 * WM * WN) {
