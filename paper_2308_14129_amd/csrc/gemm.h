@@ -279,7 +279,10 @@ __global__ void __launch_bounds__(64 * WM *WN) k_gemm(GemmArgs<T> g, Epi epi)
         pb += OB::step(g.ldb);
         left -= Mat<T>::kStep;
     };
-    auto multiply = [&](const intx4 (&x)[FM], const intx4 (&y)[FN], intx4 (&nx)[FM], intx4 (&ny)[FN], const char *from, int kk, auto loads) {
+    constexpr bool kTurned = sizeof(T) == 2 && (FA == kCol || FB == kCol);
+    auto multiply = [&](const intx4 (&x)[FM], const intx4 (&y)[FN], intx4 (&nx)[FM], intx4 (&ny)[FN], const char *from, int kk, int s, auto loads) {
+        if (decltype(loads)::value && !kTurned)
+            request(s);
 #pragma unroll
         for (int j = 0; j < FN; ++j)
             ny[j] = OB::frag(from + OA::kBytes, wn * (BN / WN) + j * 16, kk);
@@ -290,19 +293,35 @@ __global__ void __launch_bounds__(64 * WM *WN) k_gemm(GemmArgs<T> g, Epi epi)
             for (int j = 0; j < FN; ++j)
                 mma16(acc[i][j], y[j], x[i], T());
         }
+        if (decltype(loads)::value && kTurned)
+            request(s);
         // The reads go between the first rows' products: left alone they are sunk to where they are waited for, and ahead of the
         // first product they would be waited for with what it needs.  (Two behind each row's: 3 - 8 % slower.)  So do the next
         // step's loads; the barrier comes as soon as the reads are done, and what is left of the products hides how far
         // the wavefronts are apart (8192^3: with the loads ahead of all products and the barrier behind them 1070, 1030 and 1040
         // instead of 1270, 1145 and 1147 TFLOP/s for the three forms).
-        constexpr int kMma = FN * (sizeof(T) == 4 ? 4 : 1), kEach = FA == kRow && FB == kRow ? 4 : 6;
+        // Transposing reads are another matter: the compiler waits for every load into LDS ahead of them.  So the loads come
+        // behind a step's last reads, and the next ones as late as their products allow.
+        constexpr int kMma = FN * (sizeof(T) == 4 ? 4 : 1);
+        if constexpr (!kTurned) {
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, kMma, 0);
-            if (decltype(loads)::value && i < 4)
-                __builtin_amdgcn_sched_group_barrier(0x010, (OA::kLoads + OB::kLoads + 3) / 4, 0);
-            if (i + 1 < FM)
-                __builtin_amdgcn_sched_group_barrier(0x100, kEach, 0);
+            for (int i = 0; i < FM; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, kMma, 0);
+                if (decltype(loads)::value && i < 4)
+                    __builtin_amdgcn_sched_group_barrier(0x010, (OA::kLoads + OB::kLoads + 3) / 4, 0);
+                if (i + 1 < FM)
+                    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+            }
+        } else {
+            constexpr int kReads = FM * OA::kReads + FN * OB::kReads, kGaps = FM / 2, kFirst = decltype(loads)::value ? 0 : FM / 2 - 1;
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, kMma, 0);
+                if (i >= kFirst && i < kFirst + kGaps)
+                    __builtin_amdgcn_sched_group_barrier(0x100, (kReads + kGaps - 1) / kGaps, 0);
+                if (decltype(loads)::value && i >= kGaps)
+                    __builtin_amdgcn_sched_group_barrier(0x010, (OA::kLoads + OB::kLoads + kGaps - 1) / kGaps, 0);
+            }
         }
     };
     if (n_steps > 0) {
@@ -317,10 +336,9 @@ __global__ void __launch_bounds__(64 * WM *WN) k_gemm(GemmArgs<T> g, Epi epi)
             b[0][j] = OB::frag(smem + OA::kBytes, wn * (BN / WN) + j * 16, 0);
     }
     for (int s = 0; s < n_steps; ++s) {
-        multiply(a[0], b[0], a[1], b[1], smem + (s & 1) * kStage, 1, std::false_type());
+        multiply(a[0], b[0], a[1], b[1], smem + (s & 1) * kStage, 1, 0, std::false_type());
         sync_with_loads();  // (step s + 1 is there, and nobody reads step s any more)
-        request(s + 2);
-        multiply(a[1], b[1], a[0], b[0], smem + ((s + 1) & 1) * kStage, 0, std::true_type());  // (behind the last step: operands that nobody takes)
+        multiply(a[1], b[1], a[0], b[0], smem + ((s + 1) & 1) * kStage, 0, s + 2, std::true_type());  // (behind the last step: operands that nobody takes)
     }
     wait_for_loads();  // (nothing may reach LDS any more once the workgroup has given it back)
     const TileAt at = {m0 + wm * (BM / WM), n0 + wn * (BN / WN), g.M, g.N, tm, tn, wm, wn};
