@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(256) k_gemm_join(const float *part, int splits
         const int64_t m = i / per, n = i % per * 4;
         floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
         const float *p = part + m * ldp + n;
-#pragma unroll 4
+#pragma unroll 8
         for (int s = 0; s < splits; ++s)
             v += *(const floatx4 *)(p + (int64_t)s * M * ldp);
         const int left = N - n < 4 ? (int)(N - n) : 4;
