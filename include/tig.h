@@ -577,7 +577,7 @@ typedef struct tig_linear {
 /* Device bytes that the call needs as its workspace (256-byte aligned; 0: none).  Depends on the
  * sizes, strides and addresses in `p`; of the outputs only whether they are NULL.  A forward call of up to
  * TIG_LINEAR_FEW_ROWS rows needs none. */
-#define TIG_LINEAR_FEW_ROWS 64
+#define TIG_LINEAR_FEW_ROWS 16
 TIG_API int tig_linear_workspace_bytes(const tig_linear *p, int32_t backward, size_t *bytes);
 TIG_API int tig_linear_forward(const tig_linear *p, void *workspace, size_t workspace_bytes, void *hip_stream);
 TIG_API int tig_linear_backward(const tig_linear *p, void *workspace, size_t workspace_bytes, void *hip_stream);

@@ -21,10 +21,12 @@ namespace {
 
 constexpr int kStateBlock = 256, kAdamThreads = 256;
 constexpr int kAtOnce = 4 * kAdamThreads;  // elements of a workgroup's round, four of a lane
-// A chunk has four rounds, all of whose loads are on their way at once, or, where the tensors have up to 2^22 elements together,
-// one: such a call is as long as a workgroup's chain of round trips.
+// A chunk has four rounds, all of whose loads are on their way at once, or, where the tensors have up to 2^21 elements together,
+// one: such a call is as long as a workgroup's chain of round trips (us for one and four rounds in fp32, without and with
+// clipping: 2^18 elements 5.6 / 6.8 and 7.1 / 11.3, 2^21 10.2 / 14.1 and 10.7 / 15.3, 2^22 20.4 / 27.1 and 20.5 / 25.9, 2^24 66 / 100 and
+// 69 / 80).
 constexpr int kRoundsMany = 4, kRoundsFew = 1;
-constexpr int64_t kFewElements = 1 << 22;
+constexpr int64_t kFewElements = 1 << 21;
 constexpr int kNormGroups = 8192;          // workgroups that form the norm, at most
 constexpr int kFewGroups = 256;            // the same for few elements: every workgroup of the update adds their sums up
 

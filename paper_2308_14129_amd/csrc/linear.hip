@@ -1,6 +1,6 @@
 // Dense layer y = act(x W^T + b) + residual and its backward pass (include/tig.h, tig_linear_*).  gfx950.
 //
-//   up to 64 rows     k_linear_rows: the matrix is read once, straight into matrix-core operands; bound by its bytes
+//   up to 16 rows     k_linear_rows: the matrix is read once, straight into matrix-core operands
 //   more rows         the tile product of gemm.h, bias, activation and residual in its epilogue
 //   backward          k_linear_dz: dz = dy act'(z), and its column sums before it is rounded; then two tile products
 #include <type_traits>
@@ -73,77 +73,62 @@ __device__ inline intx4 operand_piece(const T *row, int64_t k, int64_t K)
     return u.q;
 }
 
-template <typename T, int MT, int WAVES, class Epi>
-__global__ void __launch_bounds__(64 * WAVES) k_linear_rows(const T *x, int64_t ldx, const T *w, int64_t ldw, int64_t M, int64_t N, int64_t K, Epi epi)
+constexpr int kRowsWaves = 8;
+
+// Up to sixteen rows: a workgroup takes sixteen columns, its wavefronts take turns along k, and both operands come straight from
+// memory: a lane's sixteen bytes of a row are its part of an operand.  Bound by the matrix' bytes and, where it is small, by a
+// launch and one chain of loads: one row, 1024 -> 4096 in bf16 3.4 us in a graph (2.5 TB/s), 16 rows, 4096 -> 16384 31 us (4.3 TB/s).
+// The limit: 13 rows of 2000 -> 1336 in fp16 take 5.4 us here and 6.3 as tiles, 16 of 4096 -> 4096 in bf16 9.8 and 9.9, 48 of them
+// (as three operands of sixteen) 18.1 and 12.1, 64 rows of 4096 -> 16384 73 and 33.  Four wavefronts instead of eight: the
+// same within 2 % from 2048 to 32768 columns.
+template <typename T, class Epi>
+__global__ void __launch_bounds__(64 * kRowsWaves) k_linear_rows(const T *x, int64_t ldx, const T *w, int64_t ldw, int64_t M, int64_t N, int64_t K, Epi epi)
 {
-    constexpr int per = Mat<T>::kPer16, kBlock = 4 * per, kUnroll = MT <= 2 ? 4 : 2;
-    __shared__ floatx4 red[WAVES][MT][64];
+    constexpr int per = Mat<T>::kPer16, kBlock = 4 * per, kUnroll = 4, WAVES = kRowsWaves;
+    __shared__ floatx4 red[WAVES][64];
     const int lane = lane_id(), wave = wave_id_uniform(), i16 = lane % 16, g = lane / 16;
     const int64_t n0 = (int64_t)blockIdx.x * 16, n = n0 + i16 < N ? n0 + i16 : N - 1;
-    const T *wr = w + n * ldw + g * per;
-    const T *xr[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int64_t m = i * 16 + i16;
-        xr[i] = x + (m < M ? m : M - 1) * ldx + g * per;
-    }
-    floatx4 acc[MT] = {};
+    const T *const wr = w + n * ldw + g * per, *const xr = x + (i16 < M ? i16 : M - 1) * ldx + g * per;
+    floatx4 acc = {};
     const int64_t full = K / kBlock;  // blocks that are whole for every lane
     int64_t b = wave;
     for (; b + (kUnroll - 1) * WAVES < full; b += kUnroll * WAVES) {
-        intx4 wv[kUnroll], xv[kUnroll][MT];
+        intx4 wv[kUnroll], xv[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             const int64_t k = (b + u * WAVES) * kBlock;
             wv[u] = operand_piece<T>(wr, k, k + per);
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-                xv[u][i] = operand_piece<T>(xr[i], k, k + per);
+            xv[u] = operand_piece<T>(xr, k, k + per);
         }
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-                mma16(acc[i], wv[u], xv[u][i], T());
+            mma16(acc, wv[u], xv[u], T());
     }
     for (; b * kBlock < K; b += WAVES) {
         const int64_t k = b * kBlock, left = K - g * per;
-        const intx4 wv = operand_piece<T>(wr, k, left);
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-            mma16(acc[i], wv, operand_piece<T>(xr[i], k, left), T());
+        mma16(acc, operand_piece<T>(wr, k, left), operand_piece<T>(xr, k, left), T());
     }
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-        red[wave][i][lane] = acc[i];
+    red[wave][lane] = acc;
     __syncthreads();
-    for (int i = wave; i < MT; i += WAVES) {
-        floatx4 v = red[0][i][lane];
+    const int64_t c = n0 + 4 * g;
+    if (wave == 0 && i16 < M && c < N) {
 #pragma unroll
         for (int u = 1; u < WAVES; ++u)
-            v += red[u][i][lane];
-        const int64_t m = i * 16 + i16, c = n0 + 4 * g;
-        if (m < M && c < N) {
-            const int left = N - c < 4 ? (int)(N - c) : 4;
-            const auto r = epi.row(m);
-            epi.template store<false>(r, epi.template col<false>(c, left), epi.template load<false>(r, c, left), c, v, left);
-        }
+            acc += red[u][lane];
+        const int left = N - c < 4 ? (int)(N - c) : 4;
+        const auto r = epi.row(i16);
+        epi.template store<false>(r, epi.template col<false>(c, left), epi.template load<false>(r, c, left), c, acc, left);
     }
 }
 
 constexpr int64_t kFewRows = TIG_LINEAR_FEW_ROWS;
+static_assert(kFewRows == 16, "one operand of rows");
 
-template <typename T, int WAVES, class Epi>
+template <typename T, class Epi>
 hipError_t launch_linear_rows(const tig_linear &p, const Epi &epi, hipStream_t s)
 {
-    const dim3 grid((unsigned)((p.out_dim + 15) / 16)), block(64 * WAVES);
-    const T *x = (const T *)p.x, *w = (const T *)p.w;
-    if (p.rows <= 16)
-        hipLaunchKernelGGL((k_linear_rows<T, 1, WAVES, Epi>), grid, block, 0, s, x, p.ldx, w, p.ldw, p.rows, p.out_dim, p.in_dim, epi);
-    else if (p.rows <= 32)
-        hipLaunchKernelGGL((k_linear_rows<T, 2, WAVES, Epi>), grid, block, 0, s, x, p.ldx, w, p.ldw, p.rows, p.out_dim, p.in_dim, epi);
-    else
-        hipLaunchKernelGGL((k_linear_rows<T, 4, WAVES, Epi>), grid, block, 0, s, x, p.ldx, w, p.ldw, p.rows, p.out_dim, p.in_dim, epi);
+    hipLaunchKernelGGL((k_linear_rows<T, Epi>), dim3((unsigned)((p.out_dim + 15) / 16)), dim3(64 * kRowsWaves), 0, s, (const T *)p.x, p.ldx, (const T *)p.w,
+                       p.ldw, p.rows, p.out_dim, p.in_dim, epi);
     return hipGetLastError();
 }
 
@@ -380,8 +365,8 @@ hipError_t forward(const tig_linear &p, const LinearPlan &L, char *ws, hipStream
         const int es = sizeof(T);
         const Epi epi = {(const T *)p.bias, (const T *)p.residual, (T *)p.y, (T *)p.z, p.ldr, p.ldy, p.ldz,
                          four_aligned(p.bias, 4, es), four_aligned(p.residual, p.ldr, es), four_aligned(p.y, p.ldy, es), four_aligned(p.z, p.ldz, es)};
-        if (L.few)  // (more wavefronts along k where the columns alone do not fill the chip)
-            return (p.out_dim + 15) / 16 >= 512 ? launch_linear_rows<T, 4>(p, epi, s) : launch_linear_rows<T, 8>(p, epi, s);
+        if (L.few)
+            return launch_linear_rows<T>(p, epi, s);
         const T *x = (const T *)p.x, *w = (const T *)p.w;
         int64_t ldx = p.ldx, ldw = p.ldw;
         hipError_t e = hipSuccess;

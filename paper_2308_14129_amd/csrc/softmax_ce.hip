@@ -457,15 +457,18 @@ CePlan ce_plan(const tig_softmax_ce &p)
         L.bytes = off;
         return L;
     }
-    if (es == 2 && d <= 128) {
+    // Narrow rows stay in registers where there are enough logits for that to count (us, with gradients, this way and by tiles: 1024 x
+    // 30000 x 128 140 and 114, x 100 118 and 127; 128 x 400000 x 128 277 and 268; 256 x 400000 x 64 227 and 330; 4000 x 250000 x 100 1134
+    // and 3003), and without a gradient over many candidates (8 x 400000 x 64 41 and 49; 512 x 30000 x 64 21 and 18).
+    if (es == 2 && d <= 128 && (n * V >= (int64_t)1 << 25 || (!L.grad && V >= 1 << 17))) {
         L.kb = d <= 64 ? 2 : 4;  // (a column more does not change it, see run_narrow_of)
         const int64_t tile = L.kb == 2 ? kNarrowTile<2> : kNarrowTile<4>;
         L.own_rows = (n + tile - 1) / tile, L.own_cands = (V + tile - 1) / tile;
         L.row_tiles = (n + kNarrowStream - 1) / kNarrowStream, L.cand_tiles = (V + kNarrowStream - 1) / kNarrowStream;
-        // A column more, where the blocks have room for one.  The copy of W costs what about 80 rows do; where W is copied
-        // anyway, nothing.
+        // A column more, where the blocks have room for one and W is copied anyway, or where rows are many (with and without, aligned
+        // rows: 1024 x 250000 x 96 389 and 369 us, 2000 x 250000 x 40 398 and 421, 8000 x 100000 x 120 981 and 1061).
         const bool fits = gemm_fits(p.w, p.ldw, d, es);
-        L.biased = d < 32 * L.kb && (!fits || n >= 512);
+        L.biased = d < 32 * L.kb && (!fits || n >= 2000);
         L.pack_x = L.biased || !gemm_fits(p.x, p.ldx, d, es);
         L.pack_w = L.biased || !fits;
         L.ld_x = L.ld_w = pack_ld(L.biased ? d + 1 : d, es);

@@ -144,7 +144,7 @@ def _activation(name):
 # the structs as bytes: a small call is as long as its way to the launch
 _linear_bytes = struct.Struct("=Iiii3q10Q8q").pack
 _ce_bytes = struct.Struct("=Ii3q5Qfi6Q4q").pack
-_FEW_ROWS = 64  # TIG_LINEAR_FEW_ROWS
+_FEW_ROWS = 16  # TIG_LINEAR_FEW_ROWS
 
 
 def linear(x, w, bias=None, residual=None, activation="none", keep=False, out=None):

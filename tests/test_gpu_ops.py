@@ -41,8 +41,14 @@ def gen_of(seed):
 
 
 def close(got, ref, tol, name):
+    # Beyond a type's range infinity is the right rounding: its largest value is (2 - eps) 2^e, and from half a step above that
+    # on, (2 - eps / 2) 2^e, the nearest is 2^(e + 1), which the type does not have.  A value within tol of ref may lie there if
+    # |ref| + tol does.  (fp16: 65520.)
+    info = torch.finfo(got.dtype)
+    edge = info.max / (2 - info.eps) * (2 - info.eps / 2)
     got = got.to(F64)
-    bad = ~((got - ref).abs() <= tol) & ~(torch.isnan(got) & torch.isnan(ref)) & ~(got == ref)
+    over = torch.isinf(got) & (got * ref > 0) & (ref.abs() + tol >= edge)
+    bad = ~((got - ref).abs() <= tol) & ~(torch.isnan(got) & torch.isnan(ref)) & ~(got == ref) & ~over
     if bad.any():
         i = tuple(int(v) for v in torch.nonzero(bad)[0])
         raise AssertionError(f"{name}: {int(bad.sum())} of {bad.numel()} off, first at {i}: {float(got[i])} for {float(ref[i])}, tolerance {float((tol + 0 * ref)[i])}")
@@ -300,6 +306,29 @@ def test_softmax_ce_narrow_rows_over_many_tiles(n, V, d, bias, dtype):
     check_ce(n, V, d, dtype, bias=bias, seed=n)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("weighted,scale,pad,shift", [(False, 1.0, 0, 0), (True, -0.5, 8, 0), (False, -2.0, 0, 1), (True, 1.0, 3, 0)])
+def test_softmax_ce_narrow_rows_and_many_logits(dtype, weighted, scale, pad, shift):
+    # products of 2^25 logits and more: around tiles of 64 streamed and 192 or 256 own rows, one range and many
+    shapes = [(2049, 16_385, 65), (4000, 8_400, 127), (64, 530_000, 64), (34_000, 1000, 128), (3, 11_200_000, 8), (1_200_000, 28, 24), (300, 112_000, 96)]
+    for i, shape in enumerate(shapes):
+        check_ce(*shape, dtype, bias=i % 2 == 0, weighted=weighted, scale=scale * (512 if dtype == "fp16" else 1), seed=80 + i, pad=pad, shift=shift)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_softmax_ce_narrow_rows_masked_candidates(dtype):
+    r = check_ce(2100, 16_100, 48, dtype, seed=3, masked=16_000)
+    assert torch.isinf(r.loss).any()  # labels among the masked ones
+    r = check_ce(2100, 16_100, 100, dtype, seed=4, masked=16_100, ignored=0.3)  # nothing left in any row
+    assert (r.lse == -math.inf).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_softmax_ce_narrow_rows_without_gradients(dtype):
+    for i, shape in enumerate([(1, 131_072, 100), (7, 140_001, 33), (200, 131_100, 128)]):
+        check_ce(*shape, dtype, bias=i != 2, seed=90 + i, grad=False)
+
+
 def test_softmax_ce_wide_rows_in_several_pieces():
     check_ce(20_000, 4000, 136, "bf16", seed=14)
     check_ce(9000, 9000, 160, "fp16", seed=15, scale=1024.0, weighted=True)
@@ -313,7 +342,7 @@ def test_softmax_ce_only_some_gradients(dtype):
     gen = gen_of(23)
     t = TYPES[dtype]
     lib = ops._lib()
-    for n, V, d in ((90, 400, 100), (300, 130, 200), (2000, 300, 64)):
+    for n, V, d in ((90, 400, 100), (300, 130, 200), (2000, 300, 64), (2100, 16_000, 100), (300, 112_000, 64)):
         x, w, b = rnd(gen, n, d, dtype=t), rnd(gen, V, d, std=0.2, dtype=t), rnd(gen, V, dtype=t)
         labels = torch.randint(0, V, (n,), device=DEV, generator=gen, dtype=torch.int32)
         full = ops.softmax_ce(x, w, labels, b)
@@ -333,9 +362,9 @@ def test_softmax_ce_only_some_gradients(dtype):
 
 def test_softmax_ce_rows_left_out_take_no_part():
     gen = gen_of(17)
-    for t in (torch.float32, torch.bfloat16):
-        x, w, b = rnd(gen, 100, 64, dtype=t), rnd(gen, 333, 64, std=0.1, dtype=t), rnd(gen, 333, dtype=t)
-        labels = torch.randint(0, 333, (100,), device=DEV, generator=gen, dtype=torch.int32)
+    for t, n, V in ((torch.float32, 100, 333), (torch.bfloat16, 100, 333), (torch.bfloat16, 2100, 16_000)):
+        x, w, b = rnd(gen, n, 64, dtype=t), rnd(gen, V, 64, std=0.1, dtype=t), rnd(gen, V, dtype=t)
+        labels = torch.randint(0, V, (n,), device=DEV, generator=gen, dtype=torch.int32)
         labels[::3] = -1
         a = ops.softmax_ce(x, w, labels, b)
         x2 = x.clone()
