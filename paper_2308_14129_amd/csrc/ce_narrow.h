@@ -12,6 +12,11 @@
 // summed over) comes from the same LDS tile with the transposing load.  So each gradient forms the logits once more (10 n V d
 // operations instead of 8), and P is never in memory.
 //
+// Bound by the exponentials and the products, of which a wavefront does one after the other and two wavefronts share a SIMD: 4000 x
+// 250000 x 100 in bf16 276 us statistics (725 TFLOP/s of 200 operations a logit), 393 dX, 461 dW (1018 and 868 of 400).
+//
+// P is rounded to 16 bits for the second product: it is at most 1 in magnitude, relative to the largest weight.
+//
 // BIASED: both matrices are copies with one column more: W's holds the candidate's bias (-infinity in the rows that fill its last
 // tile), X's ones, also in rows that do not count or fill the last tile.  The product adds the bias, and the column of dW that
 // belongs to the ones is the bias' gradient: the vector unit, which the exponentials keep busy as long as the products do the

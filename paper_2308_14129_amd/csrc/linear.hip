@@ -3,6 +3,8 @@
 //   up to 16 rows     k_linear_rows: the matrix is read once, straight into matrix-core operands
 //   more rows         the tile product of gemm.h, bias, activation and residual in its epilogue
 //   backward          k_linear_dz: dz = dy act'(z), and its column sums before it is rounded; then two tile products
+// 8192 rows, 4096 -> 16384 in bf16 with gelu and residual: forward 1130 us, k_linear_dz 166 (4.8 TB/s), products 962 and 965.
+// dz is rounded to the layer's type: it is a matrix operand of both products, and at most half a unit of dy's own last place off.
 #include <type_traits>
 
 #include "act.h"
@@ -228,25 +230,29 @@ __global__ void __launch_bounds__(1024) k_join_sums(const float *sums, int64_t l
 {
     __shared__ double part[16][64];
     const int c = threadIdx.x % 64, w = threadIdx.x / 64;
-    const int64_t n = (int64_t)blockIdx.x * 64 + c;
-    double total = 0.0;
-    if (n < N)
+    for (int64_t n0 = (int64_t)blockIdx.x * 64; n0 < N; n0 += (int64_t)gridDim.x * 64) {
+        const int64_t n = n0 + c;
+        double total = 0.0;
+        if (n < N)
 #pragma unroll 8
-        for (int64_t b = w; b < blocks; b += 16)
-            total += (double)sums[b * lds + n];
-    part[w][c] = total;
-    __syncthreads();
-    if (w == 0 && n < N) {
-        for (int k = 1; k < 16; ++k)
-            total += part[k][c];
-        out[n] = (T)(float)(total * (double)alpha * (scale ? (double)*scale : 1.0));
+            for (int64_t b = w; b < blocks; b += 16)
+                total += (double)sums[b * lds + n];
+        part[w][c] = total;
+        __syncthreads();
+        if (w == 0 && n < N) {
+            for (int k = 1; k < 16; ++k)
+                total += part[k][c];
+            out[n] = (T)(float)(total * (double)alpha * (scale ? (double)*scale : 1.0));
+        }
+        __syncthreads();
     }
 }
 
 template <typename T>
 hipError_t launch_join_sums(const float *sums, int64_t lds, int64_t blocks, int64_t N, T *out, const float *scale, float alpha, hipStream_t s)
 {
-    hipLaunchKernelGGL((k_join_sums<T>), dim3((unsigned)((N + 63) / 64)), dim3(1024), 0, s, sums, lds, blocks, N, out, scale, alpha);
+    const int64_t groups = (N + 63) / 64;
+    hipLaunchKernelGGL((k_join_sums<T>), dim3((unsigned)(groups < 65536 ? groups : 65536)), dim3(1024), 0, s, sums, lds, blocks, N, out, scale, alpha);
     return hipGetLastError();
 }
 template hipError_t launch_join_sums<float>(const float *, int64_t, int64_t, int64_t, float *, const float *, float, hipStream_t);
@@ -323,7 +329,7 @@ int check_linear(const tig_linear *p, bool backward)
         return fail_text(TIG_EINVAL, "tig_linear: NULL argument or wrong struct_size");
     if (!dtype_ok(p->dtype) || p->activation < TIG_ACT_NONE || p->activation > TIG_ACT_SILU || p->reserved != 0)
         return fail_text(TIG_EINVAL, "tig_linear: unknown dtype or activation, or reserved is not 0");
-    if (p->rows < 0 || p->rows > 0x7fffffff || p->in_dim < 1 || p->in_dim > kMaxDim || p->out_dim < 1 || p->out_dim > kMaxDim)
+    if (p->rows < 0 || p->rows > (1 << 26) || p->in_dim < 1 || p->in_dim > kMaxDim || p->out_dim < 1 || p->out_dim > kMaxDim)
         return fail_text(TIG_EINVAL, "tig_linear: rows or dimensions out of range");
     auto ld_ok = [](int64_t ld, int64_t cols) { return ld >= cols && ld <= (1 << 22); };
     auto aligned = [&](const void *q) { return (uintptr_t)q % (uintptr_t)dtype_bytes(p->dtype) == 0; };

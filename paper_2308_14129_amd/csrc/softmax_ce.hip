@@ -5,7 +5,9 @@
 //   gradient     for one piece of the vocabulary after the other: the logits once more, P = w_i (exp(l - lse) - [label]) in their
 //                epilogue, and two tile products, dX += P W and dW = P^T X.  A piece of P stays within the last-level cache.
 // s_i = S w_i with S the largest |s_i|: P holds values of at most 1, the products are scaled by S afterwards.
-// Rows of at most 128 columns in 16-bit types go the way of ce_narrow.h.
+// 8192 x 128000 x 2048 in bf16: statistics 3.45 ms (1.25 PFLOP/s), P 3.98 (1.08), dX 3.59 (1.20), dW 3.71 (1.16).  P is a matrix operand
+// and so of the matrices' type: at most 1 in magnitude, relative to the largest weight; fp16 scaled by 2^14 (kPScale).
+// Many rows of at most 128 columns in 16-bit types go the way of ce_narrow.h (ce_plan).
 #include "act.h"
 #include "ce_narrow.h"
 #include "gemm.h"
@@ -546,7 +548,7 @@ int check_ce(const tig_softmax_ce *p)
         return fail_text(TIG_EINVAL, "tig_softmax_ce: NULL argument or wrong struct_size");
     if (!dtype_ok(p->dtype) || p->reserved != 0)
         return fail_text(TIG_EINVAL, "tig_softmax_ce: unknown dtype, or reserved is not 0");
-    if (p->rows < 0 || p->rows > (1 << 24) || p->vocab < 1 || p->vocab > 0x7fffffff || p->dim < 1 || p->dim > (1 << 16))
+    if (p->rows < 0 || p->rows > (1 << 24) || p->vocab < 1 || p->vocab > (1 << 28) || p->dim < 1 || p->dim > (1 << 16))
         return fail_text(TIG_EINVAL, "tig_softmax_ce: rows, vocab or dim out of range");
     if (p->rows > 0 && (!p->x || !p->labels || !p->w))
         return fail_text(TIG_EINVAL, "tig_softmax_ce: x, w or labels is NULL");
@@ -574,7 +576,7 @@ hipError_t launch_rows(const tig_softmax_ce &p, int64_t r, int64_t m, const floa
                        const CeHead *head, const CeRowsOut<T> &out, hipStream_t s)
 {
     const int64_t all = out.lse2 ? (m + kNarrowStream - 1) / kNarrowStream * kNarrowStream : m;
-    // (a wavefront a row where the parts of 16 lanes would be long chains of loads)
+    // (a wavefront a row where the parts of 16 lanes would be long chains of loads: 103 rows of 2165 tiles 63 us with 16, 14 with 64)
     const bool wide = tiles > 128 && m < 4096;
     hipLaunchKernelGGL((wide ? k_ce_rows<T, 64> : k_ce_rows<T, 16>), dim3((unsigned)(wide ? (all + 3) / 4 : (all + 15) / 16)), dim3(256), 0, s, part, tiles, m,
                        x + r * ldx, ldx, w, ldw, (const T *)p.bias, p.dim, p.vocab, p.labels + r, p.row_scale ? p.row_scale + r : nullptr, p.scale, head, out);

@@ -1012,7 +1012,7 @@ static int check_head(const Dims &d, const tig_train_head *h, int64_t num_nodes)
         return TIG_EINVAL;
     if (h->activation < TIG_ACT_NONE || h->activation > TIG_ACT_SILU || !(h->weight - h->weight == 0.0f))
         return TIG_EINVAL;
-    if (h->first_node < 0 || h->num_items < 1 || h->num_items > num_nodes || h->first_node > num_nodes - h->num_items)
+    if (h->first_node < 0 || h->num_items < 1 || h->num_items > num_nodes || h->first_node > num_nodes - h->num_items || h->num_items > 1 << 28)
         return TIG_EINVAL;
     return train_supported(d) ? TIG_OK : TIG_EINVAL;
 }

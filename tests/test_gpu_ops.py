@@ -648,3 +648,51 @@ def test_results_do_not_change_from_call_to_call():
             assert all(torch.equal(a, b) for a, b in zip(first, ops.linear_backward(dy, x, w)))
             again = ops.softmax_ce(x, w, torch.zeros(3000, dtype=torch.int32, device=DEV))
             assert all(torch.equal(a, b) for a, b in zip(ce, again) if a is not None)
+
+
+def test_large_calls_in_a_captured_graph_and_side_by_side_on_two_streams():
+    gen = gen_of(61)
+    t = torch.bfloat16
+
+    def inputs():
+        return (rnd(gen, 4096, 512, dtype=t), rnd(gen, 4096, 512, std=0.05, dtype=t), rnd(gen, 4096, dtype=t), rnd(gen, 4096, 4096, std=0.05, dtype=t),
+                torch.randint(-1, 4096, (4096,), device=DEV, generator=gen, dtype=torch.int32), rnd(gen, 8200, 104, std=0.1, dtype=t))
+
+    def calls(x, w, b, items, labels, narrow):
+        y, z = ops.linear(x, w, b, activation="gelu", keep=True)
+        r = ops.softmax_ce(y, items, labels)
+        q = ops.softmax_ce(x[:, :96], narrow[:, :96], labels)  # narrow rows
+        return (y, *r[:5], *q, *ops.linear_backward(r.dx, x, w, z, "gelu"))
+
+    def same(got, want, what):
+        for k, (p, q) in enumerate(zip(got, want)):
+            assert (p is None) == (q is None) and (p is None or torch.equal(p, q)), (what, k)
+
+    sets = [inputs() for _ in range(3)]
+    eager = [calls(*s) for s in sets]
+    held = [q.clone() for q in sets[0]]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls(*held)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = calls(*held)
+    for turn in range(6):
+        for q, new in zip(held, sets[turn % 3]):
+            q.copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        same(out, eager[turn % 3], f"replay {turn}")
+        same(calls(*sets[(turn + 1) % 3]), eager[(turn + 1) % 3], f"eager beside replay {turn}")
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for st in streams:
+        st.wait_stream(torch.cuda.current_stream())
+    got = []
+    for turn in range(4):
+        with torch.cuda.stream(streams[turn % 2]):
+            got.append(calls(*sets[turn % 3]))
+    torch.cuda.synchronize()
+    for turn in range(4):
+        same(got[turn], eager[turn % 3], f"streams {turn}")

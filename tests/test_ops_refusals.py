@@ -32,7 +32,7 @@ def make_linear(**kw):
 
 @pytest.mark.parametrize("bad", [
     dict(struct_size=8), dict(dtype=3), dict(dtype=-1), dict(activation=4), dict(activation=-1), dict(reserved=1), dict(rows=-1),
-    dict(rows=2**31), dict(in_dim=0), dict(out_dim=0), dict(in_dim=2**20 + 1, ldx=2**21, ldw=2**21), dict(ldx=63), dict(ldw=63), dict(ldy=31),
+    dict(rows=2**31), dict(rows=2**26 + 1), dict(in_dim=0), dict(out_dim=0), dict(in_dim=2**20 + 1, ldx=2**21, ldw=2**21), dict(ldx=63), dict(ldw=63), dict(ldy=31),
     dict(ldz=31), dict(residual=HOST, ldr=31), dict(ldx=2**22 + 1), dict(x=None), dict(w=None), dict(y=None), dict(x=HOST + 1), dict(bias=HOST + 1),
     dict(y=HOST + 1)], ids=str)
 def test_linear_forward_refuses(lib, bad):
@@ -76,7 +76,7 @@ def make_ce(**kw):
 
 
 @pytest.mark.parametrize("bad", [
-    dict(struct_size=8), dict(dtype=9), dict(reserved=1), dict(rows=-1), dict(rows=2**24 + 1), dict(vocab=0), dict(vocab=2**31), dict(dim=0),
+    dict(struct_size=8), dict(dtype=9), dict(reserved=1), dict(rows=-1), dict(rows=2**24 + 1), dict(vocab=0), dict(vocab=2**31), dict(vocab=2**28 + 1), dict(dim=0),
     dict(dim=2**16 + 1, ldx=2**17, ldw=2**17, lddx=2**17, lddw=2**17), dict(x=None), dict(w=None), dict(labels=None), dict(ldx=63), dict(ldw=63),
     dict(lddx=63), dict(lddw=63), dict(w=HOST + 1), dict(labels=HOST + 2), dict(loss=HOST + 2), dict(scale=float("nan")), dict(scale=float("inf"))], ids=str)
 def test_softmax_ce_refuses(lib, bad):
@@ -128,6 +128,29 @@ def test_adamw_workspace_and_numbers_are_checked(lib):
     assert lib.tig_adamw_create(byref(c), t, 1, HOST, need.value, None, None) == tig.TIG_EINVAL
     assert lib.tig_adamw_create(byref(c), t, -1, HOST, need.value, None, byref(h)) == tig.TIG_EINVAL
     assert lib.tig_adamw_step(None, 1e-3, 1.0, 0.0, None, None) == tig.TIG_EINVAL
+
+
+@pytest.mark.parametrize("which", ["param", "m", "v", "master", "between tensors", "v_scale"])
+def test_adamw_refuses_arrays_that_overlap(lib, which):
+    eight = which == "v_scale"
+    c, _ = make_adamw(cfg=dict(state_bits=8 if eight else 32))
+    t = (ops.tig_adamw_tensor * 2)()
+    at = 1 << 20
+    for q in t:
+        q.n, q.grad = 1000, HOST  # (gradients may be shared)
+        for name in ("param", "m", "v", "master") + (("m_scale", "v_scale") if eight else ()):
+            setattr(q, name, HOST + at)
+            at += 4000
+    if which == "between tensors":
+        t[1].param = t[0].param + 3996
+    elif which == "v_scale":
+        t[0].v_scale = t[0].m_scale + 12
+    else:
+        setattr(t[1], which, getattr(t[0], which))
+    need, h = c_size_t(0), c_void_p(None)
+    assert lib.tig_adamw_workspace_bytes(byref(c), t, 2, byref(need)) == tig.TIG_OK
+    assert lib.tig_adamw_create(byref(c), t, 2, HOST, need.value, None, byref(h)) == tig.TIG_EINVAL and not h.value
+    assert b"overlap" in lib.tig_last_error(None)
 
 
 def test_python_entry_points_refuse():
