@@ -3,7 +3,7 @@
 //   up to 16 rows     k_linear_rows: the matrix is read once, straight into matrix-core operands
 //   more rows         the tile product of gemm.h, bias, activation and residual in its epilogue
 //   backward          k_linear_dz: dz = dy act'(z), and its column sums before it is rounded; then two tile products
-// 8192 rows, 4096 -> 16384 in bf16 with gelu and residual: forward 1130 us, k_linear_dz 166 (4.8 TB/s), products 962 and 965.
+// 8192 rows, 4096 -> 16384 in bf16 with gelu and residual: forward 1116 us, k_linear_dz 166 (4.8 TB/s), products 942 and 941.
 // dz is rounded to the layer's type: it is a matrix operand of both products, and at most half a unit of dy's own last place off.
 #include <type_traits>
 

@@ -5,7 +5,7 @@
 //   gradient     for one piece of the vocabulary after the other: the logits once more, P = w_i (exp(l - lse) - [label]) in their
 //                epilogue, and two tile products, dX += P W and dW = P^T X.  A piece of P stays within the last-level cache.
 // s_i = S w_i with S the largest |s_i|: P holds values of at most 1, the products are scaled by S afterwards.
-// 8192 x 128000 x 2048 in bf16: statistics 3.45 ms (1.25 PFLOP/s), P 3.98 (1.08), dX 3.59 (1.20), dW 3.71 (1.16).  P is a matrix operand
+// 8192 x 128000 x 2048 in bf16: statistics 3.36 ms (1.28 PFLOP/s), P 3.95 (1.09), dX 3.44 (1.25), dW 3.68 (1.17).  P is a matrix operand
 // and so of the matrices' type: at most 1 in magnitude, relative to the largest weight; fp16 scaled by 2^14 (kPScale).
 // Many rows of at most 128 columns in 16-bit types go the way of ce_narrow.h (ce_plan).
 #include "act.h"
