@@ -43,7 +43,6 @@ struct AdamChunk {
     int32_t n;
     int32_t dtype;
     float decay;
-    int32_t wide;  // four elements at once, of every array
 };
 
 // the step's numbers
@@ -86,17 +85,17 @@ __device__ inline AdamNow numbers(const AdamParams &p, int64_t t)
 }
 
 template <int ROUNDS, typename T>
-__device__ inline void load_grads(const T *g, int n, bool wide, floatx4 (&v)[ROUNDS])
+__device__ inline void load_grads(const T *g, int n, floatx4 (&v)[ROUNDS])
 {
-    if (wide && n == ROUNDS * kAtOnce) {  // (uniform: a load in a lane's branch would be waited for at the branch's end)
+    if (n == ROUNDS * kAtOnce) {  // (uniform: a load in a lane's branch would be waited for at the branch's end)
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r)
-            v[r] = load_four(g + r * kAtOnce + (int)threadIdx.x * 4, 4, true);
+            v[r] = load_four(g + r * kAtOnce + (int)threadIdx.x * 4, 4);
     } else {
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r) {
             const int i = r * kAtOnce + (int)threadIdx.x * 4;
-            v[r] = load_four(g + i, n - i < 4 ? (n > i ? n - i : 0) : 4, wide);
+            v[r] = load_four(g + i, n - i < 4 ? (n > i ? n - i : 0) : 4);
         }
     }
 }
@@ -129,11 +128,11 @@ __global__ void __launch_bounds__(kAdamThreads) k_adamw_norm(AdamParams p)
         for (int k = 0; k < 2; ++k) {
             const int n = k == 0 || both ? ch[k].n : 0;
             if (ch[k].dtype == TIG_F32)
-                load_grads<ROUNDS>((const float *)ch[k].grad, n, ch[k].wide, v[k]);
+                load_grads<ROUNDS>((const float *)ch[k].grad, n, v[k]);
             else if (ch[k].dtype == TIG_BF16)
-                load_grads<ROUNDS>((const __bf16 *)ch[k].grad, n, ch[k].wide, v[k]);
+                load_grads<ROUNDS>((const __bf16 *)ch[k].grad, n, v[k]);
             else
-                load_grads<ROUNDS>((const _Float16 *)ch[k].grad, n, ch[k].wide, v[k]);
+                load_grads<ROUNDS>((const _Float16 *)ch[k].grad, n, v[k]);
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k)
@@ -211,20 +210,24 @@ __device__ inline floatx4 from_8bit(uint32_t w, float scale)
     return floatx4{__builtin_amdgcn_cvt_f32_fp8((int)w, 0) * scale, __builtin_amdgcn_cvt_f32_fp8((int)w, 1) * scale,
                    __builtin_amdgcn_cvt_f32_fp8((int)w, 2) * scale, __builtin_amdgcn_cvt_f32_fp8((int)w, 3) * scale};
 }
-__device__ inline uint32_t load_bytes(const uint8_t *p, int left, bool wide)
+struct __attribute__((packed)) FourBytes {
+    uint32_t w;
+};
+__device__ inline uint32_t load_bytes(const uint8_t *p, int left)
 {
-    if (left == 4 && wide)
-        return *(const uint32_t *)p;
+    if (left == 4)
+        return ((const FourBytes *)p)->w;
     uint32_t w = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-        w |= e < left ? (uint32_t)p[e] << (8 * e) : 0u;
+        if (e < left)
+            w |= (uint32_t)p[e] << (8 * e);
     return w;
 }
-__device__ inline void store_bytes(uint8_t *p, uint32_t w, int left, bool wide)
+__device__ inline void store_bytes(uint8_t *p, uint32_t w, int left)
 {
-    if (left == 4 && wide) {
-        *(uint32_t *)p = w;
+    if (left == 4) {
+        ((FourBytes *)p)->w = w;
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -235,7 +238,7 @@ __device__ inline void store_bytes(uint8_t *p, uint32_t w, int left, bool wide)
 
 // A lane's fours of a chunk; numbers(): the step's, once the loads are on their way.  Products and sums in the order of the formulas, each rounded: a state's code does not depend
 // on what the compiler joins.  A wavefront's four times 64 elements of a round are a block of 256.
-template <typename T, int BITS, int ROUNDS, bool WIDE, class F>
+template <typename T, int BITS, int ROUNDS, bool FULL, class F>
 __device__ inline void update_chunk(const AdamParams &p, const AdamChunk &ch, const F &numbers)
 {
 #pragma clang fp contract(off)
@@ -245,16 +248,16 @@ __device__ inline void update_chunk(const AdamParams &p, const AdamChunk &ch, co
     const int i0 = (int)threadIdx.x * 4;
 #pragma unroll
     for (int r = 0; r < ROUNDS; ++r) {
-        const int i = i0 + r * kAtOnce, left = WIDE || ch.n - i >= 4 ? 4 : (ch.n > i ? ch.n - i : 0);
-        g[r] = load_four((const T *)ch.grad + i, left, WIDE);
-        x[r] = ch.master ? load_four(ch.master + i, left, WIDE) : load_four((const T *)ch.param + i, left, WIDE);
+        const int i = i0 + r * kAtOnce, left = FULL || ch.n - i >= 4 ? 4 : (ch.n > i ? ch.n - i : 0);
+        g[r] = load_four((const T *)ch.grad + i, left);
+        x[r] = ch.master ? load_four(ch.master + i, left) : load_four((const T *)ch.param + i, left);
         if constexpr (BITS == 32) {
-            m[r] = load_four((const float *)ch.m + i, left, WIDE);
-            v[r] = load_four((const float *)ch.v + i, left, WIDE);
+            m[r] = load_four((const float *)ch.m + i, left);
+            v[r] = load_four((const float *)ch.v + i, left);
         } else {
             const int block = left > 0 ? i / kStateBlock : 0;
-            wm[r] = load_bytes((const uint8_t *)ch.m + i, left, WIDE);
-            wv[r] = load_bytes((const uint8_t *)ch.v + i, left, WIDE);
+            wm[r] = load_bytes((const uint8_t *)ch.m + i, left);
+            wv[r] = load_bytes((const uint8_t *)ch.v + i, left);
             sm[r] = ch.m_scale[block];
             sv[r] = ch.v_scale[block];
         }
@@ -265,7 +268,7 @@ __device__ inline void update_chunk(const AdamParams &p, const AdamChunk &ch, co
     const float keep = 1.0f - now.lr * ch.decay;
 #pragma unroll
     for (int r = 0; r < ROUNDS; ++r) {
-        const int i = i0 + r * kAtOnce, left = WIDE || ch.n - i >= 4 ? 4 : (ch.n > i ? ch.n - i : 0);
+        const int i = i0 + r * kAtOnce, left = FULL || ch.n - i >= 4 ? 4 : (ch.n > i ? ch.n - i : 0);
         if constexpr (BITS == 8) {
             m[r] = from_8bit(wm[r], sm[r]);
             v[r] = from_8bit(wv[r], sv[r]);
@@ -286,11 +289,11 @@ __device__ inline void update_chunk(const AdamParams &p, const AdamChunk &ch, co
             x[r][e] = x[r][e] * keep - now.step_size * (m[r][e] / (root[e] * now.root_scale + p.eps));
         }
         if (ch.master)
-            store_four(ch.master + i, x[r], left, WIDE);
-        store_four((T *)ch.param + i, x[r], left, WIDE);
+            store_four(ch.master + i, x[r], left);
+        store_four((T *)ch.param + i, x[r], left);
         if constexpr (BITS == 32) {
-            store_four((float *)ch.m + i, m[r], left, WIDE);
-            store_four((float *)ch.v + i, v[r], left, WIDE);
+            store_four((float *)ch.m + i, m[r], left);
+            store_four((float *)ch.v + i, v[r], left);
         } else {
             float top_m = 0.0f, top_r = 0.0f, a, b;
             floatx4 um, ur;
@@ -303,8 +306,8 @@ __device__ inline void update_chunk(const AdamParams &p, const AdamChunk &ch, co
                 ur[e] = (float)((h + 0x80000000u) >> 8) * 0x1p-24f;
             }
             const uint32_t qm = to_8bit(m[r], wave_top(top_m), um, false, &a), qr = to_8bit(root, wave_top(top_r), ur, true, &b);
-            store_bytes((uint8_t *)ch.m + i, qm, left, WIDE);
-            store_bytes((uint8_t *)ch.v + i, qr, left, WIDE);
+            store_bytes((uint8_t *)ch.m + i, qm, left);
+            store_bytes((uint8_t *)ch.v + i, qr, left);
             if (left > 0 && lane_id() == 0) {
                 ch.m_scale[i / kStateBlock] = a;
                 ch.v_scale[i / kStateBlock] = b;
@@ -334,7 +337,7 @@ __global__ void __launch_bounds__(kAdamThreads) k_adamw_update(AdamParams p)
     };
     auto update = [&](auto type) {
         using T = decltype(type);
-        if (ch.wide && ch.n == ROUNDS * kAtOnce)  // (uniform)
+        if (ch.n == ROUNDS * kAtOnce)  // (uniform)
             update_chunk<T, BITS, ROUNDS, true>(p, ch, form);
         else
             update_chunk<T, BITS, ROUNDS, false>(p, ch, form);
@@ -493,13 +496,11 @@ int tig_adamw_create(const tig_adamw_config *cfg, const tig_adamw_tensor *tensor
     for (int64_t i = 0; i < n_tensors; ++i) {
         const tig_adamw_tensor &q = tensors[i];
         const int es = dtype_bytes(q.dtype), ss = cfg->state_bits == 32 ? 4 : 1;
-        const bool wide = four_aligned(q.param, 4, es) && four_aligned(q.grad, 4, es) && four_aligned(q.master, 4, 4) && four_aligned(q.m, 4, ss) &&
-                          four_aligned(q.v, 4, ss);
         auto at = [](const void *x, int64_t bytes) { return x ? (void *)((char *)x + bytes) : nullptr; };
         for (int64_t c = 0; c < q.n; c += L.chunk())
             *ch++ = AdamChunk{at(q.param, c * es), at(q.grad, c * es), (float *)at(q.master, c * 4), at(q.m, c * ss), at(q.v, c * ss),
                               (float *)at(q.m_scale, c / kStateBlock * 4), (float *)at(q.v_scale, c / kStateBlock * 4),
-                              (int32_t)(q.n - c < L.chunk() ? q.n - c : L.chunk()), q.dtype, q.weight_decay, wide ? 1 : 0};
+                              (int32_t)(q.n - c < L.chunk() ? q.n - c : L.chunk()), q.dtype, q.weight_decay};
     }
     hipStream_t s = (hipStream_t)hip_stream;
     hipError_t e = L.part ? hipMemcpyAsync(workspace, host, L.part, hipMemcpyHostToDevice, s) : hipSuccess;

@@ -21,33 +21,31 @@ struct EpiLinear {
     const T *bias, *res;
     T *y, *z;
     int64_t ldr, ldy, ldz;
-    bool bias_ok, res_ok, y_ok, z_ok;  // four elements at once
     struct Row {
         const T *res;
         T *y, *z;
     };
-    __device__ inline bool aligned() const { return (bias_ok || !bias) && (res_ok || !res) && y_ok && (z_ok || !z); }
     __device__ inline Row row(int64_t m) const { return {res + m * ldr, y + m * ldy, z + m * ldz}; }
     template <bool FULL>
     __device__ inline floatx4 col(int64_t n, int left) const
     {
-        return bias ? load_four(bias + n, left, FULL || bias_ok) : floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        return bias ? load_four(bias + n, FULL ? 4 : left) : floatx4{0.0f, 0.0f, 0.0f, 0.0f};
     }
     template <bool FULL>
     __device__ inline floatx4 load(const Row &r, int64_t n, int left) const
     {
-        return res ? load_four(r.res + n, left, FULL || res_ok) : floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        return res ? load_four(r.res + n, FULL ? 4 : left) : floatx4{0.0f, 0.0f, 0.0f, 0.0f};
     }
     template <bool FULL>
     __device__ inline void store(const Row &r, const floatx4 &b, const floatx4 &more, int64_t n, floatx4 v, int left) const
     {
         v += b;
         if (z)
-            store_four(r.z + n, v, left, FULL || z_ok);
+            store_four(r.z + n, v, FULL ? 4 : left);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             v[e] = activate<ACT>(v[e]);
-        store_four(r.y + n, v + more, left, FULL || y_ok);
+        store_four(r.y + n, v + more, FULL ? 4 : left);
     }
 };
 
@@ -188,9 +186,9 @@ __global__ void __launch_bounds__(64 * kDzWaves) k_linear_dz(const T *dy, int64_
             for (int u = 0; u < V; ++u) {
                 const int64_t n = n0 + 4 * u;
                 const int left = N - n < 4 ? (N > n ? (int)(N - n) : 0) : 4;
-                v[u] = load_four(dy + m * lddy + n, left, false);
+                v[u] = load_four(dy + m * lddy + n, left);
                 if constexpr (ACT != TIG_ACT_NONE)
-                    q[u] = load_four(z + m * ldz + n, left, false);
+                    q[u] = load_four(z + m * ldz + n, left);
             }
             add(m, v, q);
         }
@@ -369,8 +367,7 @@ hipError_t forward(const tig_linear &p, const LinearPlan &L, char *ws, hipStream
     return with_activation(p.activation, [&](auto act) -> hipError_t {
         using Epi = EpiLinear<T, decltype(act)::value>;
         const int es = sizeof(T);
-        const Epi epi = {(const T *)p.bias, (const T *)p.residual, (T *)p.y, (T *)p.z, p.ldr, p.ldy, p.ldz,
-                         four_aligned(p.bias, 4, es), four_aligned(p.residual, p.ldr, es), four_aligned(p.y, p.ldy, es), four_aligned(p.z, p.ldz, es)};
+        const Epi epi = {(const T *)p.bias, (const T *)p.residual, (T *)p.y, (T *)p.z, p.ldr, p.ldy, p.ldz};
         if (L.few)
             return launch_linear_rows<T>(p, epi, s);
         const T *x = (const T *)p.x, *w = (const T *)p.w;
@@ -426,7 +423,7 @@ hipError_t backward(const tig_linear &p, const LinearPlan &L, char *ws, hipStrea
             e = launch_pack(w, ldw, ws + L.pw, L.ld_pw, p.out_dim, p.in_dim, es, s);
             w = (const T *)(ws + L.pw), ldw = L.ld_pw;
         }
-        const EpiStore<T> epi = {(T *)p.dx, p.lddx, nullptr, 1.0f, four_aligned(p.dx, p.lddx, es)};
+        const EpiStore<T> epi = {(T *)p.dx, p.lddx, nullptr, 1.0f};
         if (e == hipSuccess)
             e = launch_gemm<T, kRow, kCol>(L.dx, dz, lddz, w, ldw, p.rows, p.in_dim, p.out_dim, ws + L.part, epi, s);
         if (e != hipSuccess)
@@ -439,7 +436,7 @@ hipError_t backward(const tig_linear &p, const LinearPlan &L, char *ws, hipStrea
             e = launch_pack(x, ldx, ws + L.px, L.ld_px, p.rows, p.in_dim, es, s);
             x = (const T *)(ws + L.px), ldx = L.ld_px;
         }
-        const EpiStore<T> epi = {(T *)p.dw, p.lddw, nullptr, 1.0f, four_aligned(p.dw, p.lddw, es)};
+        const EpiStore<T> epi = {(T *)p.dw, p.lddw, nullptr, 1.0f};
         if (e == hipSuccess)
             e = launch_gemm<T, kCol, kCol>(L.dw, dz, lddz, x, ldx, p.out_dim, p.in_dim, p.rows, ws + L.part, epi, s);
     }

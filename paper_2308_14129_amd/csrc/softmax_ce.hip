@@ -96,7 +96,6 @@ template <typename T>
 struct EpiStats {
     static constexpr bool kWhole = true;
     const T *bias;
-    bool bias_ok;
     float2 *part;
     int64_t rows;
     template <int BM, int BN, int WM, int WN, int FM, int FN>
@@ -110,7 +109,7 @@ struct EpiStats {
             const int left = at.N - n < 4 ? (at.N > n ? (int)(at.N - n) : 0) : 4;
             floatx4 b = {0.0f, 0.0f, 0.0f, 0.0f};
             if (bias)
-                b = load_four(bias + n, left, bias_ok);
+                b = load_four(bias + n, left);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -254,7 +253,6 @@ template <typename T>
 struct EpiP {
     static constexpr bool kWhole = true;
     const T *bias;
-    bool bias_ok;
     const CeRow *rec;
     T *P;
     int64_t ldp, v0;
@@ -271,7 +269,7 @@ struct EpiP {
             const int left = at.N - n < 4 ? (at.N > n ? (int)(at.N - n) : 0) : 4;
             b[j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
             if (bias)
-                b[j] = load_four(bias + n, left, bias_ok);
+                b[j] = load_four(bias + n, left);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 b[j][e] = e < left ? b[j][e] : -INFINITY;
@@ -305,7 +303,7 @@ struct EpiP {
                     }
                     total[j] += p;
                     if (FULL || (on && at.n0 + j * 16 + 4 * g < end))
-                        store_four(row + j * 16, p, 4, true);
+                        store_four(row + j * 16, p, 4);
                 }
                 __builtin_amdgcn_sched_barrier(0);  // (a row after the other: their values at once do not fit the registers)
             }
@@ -344,7 +342,6 @@ struct EpiAdd {
     float *acc;
     int64_t ld;
     bool first;
-    __device__ inline bool aligned() const { return true; }
     __device__ inline float *row(int64_t m) const { return acc + m * ld; }
     template <bool FULL>
     __device__ inline Nothing col(int64_t, int) const { return {}; }
@@ -359,20 +356,20 @@ struct EpiAdd {
 
 template <typename T>
 __global__ void __launch_bounds__(256) k_ce_dx(const float *acc, int64_t ld, int64_t rows, int64_t dim, const float *scale, float alpha, T *dx,
-                                               int64_t lddx, bool aligned)
+                                               int64_t lddx)
 {
     const int64_t per = (dim + 3) / 4;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * per; i += (int64_t)gridDim.x * 256) {
         const int64_t m = i / per, n = i % per * 4;
         const floatx4 v = *(const floatx4 *)(acc + m * ld + n) * (alpha * *scale);
-        store_four(dx + m * lddx + n, v, dim - n < 4 ? (int)(dim - n) : 4, aligned);
+        store_four(dx + m * lddx + n, v, dim - n < 4 ? (int)(dim - n) : 4);
     }
 }
 
 // narrow rows: dX = S w_i (sum of P W over all ranges)
 template <typename T>
 __global__ void __launch_bounds__(256) k_ce_narrow_dx(const float *grad, int splits, int64_t ld, int64_t rows, int64_t dim, const float *weight,
-                                                      const CeHead *head, float alpha, T *dx, int64_t lddx, bool aligned)
+                                                      const CeHead *head, float alpha, T *dx, int64_t lddx)
 {
     const int64_t per = (dim + 3) / 4;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * per; i += (int64_t)gridDim.x * 256) {
@@ -381,7 +378,7 @@ __global__ void __launch_bounds__(256) k_ce_narrow_dx(const float *grad, int spl
 #pragma unroll 8
         for (int s = 0; s < splits; ++s)
             v += *(const floatx4 *)(grad + ((int64_t)s * rows + m) * ld + n);
-        store_four(dx + m * lddx + n, v * (alpha * head->S * weight[m]), dim - n < 4 ? (int)(dim - n) : 4, aligned);
+        store_four(dx + m * lddx + n, v * (alpha * head->S * weight[m]), dim - n < 4 ? (int)(dim - n) : 4);
     }
 }
 
@@ -640,7 +637,7 @@ hipError_t run_narrow(const tig_softmax_ce &p, const CePlan &L, char *ws, const 
         CE_TRY(hipGetLastError());
         const int64_t blocks = (n * ((p.dim + 3) / 4) + 255) / 256;
         hipLaunchKernelGGL((k_ce_narrow_dx<T>), dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, s, a.grad, L.s_dx, a.ld_grad, n, p.dim,
-                           out.w, head, alpha, (T *)p.dx, p.lddx, four_aligned(p.dx, p.lddx, 2));
+                           out.w, head, alpha, (T *)p.dx, p.lddx);
         CE_TRY(hipGetLastError());
     }
     if (p.dw || p.dbias) {
@@ -651,7 +648,7 @@ hipError_t run_narrow(const tig_softmax_ce &p, const CePlan &L, char *ws, const 
         a.splits = L.s_dw, a.per = (L.row_tiles + L.s_dw - 1) / L.s_dw;
         a.grad = p.dw && L.s_dw > 1 ? (float *)(ws + L.join) : nullptr;
         a.sums = p.dbias ? (float *)(ws + L.sums) : nullptr;
-        const EpiStore<T> store = {(T *)p.dw, p.lddw, &head->S, alpha, four_aligned(p.dw, p.lddw, 2)};
+        const EpiStore<T> store = {(T *)p.dw, p.lddw, &head->S, alpha};
         if (p.dw && L.s_dw == 1)
             a.direct = store;
         const dim3 grid((unsigned)(L.own_cands * L.s_dw));
@@ -730,12 +727,11 @@ hipError_t run(const tig_softmax_ce &p, const CePlan &L, char *ws, hipStream_t s
     if constexpr (es == 2)
         if (L.kb)
             return L.biased ? run_narrow_of<T, true>(p, L, ws, x, ldx, w, ldw, out, s) : run_narrow_of<T, false>(p, L, ws, x, ldx, w, ldw, out, s);
-    const bool bias_ok = four_aligned(bias, 4, es);
     float2 *const part = (float2 *)(ws + L.part);
     const int64_t tiles = (V + L.stat.tile - 1) / L.stat.tile;
     for (int64_t r = 0; r < n; r += L.stat_rows) {
         const int64_t m = n - r < L.stat_rows ? n - r : L.stat_rows;
-        const EpiStats<T> epi = {bias, bias_ok, part, m};
+        const EpiStats<T> epi = {bias, part, m};
         CE_TRY((launch_gemm<T, kRow, kRow>(L.stat, x + r * ldx, ldx, w, ldw, m, V, d, nullptr, epi, s)));
         CeRowsOut<T> o = out;
         o.loss += r;
@@ -752,7 +748,7 @@ hipError_t run(const tig_softmax_ce &p, const CePlan &L, char *ws, hipStream_t s
     for (int64_t v0 = 0; v0 < V; v0 += L.piece) {
         const int64_t vc = V - v0 < L.piece ? V - v0 : L.piece;
         float *const sums = p.dbias ? (float *)(ws + L.sums) : nullptr;
-        const EpiP<T> epi = {bias ? bias + v0 : nullptr, bias && four_aligned(bias + v0, 4, es), out.rec, P, L.ldp, v0, sums};
+        const EpiP<T> epi = {bias ? bias + v0 : nullptr, out.rec, P, L.ldp, v0, sums};
         CE_TRY((launch_gemm<T, kRow, kRow>(L.logits, x, ldx, w + v0 * ldw, ldw, n, vc, d, nullptr, epi, s)));
         if (p.dbias)
             CE_TRY((launch_join_sums<T>(sums, L.ldp, (n + L.logits.tile - 1) / L.logits.tile, vc, (T *)p.dbias + v0, &head->S, alpha, s)));
@@ -761,20 +757,20 @@ hipError_t run(const tig_softmax_ce &p, const CePlan &L, char *ws, hipStream_t s
                 const EpiAdd add = {(float *)(ws + L.dxa), L.ld_acc, v0 == 0};
                 CE_TRY((launch_gemm<T, kRow, kCol>(L.dx, P, L.ldp, w + v0 * ldw, ldw, n, d, vc, ws + L.join, add, s)));
             } else {
-                const EpiStore<T> store = {(T *)p.dx, p.lddx, &head->S, alpha, four_aligned(p.dx, p.lddx, es)};
+                const EpiStore<T> store = {(T *)p.dx, p.lddx, &head->S, alpha};
                 CE_TRY((launch_gemm<T, kRow, kCol>(L.dx, P, L.ldp, w, ldw, n, d, vc, ws + L.join, store, s)));
             }
         }
         if (p.dw) {
             T *const dw = (T *)p.dw + v0 * p.lddw;
-            const EpiStore<T> store = {dw, p.lddw, &head->S, alpha, four_aligned(dw, p.lddw, es)};
+            const EpiStore<T> store = {dw, p.lddw, &head->S, alpha};
             CE_TRY((launch_gemm<T, kCol, kCol>(L.dw, P, L.ldp, out.x0, L.ld_x, vc, d, n, ws + L.join, store, s)));
         }
     }
     if (p.dx && L.acc) {
         const int64_t blocks = (n * ((d + 3) / 4) + 255) / 256;
         hipLaunchKernelGGL((k_ce_dx<T>), dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, s, (const float *)(ws + L.dxa), L.ld_acc, n, d,
-                           &head->S, alpha, (T *)p.dx, p.lddx, four_aligned(p.dx, p.lddx, es));
+                           &head->S, alpha, (T *)p.dx, p.lddx);
         CE_TRY(hipGetLastError());
     }
     return hipSuccess;
