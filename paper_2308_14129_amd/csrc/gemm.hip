@@ -56,14 +56,17 @@ __global__ void __launch_bounds__(256) k_pack(const E *src, int64_t ld_src, E *d
     const int64_t pieces = ld_dst / per, items = rows * pieces;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / pieces, c = i % pieces * per;
-        struct alignas(16) Piece {
+        struct __attribute__((packed, aligned(sizeof(E)))) Piece {  // (read wherever it starts)
             E v[per];
         } q;
         const E *p = src + r * ld_src + c;
+        if (c + per <= cols)
+            q = *(const Piece *)p;
+        else
 #pragma unroll
-        for (int e = 0; e < per; ++e)
-            q.v[e] = c + e < cols ? p[e] : (E)0;
-        *(Piece *)(dst + r * ld_dst + c) = q;
+            for (int e = 0; e < per; ++e)
+                q.v[e] = c + e < cols ? p[e] : (E)0;
+        *(Piece *)__builtin_assume_aligned(dst + r * ld_dst + c, 16) = q;
     }
 }
 

@@ -392,14 +392,17 @@ __global__ void __launch_bounds__(256) k_ce_copy(const T *src, int64_t ld_src, i
     const int64_t pieces = ld_dst / per;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all * pieces; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / pieces, c = i % pieces * per;
-        struct alignas(16) Piece {
+        struct __attribute__((packed, aligned(sizeof(T)))) Piece {  // (read wherever it starts)
             T v[per];
         } q;
         const T *p = src + r * ld_src + c;
+        if (c + per <= cols && r < rows)
+            q = *(const Piece *)p;
+        else
 #pragma unroll
-        for (int e = 0; e < per; ++e)
-            q.v[e] = c + e < cols && r < rows ? p[e] : c + e != cols ? (T)0.0f : r >= rows ? (T)behind : extra ? extra[r] : (T)fill;
-        *(Piece *)(dst + r * ld_dst + c) = q;
+            for (int e = 0; e < per; ++e)
+                q.v[e] = c + e < cols && r < rows ? p[e] : c + e != cols ? (T)0.0f : r >= rows ? (T)behind : extra ? extra[r] : (T)fill;
+        *(Piece *)__builtin_assume_aligned(dst + r * ld_dst + c, 16) = q;
     }
 }
 
