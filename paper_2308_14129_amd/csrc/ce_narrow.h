@@ -33,7 +33,11 @@ constexpr int kNarrowOwn = KB <= 2 ? 4 : 3;  // sixteens of own rows of a wavefr
 template <int KB>
 constexpr int kNarrowTile = 16 * kNarrowOwn<KB> * kNarrowWaves;
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
+// Logits go to powers of two in one instruction, l log2 e - (largest) log2 e, where the largest is at most this far from zero.  The
+// last product is rounded: beyond, where a candidate is masked by a large number, the error would reach the power itself (at -1e9 up to
+// 64), and its overflow would make a sum of masked candidates infinite.  There the difference is formed first.
+constexpr float kNarrowFar = 256.0f;
 
 template <typename T>
 struct NarrowArgs {
@@ -207,25 +211,36 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, 2) k_narrow_stats(NarrowArg
                     mma16(acc[i][j], f, own[i][kk], T());
             }
         }
+        float m[FM], most = 0.0f;
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-            float m = top[i];
+            m[i] = top[i];
 #pragma unroll
             for (int j = 0; j < FN; ++j)
 #pragma unroll
                 for (int v = 0; v < 4; ++v)
-                    m = fmaxf(m, acc[i][j][v]);
-            const float from = m == -INFINITY ? 0.0f : m * kLog2e;
-            float s = sum[i] * __builtin_amdgcn_exp2f((top[i] - m) * kLog2e);
-            s = m == -INFINITY ? sum[i] : s;
-#pragma unroll
-            for (int j = 0; j < FN; ++j)
-#pragma unroll
-                for (int v = 0; v < 4; ++v)
-                    s += __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], kLog2e, -from));
-            top[i] = m;
-            sum[i] = s;
+                    m[i] = fmaxf(m[i], acc[i][j][v]);
+            most = fmaxf(most, fabsf(m[i]));
         }
+        auto add = [&](auto some_far) {  // (each lane by its own rule: a row's bits do not depend on its neighbours)
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const float from = m[i] * kLog2e, far_from = m[i] == -INFINITY ? 0.0f : m[i];
+                const bool far = decltype(some_far)::value && fabsf(m[i]) > kNarrowFar;
+                float s = sum[i] * __builtin_amdgcn_exp2f((far ? top[i] - far_from : top[i] - m[i]) * kLog2e);
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        s += __builtin_amdgcn_exp2f(far ? (acc[i][j][v] - far_from) * kLog2e : fmaf(acc[i][j][v], kLog2e, -from));
+                sum[i] = s;
+                top[i] = m[i];
+            }
+        };
+        if (__ballot(most > kNarrowFar) == 0ull)
+            add(std::false_type());
+        else
+            add(std::true_type());
     }
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
