@@ -37,7 +37,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 // Logits go to powers of two in one instruction, l log2 e - (largest) log2 e, where the largest is at most this far from zero.  The
 // last product is rounded: beyond, where a candidate is masked by a large number, the error would reach the power itself (at -1e9 up to
 // 64), and its overflow would make a sum of masked candidates infinite.  There the difference is formed first.
-constexpr float kNarrowFar = 256.0f;
+// A gradient's powers, l log2 e - (lse log2 e), are the same: of rows whose lse log2 e is beyond kNarrowFar2 they are formed
+// as exp(l - top) / sum.
+constexpr float kNarrowFar = 256.0f, kNarrowFar2 = 370.0f;
+__device__ inline bool narrow_far(float lse2) { return fabsf(lse2) > kNarrowFar2 && lse2 != INFINITY; }  // (infinity: no probabilities)
 
 template <typename T>
 struct NarrowArgs {
@@ -48,8 +51,9 @@ struct NarrowArgs {
     int64_t per;              // tiles of a range
     const float *own_add;     // not BIASED: [n_own] added to an own row's logits (a candidate's bias), or NULL
     const float *stream_add;  // not BIASED: [whole tiles] added to a streamed row's logits, -infinity behind the last, or NULL
-    const float *lse2_own;    // statistics: unused; dX: [n_own] lse log2 e - log2 of P's scale
-    const float *lse2_stream; // dW: [whole tiles]
+    const float *lse2;        // rows of X, for the gradients [whole tiles]: lse log2 e - log2 of P's scale; infinity: no probabilities
+    const float *top, *per_sum;  // ... and what far rows take: largest logit (infinity), P's scale over the sum (0)
+    const int *some_far;         // is there a far row at all?
     const float *w_stream;    // dW, weighted rows: [whole tiles]
     const int32_t *labels;    // labels of the rows of X (-1: ignored): dX [n_own], dW [whole tiles] (-1 behind the last)
     float p_scale;            // P's scale (1, or 2^14)
@@ -277,7 +281,7 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, 2) k_narrow_grad(NarrowArgs
         st.load(a.stream + t * kNarrowStream * a.ld_stream, a.n_stream - t * kNarrowStream, lds);
         if constexpr (CANDS) {
             if (wave == 0)
-                load_with(a.lse2_stream, t * kNarrowStream, lds + S::kBytes);
+                load_with(a.lse2, t * kNarrowStream, lds + S::kBytes);
             if (wave == 1)
                 load_with((const float *)a.labels, t * kNarrowStream, lds + S::kBytes + 256);
             if (WEIGHTED && wave == 2)
@@ -289,117 +293,139 @@ __global__ void __launch_bounds__(64 * kNarrowWaves, 2) k_narrow_grad(NarrowArgs
     };
     intx4 own[FM][KB];
     load_own<T, KB, FM>(a, m0, own);
-    float mine[FM];  // dX: -lse log2 e of the row; dW: bias of the candidate, times log2 e
+    float mine[FM];  // dX: -lse log2 e of the row; dW: bias of the candidate
     float total[FM] = {};
     int mine_label[FM];
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
         const int64_t m = m0 + i * 16 + i16, mm = m < a.n_own ? m : 0;
         if constexpr (CANDS) {
-            mine[i] = a.own_add ? a.own_add[mm] * kLog2e : 0.0f;
+            mine[i] = !BIASED && a.own_add ? a.own_add[mm] : 0.0f;
         } else {
-            mine[i] = -a.lse2_own[mm];
+            mine[i] = -a.lse2[mm];
             mine_label[i] = m < a.n_own ? a.labels[mm] : -1;
         }
     }
     floatx4 out[FM][DT] = {};
     if (t0 < t1)
         request(t0, smem[0]);
-    for (int64_t t = t0; t < t1; ++t) {
-        const char *const now = smem[(t - t0) & 1];
-        sync_with_loads();
-        if (t + 1 < t1)
-            request(t + 1, smem[(t + 1 - t0) & 1]);
-        const int base = (int)(t * kNarrowStream) + 4 * g;
-        bool hot = false;  // a label of one of the rows is among the candidates of this wavefront and tile: seldom
-        if constexpr (CANDS) {
-            const int label = *(const int *)(now + S::kBytes + 256 + lane * 4);
-            hot = __ballot((uint32_t)(label - (int)m0) < (uint32_t)(16 * FM)) != 0ull;
-        } else {
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-                hot |= (uint32_t)(mine_label[i] - (int)(t * kNarrowStream)) < (uint32_t)kNarrowStream;
-            hot = __ballot(hot) != 0ull;
-        }
-#pragma unroll
-        for (int x = 0; x < kNarrowStream; x += 32) {
-            intx4 P[FM];
-            {
-                floatx4 acc[FM][2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    floatx4 from = {0.0f, 0.0f, 0.0f, 0.0f};
-                    if constexpr (!CANDS)
-                        from = start_of<BIASED>(a, t, x + 16 * j + 4 * g, now + S::kBytes);
-#pragma unroll
-                    for (int i = 0; i < FM; ++i)
-                        acc[i][j] = from;
-#pragma unroll
-                    for (int kk = 0; kk < KB; ++kk) {
-                        const intx4 f = S::frag(now, x + 16 * j, kk);
-#pragma unroll
-                        for (int i = 0; i < FM; ++i)
-                            mma16(acc[i][j], f, own[i][kk], T());
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    floatx4 lse = {0.0f, 0.0f, 0.0f, 0.0f}, w = lse;
-                    const char *const with = now + S::kBytes + (x + 16 * j + 4 * g) * 4;
-                    if constexpr (CANDS) {
-                        lse = *(const floatx4 *)with;
-                        if constexpr (WEIGHTED)
-                            w = *(const floatx4 *)(with + 512);
-                    }
-#pragma unroll
-                    for (int i = 0; i < FM; ++i)
-#pragma unroll
-                        for (int v = 0; v < 4; ++v)
-                            acc[i][j][v] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], kLog2e, CANDS ? (BIASED ? -lse[v] : mine[i] - lse[v]) : mine[i]));
-                    if constexpr (!CANDS)
-                        if (hot)
-#pragma unroll
-                            for (int v = 0; v < 4; ++v)
-#pragma unroll
-                                for (int i = 0; i < FM; ++i)
-                                    acc[i][j][v] -= mine_label[i] == base + x + 16 * j + v ? a.p_scale : 0.0f;
-                    if constexpr (CANDS) {
-                        if (hot) {
-                            const intx4 label = *(const intx4 *)(with + 256);
-#pragma unroll
-                            for (int v = 0; v < 4; ++v)
-#pragma unroll
-                                for (int i = 0; i < FM; ++i)
-                                    acc[i][j][v] -= label[v] == (int)(m0 + i * 16 + i16) ? a.p_scale : 0.0f;
-                        }
-#pragma unroll
-                        for (int i = 0; i < FM; ++i) {
-                            if constexpr (WEIGHTED)
-                                acc[i][j] *= w;
-                            if (!BIASED && a.sums)
-                                total[i] += (acc[i][j][0] + acc[i][j][1]) + (acc[i][j][2] + acc[i][j][3]);
-                        }
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < FM; ++i) {
-                    typedef T eight __attribute__((ext_vector_type(8)));
-                    eight q;
-#pragma unroll
-                    for (int v = 0; v < 4; ++v)
-                        q[v] = (T)acc[i][0][v], q[4 + v] = (T)acc[i][1][v];
-                    P[i] = __builtin_bit_cast(intx4, q);
-                }
-            }
-#pragma unroll
-            for (int c = 0; c < DT; ++c) {
-                const intx4 f = S::frag_t(now, x, c);
+    auto stream = [&](auto some_far) {
+        for (int64_t t = t0; t < t1; ++t) {
+            const char *const now = smem[(t - t0) & 1];
+            sync_with_loads();
+            if (t + 1 < t1)
+                request(t + 1, smem[(t + 1 - t0) & 1]);
+            const int base = (int)(t * kNarrowStream) + 4 * g;
+            bool hot = false;  // a label of one of the rows is among the candidates of this wavefront and tile: seldom
+            if constexpr (CANDS) {
+                const int label = *(const int *)(now + S::kBytes + 256 + lane * 4);
+                hot = __ballot((uint32_t)(label - (int)m0) < (uint32_t)(16 * FM)) != 0ull;
+            } else {
 #pragma unroll
                 for (int i = 0; i < FM; ++i)
-                    mma16(out[i][c], f, P[i], T());
+                    hot |= (uint32_t)(mine_label[i] - (int)(t * kNarrowStream)) < (uint32_t)kNarrowStream;
+                hot = __ballot(hot) != 0ull;
+            }
+#pragma unroll
+            for (int x = 0; x < kNarrowStream; x += 32) {
+                intx4 P[FM];
+                {
+                    floatx4 acc[FM][2];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        floatx4 from = {0.0f, 0.0f, 0.0f, 0.0f};
+                        if constexpr (!CANDS)
+                            from = start_of<BIASED>(a, t, x + 16 * j + 4 * g, now + S::kBytes);
+#pragma unroll
+                        for (int i = 0; i < FM; ++i)
+                            acc[i][j] = CANDS ? floatx4{mine[i], mine[i], mine[i], mine[i]} : from;
+#pragma unroll
+                        for (int kk = 0; kk < KB; ++kk) {
+                            const intx4 f = S::frag(now, x + 16 * j, kk);
+#pragma unroll
+                            for (int i = 0; i < FM; ++i)
+                                mma16(acc[i][j], f, own[i][kk], T());
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        floatx4 lse = {0.0f, 0.0f, 0.0f, 0.0f}, w = lse;
+                        const char *const with = now + S::kBytes + (x + 16 * j + 4 * g) * 4;
+                        if constexpr (CANDS) {
+                            lse = *(const floatx4 *)with;
+                            if constexpr (WEIGHTED)
+                                w = *(const floatx4 *)(with + 512);
+                        }
+                        if constexpr (!decltype(some_far)::value) {
+#pragma unroll
+                            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                                for (int v = 0; v < 4; ++v)
+                                    acc[i][j][v] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], kLog2e, CANDS ? -lse[v] : mine[i]));
+                        } else {  // (each row by its own rule: its bits do not depend on its neighbours)
+#pragma unroll
+                            for (int i = 0; i < FM; ++i) {
+                                const int m = (int)m0 + i * 16 + i16;
+#pragma unroll
+                                for (int v = 0; v < 4; ++v) {
+                                    const uint32_t r = CANDS ? base + x + 16 * j + v : m < a.n_own ? m : 0;
+                                    const float lse2 = CANDS ? lse[v] : -mine[i], l = acc[i][j][v];
+                                    acc[i][j][v] = narrow_far(lse2) ? __builtin_amdgcn_exp2f((l - a.top[r]) * kLog2e) * a.per_sum[r]
+                                                                    : __builtin_amdgcn_exp2f(fmaf(l, kLog2e, -lse2));
+                                }
+                                __builtin_amdgcn_sched_barrier(0);  // (seldom taken: no registers for several rows at once)
+                            }
+                        }
+                        if constexpr (!CANDS)
+                            if (hot)
+#pragma unroll
+                                for (int v = 0; v < 4; ++v)
+#pragma unroll
+                                    for (int i = 0; i < FM; ++i)
+                                        acc[i][j][v] -= mine_label[i] == base + x + 16 * j + v ? a.p_scale : 0.0f;
+                        if constexpr (CANDS) {
+                            if (hot) {
+                                const intx4 label = *(const intx4 *)(with + 256);
+#pragma unroll
+                                for (int v = 0; v < 4; ++v)
+#pragma unroll
+                                    for (int i = 0; i < FM; ++i)
+                                        acc[i][j][v] -= label[v] == (int)(m0 + i * 16 + i16) ? a.p_scale : 0.0f;
+                            }
+#pragma unroll
+                            for (int i = 0; i < FM; ++i) {
+                                if constexpr (WEIGHTED)
+                                    acc[i][j] *= w;
+                                if (!BIASED && a.sums)
+                                    total[i] += (acc[i][j][0] + acc[i][j][1]) + (acc[i][j][2] + acc[i][j][3]);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < FM; ++i) {
+                        typedef T eight __attribute__((ext_vector_type(8)));
+                        eight q;
+#pragma unroll
+                        for (int v = 0; v < 4; ++v)
+                            q[v] = (T)acc[i][0][v], q[4 + v] = (T)acc[i][1][v];
+                        P[i] = __builtin_bit_cast(intx4, q);
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < DT; ++c) {
+                    const intx4 f = S::frag_t(now, x, c);
+#pragma unroll
+                    for (int i = 0; i < FM; ++i)
+                        mma16(out[i][c], f, P[i], T());
+                }
             }
         }
-    }
+    };
+    // (two loops: the far rows' instructions in the usual one cost it its registers, 581 -> 717 us at 1000 x 400000 x 128 in bf16)
+    if (__builtin_amdgcn_readfirstlane(*a.some_far) == 0)
+        stream(std::false_type());
+    else
+        stream(std::true_type());
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
         const int64_t m = m0 + i * 16 + i16;

@@ -17,11 +17,14 @@ namespace tig {
 namespace {
 
 struct CeHead {
-    float S;  // largest |s_i|
+    float S;       // largest |s_i|
+    int some_far;  // narrow rows: is one of them far (ce_narrow.h)?
 };
-// what the epilogue of P needs of a row: lse (+infinity: no probabilities), w_i * P's scale, the label (-1: ignored)
-struct CeRow {
-    float lse, w;
+// What the epilogue of P needs of a row: the largest logit (+infinity: no probabilities), w_i * P's scale over the sum of exponentials and
+// by itself, the label (-1: ignored).  (Not the log-sum-exp: where a row's logits are far from zero its rounding would go into
+// every probability; all candidates masked by -1e9 had 1 each instead of 1 / V.)
+struct alignas(16) CeRow {
+    float top, per_sum, w;
     int32_t label;
 };
 
@@ -59,21 +62,23 @@ __global__ void __launch_bounds__(1024) k_ce_top(const int32_t *labels, const fl
     }
 }
 
-// number of rows that count; their mean loss, in double, always in the same order; S without weights
+// number of rows that count; their mean loss, in double, always in the same order; S without weights; lse2: narrow rows', or NULL
 __global__ void __launch_bounds__(1024) k_ce_mean(const float *loss, const int32_t *labels, int64_t rows, int64_t vocab, bool weighted, float scale,
-                                                  CeHead *head, float *mean)
+                                                  const float *lse2, CeHead *head, float *mean)
 {
     __shared__ double part[1024];
     __shared__ int count[1024];
     double total = 0.0;
     int n = 0;
+    bool far = false;
     for (int64_t i = threadIdx.x; i < rows; i += 1024) {
         total += (double)loss[i];
         n += labels[i] >= 0 && labels[i] < vocab;
+        far |= lse2 && narrow_far(lse2[i]);
     }
     part[threadIdx.x] = total;
     count[threadIdx.x] = n;
-    __syncthreads();
+    far = __syncthreads_or(far);
     for (int d = 512; d > 0; d >>= 1) {
         if ((int)threadIdx.x < d) {
             part[threadIdx.x] += part[threadIdx.x + d];
@@ -87,6 +92,7 @@ __global__ void __launch_bounds__(1024) k_ce_mean(const float *loss, const int32
             *mean = (float)(part[0] / (double)n);
         if (!weighted)
             head->S = fabsf(scale) / (float)n;
+        head->some_far = far;
     }
 }
 
@@ -161,7 +167,7 @@ template <typename T>
 struct CeRowsOut {
     float *loss, *lse;
     CeRow *rec;
-    float *lse2, *w;   // narrow
+    float *lse2, *top, *per_sum, *w;  // narrow
     int32_t *label;
     T *x0;
     int64_t ld_x0;
@@ -228,7 +234,7 @@ __global__ void __launch_bounds__(256) k_ce_rows(const float2 *part, int64_t til
         if (out.lse)
             out.lse[i] = lse;
         if (out.loss)
-            out.loss[i] = !counts ? 0.0f : (dot == -INFINITY ? INFINITY : lse - dot);
+            out.loss[i] = !counts ? 0.0f : (dot == -INFINITY ? INFINITY : (top - dot) + logf(sum));  // (far from zero, lse has lost what the sum says)
     }
     if (!out.rec && !out.lse2)
         return;
@@ -238,10 +244,12 @@ __global__ void __launch_bounds__(256) k_ce_rows(const float2 *part, int64_t til
     const bool none = wi == 0.0f || lse == -INFINITY;
     if (out.rec) {
         if (on)
-            out.rec[i] = CeRow{none ? INFINITY : lse, wi * kPScale<T>, wi != 0.0f ? label : -1};
+            out.rec[i] = CeRow{none ? INFINITY : top, none ? 0.0f : wi * kPScale<T> / sum, wi * kPScale<T>, wi != 0.0f ? label : -1};
     } else {
         constexpr float shift = sizeof(T) == 2 && kPScale<T> != 1.0f ? 14.0f : 0.0f;
-        out.lse2[i] = none ? INFINITY : lse * kLog2e - shift;
+        out.lse2[i] = none ? INFINITY : fmaf(top, kLog2e, log2f(sum)) - shift;
+        out.top[i] = none ? INFINITY : top;
+        out.per_sum[i] = none ? 0.0f : kPScale<T> / sum;
         out.w[i] = wi;
         out.label[i] = wi != 0.0f ? label : -1;
     }
@@ -278,7 +286,7 @@ struct EpiP {
         CeRow *const of_row = (CeRow *)(smem + WM * BN * sizeof(float));
         for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) {
             const int64_t m = (int64_t)at.tm * BM + r;
-            of_row[r] = m < at.M ? rec[m] : CeRow{INFINITY, 0.0f, -1};
+            of_row[r] = m < at.M ? rec[m] : CeRow{INFINITY, 0.0f, 0.0f, -1};
         }
         __syncthreads();
         floatx4 total[FN] = {};
@@ -289,7 +297,6 @@ struct EpiP {
                 const int64_t m = at.m0 + i * 16 + i16;
                 const bool on = FULL || m < at.M;
                 const CeRow r = of_row[at.wm * (BM / WM) + i * 16 + i16];
-                const float lse = r.lse;
                 T *const row = P + m * ldp + at.n0 + 4 * g;
                 const int64_t from = (int64_t)r.label - v0 - at.n0 - 4 * g;
                 const int hot = r.label >= 0 && from >= 0 && from < 16 * FN ? (int)from : -1;  // (of this lane's columns 16 j + e)
@@ -298,8 +305,8 @@ struct EpiP {
                     floatx4 p;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        p[e] = lse != INFINITY ? exp_of<T>(acc[i][j][e] + b[j][e] - lse) : 0.0f;
-                        p[e] = (p[e] - (hot == 16 * j + e ? 1.0f : 0.0f)) * r.w;
+                        p[e] = r.top != INFINITY ? exp_of<T>(acc[i][j][e] + b[j][e] - r.top) : 0.0f;
+                        p[e] = fmaf(p[e], r.per_sum, hot == 16 * j + e ? -r.w : 0.0f);
                     }
                     total[j] += p;
                     if (FULL || (on && at.n0 + j * 16 + 4 * g < end))
@@ -432,7 +439,7 @@ struct CePlan {
     int64_t own_rows, own_cands;  // tiles of own rows
     int s_stat, s_dx, s_dw;  // ranges of the streamed rows
     int64_t row_tiles, cand_tiles;  // whole tiles of 64
-    size_t bias32, lse2, weight;
+    size_t bias32, lse2, top, per_sum, weight;
     size_t head, loss, rec, label, part, px, pw, px0, P, dxa, join, sums;
     size_t bytes;
 };
@@ -487,6 +494,8 @@ CePlan ce_plan(const tig_softmax_ce &p)
         if (L.grad) {
             const size_t tab = (size_t)L.row_tiles * kNarrowStream * 4;
             L.lse2 = take(tab);
+            L.top = take(tab);
+            L.per_sum = take(tab);
             L.weight = take(tab);
             L.label = take(tab);
             L.px0 = take((size_t)L.row_tiles * kNarrowStream * L.ld_x * es);
@@ -583,9 +592,9 @@ hipError_t launch_rows(const tig_softmax_ce &p, int64_t r, int64_t m, const floa
     return hipGetLastError();
 }
 
-hipError_t launch_mean(const tig_softmax_ce &p, const float *loss, CeHead *head, hipStream_t s)
+hipError_t launch_mean(const tig_softmax_ce &p, const float *loss, const float *lse2, CeHead *head, hipStream_t s)
 {
-    hipLaunchKernelGGL(k_ce_mean, dim3(1), dim3(1024), 0, s, loss, p.labels, p.rows, p.vocab, p.row_scale != nullptr, p.scale, head, p.mean);
+    hipLaunchKernelGGL(k_ce_mean, dim3(1), dim3(1024), 0, s, loss, p.labels, p.rows, p.vocab, p.row_scale != nullptr, p.scale, lse2, head, p.mean);
     return hipGetLastError();
 }
 
@@ -625,15 +634,15 @@ hipError_t run_narrow(const tig_softmax_ce &p, const CePlan &L, char *ws, const 
     hipLaunchKernelGGL((k_narrow_stats<T, KB, BIASED>), dim3((unsigned)(L.own_rows * L.s_stat)), threads, 0, s, a);
     CE_TRY(hipGetLastError());
     CE_TRY(launch_rows(p, 0, n, a.part, L.s_stat, x, ldx, w, ldw, head, out, s));
-    CE_TRY(launch_mean(p, out.loss, head, s));
+    CE_TRY(launch_mean(p, out.loss, out.lse2, head, s));
     if (!L.grad)
         return hipSuccess;
     a.own = out.x0, a.ld_own = out.ld_x0;
     a.ld_grad = L.ld_acc;
     a.p_scale = kPScale<T>;
+    a.lse2 = out.lse2, a.top = out.top, a.per_sum = out.per_sum, a.some_far = &head->some_far;
     if (p.dx) {
         a.splits = L.s_dx, a.per = (L.cand_tiles + L.s_dx - 1) / L.s_dx;
-        a.lse2_own = out.lse2;
         a.labels = out.label;
         a.grad = (float *)(ws + L.dxa);
         hipLaunchKernelGGL((k_narrow_grad<T, KB, DT, BIASED, false, false>), dim3((unsigned)(L.own_rows * L.s_dx)), threads, 0, s, a);
@@ -647,7 +656,7 @@ hipError_t run_narrow(const tig_softmax_ce &p, const CePlan &L, char *ws, const 
         a.own = w, a.ld_own = ldw, a.n_own = V;
         a.stream = out.x0, a.ld_stream = out.ld_x0, a.n_stream = BIASED ? L.row_tiles * kNarrowStream : n;
         a.own_add = bias32, a.stream_add = nullptr;
-        a.lse2_stream = out.lse2, a.w_stream = out.w, a.labels = out.label;
+        a.w_stream = out.w, a.labels = out.label;
         a.splits = L.s_dw, a.per = (L.row_tiles + L.s_dw - 1) / L.s_dw;
         a.grad = p.dw && L.s_dw > 1 ? (float *)(ws + L.join) : nullptr;
         a.sums = p.dbias ? (float *)(ws + L.sums) : nullptr;
@@ -722,7 +731,7 @@ hipError_t run(const tig_softmax_ce &p, const CePlan &L, char *ws, hipStream_t s
     CeRowsOut<T> out = {};
     out.loss = loss, out.lse = p.lse;
     if (L.grad && L.kb)
-        out.lse2 = (float *)(ws + L.lse2), out.w = (float *)(ws + L.weight), out.label = (int32_t *)(ws + L.label);
+        out.lse2 = (float *)(ws + L.lse2), out.top = (float *)(ws + L.top), out.per_sum = (float *)(ws + L.per_sum), out.w = (float *)(ws + L.weight), out.label = (int32_t *)(ws + L.label);
     else if (L.grad)
         out.rec = (CeRow *)(ws + L.rec);
     if (L.grad && (L.kb || p.dw))
@@ -743,7 +752,7 @@ hipError_t run(const tig_softmax_ce &p, const CePlan &L, char *ws, hipStream_t s
         o.x0 = o.x0 ? o.x0 + r * o.ld_x0 : nullptr;
         CE_TRY(launch_rows(p, r, m, part, tiles, x, ldx, w, ldw, head, o, s));
     }
-    CE_TRY(launch_mean(p, loss, head, s));
+    CE_TRY(launch_mean(p, loss, nullptr, head, s));
     if (!L.grad)
         return hipSuccess;
     const float alpha = 1.0f / kPScale<T>;
