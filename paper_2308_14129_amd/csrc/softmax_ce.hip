@@ -470,7 +470,7 @@ CePlan ce_plan(const tig_softmax_ce &p)
     // 30000 x 128 140 and 114, x 100 118 and 127; 128 x 400000 x 128 277 and 268; 256 x 400000 x 64 227 and 330; 4000 x 250000 x 100 1134
     // and 3003), and without a gradient over many candidates (8 x 400000 x 64 41 and 49; 512 x 30000 x 64 21 and 18).
     if (es == 2 && d <= 128 && (n * V >= (int64_t)1 << 25 || (!L.grad && V >= 1 << 17))) {
-        L.kb = d <= 64 ? 2 : 4;  // (a column more does not change it, see run_narrow_of)
+        L.kb = d <= 64 ? 2 : 4;  // (a column more does not change it)
         const int64_t tile = L.kb == 2 ? kNarrowTile<2> : kNarrowTile<4>;
         L.own_rows = (n + tile - 1) / tile, L.own_cands = (V + tile - 1) / tile;
         L.row_tiles = (n + kNarrowStream - 1) / kNarrowStream, L.cand_tiles = (V + kNarrowStream - 1) / kNarrowStream;
@@ -681,14 +681,13 @@ template <typename T, bool BIASED>
 hipError_t run_narrow_of(const tig_softmax_ce &p, const CePlan &L, char *ws, const T *x, int64_t ldx, const T *w, int64_t ldw, const CeRowsOut<T> &out,
                          hipStream_t s)
 {
-    const int64_t columns = p.dim + (BIASED ? 1 : 0);
-    if (columns <= 32)
+    if (p.dim <= 32)
         return run_narrow<T, 2, 2, BIASED>(p, L, ws, x, ldx, w, ldw, out, s);
-    if (columns <= 64)
+    if (p.dim <= 64)
         return run_narrow<T, 2, 4, BIASED>(p, L, ws, x, ldx, w, ldw, out, s);
-    if (columns <= 96)
+    if (p.dim <= 96)
         return run_narrow<T, 4, 6, BIASED>(p, L, ws, x, ldx, w, ldw, out, s);
-    if (columns <= 112)
+    if (p.dim <= 112)
         return run_narrow<T, 4, 7, BIASED>(p, L, ws, x, ldx, w, ldw, out, s);
     return run_narrow<T, 4, 8, BIASED>(p, L, ws, x, ldx, w, ldw, out, s);
 }
