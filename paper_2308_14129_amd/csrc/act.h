@@ -7,13 +7,20 @@
 
 namespace tig {
 
-// The normal distribution's upper tail at |z|, times two, over exp(-z^2 / 2): erfc(x) exp(x^2) at x = |z| / sqrt 2 by formula 7.1.26
-// of Abramowitz and Stegun's handbook (a polynomial of degree five in 1 / (1 + 0.3275911 x), 1.5e-7 off at most; the library's
-// erff takes about three times as many instructions, both of its branches for nearly every wavefront).
+// The normal distribution's upper tail at |z| over exp(-z^2 / 2), that is erfc(x) exp(x^2) / 2 at x = |z| / sqrt 2: t Q(t) with
+// t = 1 / (1 + 0.35 |z|) and Q of degree eight, fitted to the least relative error over 0 <= |z| <= 15 (6e-8 with these coefficients; with the operations'
+// own roundings 5 units of 2^-24 by an emulation).  Relative, so that gelu's lower tail is right too, where it is this times z
+// exp(-z^2 / 2).  (The library's erff takes about twice as many instructions, both of its branches for nearly every wavefront, and
+// 1 + erf has no lower tail.)
 __device__ inline float tail_over_density(float z)
 {
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.0f));
-    return t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    constexpr float c[9] = {0.13962126f, 0.13986433f, 0.11981556f, 0.10557454f, -0.023263184f, 0.15939192f, -0.25590098f, 0.14406036f, -0.029163832f};
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.35f, fabsf(z), 1.0f));
+    float q = c[8];
+#pragma unroll
+    for (int i = 7; i >= 0; --i)
+        q = fmaf(t, q, c[i]);
+    return t * q;
 }
 
 template <int ACT>
@@ -22,7 +29,7 @@ __device__ inline float activate(float z)
     if constexpr (ACT == TIG_ACT_RELU) {
         return z < 0.0f ? 0.0f : z;  // (a NaN stays one)
     } else if constexpr (ACT == TIG_ACT_GELU) {
-        const float q = 0.5f * tail_over_density(z) * __builtin_amdgcn_exp2f(z * z * -0.72134752f);  // the tail beyond |z|
+        const float q = tail_over_density(z) * __builtin_amdgcn_exp2f(z * z * -0.72134752f);  // the tail beyond |z|
         const float zq = q > 0.0f ? z * q : q;  // (a tail of zero: also at infinity; a NaN stays one)
         return z > 0.0f ? z - zq : zq;
     } else if constexpr (ACT == TIG_ACT_SILU) {
@@ -38,7 +45,7 @@ __device__ inline float slope(float z)
     if constexpr (ACT == TIG_ACT_RELU) {
         return z > 0.0f ? 1.0f : 0.0f;
     } else if constexpr (ACT == TIG_ACT_GELU) {
-        const float e = __builtin_amdgcn_exp2f(z * z * -0.72134752f), q = 0.5f * tail_over_density(z) * e;
+        const float e = __builtin_amdgcn_exp2f(z * z * -0.72134752f), q = tail_over_density(z) * e;
         return fmaf(e > 0.0f ? z * e : e, 0.39894228f, z > 0.0f ? 1.0f - q : q);
     } else if constexpr (ACT == TIG_ACT_SILU) {
         const float g = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
