@@ -695,9 +695,10 @@ TIG_API int tig_train_head_get(tig_ctx *ctx, int32_t what, const tig_train_head 
 /* AdamW (tig_adamw_*) in place of SGD for a context's training steps: over the model's weights and an
  * attached head's parameters, with weight decay for matrices (not for biases and the time encoding),
  * clipped together to max_norm (0: not clipped).  tig_train_step's lr is its learning rate; lr = 0 makes
- * no step.  States start at zero; they and the step counter lie in `workspace` (device, 256-byte aligned,
- * the caller's until tig_destroy), which continues where it was if it is copied out and back.
- * Synchronous. */
+ * no step.  States start at zero; they and the step counter are all that lies in `workspace` (device,
+ * 256-byte aligned, the caller's until tig_destroy), and no addresses do: copied out and, after an attach
+ * with the same sizes and state_bits (of this context or another one, wherever its workspaces lie), back, it
+ * continues where it was.  Synchronous. */
 typedef struct tig_train_adamw {
     uint32_t struct_size;
     int32_t state_bits;  /* 32 or 8 */

@@ -381,6 +381,18 @@ AdamLayout adam_layout(const tig_adamw_tensor *t, int64_t n)
     return L;
 }
 
+}  // namespace
+
+size_t adamw_list_bytes(const int64_t *n, int n_tensors)
+{
+    tig_adamw_tensor t[kMaxTrainTensors] = {};
+    for (int i = 0; i < n_tensors; ++i)
+        t[i].n = n[i];
+    return adam_layout(t, n_tensors).bytes;
+}
+
+namespace {
+
 int check_adamw(const tig_adamw_config *c, const tig_adamw_tensor *t, int64_t n)
 {
     if (!c || c->struct_size != sizeof(tig_adamw_config))

@@ -1076,12 +1076,13 @@ int tig_train_head_get(tig_ctx *ctx, int32_t what, const tig_train_head *dst)
     return e == hipSuccess ? TIG_OK : fail(ctx, TIG_EHIP, "tig_train_head_get", e);
 }
 
-// The optimiser's workspace: the step counter, its list of tensors, the states (all but the list start at zero).
+// The optimiser's workspace: the step counter and the states, nothing that depends on where anything lies (its list of chunks
+// does, see train_opt_list).
 struct AdamPlace {
     tig_adamw_tensor t[kMaxTrainTensors];
     tig_adamw_config cfg;
     int n;
-    size_t list, list_bytes, states, bytes;
+    size_t list_bytes, bytes;
 };
 
 static int adam_place(const tig_ctx *ctx, const tig_train_adamw &c, char *ws, AdamPlace *out)
@@ -1107,11 +1108,8 @@ static int adam_place(const tig_ctx *ctx, const tig_train_adamw &c, char *ws, Ad
             A.t[i].v_scale = (float *)take((n + 255) / 256 * 4);
         }
     }
-    A.states = off;
-    const int rc = tig_adamw_workspace_bytes(&A.cfg, A.t, A.n, &A.list_bytes);
-    A.list = off;
-    A.bytes = off + align_up(A.list_bytes);
-    return rc;
+    A.bytes = off;
+    return tig_adamw_workspace_bytes(&A.cfg, A.t, A.n, &A.list_bytes);
 }
 
 static int check_train_adamw(const tig_ctx *ctx, const tig_train_adamw *c)
@@ -1147,13 +1145,15 @@ int tig_train_adamw_attach(tig_ctx *ctx, const tig_train_adamw *cfg, void *works
         return fail(ctx, rc, "tig_train_adamw_attach: state_bits is 8 or 32, beta1 and beta2 in [0, 1), eps positive");
     if (workspace_bytes < A.bytes)
         return fail(ctx, TIG_ENOSPACE, "tig_train_adamw_attach: workspace too small");
-    hipError_t e = launch_fill_zero(workspace, A.states, ctx->stream);
+    hipError_t e = launch_fill_zero(workspace, A.bytes, ctx->stream);
     if (e == hipSuccess)
         e = hipStreamSynchronize(ctx->stream);
     if (e != hipSuccess)
         return fail(ctx, TIG_EHIP, "tig_train_adamw_attach", e);
     tig_adamw *opt = nullptr;
-    if ((rc = tig_adamw_create(&A.cfg, A.t, A.n, (char *)workspace + A.list, A.list_bytes, ctx->stream, &opt)) != TIG_OK)
+    const TrainHead &head = ctx->train_extra.head;
+    void *const list = head.ws ? train_head_opt_list(ctx->d, head) : train_opt_list(ctx->d, ctx->train_ws);
+    if ((rc = tig_adamw_create(&A.cfg, A.t, A.n, list, A.list_bytes, ctx->stream, &opt)) != TIG_OK)
         return fail(ctx, rc, "tig_train_adamw_attach: the optimiser could not be made");
     tig_adamw_destroy(ctx->train_extra.opt);
     ctx->train_extra.opt = opt;

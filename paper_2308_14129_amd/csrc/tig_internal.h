@@ -345,6 +345,12 @@ hipError_t launch_train_head(const Dims &d, const StepArgs &a, const TrainHead &
 hipError_t launch_train_head_sgd(const Dims &d, const TrainHead &h, float lr, int *launches, hipStream_t s);
 // the optimiser's list of tensors: the masters and an attached head's parameters (their number is returned)
 constexpr int kMaxTrainTensors = 26;
+// (its list of chunks holds addresses: it lies in the head's workspace, or in the training workspace without one, and not beside the
+// states, which a caller may save and bring back elsewhere)
+size_t adamw_list_bytes(const int64_t *n, int n_tensors);
+void train_counts(const Dims &d, int64_t (&n)[22]);
+void *train_opt_list(const Dims &d, void *train_ws);
+void *train_head_opt_list(const Dims &d, const TrainHead &h);
 int train_head_tensors(const Dims &d, const TrainHead &h, float weight_decay, tig_adamw_tensor *out);
 int train_tensors(const Dims &d, void *train_ws, const TrainHead &h, float weight_decay, tig_adamw_tensor *out);
 // after training steps with lr != 0 the prepared weights follow the masters through fold_weights (products in double, two

@@ -678,6 +678,7 @@ struct TrainLayout {
     float *phi0, *dphi0;  // [T] Phi(0) = cos(time_b), and its gradient
     float *part;        // partial blocks of the contractions whose rows are split over workgroups
     void *pack_scratch;
+    void *opt_list;     // an optimiser's list of chunks (without a ranking head)
     size_t zero_lo, zero_hi;  // byte range that train_attach clears
     size_t bytes;
 };
@@ -692,6 +693,15 @@ static int wgrad_tiles(const Dims &d, int mi)
            3 * wgrad_job_tiles(E, E, mi) + wgrad_job_tiles(3 * M, d.Dmsg, mi) + wgrad_job_tiles(3 * M, M, mi);
 }
 
+// elements of the fields of tig_weights
+void train_counts(const Dims &d, int64_t (&n)[22])
+{
+    const int64_t M = d.M, T = d.T, E = d.E, da = d.da, dkv = d.dkv, D = d.Dmsg;
+    const int64_t counts[22] = {T, T, 3 * M * D, 3 * M, 3 * M * M, 3 * M, da * da, da, da * dkv, da, da * dkv, da,
+                                da * da, da, E * (da + M), E, E * E, E, E * 2 * E, E, E, 1};
+    memcpy(n, counts, sizeof(n));
+}
+
 static TrainLayout train_layout(const Dims &d, void *base)
 {
     TrainLayout L;
@@ -703,13 +713,13 @@ static TrainLayout train_layout(const Dims &d, void *base)
         off += align_up(4 * (n_floats ? n_floats : 1));
         return q;
     };
-    const size_t M = d.M, T = d.T, E = d.E, da = d.da, dkv = d.dkv, D = d.Dmsg, N1 = d.N1;
+    const size_t M = d.M, T = d.T, E = d.E, da = d.da, D = d.Dmsg, N1 = d.N1;
     const size_t B = d.max_batch, R = 3 * B, U = 2 * B;
-    const size_t counts[22] = {T, T, 3 * M * D, 3 * M, 3 * M * M, 3 * M, da * da, da, da * dkv, da, da * dkv, da,
-                               da * da, da, E * (da + M), E, E * E, E, E * 2 * E, E, E, 1};
+    int64_t counts[22];
+    train_counts(d, counts);
     size_t n = 0;
-    for (size_t c : counts)
-        n += c;
+    for (int64_t c : counts)
+        n += (size_t)c;
     L.n_params = n;
     L.P = take(n);
     L.zero_lo = off;
@@ -733,7 +743,7 @@ static TrainLayout train_layout(const Dims &d, void *base)
     for (int i = 0; i < 22; ++i) {
         *wf[i] = L.P ? L.P + o : nullptr;
         *gf[i] = L.G ? L.G + o : nullptr;
-        o += counts[i];
+        o += (size_t)counts[i];
     }
     L.w.struct_size = L.g.struct_size = sizeof(tig_weights);
     t.S = take(R * (M + 1));
@@ -763,9 +773,13 @@ static TrainLayout train_layout(const Dims &d, void *base)
     L.part = R >= kSplitRows && wgrad_tiles(d, 4) <= kSplitTiles ? take((size_t)wgrad_tiles(d, 4) * kXcds * kPartFloats) : nullptr;
     L.pack_scratch = base ? p + off : nullptr;
     off += align_up(pack_scratch_bytes(d));
+    L.opt_list = base ? p + off : nullptr;
+    off += align_up(adamw_list_bytes(counts, 22));
     L.bytes = off;
     return L;
 }
+
+void *train_opt_list(const Dims &d, void *train_ws) { return train_layout(d, train_ws).opt_list; }
 
 size_t train_workspace_bytes(const Dims &d) { return train_layout(d, nullptr).bytes; }
 

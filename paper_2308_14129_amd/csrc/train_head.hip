@@ -20,6 +20,7 @@ struct HeadLayout {
     int32_t *labels;         // [B]
     double *demb;            // [2B x E]
     float *mean;
+    void *opt_list;          // an optimiser's list of chunks
     void *ops;               // the operators' workspace
     size_t ops_bytes, bytes;
 };
@@ -81,6 +82,12 @@ HeadLayout head_layout(const Dims &d, const TrainHead &h)
     L.labels = (int32_t *)take(4 * B);
     L.demb = (double *)take(8 * 2 * B * E);
     L.mean = (float *)take(4);
+    int64_t n[kMaxTrainTensors], model[22];
+    train_counts(d, model);
+    memcpy(n, model, sizeof(model));
+    for (int i = 0; i < 4; ++i)
+        n[22 + i] = (int64_t)len[i];
+    L.opt_list = take(adamw_list_bytes(n, kMaxTrainTensors));
     L.ops_bytes = h.ops_bytes;
     L.ops = take(L.ops_bytes);
     L.bytes = off;
@@ -142,6 +149,7 @@ size_t train_head_ops_bytes(const Dims &d, const TrainHead &h)
 }
 
 size_t train_head_bytes(const Dims &d, const TrainHead &h) { return head_layout(d, h).bytes; }
+void *train_head_opt_list(const Dims &d, const TrainHead &h) { return head_layout(d, h).opt_list; }
 
 hipError_t train_head_attach(const Dims &d, const TrainHead &h, const tig_train_head &from, hipStream_t s)
 {
