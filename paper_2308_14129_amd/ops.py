@@ -254,7 +254,10 @@ class AdamW:
     """AdamW over lists of tensors of any shape (contiguous).  States are the caller's: m and v in float32, or for 8 bits
     in torch.float8_e4m3fn with float32 scales, one for every 256 elements, m_scales and v_scales (v then holds sqrt(v)).
     step: int64 device tensor [1], the steps made so far.  masters: float32 tensors that are stepped in place of
-    16-bit params, which receive their rounded copies (None, or None for a tensor, where there is none)."""
+    16-bit params, which receive their rounded copies (None, or None for a tensor, where there is none).
+
+    The object steps the memory that it was given, and keeps it alive: a tensor put into one of the lists afterwards is not
+    seen (gradients are copied into the given ones).  A captured step needs the object for as long as it is replayed."""
 
     def __init__(self, params, grads, m, v, step, masters=None, m_scales=None, v_scales=None, betas=(0.9, 0.999), eps=1e-8,
                  weight_decay=0.0):
@@ -293,7 +296,8 @@ class AdamW:
             if eight:
                 e.m_scale = flat(m_scales[i], -(-n // 256), torch.float32, "m_scales", i)
                 e.v_scale = flat(v_scales[i], -(-n // 256), torch.float32, "v_scales", i)
-        self.kept = (params, grads, m, v, step, masters, m_scales, v_scales)  # the handle holds their addresses
+        # The handle has these tensors' addresses: aliases of them, whatever becomes of the caller's lists and tensors.
+        self.kept = tuple(t.detach() for l in (params, *lists.values(), (step,)) for t in l if t is not None)
         self.norm = torch.zeros(1, dtype=torch.float32, device=self.device)
         cfg = tig_adamw_config(ctypes.sizeof(tig_adamw_config), 8 if eight else 32, betas[0], betas[1], eps, step.data_ptr())
         self.lib = _lib()
