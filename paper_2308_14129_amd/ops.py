@@ -303,6 +303,7 @@ class AdamW:
         self.lib = _lib()
         h, need = c_void_p(None), c_size_t(0)
         with _On(self.device) as stream:
+            self.stream = stream  # (the one that ws and norm belong to)
             _check(self.lib.tig_adamw_workspace_bytes(byref(cfg), table, len(params), byref(need)))
             self.ws = _workspace(need.value, self.device)
             _check(self.lib.tig_adamw_create(byref(cfg), table, len(params), self.ws.data_ptr(), need.value, stream, byref(h)))
@@ -311,6 +312,10 @@ class AdamW:
     def step(self, lr, grad_scale=1.0, max_norm=0.0):
         """Enqueues one step; returns the device tensor [1] that receives the gradients' norm (with max_norm > 0)."""
         with _On(self.device) as stream:
+            if stream != self.stream:  # (the allocator has to know, should the object go before the step has run)
+                other = torch.cuda.current_stream(self.device)
+                self.ws.record_stream(other)
+                self.norm.record_stream(other)
             _check(self.lib.tig_adamw_step(self.handle, lr, grad_scale, max_norm, self.norm.data_ptr(), stream))
         return self.norm
 

@@ -99,3 +99,31 @@ def test_memory_of_8bit_states_is_held_too(host):
     del opt
     gc.collect()
     assert len(gone) == 6
+
+
+class Recorder:
+    def __init__(self):
+        self.on = []
+
+    def data_ptr(self):
+        return 256
+
+    def record_stream(self, stream):
+        self.on.append(stream)
+
+
+def test_a_step_on_another_stream_is_noted_on_the_handles_own_memory(host, monkeypatch):
+    """The allocator must not give the list of chunks away while a step on another stream than its own may still read it."""
+    now = [7]
+    monkeypatch.setattr(OnHost, "__enter__", lambda self: now[0])
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: ("stream", now[0]))
+    t = [torch.zeros(10) for _ in range(4)]
+    opt = ops.AdamW([t[0]], [t[1]], [t[2]], [t[3]], torch.zeros(1, dtype=torch.int64))
+    opt.ws, opt.norm = Recorder(), Recorder()
+    opt.step(1e-3)
+    assert opt.ws.on == [] and opt.norm.on == []
+    now[0] = 8
+    opt.step(1e-3)
+    now[0] = 7
+    opt.step(1e-3)
+    assert opt.ws.on == [("stream", 8)] and opt.norm.on == [("stream", 8)]
