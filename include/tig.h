@@ -554,7 +554,8 @@ typedef enum tig_activation {
  *             residual's gradient is dy itself.)  dz is rounded to `dtype` for the two products;
  *             dbias is summed before that rounding.  z is not read for TIG_ACT_NONE.
  * All tensors have the type `dtype`.  rows may be 0 (forward: nothing; backward: dw and dbias are
- * zero).  y may be residual; no other output may overlap another tensor of the call.
+ * zero).  y may be residual; any other output that overlaps another tensor of the call is refused
+ * (TIG_EINVAL; column ranges of one buffer do not overlap).
  * Rows of x, z, dy and so on lie ld* elements apart. */
 typedef struct tig_linear {
     uint32_t struct_size;
@@ -594,7 +595,8 @@ TIG_API int tig_linear_backward(const tig_linear *p, void *workspace, size_t wor
  * (w_v must be finite).  A row whose label is masked has loss +infinity and, where nothing is left,
  * lse = -infinity; its gradient is P with the probabilities that are left.
  * P is rounded to the type `dtype` for the two products (fp16: after scaling by 2^14, so that small
- * probabilities stay), relative to the largest |s_i|. */
+ * probabilities stay), relative to the largest |s_i|.
+ * An output that overlaps another tensor of the call is refused (TIG_EINVAL). */
 typedef struct tig_softmax_ce {
     uint32_t struct_size;
     int32_t dtype;           /* tig_dtype of x, w, bias, dx, dw, dbias */

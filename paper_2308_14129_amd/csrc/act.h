@@ -1,6 +1,7 @@
 // Activations of the dense layer and their slopes, in fp32.
 #pragma once
 
+#include <numeric>
 #include <type_traits>
 
 #include "kernels_common.h"
@@ -76,6 +77,42 @@ inline auto with_dtype(int dtype, F &&f)
     }
 }
 inline int dtype_bytes(int dtype) { return dtype == TIG_F32 ? 4 : 2; }
+// A matrix of a call (p NULL: none), strides in elements.
+struct Placed {
+    const void *p;
+    int64_t rows, cols, ld;
+    int elem;
+};
+// No element of one is an element of the other: their ranges do not meet, or their columns do not (two column ranges, or every other
+// row, of one buffer): then their rows keep apart within what both strides are multiples of.
+inline bool apart(const Placed &a, const Placed &b)
+{
+    if (!a.p || !b.p || a.rows == 0 || b.rows == 0)
+        return true;
+    const int64_t wa = a.cols * a.elem, wb = b.cols * b.elem, sa = a.rows > 1 ? a.ld * a.elem : 0, sb = b.rows > 1 ? b.ld * b.elem : 0;
+    const uintptr_t la = (uintptr_t)a.p, lb = (uintptr_t)b.p;
+    if (la + (uintptr_t)((a.rows - 1) * sa + wa) <= lb || lb + (uintptr_t)((b.rows - 1) * sb + wb) <= la)
+        return true;
+    const int64_t g = std::gcd(sa, sb);
+    if (g == 0)
+        return false;
+    const int64_t d = (((int64_t)(lb - la)) % g + g) % g;
+    return d >= wa && d + wb <= g;
+}
+// ... of each of `out` and everything in `in` and the rest of `out`
+template <int I, int O>
+inline bool all_apart(const Placed (&in)[I], const Placed (&out)[O])
+{
+    for (int o = 0; o < O; ++o) {
+        for (int i = 0; i < I; ++i)
+            if (!apart(out[o], in[i]))
+                return false;
+        for (int k = 0; k < o; ++k)
+            if (!apart(out[o], out[k]))
+                return false;
+    }
+    return true;
+}
 inline bool dtype_ok(int dtype) { return dtype == TIG_F32 || dtype == TIG_BF16 || dtype == TIG_F16; }
 
 }  // namespace tig

@@ -352,6 +352,26 @@ int check_linear(const tig_linear *p, bool backward)
     return TIG_OK;
 }
 
+// y may be residual itself; all else that is written keeps apart from what the call reads and writes.
+int check_linear_apart(const tig_linear &p, bool backward)
+{
+    const int es = dtype_bytes(p.dtype);
+    const int64_t r = p.rows, k = p.in_dim, n = p.out_dim;
+    bool ok;
+    if (!backward) {
+        const bool in_place = p.y == p.residual && (p.ldy == p.ldr || r == 1);
+        const Placed in[] = {{p.x, r, k, p.ldx, es}, {p.w, n, k, p.ldw, es}, {p.bias, 1, n, n, es}, {in_place ? nullptr : p.residual, r, n, p.ldr, es}};
+        const Placed out[] = {{p.y, r, n, p.ldy, es}, {p.z, r, n, p.ldz, es}};
+        ok = all_apart(in, out);
+    } else {
+        const Placed in[] = {{p.dy, r, n, p.lddy, es}, {p.dw ? p.x : nullptr, r, k, p.ldx, es}, {p.dx ? p.w : nullptr, n, k, p.ldw, es},
+                             {p.activation != TIG_ACT_NONE ? p.z : nullptr, r, n, p.ldz, es}};
+        const Placed out[] = {{p.dx, r, k, p.lddx, es}, {p.dw, n, k, p.lddw, es}, {p.dbias, 1, n, n, es}};
+        ok = all_apart(in, out);
+    }
+    return ok ? TIG_OK : fail_text(TIG_EINVAL, "tig_linear: an output overlaps another tensor of the call");
+}
+
 int check_workspace(const void *workspace, size_t have, size_t need)
 {
     if (need == 0)
@@ -466,7 +486,7 @@ int tig_linear_forward(const tig_linear *p, void *workspace, size_t workspace_by
     if (rc != TIG_OK || p->rows == 0)
         return rc;
     const LinearPlan L = linear_plan(*p, false);
-    if ((rc = check_workspace(workspace, workspace_bytes, L.bytes)) != TIG_OK)
+    if ((rc = check_workspace(workspace, workspace_bytes, L.bytes)) != TIG_OK || (rc = check_linear_apart(*p, false)) != TIG_OK)
         return rc;
     const hipError_t e = with_dtype(p->dtype, [&](auto t) { return forward<decltype(t)>(*p, L, (char *)workspace, (hipStream_t)hip_stream); });
     return e == hipSuccess ? TIG_OK : fail_global("tig_linear_forward", e);
@@ -478,7 +498,7 @@ int tig_linear_backward(const tig_linear *p, void *workspace, size_t workspace_b
     if (rc != TIG_OK)
         return rc;
     const LinearPlan L = linear_plan(*p, true);
-    if ((rc = check_workspace(workspace, workspace_bytes, L.bytes)) != TIG_OK)
+    if ((rc = check_workspace(workspace, workspace_bytes, L.bytes)) != TIG_OK || (rc = check_linear_apart(*p, true)) != TIG_OK)
         return rc;
     const hipError_t e = with_dtype(p->dtype, [&](auto t) { return backward<decltype(t)>(*p, L, (char *)workspace, (hipStream_t)hip_stream); });
     return e == hipSuccess ? TIG_OK : fail_global("tig_linear_backward", e);

@@ -573,6 +573,17 @@ int check_ce(const tig_softmax_ce *p)
     return TIG_OK;
 }
 
+int check_ce_apart(const tig_softmax_ce &p)
+{
+    const int es = dtype_bytes(p.dtype);
+    const int64_t n = p.rows, V = p.vocab, d = p.dim;
+    const Placed in[] = {{p.x, n, d, p.ldx, es}, {p.w, V, d, p.ldw, es}, {p.bias, 1, V, V, es}, {n > 0 ? p.labels : nullptr, 1, n, n, 4},
+                         {n > 0 ? p.row_scale : nullptr, 1, n, n, 4}};
+    const Placed out[] = {{p.dx, n, d, p.lddx, es}, {p.dw, V, d, p.lddw, es}, {p.dbias, 1, V, V, es}, {n > 0 ? p.loss : nullptr, 1, n, n, 4},
+                          {n > 0 ? p.lse : nullptr, 1, n, n, 4}, {p.mean, 1, 1, 1, 4}};
+    return all_apart(in, out) ? TIG_OK : fail_text(TIG_EINVAL, "tig_softmax_ce: an output overlaps another tensor of the call");
+}
+
 #define CE_TRY(call)                 \
     do {                             \
         const hipError_t e_ = call;  \
@@ -806,7 +817,7 @@ int tig_softmax_ce_workspace_bytes(const tig_softmax_ce *p, size_t *bytes)
 
 int tig_softmax_ce_run(const tig_softmax_ce *p, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
-    const int rc = check_ce(p);
+    int rc = check_ce(p);
     if (rc != TIG_OK)
         return rc;
     if (!workspace || ((uintptr_t)workspace & 255))
@@ -814,6 +825,8 @@ int tig_softmax_ce_run(const tig_softmax_ce *p, void *workspace, size_t workspac
     const CePlan L = ce_plan(*p);
     if (workspace_bytes < L.bytes)
         return fail_text(TIG_ENOSPACE, "tig_softmax_ce_run: workspace too small");
+    if ((rc = check_ce_apart(*p)) != TIG_OK)
+        return rc;
     const hipError_t e = with_dtype(p->dtype, [&](auto t) { return run<decltype(t)>(*p, L, (char *)workspace, (hipStream_t)hip_stream); });
     return e == hipSuccess ? TIG_OK : fail_global("tig_softmax_ce_run", e);
 }

@@ -149,7 +149,8 @@ _FEW_ROWS = 16  # TIG_LINEAR_FEW_ROWS
 
 def linear(x, w, bias=None, residual=None, activation="none", keep=False, out=None):
     """act(x w^T + bias) + residual for x [rows x in], w [out x in]; fp32, bf16 or fp16, sums in fp32.  With keep=True
-    returns (y, z), z = x w^T + bias as linear_backward wants it.  out: where y goes (residual itself is fine)."""
+    returns (y, z), z = x w^T + bias as linear_backward wants it.  out: where y goes; residual itself is fine, anything else that overlaps
+    x, w, bias or residual is refused."""
     if x.dim() != 2 or w.dim() != 2:
         _refuse("x and w are matrices")
     rows, k = x.shape

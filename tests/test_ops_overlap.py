@@ -1,0 +1,81 @@
+"""Outputs on top of what the same call reads or writes are refused, before anything reaches a GPU (no GPU needed)."""
+from ctypes import byref, c_size_t
+
+import pytest
+
+from paper_2308_14129_amd import ops, tig
+from tests.test_ops_refusals import HOST, lib, make_ce, make_linear  # noqa: F401
+
+MB = 1 << 20
+
+
+def apart(p, names):
+    for i, n in enumerate(names):
+        setattr(p, n, HOST + (i + 1) * MB)
+    return p
+
+
+def forward(**kw):
+    p = apart(make_linear(), ("x", "w", "y", "z", "bias", "residual"))
+    p.ldr = 32
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return p
+
+
+def backward(**kw):
+    p = apart(make_linear(), ("x", "w", "y", "z", "dy", "dx", "dw", "dbias"))
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return p
+
+
+X, W, Y, Z, BIAS, RES = (HOST + k * MB for k in range(1, 7))
+
+# 100 rows of 64 -> 32 in bf16: rows of 128 and 64 bytes
+FORWARD = [
+    dict(y=X), dict(y=X + 100 * 128 - 2), dict(y=X - 99 * 64), dict(y=W), dict(y=W + 32 * 128 - 2), dict(y=BIAS), dict(y=BIAS + 62), dict(y=RES + 2),
+    dict(y=RES, ldy=40), dict(y=RES + 64), dict(z=X), dict(z=W), dict(z=BIAS), dict(z=RES), dict(z=Y), dict(z=Y + 2), dict(y=X + 64, ldy=48), dict(y=X + 62, ldy=64),
+    dict(y=X, ldy=64, ldx=64), dict(y=X + 128, ldy=128, ldx=128, in_dim=64, out_dim=65, ldw=65, ldz=65, ldr=65),
+    dict(rows=3, y=X), dict(rows=1, y=X + 126), dict(rows=16, z=X + 2000),
+]
+# in place of y and z: DY is the fifth
+DY, DX, DW, DB = (HOST + k * MB for k in range(5, 9))
+BACKWARD = [
+    dict(dx=DY), dict(dx=X), dict(dx=W), dict(dx=Z), dict(dw=DY), dict(dw=X), dict(dw=W + 2), dict(dw=Z), dict(dbias=DY + 64), dict(dbias=X), dict(dbias=W),
+    dict(dbias=Z), dict(dx=DW), dict(dx=DB), dict(dw=DB), dict(dw=DX + 100 * 128 - 2),
+]
+
+
+@pytest.mark.parametrize("bad", FORWARD, ids=str)
+def test_linear_forward_refuses_outputs_on_top_of_others(lib, bad):  # noqa: F811
+    p, need = forward(**bad), c_size_t(0)
+    assert lib.tig_linear_workspace_bytes(byref(p), 0, byref(need)) == tig.TIG_OK
+    assert lib.tig_linear_forward(byref(p), HOST, need.value, None) == tig.TIG_EINVAL
+    assert b"overlap" in lib.tig_last_error(None)
+
+
+@pytest.mark.parametrize("bad", BACKWARD, ids=str)
+def test_linear_backward_refuses_outputs_on_top_of_others(lib, bad):  # noqa: F811
+    p, need = backward(**bad), c_size_t(0)
+    assert lib.tig_linear_workspace_bytes(byref(p), 1, byref(need)) == tig.TIG_OK
+    assert lib.tig_linear_backward(byref(p), HOST, need.value, None) == tig.TIG_EINVAL
+    assert b"overlap" in lib.tig_last_error(None)
+
+
+CE = ("x", "w", "bias", "labels", "row_scale", "loss", "lse", "mean", "dx", "dw", "dbias")
+
+
+@pytest.mark.parametrize("out", CE[5:])
+@pytest.mark.parametrize("on", CE)
+def test_softmax_ce_refuses_outputs_on_top_of_others(lib, out, on):  # noqa: F811
+    if out == on:
+        return
+    for shift in (0, 4):
+        p, need = apart(make_ce(), CE), c_size_t(0)
+        if shift and (out == "mean" or on == "mean"):
+            continue
+        setattr(p, out, getattr(p, on) + shift)
+        assert lib.tig_softmax_ce_workspace_bytes(byref(p), byref(need)) == tig.TIG_OK
+        assert lib.tig_softmax_ce_run(byref(p), HOST, need.value, None) == tig.TIG_EINVAL
+        assert b"overlap" in lib.tig_last_error(None)
