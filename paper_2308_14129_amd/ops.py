@@ -1,6 +1,7 @@
 """Thin ctypes binding over the operators of a trained head in include/tig.h (tig_linear_*, tig_softmax_ce_*,
 tig_adamw_*).  Argument marshalling only; PyTorch supplies device memory and the stream handle.  Every call enqueues on
-the current stream of its tensors' device and does not synchronise."""
+the current stream of its tensors' device and does not synchronise.  No graph is recorded: linear() and softmax_ce() refuse
+tensors that require a gradient where torch.is_grad_enabled(); linear_backward() and softmax_ce() give the gradients."""
 from __future__ import annotations
 
 import ctypes
@@ -89,6 +90,12 @@ def _dtype_code(dtype):
     return code
 
 
+def _no_graph(name):
+    if torch.is_grad_enabled():
+        _refuse(f"{name} requires a gradient, but the operators record no graph: call them under torch.no_grad(), with linear_backward "
+                "and softmax_ce's gradients for the way back")
+
+
 def _matrix(t, rows, cols, dtype, device, name):
     """Address and row stride of a [rows x cols] tensor whose columns are adjacent."""
     if t is None:
@@ -100,6 +107,8 @@ def _matrix(t, rows, cols, dtype, device, name):
         ld = cols
     if (step != 1 and cols > 1) or ld < cols:
         _refuse(f"{name}: columns have to be adjacent and rows may not overlap")
+    if t.requires_grad:
+        _no_graph(name)
     return t.data_ptr(), ld
 
 
@@ -108,6 +117,8 @@ def _vector(t, n, dtype, device, name):
         return 0
     if t.shape != (n,) or t.dtype is not dtype or t.device != device or (n > 1 and t.stride(0) != 1):
         _refuse(f"{name} is not a contiguous [{n}] tensor of {dtype} on {device}")
+    if t.requires_grad:
+        _no_graph(name)
     return t.data_ptr()
 
 
@@ -161,14 +172,13 @@ def linear(x, w, bias=None, residual=None, activation="none", keep=False, out=No
     pw, ldw = _matrix(w, n, k, dtype, dev, "w")
     pb = _vector(bias, n, dtype, dev, "bias")
     pr, ldr = _matrix(residual, rows, n, dtype, dev, "residual")
+    y = out
+    py, ldy = _matrix(y, rows, n, dtype, dev, "out")
     lib = _lib()
     with _On(dev) as stream:
-        if out is None:
+        if y is None:
             y = torch.empty((rows, n), dtype=dtype, device=dev)
             py, ldy = y.data_ptr(), n
-        else:
-            y = out
-            py, ldy = _matrix(y, rows, n, dtype, dev, "out")
         z, pz = None, 0
         if keep:
             z = torch.empty((rows, n), dtype=dtype, device=dev)
