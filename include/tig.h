@@ -656,8 +656,9 @@ typedef struct tig_adamw tig_adamw;
 TIG_API int tig_adamw_workspace_bytes(const tig_adamw_config *cfg, const tig_adamw_tensor *tensors, int64_t n_tensors, size_t *bytes);
 /* Lays the list of tensors out in `workspace` (device, 256-byte aligned, the caller's until
  * tig_adamw_destroy).  Synchronous.  The tensors and their states stay the caller's, at the addresses
- * given here; v (sqrt(v) in 8 bits) must not be negative.  Arrays that a step writes may not overlap: a tensor
- * given twice is refused (TIG_EINVAL).  n_tensors <= 2^20, fewer than 2^24 chunks of 4096 elements. */
+ * given here; v (sqrt(v) in 8 bits) must not be negative.  What a step writes (parameters,
+ * states, the counter, the workspace) may overlap nothing else of the call: a tensor given twice is refused
+ * (TIG_EINVAL).  Gradients may overlap each other.  n_tensors <= 2^20, fewer than 2^24 chunks of 4096 elements. */
 TIG_API int tig_adamw_create(const tig_adamw_config *cfg, const tig_adamw_tensor *tensors, int64_t n_tensors, void *workspace,
                              size_t workspace_bytes, void *hip_stream, tig_adamw **out);
 /* Enqueues one step with learning rate lr >= 0, grad_scale finite, max_norm >= 0.  norm_out: device [1] or

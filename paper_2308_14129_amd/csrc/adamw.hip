@@ -426,24 +426,29 @@ int check_adamw(const tig_adamw_config *c, const tig_adamw_tensor *t, int64_t n)
     return TIG_OK;
 }
 
-// Two workgroups must not step the same element: no array that the step writes overlaps another.
-int check_apart(const tig_adamw_config &c, const tig_adamw_tensor *t, int64_t n)
+// Two workgroups must not step the same element, nor one step what another still reads: no array that the step writes overlaps
+// another one.  (Gradients may overlap each other.)
+int check_apart(const tig_adamw_config &c, const tig_adamw_tensor *t, int64_t n, const void *workspace, size_t workspace_bytes)
 {
     struct Range {
         uintptr_t from, to;
+        bool grad;
     };
-    Range *const r = new (std::nothrow) Range[(size_t)(6 * n + 1)];
+    Range *const r = new (std::nothrow) Range[(size_t)(7 * n + 2)];
     if (!r)
         return fail_text(TIG_ENOMEM, "tig_adamw_create: out of host memory");
     int64_t k = 0;
-    auto add = [&](const void *p, int64_t bytes) {
+    auto add = [&](const void *p, int64_t bytes, bool grad = false) {
         if (p && bytes > 0)
-            r[k++] = Range{(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes};
+            r[k++] = Range{(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, grad};
     };
+    add(c.step, 8);
+    add(workspace, (int64_t)workspace_bytes);
     for (int64_t i = 0; i < n; ++i) {
         const tig_adamw_tensor &q = t[i];
         const int64_t ss = c.state_bits == 32 ? 4 : 1, scales = (q.n + kStateBlock - 1) / kStateBlock * 4;
         add(q.param, q.n * dtype_bytes(q.dtype));
+        add(q.grad, q.n * dtype_bytes(q.dtype), true);
         add(q.master, q.n * 4);
         add(q.m, q.n * ss);
         add(q.v, q.n * ss);
@@ -452,10 +457,14 @@ int check_apart(const tig_adamw_config &c, const tig_adamw_tensor *t, int64_t n)
     }
     std::sort(r, r + k, [](const Range &a, const Range &b) { return a.from < b.from; });
     bool apart = true;
-    for (int64_t i = 1; i < k; ++i)
-        apart = apart && r[i - 1].to <= r[i].from;
+    uintptr_t read = 0, written = 0;  // ends of the ranges before
+    for (int64_t i = 0; i < k; ++i) {
+        apart = apart && written <= r[i].from && (r[i].grad || read <= r[i].from);
+        uintptr_t &end = r[i].grad ? read : written;
+        end = r[i].to > end ? r[i].to : end;
+    }
     delete[] r;
-    return apart ? TIG_OK : fail_text(TIG_EINVAL, "tig_adamw_create: two arrays that a step writes overlap (a tensor given twice?)");
+    return apart ? TIG_OK : fail_text(TIG_EINVAL, "tig_adamw_create: an array that a step writes overlaps another one (a tensor given twice?)");
 }
 
 }  // namespace
@@ -494,7 +503,7 @@ int tig_adamw_create(const tig_adamw_config *cfg, const tig_adamw_tensor *tensor
     const AdamLayout L = adam_layout(tensors, n_tensors);
     if (workspace_bytes < L.bytes)
         return fail_text(TIG_ENOSPACE, "tig_adamw_create: workspace too small");
-    if ((rc = check_apart(*cfg, tensors, n_tensors)) != TIG_OK)
+    if ((rc = check_apart(*cfg, tensors, n_tensors, workspace, L.bytes)) != TIG_OK)
         return rc;
     tig_adamw *const opt = new (std::nothrow) tig_adamw;
     char *const host = new (std::nothrow) char[L.part ? L.part : 1];  // the list of chunks

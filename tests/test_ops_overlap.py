@@ -1,5 +1,6 @@
 """Outputs on top of what the same call reads or writes are refused, before anything reaches a GPU (no GPU needed)."""
-from ctypes import byref, c_size_t
+import ctypes
+from ctypes import byref, c_size_t, c_void_p
 
 import pytest
 
@@ -79,3 +80,40 @@ def test_softmax_ce_refuses_outputs_on_top_of_others(lib, out, on):  # noqa: F81
         assert lib.tig_softmax_ce_workspace_bytes(byref(p), byref(need)) == tig.TIG_OK
         assert lib.tig_softmax_ce_run(byref(p), HOST, need.value, None) == tig.TIG_EINVAL
         assert b"overlap" in lib.tig_last_error(None)
+
+
+def make_two(eight=False):
+    """Two tensors of 1000 fp32 elements, nothing of which overlaps; the counter and the workspace lie apart as well."""
+    c = ops.tig_adamw_config(ctypes.sizeof(ops.tig_adamw_config), 8 if eight else 32, 0.9, 0.999, 1e-8, HOST)
+    t = (ops.tig_adamw_tensor * 2)()
+    at = MB
+    for q in t:
+        q.n = 1000
+        for name in ("param", "grad", "m", "v", "master") + (("m_scale", "v_scale") if eight else ()):
+            setattr(q, name, HOST + at)
+            at += 4000
+    return c, t
+
+
+WORKSPACE = HOST + 64 * MB
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("which", ["param", "m", "v", "master", "other's param", "other's m", "counter", "workspace", "param in workspace", "counter in m"])
+def test_adamw_refuses_gradients_counter_or_workspace_on_what_it_writes(lib, which, eight):  # noqa: F811
+    c, t = make_two(eight)
+    if which == "counter":
+        t[1].grad = HOST - 3996
+    elif which == "workspace":
+        t[0].grad = WORKSPACE - 3996
+    elif which == "param in workspace":
+        t[0].param = WORKSPACE
+    elif which == "counter in m":
+        c.step = t[1].m + 992
+    else:
+        on = t[1] if "other" in which else t[0]
+        t[0].grad = getattr(on, which.split()[-1]) + (996 if eight and which.split()[-1] in "mv" else 3996)
+    need, h = c_size_t(0), c_void_p(None)
+    assert lib.tig_adamw_workspace_bytes(byref(c), t, 2, byref(need)) == tig.TIG_OK
+    assert lib.tig_adamw_create(byref(c), t, 2, WORKSPACE, need.value, None, byref(h)) == tig.TIG_EINVAL and not h.value
+    assert b"overlap" in lib.tig_last_error(None)
