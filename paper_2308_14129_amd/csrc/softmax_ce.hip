@@ -815,6 +815,12 @@ int tig_softmax_ce_workspace_bytes(const tig_softmax_ce *p, size_t *bytes)
     return TIG_OK;
 }
 
+// For tests: does the call go the way of ce_narrow.h (1), or by tiles (0)?  -1: it is refused.
+extern "C" __attribute__((visibility("default"))) int tig_debug_softmax_ce_narrow(const tig_softmax_ce *p)
+{
+    return check_ce(p) != TIG_OK ? -1 : ce_plan(*p).kb != 0;
+}
+
 int tig_softmax_ce_run(const tig_softmax_ce *p, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     int rc = check_ce(p);
