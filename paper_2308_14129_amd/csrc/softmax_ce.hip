@@ -68,6 +68,7 @@ __global__ void __launch_bounds__(1024) k_ce_mean(const float *loss, const int32
 {
     __shared__ double part[1024];
     __shared__ int count[1024];
+    __shared__ bool some_far[16];
     double total = 0.0;
     int n = 0;
     bool far = false;
@@ -78,7 +79,10 @@ __global__ void __launch_bounds__(1024) k_ce_mean(const float *loss, const int32
     }
     part[threadIdx.x] = total;
     count[threadIdx.x] = n;
-    far = __syncthreads_or(far);
+    far = __ballot(far) != 0ull;
+    if (lane_id() == 0)
+        some_far[wave_id()] = far;
+    __syncthreads();
     for (int d = 512; d > 0; d >>= 1) {
         if ((int)threadIdx.x < d) {
             part[threadIdx.x] += part[threadIdx.x + d];
@@ -92,6 +96,8 @@ __global__ void __launch_bounds__(1024) k_ce_mean(const float *loss, const int32
             *mean = (float)(part[0] / (double)n);
         if (!weighted)
             head->S = fabsf(scale) / (float)n;
+        for (int w = 1; lse2 && w < 16; ++w)
+            far |= some_far[w];
         head->some_far = far;
     }
 }
