@@ -234,6 +234,11 @@ class TigContext:
             raise TigError(rc, self.lib.tig_strerror(rc).decode() + " / " +
                            self.lib.tig_last_error(self.handle).decode())
 
+    def _workspace(self, n: int):
+        """Device memory for the context's stream: the allocator's memory of another stream may still be in use there."""
+        with self._torch.cuda.stream(self.stream):
+            return self._torch.empty(n, dtype=self._torch.uint8, device=self.device)
+
     def alloc_outputs(self, count: int, with_neg: bool = True, inspect: bool = False) -> StepOutputs:
         torch = self._torch
         Q = (3 if with_neg else 2) * count
@@ -291,7 +296,7 @@ class TigContext:
         n = c_size_t(0)
         self._check(self.lib.tig_modules_workspace_bytes(ctypes.byref(self.cfg), ctypes.byref(m), self.num_nodes,
                                                          ctypes.byref(n)))
-        self.mods_ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+        self.mods_ws = self._workspace(n.value)
         w = tig_weights(ctypes.sizeof(tig_weights), 0, *[_addr(weights.get(k)) for k in WEIGHT_NAMES])
         self._check(self.lib.tig_modules_attach(self.handle, ctypes.byref(m), ctypes.byref(w), self.mods_ws.data_ptr(),
                                                 n.value))
@@ -302,7 +307,7 @@ class TigContext:
         torch = self._torch
         n = c_size_t(0)
         self._check(self.lib.tig_train_workspace_bytes(ctypes.byref(self.cfg), ctypes.byref(n)))
-        self.train_ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+        self.train_ws = self._workspace(n.value)
         w = tig_weights(ctypes.sizeof(tig_weights), 0, *[_addr(weights[k]) for k in WEIGHT_NAMES])
         self._check(self.lib.tig_train_attach(self.handle, ctypes.byref(w), self.train_ws.data_ptr(), n.value))
         self._shapes = {k: np.asarray(weights[k]).shape for k in WEIGHT_NAMES}
@@ -339,7 +344,7 @@ class TigContext:
                            *[_addr(head[k]) for k in HEAD_NAMES])
         n = c_size_t(0)
         self._check(self.lib.tig_train_head_workspace_bytes(ctypes.byref(self.cfg), ctypes.byref(h), ctypes.byref(n)))
-        ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+        ws = self._workspace(n.value)
         self._check(self.lib.tig_train_head_attach(self.handle, ctypes.byref(h), ws.data_ptr(), n.value))
         self.head_ws, self._head_shapes = ws, want
 
@@ -358,7 +363,7 @@ class TigContext:
         c = tig_train_adamw(ctypes.sizeof(tig_train_adamw), state_bits, betas[0], betas[1], eps, weight_decay, max_norm)
         n = c_size_t(0)
         self._check(self.lib.tig_train_adamw_workspace_bytes(self.handle, ctypes.byref(c), ctypes.byref(n)))
-        ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+        ws = self._workspace(n.value)
         self._check(self.lib.tig_train_adamw_attach(self.handle, ctypes.byref(c), ws.data_ptr(), n.value))
         self.adamw_ws = ws
 

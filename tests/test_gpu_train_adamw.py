@@ -5,7 +5,7 @@ import torch
 
 import tig_synth as S
 from oracle import train_oracle as T
-from paper_2308_14129_amd import ops
+from paper_2308_14129_amd import ops, tig
 from tests.test_gpu_parity import Bundle, make_ctx
 from tests.test_gpu_train_head import make_head
 
@@ -115,3 +115,36 @@ def test_optimiser_continues_in_another_context_from_a_copy_of_its_workspace(c1,
     assert int(a.adamw_ws[:8].view(torch.int64)) == 4
     a.close()
     b.close()
+
+
+def test_workspaces_are_the_contexts_streams(c1):
+    """A context on a stream of its own, while the current stream still writes into memory that it has given back."""
+    w, g = c1.w, c1.g
+    cfg = tig.make_config(w.mem_dim, w.time_dim, w.feat_dim, w.emb_dim, w.num_neighbors, w.num_heads, COUNT, "fp32", "deferred")
+    side = torch.cuda.Stream()
+    ctx = tig.TigContext(cfg, g.num_nodes, g.src, g.dst, g.ts, g.edge_feat, c1.W, device="cuda:0", stream=side)
+    head = make_head(w.emb_dim, 300)
+
+    def attach():
+        ctx.train_attach(c1.W)
+        ctx.train_head_attach(head, 10)
+        ctx.train_adamw_attach()
+        return ctx.train_ws.numel(), ctx.head_ws.numel(), ctx.adamw_ws.numel()
+
+    sizes = attach()
+    torch.cuda.synchronize()
+    held = [torch.empty(n, dtype=torch.uint8, device="cuda:0") for n in sizes]
+    torch.cuda._sleep(400_000_000)
+    for t in held:
+        t.fill_(255)
+    at = {t.data_ptr() for t in held}
+    del held, t
+    attach()
+    assert not at & {ctx.train_ws.data_ptr(), ctx.head_ws.data_ptr(), ctx.adamw_ws.data_ptr()}
+    torch.cuda.synchronize()
+    for k, v in ctx.train_get("weights").items():
+        assert np.array_equal(v.reshape(-1), c1.W[k].reshape(-1)), k
+    for k, v in ctx.train_head_get("weights").items():
+        assert np.array_equal(v, head[k]), k
+    assert not ctx.adamw_ws.any()
+    ctx.close()
