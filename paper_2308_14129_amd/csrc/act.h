@@ -34,7 +34,8 @@ __device__ inline float activate(float z)
         const float zq = q > 0.0f ? z * q : q;  // (a tail of zero: also at infinity; a NaN stays one)
         return z > 0.0f ? z - zq : zq;
     } else if constexpr (ACT == TIG_ACT_SILU) {
-        return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
+        const float g = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
+        return g > 0.0f ? z * g : g;  // (zero at -infinity too; a NaN stays one)
     } else {
         return z;
     }
@@ -50,7 +51,8 @@ __device__ inline float slope(float z)
         return fmaf(e > 0.0f ? z * e : e, 0.39894228f, z > 0.0f ? 1.0f - q : q);
     } else if constexpr (ACT == TIG_ACT_SILU) {
         const float g = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
-        return g * (1.0f + z * (1.0f - g));
+        const float h = 1.0f - g, zh = h > 0.0f ? z * h : h;  // (one at infinity, zero at -infinity; a NaN stays one)
+        return g > 0.0f ? g * (1.0f + zh) : g;
     } else {
         return 1.0f;
     }

@@ -32,3 +32,22 @@ def test_gelu_relative_to_its_value(rows, dtype):
         more = Z * torch.exp(-Z * Z / 2) / math.sqrt(2 * math.pi)
         S = phi + more
         close(slope, S, h * S.abs() + (1 + h) * rel * (phi + more.abs()) + tiny(t) + 2.0**-126, "slope")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
+@pytest.mark.parametrize("rows", [4, 64])
+def test_activations_at_infinity(rows, act, dtype):
+    """Their limits, and those of their slopes; a NaN stays one (relu's slope has none)."""
+    t = TYPES[dtype]
+    inf = math.inf
+    x = torch.tensor([inf, -inf, 3.0e38 if dtype != "fp16" else 65504.0, -3.0e38 if dtype != "fp16" else -65504.0] * (rows // 4), device=DEV).to(t).view(-1, 1)
+    one = torch.ones(1, 1, dtype=t, device=DEV)
+    y, z = ops.linear(x, one, activation=act, keep=True)
+    slope = ops.linear_backward(torch.ones_like(x), x, one, z, act, dw=False, dbias=False)[0]
+    low = act == "none"
+    assert torch.equal(y, torch.where(x > 0, x, x if low else torch.zeros_like(x)))
+    assert torch.equal(slope, torch.where(x > 0, torch.ones_like(x), torch.full_like(x, float(low))))
+    y, z = ops.linear(torch.full_like(x, math.nan), one, activation=act, keep=True)
+    slope = ops.linear_backward(torch.ones_like(x), x, one, z, act, dw=False, dbias=False)[0]
+    assert torch.isnan(y).all() and (torch.isnan(slope).all() or act in ("none", "relu"))
