@@ -551,8 +551,9 @@ typedef enum tig_activation {
 /* Dense layer:  z = x W^T + b,  y = act(z) + residual.
  *   forward   reads x, w, bias, residual; writes y and, if wanted, z (kept for the backward pass)
  *   backward  dz = dy * act'(z);  dx = dz W,  dw = dz^T x,  dbias = sum over rows of dz.  (The
- *             residual's gradient is dy itself.)  dz is rounded to `dtype` for the two products;
- *             dbias is summed before that rounding.  z is not read for TIG_ACT_NONE.
+ *             residual's gradient is dy itself.)  The kept z is rounded to `dtype`, and act' taken
+ *             there; dz is rounded to `dtype` for the two products; dbias is summed before that
+ *             rounding.  z is not read for TIG_ACT_NONE.
  * All tensors have the type `dtype`.  rows may be 0 (forward: nothing; backward: dw and dbias are
  * zero).  y may be residual; any other output that overlaps another tensor of the call is refused
  * (TIG_EINVAL; column ranges of one buffer do not overlap).
@@ -591,11 +592,13 @@ TIG_API int tig_linear_backward(const tig_linear *p, void *workspace, size_t wor
  *   gradients of sum_i s_i loss_i:  P_iv = s_i (exp(l_iv - lse_i) - [v == label_i]),
  *       dx = P W,  dw = P^T x,  dbias = sum_i P
  *   mean = sum of the loss_i that count / their number (0 if none counts)
- * A candidate is masked by bias_v = -infinity: it gets no probability and its gradient is zero
- * (w_v must be finite).  A row whose label is masked has loss +infinity and, where nothing is left,
- * lse = -infinity; its gradient is P with the probabilities that are left.
+ * A candidate is masked by bias_v = -infinity (w_v must be finite): it gets no probability, and its
+ * gradient is zero but for the -s_i of rows that are labelled with it.  Such a row has loss +infinity
+ * and, where nothing is left, lse = -infinity; its gradient is that of the probabilities that are left,
+ * less the label's.  A large finite bias masks as well (down to the type's lowest value); where it masks
+ * every candidate, probabilities and losses are those of the logits as fp32 holds them beside it.
  * P is rounded to the type `dtype` for the two products (fp16: after scaling by 2^14, so that small
- * probabilities stay), relative to the largest |s_i|.
+ * probabilities stay), relative to the largest |s_i|; dbias is summed before that rounding.
  * An output that overlaps another tensor of the call is refused (TIG_EINVAL). */
 typedef struct tig_softmax_ce {
     uint32_t struct_size;

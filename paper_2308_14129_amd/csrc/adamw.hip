@@ -3,8 +3,8 @@
 // The tensors are cut into chunks, one workgroup each, listed once in the workspace: one launch whatever their
 // number.  Bound by memory: every element's parameter and states are read and written once, its gradient read once, and once
 // more where the norm is wanted.
-// 184 M elements with bf16 parameters and gradients, fp32 masters and states: the step 941 us (28 bytes an element, 5.5 TB/s), the
-// norm 107 (3.4 TB/s); 219 M with 8-bit states 670 (16 bytes, 5.3 TB/s).
+// 184 M elements with bf16 parameters and gradients, fp32 masters and states: the step 948 us (28 bytes an element, 5.4 TB/s), the
+// norm 107 (3.4 TB/s); 219 M with 8-bit states 678 (16 bytes, 5.2 TB/s).
 //   k_adamw_norm    sums of squares, in double (only with clipping)
 //   k_adamw_begin   the step's numbers: clip coefficient, bias corrections, counter; few elements' update does that itself
 //   k_adamw_update  the step

@@ -1,5 +1,5 @@
-// Softmax cross entropy over a vocabulary where rows are narrow (16-bit types, at most 32 KB columns): the logits of a tile and
-// what becomes of them stay in registers.  Included by softmax_ce.hip.
+// Softmax cross entropy over a vocabulary where rows are narrow (16-bit types, at most 128 columns): the logits of a tile and
+// what becomes of them stay in registers.  Included by softmax_ce.hip.  KB: blocks of 32 columns that a row has.
 //
 // With 100 columns a logit costs 200 operations of the matrix units, less than writing and reading it: P in memory (see
 // softmax_ce.hip) is what bounds wide rows' way there.  Here a wavefront keeps FM x 16 rows of its OWN matrix as matrix operands and
@@ -13,7 +13,7 @@
 // operations instead of 8), and P is never in memory.
 //
 // Bound by the exponentials and the products, of which a wavefront does one after the other and two wavefronts share a SIMD: 4000 x
-// 250000 x 100 in bf16 276 us statistics (725 TFLOP/s of 200 operations a logit), 393 dX, 461 dW (1018 and 868 of 400).
+// 250000 x 100 in bf16 258 us statistics (775 TFLOP/s of 200 operations a logit), 371 dX, 449 dW (1078 and 891 of 400).
 //
 // P is rounded to 16 bits for the second product: it is at most 1 in magnitude, relative to the largest weight.
 //

@@ -3,8 +3,10 @@
 //   up to 16 rows     k_linear_rows: the matrix is read once, straight into matrix-core operands
 //   more rows         the tile product of gemm.h, bias, activation and residual in its epilogue
 //   backward          k_linear_dz: dz = dy act'(z), and its column sums before it is rounded; then two tile products
-// 8192 rows, 4096 -> 16384 in bf16 with gelu and residual: forward 1116 us, k_linear_dz 166 (4.8 TB/s), products 942 and 941.
-// dz is rounded to the layer's type: it is a matrix operand of both products, and at most half a unit of dy's own last place off.
+// 8192 rows, 4096 -> 16384 in bf16 with gelu and residual: forward 1131 us, k_linear_dz 171 (4.7 TB/s), products 968 and 965.
+// z is rounded to the layer's type when it is kept, and the slope is that of the rounded z.  dz is rounded too, to half a step of its
+// own: it is a matrix operand of both products.  (With normal inputs dz's rounding adds as much error to the
+// gradients as their own has, 1.7e-3 in bf16, and z's a third of that: 2.4e-3 together.)
 #include <type_traits>
 
 #include "act.h"
@@ -78,9 +80,10 @@ constexpr int kRowsWaves = 8;
 // Up to sixteen rows: a workgroup takes sixteen columns, its wavefronts take turns along k, and both operands come straight from
 // memory: a lane's sixteen bytes of a row are its part of an operand.  Bound by the matrix' bytes and, where it is small, by a
 // launch and one chain of loads: one row, 1024 -> 4096 in bf16 3.4 us in a graph (2.5 TB/s), 16 rows, 4096 -> 16384 31 us (4.3 TB/s).
-// The limit: 13 rows of 2000 -> 1336 in fp16 take 5.4 us here and 6.3 as tiles, 16 of 4096 -> 4096 in bf16 9.8 and 9.9, 48 of them
-// (as three operands of sixteen) 18.1 and 12.1, 64 rows of 4096 -> 16384 73 and 33.  Four wavefronts instead of eight: the
-// same within 2 % from 2048 to 32768 columns.
+// The limit: 13 rows of 2000 -> 1333 in fp16 take 5.2 us here and 6.6 as tiles, 16 of 4096 -> 4096 in bf16 9.9 and 10.1, 48 of them
+// (as three operands of sixteen) 18.1 and 12.1, 64 rows of 4096 -> 16384 73 and 33; in fp32 one row of 1024 -> 4096 4.8 and 9.3,
+// 13 of 2000 -> 1333 6.9 and 11.1, 16 of 4096 -> 4096 17.4 and 23.6, 16 of 4096 -> 16384 62 and 80.  Four wavefronts instead of
+// eight: the same within 2 % from 2048 to 32768 columns.
 template <typename T, class Epi>
 __global__ void __launch_bounds__(64 * kRowsWaves) k_linear_rows(const T *x, int64_t ldx, const T *w, int64_t ldw, int64_t M, int64_t N, int64_t K, Epi epi)
 {

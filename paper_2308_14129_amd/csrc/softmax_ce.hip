@@ -2,10 +2,10 @@
 //
 //   statistics   a tile product X W^T (gemm.h) whose epilogue leaves, for every row and tile of candidates, the largest logit and
 //                the sum of exp(l - largest); k_ce_rows joins them to the row's log-sum-exp and takes the label's logit
-//   gradient     for one piece of the vocabulary after the other: the logits once more, P = w_i (exp(l - lse) - [label]) in their
+//   gradient     for one piece of the vocabulary after the other: the logits once more, P = w_i (softmax - [label]) in their
 //                epilogue, and two tile products, dX += P W and dW = P^T X.  A piece of P stays within the last-level cache.
 // s_i = S w_i with S the largest |s_i|: P holds values of at most 1, the products are scaled by S afterwards.
-// 8192 x 128000 x 2048 in bf16: statistics 3.36 ms (1.28 PFLOP/s), P 3.95 (1.09), dX 3.44 (1.25), dW 3.68 (1.17).  P is a matrix operand
+// 8192 x 128000 x 2048 in bf16: statistics 3.51 ms (1.23 PFLOP/s), P 4.04 (1.06), dX 3.71 (1.16), dW 3.81 (1.13).  P is a matrix operand
 // and so of the matrices' type: at most 1 in magnitude, relative to the largest weight; fp16 scaled by 2^14 (kPScale).
 // Many rows of at most 128 columns in 16-bit types go the way of ce_narrow.h (ce_plan).
 #include "act.h"
@@ -473,15 +473,17 @@ CePlan ce_plan(const tig_softmax_ce &p)
         return L;
     }
     // Narrow rows stay in registers where there are enough logits for that to count (us, with gradients, this way and by tiles: 1024 x
-    // 30000 x 128 140 and 114, x 100 118 and 127; 128 x 400000 x 128 277 and 268; 256 x 400000 x 64 227 and 330; 4000 x 250000 x 100 1134
-    // and 3003), and without a gradient over many candidates (8 x 400000 x 64 41 and 49; 512 x 30000 x 64 21 and 18).
+    // 30000 x 128 128 and 107, x 100 111 and 119; 128 x 262144 x 128 175 and 178, x 64 142 and 141; 128 x 400000 x 128 217 and 262;
+    // 256 x 400000 x 64 193 and 325; 4000 x 250000 x 100 1070 and 3007), and without a gradient over many candidates (8 x 400000 x 64
+    // 39 and 47; 512 x 30000 x 64 19 and 17).
     if (es == 2 && d <= 128 && (n * V >= (int64_t)1 << 25 || (!L.grad && V >= 1 << 17))) {
         L.kb = d <= 64 ? 2 : 4;  // (a column more does not change it)
         const int64_t tile = L.kb == 2 ? kNarrowTile<2> : kNarrowTile<4>;
         L.own_rows = (n + tile - 1) / tile, L.own_cands = (V + tile - 1) / tile;
         L.row_tiles = (n + kNarrowStream - 1) / kNarrowStream, L.cand_tiles = (V + kNarrowStream - 1) / kNarrowStream;
         // A column more, where the blocks have room for one and W is copied anyway, or where rows are many (with and without, aligned
-        // rows: 1024 x 250000 x 96 389 and 369 us, 2000 x 250000 x 40 398 and 421, 8000 x 100000 x 120 981 and 1061).
+        // rows: 300 x 250000 x 120 205 and 188 us, 1024 x 250000 x 96 344 and 335, 1500 x 100000 x 120 265 and 264, 1500 x 250000 x 40
+        // 329 and 332, 2000 x 250000 x 96 581 and 582, x 40 405 and 410, 8000 x 100000 x 120 962 and 985).
         const bool fits = gemm_fits(p.w, p.ldw, d, es);
         L.biased = d < 32 * L.kb && (!fits || n >= 2000);
         L.pack_x = L.biased || !gemm_fits(p.x, p.ldx, d, es);
@@ -625,7 +627,7 @@ hipError_t launch_copy(const T *src, int64_t ld_src, int64_t rows, int64_t cols,
     return hipGetLastError();
 }
 
-// 16-bit rows of at most 32 KB columns; x and w are rows of whole 16-byte pieces
+// 16-bit rows of at most 32 times KB columns; x and w are rows of whole 16-byte pieces
 template <typename T, int KB, int DT, bool BIASED>
 hipError_t run_narrow(const tig_softmax_ce &p, const CePlan &L, char *ws, const T *x, int64_t ldx, const T *w, int64_t ldw, const CeRowsOut<T> &out,
                       hipStream_t s)
