@@ -716,6 +716,135 @@ typedef struct tig_train_adamw {
 TIG_API int tig_train_adamw_workspace_bytes(const tig_ctx *ctx, const tig_train_adamw *cfg, size_t *bytes);
 TIG_API int tig_train_adamw_attach(tig_ctx *ctx, const tig_train_adamw *cfg, void *workspace, size_t workspace_bytes);
 
+/* ------------------------------------------------------------------------------------------
+ * Histories in a paged key-value cache: what a served head keeps of a node's (a request's) past, how a new
+ * event enters it, how a query attends to the whole of it (tig_step's embedding sees the K most recent events), and which
+ * candidates come next.  The conventions of the operators above hold: device memory of the current device, any
+ * element-aligned address and stride, fp32 statistics, calls that enqueue only and can be captured, a
+ * workspace for each call in flight, errors before anything is enqueued.  No call has an atomic whose order shows: results are the
+ * same from call to call.
+ *
+ * A cache is `pages` pages of page_size rows of `heads` heads of head_dim columns, of keys and, with the same
+ * strides, of values; columns are adjacent, pages, rows and heads lie in any order and apart.  A sequence is
+ * a row of a table of page numbers, [seqs x max_pages] int32, and a length (int32): its row p lies in page table[p /
+ * page_size] at p % page_size.  Pages may belong to several sequences.  What a table or a length says is checked where it is
+ * used, on the device: a length below 0 is 0, beyond max_pages * page_size it ends there; a page number outside of 0 .. pages - 1
+ * is no page, which nothing is written to, and whose rows no query sees.  Rows that no sequence has may hold anything.
+ * ------------------------------------------------------------------------------------------ */
+typedef struct tig_cache {
+    uint32_t struct_size;
+    int32_t dtype;          /* tig_dtype of the cache and of the rows that go with it */
+    int64_t pages;          /* 1 .. 2^31 - 1 */
+    int32_t page_size;      /* 1 .. 2^16 */
+    int32_t heads;          /* 1 .. 2^10 */
+    int32_t head_dim;       /* 8 .. 256 */
+    int32_t max_pages;      /* 1 .. 2^24, max_pages * page_size < 2^31 */
+    void *k, *v;            /* element (page, row, head, column) at page * page_stride + row * token_stride + head * head_stride + column */
+    int64_t page_stride, token_stride, head_stride; /* elements, 0 .. 2^40; page_size * token_stride bytes, and a page's own, < 2^31 */
+} tig_cache;
+
+/* New tokens of many sequences enter the cache: values as they are, keys rotated by their position, and queries that come with them
+ * rotated beside it.  Token t of sequence i (starts[i] <= t < starts[i + 1]; without `starts` token i is sequence i's) goes to
+ * row p = lengths[i] - (starts[i + 1] - t): lengths count the new tokens already.
+ *   rotation: the first `rotary` columns are pairs (a, b) -- columns (j, j + rotary / 2), or (2 j, 2 j + 1) if interleaved --
+ *   angle_j = position * freq[j], formed and reduced in fp64;  a' = a cos - b sin,  b' = b cos + a sin (fp32, rounded once)
+ * The position is p, or positions[t] (any finite number of magnitude up to 2^53 as int64, or fp64: event times).  A token without a row
+ * (p < 0, beyond the table, or on no page) is left out: nothing is written for it, q_out neither.  Tokens before starts[0]
+ * and from starts[seqs] on belong to nobody and are left out too.  No two tokens of a call may have the same row.
+ * An output that overlaps another tensor of the call is refused; q_out may be q. */
+typedef struct tig_cache_append {
+    uint32_t struct_size;
+    int32_t rotary;          /* even, 0 .. head_dim */
+    int32_t interleaved;     /* 0 or 1 */
+    int32_t position_type;   /* 0: p; 1: int64; 2: double */
+    int64_t seqs;            /* 0 .. 2^20 */
+    int64_t tokens;          /* 0 .. 2^23; seqs if starts is NULL */
+    const int32_t *table;    /* [seqs x max_pages], rows ld_table apart */
+    int64_t ld_table;
+    const int32_t *lengths;  /* [seqs], the new tokens among them */
+    const int32_t *starts;   /* [seqs + 1], not decreasing, or NULL */
+    const void *positions;   /* [tokens], or NULL for position_type 0 */
+    const double *freq;      /* [rotary / 2], or NULL if rotary is 0 */
+    const void *k, *v;       /* [tokens x heads x head_dim] */
+    const void *q;           /* [tokens x q_heads x head_dim] or NULL */
+    void *q_out;             /* the same, or NULL */
+    int32_t q_heads;         /* 1 .. 2^14 with q, else 0 */
+    int32_t reserved;
+    int64_t k_token, k_head, v_token, v_head, q_token, q_head, qo_token, qo_head; /* strides, 0 .. 2^32 */
+} tig_cache_append;
+TIG_API int tig_cache_append_run(const tig_cache *cache, const tig_cache_append *p, void *hip_stream);
+
+/* Attention of one query per sequence and query head; q_heads / heads query heads share a head of the cache.
+ *   s_p = scale <q, k_p>  for the rows p of the sequence, with `window` > 0 for its last `window` rows
+ *   out = sum_p exp(s_p - lse) v_p,  lse = log sum_p exp(s_p)
+ * A sequence without rows gives out = 0 and lse = -infinity.  16-bit types: the weights exp(s_p - ...) meet the values as two
+ * parts (their rounding and what it leaves), so that they have 16 bits at least; sums are fp32, out is rounded once. */
+typedef struct tig_cache_attend {
+    uint32_t struct_size;
+    int32_t window;          /* >= 0; 0: all rows */
+    int64_t seqs;            /* 0 .. 2^20 */
+    int32_t q_heads;         /* a multiple of the cache's heads, up to 2^14 */
+    float scale;             /* finite */
+    const int32_t *table;    /* [seqs x max_pages], rows ld_table apart */
+    int64_t ld_table;
+    const int32_t *lengths;  /* [seqs] */
+    const void *q;           /* [seqs x q_heads x head_dim] */
+    void *out;               /* the same; may be q */
+    float *lse;              /* [seqs x q_heads] or NULL */
+    int64_t q_seq, q_head, o_seq, o_head; /* strides, 0 .. 2^32 */
+} tig_cache_attend;
+TIG_API int tig_cache_attend_workspace_bytes(const tig_cache *cache, const tig_cache_attend *p, size_t *bytes);
+TIG_API int tig_cache_attend_run(const tig_cache *cache, const tig_cache_attend *p, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* The k best continuations over the beams of a batch entry and their candidates:
+ *   candidate (j, v) of entry b has the score  scores[b, j] + l_bjv - log sum_u exp l_bju
+ *   a finished beam has one candidate, (j, end), with its score unchanged
+ * in descending order of the scores (formed and compared in fp64), ties to the lowest (j, v).  Candidates with a score of
+ * -infinity (masked logits) or none (NaN: a row that holds +infinity or NaN) are not taken; places that no candidate is left for get score -infinity, parent -1,
+ * token -1.  `parents` are rows of logits, b * beams + j.  finished_out: the parent was finished, or the token is `end`.
+ * beams = 1 is a plain selection of the k best of a vocabulary. */
+typedef struct tig_beam_select {
+    uint32_t struct_size;
+    int32_t dtype;             /* tig_dtype of logits */
+    int64_t batch;             /* 0 .. 2^20 */
+    int32_t beams;             /* 1 .. 64 */
+    int32_t k;                 /* 1 .. 128 */
+    int64_t vocab;             /* 1 .. 2^28; beams * vocab < 2^31, batch * beams <= 2^24 */
+    const void *logits;        /* [batch x beams x vocab] */
+    int64_t l_batch, l_beam;   /* its strides, 0 .. 2^40 */
+    const float *scores;       /* [batch x beams], or NULL: 0 */
+    const uint8_t *finished;   /* [batch x beams], or NULL: none */
+    int32_t end;               /* 0 .. vocab - 1, or -1: no such candidate (then finished is NULL) */
+    int32_t reserved;
+    float *scores_out;         /* [batch x k] */
+    int32_t *parents, *tokens; /* [batch x k] */
+    uint8_t *finished_out;     /* [batch x k] or NULL */
+} tig_beam_select;
+TIG_API int tig_beam_select_workspace_bytes(const tig_beam_select *p, size_t *bytes);
+TIG_API int tig_beam_select_run(const tig_beam_select *p, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Sequences taken over by their selected continuations: new sequence r is sequence parents[r], in its full pages as they are, and in
+ * spare[r] a copy of the rows of a last page that is not full, so that each may be appended to.
+ *   n = length / page_size;  table_out[r] = table[parents[r]][0 .. n - 1], spare[r], -1 ...;  lengths_out[r] = the length
+ * (Where n == max_pages there is no place for spare[r], and nothing to copy.)  Without a page of its own (spare[r] outside of 0 .. pages - 1)
+ * a sequence shares its parent's last page: for one that is the only one to go on with it.  A parent outside of 0 ..
+ * rows_in - 1 gives an empty sequence: length 0, its table spare[r], -1 ....  A spare page must be in no other sequence of the call and no
+ * other spare.  Outputs that overlap another tensor of the call are refused. */
+typedef struct tig_cache_fork {
+    uint32_t struct_size;
+    int32_t reserved;
+    int64_t rows_in, rows_out;  /* 0 .. 2^20 each */
+    const int32_t *table;       /* [rows_in x max_pages], rows ld_table apart */
+    int64_t ld_table;
+    const int32_t *lengths;     /* [rows_in] */
+    const int32_t *parents;     /* [rows_out] */
+    const int32_t *spare;       /* [rows_out] */
+    int32_t *table_out;         /* [rows_out x max_pages], rows ld_out apart */
+    int64_t ld_out;
+    int32_t *lengths_out;       /* [rows_out] */
+} tig_cache_fork;
+TIG_API int tig_cache_fork_run(const tig_cache *cache, const tig_cache_fork *p, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

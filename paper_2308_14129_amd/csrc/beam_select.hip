@@ -1,0 +1,430 @@
+// The k best continuations over beams and vocabulary (include/tig.h, tig_beam_select).  gfx950.
+//
+//   score of candidate (j, v) = scores_j + l_jv - log sum_u exp l_ju, the k largest, ties to the lowest (j, v)
+//
+//   k_select_segments  reads the logits once: for every segment (a sixteenth of a wavefront's stretch) its largest logit and the sum of
+//                      exp(l - largest); bound by memory
+//   k_select_pick      a workgroup per batch entry: log-sums from the segments'; a bound that at least k candidates reach; the few
+//                      segments that reach it are read again, and the candidates at or above it are ranked
+// Which bound: the segments are dealt to 128 groups of threads, and the k-th largest of the groups' maxima is the score of a candidate
+// that k - 1 others reach at least.  For values in no particular order a few more than k lie above it; whatever order they are
+// in, nothing above it is missed.  Scores are compared in fp64: candidates of one beam in the order of their logits, those of several
+// beams with log-sums whose error, fp32 exponentials' of random sign over a vocabulary, is about 1e-8.
+#include <cmath>
+
+#include "act.h"
+#include "gemm.h"
+
+namespace tig {
+
+namespace {
+
+struct SelectArgs {
+    const void *logits;
+    int64_t l_batch, l_beam;  // elements
+    int64_t batch;
+    int32_t beams, k, vocab, steps, chunks;  // steps of 512 logits per wavefront; wavefronts per row
+    const float *scores;
+    const uint8_t *finished;
+    int32_t end;
+    float2 *seg;  // [batch x beams][chunks x 4]: largest logit, sum of exp(l - largest)
+    float *scores_out;
+    int32_t *parents, *tokens;
+    uint8_t *finished_out;
+};
+
+template <typename T>
+struct __attribute__((packed, aligned(sizeof(T)))) Eight {
+    T v[8];
+};
+
+// logits at .. at + 7 of a row; -infinity behind its end
+template <typename T>
+__device__ inline void load_eight(const T *row, int at, int vocab, float (&x)[8])
+{
+    if (at + 8 <= vocab) {
+        const Eight<T> q = *(const Eight<T> *)(row + at);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            x[e] = to_float(q.v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            x[e] = at + e < vocab ? to_float(row[at + e]) : -INFINITY;
+    }
+}
+
+constexpr float kLog2e = 1.44269504f;
+
+template <typename T>
+__global__ void __launch_bounds__(256) k_select_segments(SelectArgs a)
+{
+    const int lane = lane_id();
+    const int64_t id = (int64_t)blockIdx.x * 4 + wave_id_uniform();
+    const int64_t r = id / a.chunks;
+    const int chunk = (int)(id - r * a.chunks);
+    if (r >= a.batch * a.beams)
+        return;
+    float m = -INFINITY, s = 0.0f;
+    if (!a.finished || !a.finished[r]) {
+        const T *const row = (const T *)a.logits + r / a.beams * a.l_batch + r % a.beams * a.l_beam;
+        for (int t = 0; t < a.steps; ++t) {
+            const int at = (chunk * a.steps + t) * 512 + lane * 8;
+            float x[8];
+            load_eight(row, at, a.vocab, x);
+            float top = m;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                top = x[e] > top || x[e] != x[e] ? x[e] : top;  // (a NaN stays)
+            const float from = top == -INFINITY ? 0.0f : top;
+            s *= __builtin_amdgcn_exp2f((m - from) * kLog2e);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                s += __builtin_amdgcn_exp2f((x[e] - from) * kLog2e);
+            m = top;
+        }
+    }
+    float top = m;
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) {
+        const float other = __shfl_xor(top, d);
+        top = other > top || other != other ? other : top;
+    }
+    s *= __builtin_amdgcn_exp2f((m - (top == -INFINITY ? 0.0f : top)) * kLog2e);
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2)
+        s += __shfl_xor(s, d);
+    if (lane % 16 == 0)
+        a.seg[(r * a.chunks + chunk) * 4 + lane / 16] = {top, s};
+}
+
+constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64, kGroups = 128, kMaxBeams = 64, kMaxK = 128;
+constexpr int kMaxSegments = 8192;  // of a batch entry
+constexpr int kRoom = 2048;         // candidates in LDS
+
+struct PickShared {
+    double top[kMaxBeams], log_sum[kMaxBeams], score[kMaxBeams];  // a row's log-sum-exp is top + log_sum: beside a mask of -3e38 one number loses the sum
+    double part_sum[kPickWaves];
+    float part_max[kPickWaves];
+    double group[kGroups];
+    double bound;
+    int count, listed;
+    int is_finished[kMaxBeams];
+    double value[kRoom];
+    int32_t id[kRoom];
+    int32_t list[kMaxSegments];
+};
+
+// descending by value, then ascending by id
+__device__ inline bool before(double va, int32_t ia, double vb, int32_t ib) { return va > vb || (va == vb && ia < ib); }
+
+// puts the first `n` candidates into their order
+__device__ inline void sort_candidates(PickShared &sh, int n)
+{
+    int size = 64;
+    while (size < n)
+        size *= 2;
+    for (int i = n + threadIdx.x; i < size; i += kPickThreads)
+        sh.value[i] = -INFINITY, sh.id[i] = 0x7fffffff;
+    __syncthreads();
+    for (int k = 2; k <= size; k *= 2)
+        for (int j = k / 2; j > 0; j /= 2) {
+            const int i = threadIdx.x / j * 2 * j + threadIdx.x % j, o = i + j;
+            if (o < size) {
+                const double vi = sh.value[i], vo = sh.value[o];
+                const int32_t ii = sh.id[i], io = sh.id[o];
+                if (before(vo, io, vi, ii) == ((i & k) == 0))
+                    sh.value[i] = vo, sh.value[o] = vi, sh.id[i] = io, sh.id[o] = ii;
+            }
+            __syncthreads();
+        }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
+{
+    __shared__ PickShared sh;
+    const int tid = threadIdx.x, lane = lane_id(), wave = wave_id_uniform();
+    const int64_t b = blockIdx.x;
+    const int per_beam = a.chunks * 4, all = a.beams * per_beam;
+    const float2 *const seg = a.seg + b * all;
+    // log-sums: some wavefronts per beam
+    const int per = kPickWaves >= a.beams ? kPickWaves / a.beams : 1;  // wavefronts of a beam
+    for (int j0 = 0; j0 < a.beams; j0 += kPickWaves / per) {
+        const int j = j0 + wave / per, part = wave % per;
+        const bool is = j < a.beams && wave / per < kPickWaves / per;
+        float m = -INFINITY;
+        if (is)
+            for (int i = part * 64 + lane; i < per_beam; i += per * 64) {
+                const float x = seg[j * per_beam + i].x;
+                m = x > m || x != x ? x : m;
+            }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const float o = __shfl_xor(m, d);
+            m = o > m || o != o ? o : m;
+        }
+        double s = 0.0;
+        if (is && m != -INFINITY)
+            for (int i = part * 64 + lane; i < per_beam; i += per * 64) {
+                const float2 x = seg[j * per_beam + i];
+                s += (double)x.y * exp((double)x.x - (double)m);
+            }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2)
+            s += __shfl_xor(s, d);
+        if (lane == 0)
+            sh.part_max[wave] = m, sh.part_sum[wave] = s;
+        __syncthreads();
+        if (tid < kPickWaves / per && j0 + tid < a.beams) {
+            float top = -INFINITY;
+            for (int i = 0; i < per; ++i) {
+                const float o = sh.part_max[tid * per + i];
+                top = o > top || o != o ? o : top;
+            }
+            double sum = 0.0;
+            for (int i = 0; i < per; ++i) {
+                const float o = sh.part_max[tid * per + i];
+                sum += o == -INFINITY ? 0.0 : sh.part_sum[tid * per + i] * exp((double)o - (double)top);
+            }
+            const int64_t row = b * a.beams + j0 + tid;
+            sh.top[j0 + tid] = (double)top, sh.log_sum[j0 + tid] = log(sum);
+            sh.score[j0 + tid] = a.scores ? (double)a.scores[row] : 0.0;
+            sh.is_finished[j0 + tid] = a.finished && a.finished[row];
+        }
+        __syncthreads();
+    }
+    auto value = [&](float logit, int j) {
+        const double v = (((double)logit - sh.top[j]) - sh.log_sum[j]) + sh.score[j];
+        return v > -INFINITY && logit > -INFINITY ? v : (double)-INFINITY;  // (NaN is none)
+    };
+    auto segment = [&](int n) {
+        const int j = n / per_beam;
+        return sh.is_finished[j] ? (double)-INFINITY : value(seg[n].x, j);
+    };
+    // the bound
+    double top = -INFINITY;
+    for (int n = tid; n < all; n += kPickThreads)
+        top = fmax(top, segment(n));
+#pragma unroll
+    for (int d = 1; d < kPickThreads / kGroups; d *= 2)
+        top = fmax(top, __shfl_xor(top, d));
+    if (tid % (kPickThreads / kGroups) == 0)
+        sh.group[tid / (kPickThreads / kGroups)] = top;
+    if (tid == 0)
+        sh.count = sh.listed = 0;
+    __syncthreads();
+    {
+        constexpr int kParts = kPickThreads / kGroups;
+        const int t = tid / kParts, part = tid % kParts;
+        const double mine = sh.group[t];
+        int rank = 0;
+        for (int i = part; i < kGroups; i += kParts)
+            rank += before(sh.group[i], i, mine, t);
+#pragma unroll
+        for (int d = 1; d < kParts; d *= 2)
+            rank += __shfl_xor(rank, d);
+        if (part == 0 && rank == a.k - 1)
+            sh.bound = mine;
+    }
+    __syncthreads();
+    double bound = sh.bound;
+    auto push = [&](double v, int32_t id) {
+        const int at = atomicAdd(&sh.count, 1);
+        if (at < kRoom)
+            sh.value[at] = v, sh.id[at] = id;
+    };
+    auto push_finished = [&]() {
+        if (tid < a.beams && sh.is_finished[tid] && sh.score[tid] >= bound && sh.score[tid] > -INFINITY)
+            push(sh.score[tid], tid * a.vocab + a.end);
+    };
+    for (int n = tid; n < all; n += kPickThreads) {
+        const double v = segment(n);
+        if (v >= bound && v > -INFINITY)
+            sh.list[atomicAdd(&sh.listed, 1)] = n;
+    }
+    push_finished();
+    __syncthreads();
+    const int listed = sh.listed;
+    // a listed segment's row, its first logit there, and its beam
+    struct Place {
+        const T *row;
+        int at, j;
+    };
+    auto place = [&](int n) {
+        const int j = n / per_beam, c = n % per_beam;
+        return Place{(const T *)a.logits + b * a.l_batch + j * a.l_beam, c / 4 * a.steps * 512 + c % 4 * 128 + lane % 16 * 8, j};
+    };
+    for (int i = tid / 16; i < listed; i += kPickThreads / 16) {
+        const Place p = place(sh.list[i]);
+        for (int t = 0; t < a.steps; ++t) {
+            float x[8];
+            load_eight(p.row, p.at + t * 512, a.vocab, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const double v = value(x[e], p.j);
+                if (v >= bound && v > -INFINITY)
+                    push(v, p.j * a.vocab + p.at + t * 512 + e);
+            }
+        }
+    }
+    __syncthreads();
+    if (sh.count > kRoom) {  // many of one value, or in an unlucky order: again, a thousand at a time, the k best of them kept
+        __syncthreads();
+        if (tid == 0)
+            sh.count = 0;
+        __syncthreads();
+        push_finished();
+        __syncthreads();
+        for (int i0 = 0; i0 < listed; i0 += kPickThreads / 16)
+            for (int t = 0; t < a.steps; ++t)
+                for (int e = 0; e < 8; ++e) {
+                    if (sh.count > kRoom - kPickThreads) {
+                        const int n = sh.count;
+                        sort_candidates(sh, n);
+                        if (n >= a.k)
+                            bound = sh.value[a.k - 1];
+                        if (tid == 0)
+                            sh.count = n < a.k ? n : a.k;
+                    }
+                    __syncthreads();
+                    const int i = i0 + tid / 16;
+                    if (i < listed) {
+                        const Place p = place(sh.list[i]);
+                        const int at = p.at + t * 512 + e;
+                        if (at < a.vocab) {
+                            const double v = value(to_float(p.row[at]), p.j);
+                            if (v >= bound && v > -INFINITY)
+                                push(v, p.j * a.vocab + at);
+                        }
+                    }
+                    __syncthreads();
+                }
+    }
+    const int count = sh.count;
+    auto write = [&](int rank, double v, int32_t id) {
+        const int64_t o = b * a.k + rank;
+        const int j = id < 0 ? 0 : id / a.vocab, token = id < 0 ? -1 : id - j * a.vocab;
+        a.scores_out[o] = (float)v;
+        a.parents[o] = id < 0 ? -1 : (int32_t)(b * a.beams + j);
+        a.tokens[o] = token;
+        if (a.finished_out)
+            a.finished_out[o] = id >= 0 && (sh.is_finished[j] || token == a.end);
+    };
+    if (count <= 512) {  // each candidate's rank: how many come before it
+        int parts = kPickThreads / 64;
+        while (parts > 1 && kPickThreads / parts < count)
+            parts /= 2;
+        const int t = tid / parts, part = tid % parts;
+        int rank = 0;
+        if (t < count)
+            for (int i = part; i < count; i += parts)
+                rank += before(sh.value[i], sh.id[i], sh.value[t], sh.id[t]);
+        for (int d = 1; d < parts; d *= 2)
+            rank += __shfl_xor(rank, d);
+        if (t < count && part == 0 && rank < a.k)
+            write(rank, sh.value[t], sh.id[t]);
+    } else {
+        sort_candidates(sh, count);
+        if (tid < a.k && tid < count)
+            write(tid, sh.value[tid], sh.id[tid]);
+    }
+    if (tid >= count && tid < a.k)
+        write(tid, -INFINITY, -1);
+}
+
+struct SelectPlan {
+    int steps, chunks;
+    size_t bytes;
+};
+// More steps per wavefront where there are wavefronts enough, and so many that an entry's segments fit.
+SelectPlan select_plan(const tig_beam_select &p)
+{
+    SelectPlan L = {};
+    const int64_t blocks = (p.vocab + 511) / 512, rows = p.batch * p.beams;
+    int64_t steps = std::min<int64_t>(8, std::max<int64_t>(1, rows * blocks / 8192));
+    while (p.beams * ((blocks + steps - 1) / steps) * 4 > kMaxSegments)
+        ++steps;
+    while (rows * ((blocks + steps - 1) / steps) > (1 << 25))  // (a launch's threads fit 32 bits)
+        steps *= 2;
+    L.steps = (int)steps, L.chunks = (int)((blocks + steps - 1) / steps);
+    L.bytes = ((size_t)rows * L.chunks * 4 * sizeof(float2) + 255) / 256 * 256;
+    return L;
+}
+
+int check_select(const tig_beam_select *p)
+{
+    if (!p || p->struct_size != sizeof(tig_beam_select))
+        return fail_text(TIG_EINVAL, "tig_beam_select: NULL argument or wrong struct_size");
+    if (!dtype_ok(p->dtype) || p->reserved != 0)
+        return fail_text(TIG_EINVAL, "tig_beam_select: unknown dtype, or reserved is not 0");
+    if (p->batch < 0 || p->batch > (1 << 20) || p->beams < 1 || p->beams > kMaxBeams || p->k < 1 || p->k > kMaxK || p->vocab < 1 || p->vocab > (1 << 28) ||
+        p->beams * p->vocab > 0x7fffffff || p->batch * p->beams > (1 << 24))
+        return fail_text(TIG_EINVAL, "tig_beam_select: batch, beams, k or vocab out of range");
+    if (p->end < -1 || p->end >= p->vocab || (p->finished && p->end < 0))
+        return fail_text(TIG_EINVAL, "tig_beam_select: end is no candidate (finished beams need one)");
+    if (p->batch > 0 && (!p->logits || !p->scores_out || !p->parents || !p->tokens))
+        return fail_text(TIG_EINVAL, "tig_beam_select: logits, scores_out, parents or tokens is NULL");
+    const int64_t most = (int64_t)1 << 40;
+    if (p->l_batch < 0 || p->l_beam < 0 || p->l_batch > most || p->l_beam > most)
+        return fail_text(TIG_EINVAL, "tig_beam_select: a stride is out of range");
+    if ((uintptr_t)p->logits % (uintptr_t)dtype_bytes(p->dtype) || (((uintptr_t)p->scores | (uintptr_t)p->scores_out | (uintptr_t)p->parents | (uintptr_t)p->tokens) & 3))
+        return fail_text(TIG_EINVAL, "tig_beam_select: an address is not aligned to its element");
+    return TIG_OK;
+}
+
+int check_select_apart(const tig_beam_select &p)
+{
+    const int64_t n = p.batch * p.beams, o = p.batch * p.k;
+    const int es = dtype_bytes(p.dtype);
+    // (what lies between the rows of logits counts as theirs)
+    const int64_t span = (p.batch - 1) * p.l_batch + (p.beams - 1) * p.l_beam + p.vocab;
+    const Placed in[] = {{p.logits, 1, span, span, es}, {p.scores, 1, n, n, 4}, {p.finished, 1, n, n, 1}};
+    const Placed out[] = {{p.scores_out, 1, o, o, 4}, {p.parents, 1, o, o, 4}, {p.tokens, 1, o, o, 4}, {p.finished_out, 1, o, o, 1}};
+    return all_apart(in, out) ? TIG_OK : fail_text(TIG_EINVAL, "tig_beam_select: an output overlaps another tensor of the call");
+}
+
+}  // namespace
+
+}  // namespace tig
+
+using namespace tig;
+
+int tig_beam_select_workspace_bytes(const tig_beam_select *p, size_t *bytes)
+{
+    const int rc = check_select(p);
+    if (rc != TIG_OK)
+        return rc;
+    if (!bytes)
+        return fail_text(TIG_EINVAL, "tig_beam_select_workspace_bytes: bytes is NULL");
+    *bytes = p->batch > 0 ? select_plan(*p).bytes : 0;
+    return TIG_OK;
+}
+
+int tig_beam_select_run(const tig_beam_select *p, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    int rc = check_select(p);
+    if (rc != TIG_OK || p->batch == 0)
+        return rc;
+    const SelectPlan L = select_plan(*p);
+    if (!workspace || ((uintptr_t)workspace & 255))
+        return fail_text(TIG_EINVAL, "tig_beam_select_run: workspace is NULL or not 256-byte aligned");
+    if (workspace_bytes < L.bytes)
+        return fail_text(TIG_ENOSPACE, "tig_beam_select_run: workspace too small");
+    if ((rc = check_select_apart(*p)) != TIG_OK)
+        return rc;
+    const hipStream_t s = (hipStream_t)hip_stream;
+    SelectArgs a = {p->logits, p->l_batch, p->l_beam, p->batch, p->beams, p->k, (int32_t)p->vocab, L.steps, L.chunks, p->scores, p->finished, p->end,
+                    (float2 *)workspace, p->scores_out, p->parents, p->tokens, p->finished_out};
+    const int64_t waves = p->batch * p->beams * L.chunks;
+    const hipError_t e = with_dtype(p->dtype, [&](auto t) {
+        using T = decltype(t);
+        hipLaunchKernelGGL((k_select_segments<T>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
+        hipLaunchKernelGGL((k_select_pick<T>), dim3((unsigned)p->batch), dim3(kPickThreads), 0, s, a);
+        return hipGetLastError();
+    });
+    return e == hipSuccess ? TIG_OK : fail_global("tig_beam_select_run", e);
+}

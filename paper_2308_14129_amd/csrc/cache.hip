@@ -1,0 +1,389 @@
+// Paged key-value cache (include/tig.h): what is common, new tokens (tig_cache_append), and sequences that are taken over by
+// several others (tig_cache_fork).  gfx950.
+#include "cache.h"
+
+namespace tig {
+
+Placed placed(const void *p, std::initializer_list<Dim> dims, int64_t cols, int elem)
+{
+    Dim d[3] = {};
+    int n = 0;
+    for (const Dim &x : dims)
+        if (x.n > 1)
+            d[n++] = x;
+    std::sort(d, d + n, [](const Dim &a, const Dim &b) { return a.stride > b.stride; });
+    while (n > 1 && d[0].stride == d[1].n * d[1].stride) {
+        d[1].n *= d[0].n;
+        for (int i = 1; i < n; ++i)
+            d[i - 1] = d[i];
+        --n;
+    }
+    for (int i = 1; i < n; ++i)
+        cols += (d[i].n - 1) * d[i].stride;
+    if (n == 0)
+        return {p, 1, cols, cols, elem};
+    if (cols > d[0].stride)  // not rows: one range
+        return {p, 1, cols + (d[0].n - 1) * d[0].stride, cols, elem};
+    return {p, d[0].n, cols, d[0].stride, elem};
+}
+
+int check_cache(const tig_cache *c)
+{
+    if (!c || c->struct_size != sizeof(tig_cache))
+        return fail_text(TIG_EINVAL, "tig_cache: NULL argument or wrong struct_size");
+    if (!dtype_ok(c->dtype))
+        return fail_text(TIG_EINVAL, "tig_cache: unknown dtype");
+    if (c->pages < 1 || c->pages > 0x7fffffff || c->page_size < 1 || c->page_size > (1 << 16) || c->heads < 1 || c->heads > (1 << 10) || c->head_dim < 8 ||
+        c->head_dim > 256 || c->max_pages < 1 || c->max_pages > (1 << 24) || (int64_t)c->max_pages * c->page_size > 0x7fffffff)
+        return fail_text(TIG_EINVAL, "tig_cache: pages, page_size, heads, head_dim or max_pages out of range");
+    const int es = dtype_bytes(c->dtype);
+    if (!c->k || !c->v || !element_aligned(c->k, es) || !element_aligned(c->v, es))
+        return fail_text(TIG_EINVAL, "tig_cache: k or v is NULL or not aligned to its element");
+    const int64_t most = (int64_t)1 << 40;
+    if (c->page_stride < 0 || c->token_stride < 0 || c->head_stride < 0 || c->page_stride > most || c->token_stride > most || c->head_stride > most ||
+        c->token_stride > 0x7fffffff || c->page_size * c->token_stride * es > 0x7fffffff)
+        return fail_text(TIG_EINVAL, "tig_cache: a stride is out of range");
+    if ((int64_t)c->page_size * c->heads * c->head_dim * es > 0x7fffffff)
+        return fail_text(TIG_EINVAL, "tig_cache: a page is 2 GiB or larger");
+    Dim d[3] = {{c->pages, c->page_stride}, {c->page_size, c->token_stride}, {c->heads, c->head_stride}};
+    std::sort(d, d + 3, [](const Dim &a, const Dim &b) { return a.stride < b.stride; });
+    int64_t span = c->head_dim;
+    for (const Dim &x : d) {
+        if (x.n > 1 && x.stride < span)
+            return fail_text(TIG_EINVAL, "tig_cache: pages, rows and heads overlap");
+        span += (x.n - 1) * x.stride;
+        if (x.n > 1 && span > ((int64_t)1 << 46))
+            return fail_text(TIG_EINVAL, "tig_cache: a stride is out of range");
+    }
+    return TIG_OK;
+}
+
+int check_sequences(const tig_cache &c, int64_t seqs, const int32_t *table, int64_t ld, const int32_t *lengths)
+{
+    if (seqs < 0 || seqs > (1 << 20))
+        return fail_text(TIG_EINVAL, "tig_cache: number of sequences out of range");
+    if (seqs > 0 && (!table || !lengths || !element_aligned(table, 4) || !element_aligned(lengths, 4)))
+        return fail_text(TIG_EINVAL, "tig_cache: table or lengths is NULL or not aligned to its element");
+    if (ld < c.max_pages || ld > ((int64_t)1 << 32))
+        return fail_text(TIG_EINVAL, "tig_cache: the table's row stride is smaller than max_pages or above 2^32");
+    return TIG_OK;
+}
+
+namespace {
+
+// ------------------------------------------------------------------------------------------
+// New tokens.
+
+struct AppendArgs {
+    CacheView c;
+    int64_t seqs, tokens;
+    const int32_t *starts;
+    const void *positions;
+    const double *freq;
+    const char *k, *v, *q;
+    char *qo;
+    int64_t k_token, k_head, v_token, v_head, q_token, q_head, qo_token, qo_head;  // bytes
+    int32_t q_heads, rotary, interleaved, position_type;
+};
+
+constexpr double kTurn8 = 0.63661977236758134308;  // 2 / pi
+// pi / 2 in two parts
+constexpr double kQuarterHi = 1.57079632679489655800, kQuarterLo = 6.12323399573676603587e-17;
+
+// Cosine and sine of an angle in fp64: quarter turns are taken off (exactly, by fused products with the two parts of pi / 2), the rest, at
+// most pi / 4, goes through the Taylor polynomials to the thirteenth and twelfth degree (their next terms are 2e-14 and 4e-13 there), and
+// each is rounded once.  About 25 operations at fp64's rate, which is fp32's on this card.
+__device__ inline void cos_sin(double angle, float &c, float &s)
+{
+    const double n = rint(angle * kTurn8);
+    double x = fma(n, -kQuarterHi, angle);
+    x = fma(n, -kQuarterLo, x);
+    const double y = x * x;
+    double ps = 1.0 / 6227020800.0, pc = 1.0 / 479001600.0;
+    ps = fma(y, ps, -1.0 / 39916800.0);
+    ps = fma(y, ps, 1.0 / 362880.0);
+    ps = fma(y, ps, -1.0 / 5040.0);
+    ps = fma(y, ps, 1.0 / 120.0);
+    ps = fma(y, ps, -1.0 / 6.0);
+    ps = fma(x * y, ps, x);
+    pc = fma(y, pc, -1.0 / 3628800.0);
+    pc = fma(y, pc, 1.0 / 40320.0);
+    pc = fma(y, pc, -1.0 / 720.0);
+    pc = fma(y, pc, 1.0 / 24.0);
+    pc = fma(y, pc, -0.5);
+    pc = fma(y, pc, 1.0);
+    const int quarter = (int)(n - 4.0 * floor(n * 0.25));  // 0 .. 3
+    const double a = quarter & 1 ? ps : pc, b = quarter & 1 ? pc : ps;
+    c = (float)((quarter + 1) & 2 ? -a : a);
+    s = (float)(quarter & 2 ? -b : b);
+}
+
+template <typename T>
+struct __attribute__((packed, aligned(sizeof(T)))) Piece16 {
+    T v[16 / sizeof(T)];
+};
+
+// a' = a cos - b sin, b' = b cos + a sin for `n` pairs
+template <typename T>
+__device__ inline void rotate_pair(T &a, T &b, float c, float s)
+{
+    const float x = to_float(a), y = to_float(b);
+    a = (T)fmaf(x, c, -(y * s));
+    b = (T)fmaf(y, c, x * s);
+}
+
+// A wavefront (or, where a token has many rows, a workgroup) per token: cosines and sines of its pairs into LDS once, then all its rows in
+// pieces of 16 bytes, a rotated pair of pieces to a lane.
+template <typename T>
+__global__ void __launch_bounds__(256) k_cache_append(AppendArgs a, int lanes)
+{
+    constexpr int VE = 16 / sizeof(T), ES = sizeof(T);
+    __shared__ float turn[4][2][128];  // by token of the workgroup: cosines, sines
+    const int group = threadIdx.x / lanes, tid = threadIdx.x % lanes;
+    const int64_t token = (int64_t)blockIdx.x * (256 / lanes) + group;
+    const CacheView &c = a.c;
+    const int d = c.head_dim, pairs = a.rotary / 2;
+    int page = -1, row = 0;
+    if (token < a.tokens) {
+        int64_t seq = token;
+        int place = -1;
+        if (a.starts) {  // the last sequence that starts at or before the token
+            int64_t lo = 0, hi = a.seqs;
+            while (lo < hi) {
+                const int64_t mid = (lo + hi + 1) / 2;
+                if (a.starts[mid] <= token)
+                    lo = mid;
+                else
+                    hi = mid - 1;
+            }
+            seq = lo;
+            if (seq < a.seqs && a.starts[seq] <= token && token < a.starts[seq + 1])
+                place = (int)std::max<int64_t>(c.lengths[seq] - (a.starts[seq + 1] - token), -1);
+        } else {
+            place = std::max(c.lengths[seq], 0) - 1;
+        }
+        if (place >= 0 && place < c.capacity()) {
+            const int n = c.div.quotient(place);
+            row = place - n * c.page_size;
+            page = c.table[seq * c.ld_table + n];
+            if (!c.page_ok(page))
+                page = -1;
+        }
+        if (page >= 0)
+            for (int j = tid; j < pairs; j += lanes) {
+                const double pos = a.position_type == 0 ? (double)place : a.position_type == 1 ? (double)((const int64_t *)a.positions)[token]
+                                                                                               : ((const double *)a.positions)[token];
+                cos_sin(pos * a.freq[j], turn[group][0][j], turn[group][1][j]);
+            }
+    }
+    __syncthreads();
+    if (page < 0)
+        return;
+    const int n_pair = (pairs + VE - 1) / VE, rest = d - a.rotary, n_rest = (rest + VE - 1) / VE, per_row = n_pair + n_rest;
+    const int rotated = (a.q_heads + c.heads) * per_row, n_v = (d + VE - 1) / VE, all = rotated + c.heads * n_v;
+    const float *const cs = turn[group][0], *const sn = turn[group][1];
+    for (int u = tid; u < all; u += lanes) {
+        if (u >= rotated) {
+            const int h = (u - rotated) / n_v, at = piece_start((u - rotated) % n_v, d * ES);
+            *(Sixteen *)(c.v + c.offset(page, row, h) + at) = *(const Sixteen *)(a.v + token * a.v_token + h * a.v_head + at);
+            continue;
+        }
+        const int r = u / per_row, w = u % per_row;
+        const bool is_q = r < a.q_heads;
+        const int h = is_q ? r : r - a.q_heads;
+        const T *const from = (const T *)(is_q ? a.q + token * a.q_token + h * a.q_head : a.k + token * a.k_token + h * a.k_head);
+        T *const to = (T *)(is_q ? a.qo + token * a.qo_token + h * a.qo_head : c.k + c.offset(page, row, h));
+        if (w >= n_pair) {
+            const int at = a.rotary + (w - n_pair) * VE;
+            if (at + VE <= d)
+                *(Piece16<T> *)(to + at) = *(const Piece16<T> *)(from + at);
+            else
+                for (int e = at; e < d; ++e)
+                    to[e] = from[e];
+            continue;
+        }
+        const int j = w * VE;
+        const int at_a = a.interleaved ? 2 * j : j, at_b = a.interleaved ? 2 * j + VE : pairs + j;
+        if (j + VE <= pairs) {
+            Piece16<T> x = *(const Piece16<T> *)(from + at_a), y = *(const Piece16<T> *)(from + at_b);
+            if (a.interleaved) {
+#pragma unroll
+                for (int e = 0; e < VE / 2; ++e) {
+                    rotate_pair(x.v[2 * e], x.v[2 * e + 1], cs[j + e], sn[j + e]);
+                    rotate_pair(y.v[2 * e], y.v[2 * e + 1], cs[j + VE / 2 + e], sn[j + VE / 2 + e]);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < VE; ++e)
+                    rotate_pair(x.v[e], y.v[e], cs[j + e], sn[j + e]);
+            }
+            *(Piece16<T> *)(to + at_a) = x;
+            *(Piece16<T> *)(to + at_b) = y;
+        } else {
+            for (int e = j; e < pairs; ++e) {
+                const int p = a.interleaved ? 2 * e : e, o = a.interleaved ? 2 * e + 1 : pairs + e;
+                T x = from[p], y = from[o];
+                rotate_pair(x, y, cs[e], sn[e]);
+                to[p] = x, to[o] = y;
+            }
+        }
+    }
+}
+
+int check_append(const tig_cache *c, const tig_cache_append *p)
+{
+    int rc = check_cache(c);
+    if (rc != TIG_OK)
+        return rc;
+    if (!p || p->struct_size != sizeof(tig_cache_append))
+        return fail_text(TIG_EINVAL, "tig_cache_append: NULL argument or wrong struct_size");
+    if ((rc = check_sequences(*c, p->seqs, p->table, p->ld_table, p->lengths)) != TIG_OK)
+        return rc;
+    if (p->rotary < 0 || p->rotary > c->head_dim || p->rotary % 2 || p->interleaved < 0 || p->interleaved > 1 || p->reserved != 0)
+        return fail_text(TIG_EINVAL, "tig_cache_append: rotary or interleaved out of range, or reserved is not 0");
+    if (p->tokens < 0 || p->tokens > (1 << 23) || (!p->starts && p->tokens != p->seqs))
+        return fail_text(TIG_EINVAL, "tig_cache_append: tokens out of range, or not one for each sequence without starts");
+    if (p->position_type < 0 || p->position_type > 2 || (p->tokens > 0 && (p->position_type != 0) != (p->positions != nullptr)) ||
+        ((p->rotary > 0) != (p->freq != nullptr)) || !element_aligned(p->positions, 8) || !element_aligned(p->freq, 8) || !element_aligned(p->starts, 4))
+        return fail_text(TIG_EINVAL, "tig_cache_append: positions do not go with position_type, or freq with rotary, or one is not aligned");
+    if (p->q_heads < 0 || p->q_heads > (1 << 14) || (p->tokens > 0 && ((p->q_heads != 0) != (p->q != nullptr) || (p->q != nullptr) != (p->q_out != nullptr))))
+        return fail_text(TIG_EINVAL, "tig_cache_append: q, q_out and q_heads do not go together, or q_heads is out of range");
+    const int es = dtype_bytes(c->dtype);
+    if (p->tokens > 0 && (!p->k || !p->v))
+        return fail_text(TIG_EINVAL, "tig_cache_append: k or v is NULL");
+    if (!element_aligned(p->k, es) || !element_aligned(p->v, es) || !element_aligned(p->q, es) || !element_aligned(p->q_out, es))
+        return fail_text(TIG_EINVAL, "tig_cache_append: an address is not aligned to its element");
+    for (const int64_t s : {p->k_token, p->k_head, p->v_token, p->v_head, p->q_token, p->q_head, p->qo_token, p->qo_head})
+        if (s < 0 || s > ((int64_t)1 << 32))
+            return fail_text(TIG_EINVAL, "tig_cache_append: a stride is out of range");
+    if (p->q_out && ((p->tokens > 1 && p->qo_token < c->head_dim) || (p->q_heads > 1 && p->qo_head < c->head_dim)))
+        return fail_text(TIG_EINVAL, "tig_cache_append: rows of q_out overlap");
+    return TIG_OK;
+}
+
+int check_append_apart(const tig_cache &c, const tig_cache_append &p)
+{
+    const int es = dtype_bytes(c.dtype);
+    const int64_t n = p.tokens;
+    auto rows = [&](const void *x, int64_t token, int64_t heads, int64_t head) { return placed(x, {{n, token}, {heads, head}}, c.head_dim, es); };
+    const bool in_place = p.q == p.q_out && p.q_token == p.qo_token && p.q_head == p.qo_head;
+    const Placed in[] = {rows(p.k, p.k_token, c.heads, p.k_head), rows(p.v, p.v_token, c.heads, p.v_head), rows(in_place ? nullptr : p.q, p.q_token, p.q_heads, p.q_head),
+                         {p.table, p.seqs, c.max_pages, p.ld_table, 4}, {p.lengths, 1, p.seqs, p.seqs, 4}, {p.starts, 1, p.seqs + 1, p.seqs + 1, 4},
+                         {p.positions, 1, n, n, 8}, {p.freq, 1, p.rotary / 2, p.rotary / 2, 8}};
+    const Placed out[] = {placed_keys(c, c.k), placed_keys(c, c.v), rows(p.q_out, p.qo_token, p.q_heads, p.qo_head)};
+    return all_apart(in, out) ? TIG_OK : fail_text(TIG_EINVAL, "tig_cache_append: an output overlaps another tensor of the call");
+}
+
+// ------------------------------------------------------------------------------------------
+// Sequences that are taken over: a workgroup's share of a last page's rows; the first of a sequence's also writes its table.
+
+struct ForkArgs {
+    CacheView c;
+    int64_t rows_in, rows_out, ld_out;
+    const int32_t *parents, *spare;
+    int32_t *table_out, *lengths_out;
+    int32_t heads_inner;  // heads lie closer together than rows
+};
+
+__global__ void __launch_bounds__(256) k_cache_fork(ForkArgs a, int es)
+{
+    const CacheView &c = a.c;
+    const int64_t r = blockIdx.x;
+    const int64_t parent = a.parents[r];
+    const bool some = parent >= 0 && parent < a.rows_in;
+    const int length = some ? c.length(parent) : 0;
+    const int n = c.div.quotient(length), left = length - n * c.page_size;
+    const int32_t *const from = c.table + (some ? parent : 0) * c.ld_table;
+    const int spare = a.spare[r], last = left > 0 ? from[n] : -1;
+    const bool copies = left > 0 && c.page_ok(spare) && c.page_ok(last);
+    if (blockIdx.y == 0) {
+        for (int i = threadIdx.x; i < c.max_pages; i += 256)
+            a.table_out[r * a.ld_out + i] = i < n ? from[i] : i > n ? -1 : left > 0 && !copies ? last : c.page_ok(spare) ? spare : -1;
+        if (threadIdx.x == 0)
+            a.lengths_out[r] = length;
+    }
+    if (!copies)
+        return;
+    const int row_bytes = c.head_dim * es, pieces = (row_bytes + 15) / 16, per_cache = left * c.heads * pieces;
+    const int inner = a.heads_inner ? c.heads : left;
+    for (int u = blockIdx.y * 256 + threadIdx.x; u < 2 * per_cache; u += 256 * gridDim.y) {
+        char *const base = u < per_cache ? c.k : c.v;
+        const int w = u < per_cache ? u : u - per_cache, x = w / pieces, o = x / inner, i = x % inner;
+        const int row = a.heads_inner ? o : i, head = a.heads_inner ? i : o, at = piece_start(w % pieces, row_bytes);
+        *(Sixteen *)(base + c.offset(spare, row, head) + at) = *(const Sixteen *)(base + c.offset(last, row, head) + at);
+    }
+}
+
+int check_fork(const tig_cache *c, const tig_cache_fork *p)
+{
+    int rc = check_cache(c);
+    if (rc != TIG_OK)
+        return rc;
+    if (!p || p->struct_size != sizeof(tig_cache_fork) || p->reserved != 0)
+        return fail_text(TIG_EINVAL, "tig_cache_fork: NULL argument, wrong struct_size, or reserved is not 0");
+    if (p->rows_out < 0 || p->rows_out > (1 << 20))
+        return fail_text(TIG_EINVAL, "tig_cache_fork: rows_out out of range");
+    if ((rc = check_sequences(*c, p->rows_in, p->table, p->ld_table, p->lengths)) != TIG_OK)
+        return rc;
+    if (p->rows_out > 0 && (!p->parents || !p->spare || !p->table_out || !p->lengths_out))
+        return fail_text(TIG_EINVAL, "tig_cache_fork: parents, spare, table_out or lengths_out is NULL");
+    if (!element_aligned(p->parents, 4) || !element_aligned(p->spare, 4) || !element_aligned(p->table_out, 4) || !element_aligned(p->lengths_out, 4))
+        return fail_text(TIG_EINVAL, "tig_cache_fork: an address is not aligned to its element");
+    if (p->ld_out < c->max_pages || p->ld_out > ((int64_t)1 << 32))
+        return fail_text(TIG_EINVAL, "tig_cache_fork: the table's row stride is smaller than max_pages or above 2^32");
+    const Placed in[] = {{p->table, p->rows_in, c->max_pages, p->ld_table, 4}, {p->lengths, 1, p->rows_in, p->rows_in, 4},
+                         {p->parents, 1, p->rows_out, p->rows_out, 4}, {p->spare, 1, p->rows_out, p->rows_out, 4}};
+    const Placed out[] = {{p->table_out, p->rows_out, c->max_pages, p->ld_out, 4}, {p->lengths_out, 1, p->rows_out, p->rows_out, 4}, placed_keys(*c, c->k),
+                          placed_keys(*c, c->v)};
+    return all_apart(in, out) ? TIG_OK : fail_text(TIG_EINVAL, "tig_cache_fork: an output overlaps another tensor of the call");
+}
+
+}  // namespace
+
+}  // namespace tig
+
+using namespace tig;
+
+int tig_cache_append_run(const tig_cache *cache, const tig_cache_append *p, void *hip_stream)
+{
+    int rc = check_append(cache, p);
+    if (rc != TIG_OK || p->tokens == 0 || p->seqs == 0)
+        return rc;
+    if ((rc = check_append_apart(*cache, *p)) != TIG_OK)
+        return rc;
+    const int64_t es = dtype_bytes(cache->dtype);
+    AppendArgs a = {};
+    a.c = cache_view(*cache, p->table, p->ld_table, p->lengths);
+    a.seqs = p->seqs, a.tokens = p->tokens, a.starts = p->starts, a.positions = p->positions, a.freq = p->freq;
+    a.k = (const char *)p->k, a.v = (const char *)p->v, a.q = (const char *)p->q, a.qo = (char *)p->q_out;
+    a.k_token = p->k_token * es, a.k_head = p->k_head * es, a.v_token = p->v_token * es, a.v_head = p->v_head * es;
+    a.q_token = p->q_token * es, a.q_head = p->q_head * es, a.qo_token = p->qo_token * es, a.qo_head = p->qo_head * es;
+    a.q_heads = p->q_heads, a.rotary = p->rotary, a.interleaved = p->interleaved, a.position_type = p->position_type;
+    const int64_t pieces = (int64_t)(p->q_heads + 2 * cache->heads) * (cache->head_dim * es + 15) / 16;
+    const int lanes = pieces > 256 ? 256 : 64;
+    const dim3 grid((unsigned)((p->tokens + 256 / lanes - 1) / (256 / lanes)));
+    with_dtype(cache->dtype, [&](auto t) {
+        hipLaunchKernelGGL((k_cache_append<decltype(t)>), grid, dim3(256), 0, (hipStream_t)hip_stream, a, lanes);
+        return 0;
+    });
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? TIG_OK : fail_global("tig_cache_append_run", e);
+}
+
+int tig_cache_fork_run(const tig_cache *cache, const tig_cache_fork *p, void *hip_stream)
+{
+    const int rc = check_fork(cache, p);
+    if (rc != TIG_OK || p->rows_out == 0)
+        return rc;
+    const int es = dtype_bytes(cache->dtype);
+    ForkArgs a = {};
+    a.c = cache_view(*cache, p->table, p->ld_table, p->lengths);
+    a.rows_in = p->rows_in, a.rows_out = p->rows_out, a.ld_out = p->ld_out;
+    a.parents = p->parents, a.spare = p->spare, a.table_out = p->table_out, a.lengths_out = p->lengths_out;
+    a.heads_inner = cache->head_stride <= cache->token_stride;
+    const int64_t pieces = 2 * (int64_t)cache->page_size * cache->heads * ((cache->head_dim * es + 15) / 16);
+    const int64_t blocks = std::min<int64_t>(std::max<int64_t>(1, pieces / 2048), 64);
+    hipLaunchKernelGGL(k_cache_fork, dim3((unsigned)p->rows_out, (unsigned)blocks), dim3(256), 0, (hipStream_t)hip_stream, a, es);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? TIG_OK : fail_global("tig_cache_fork_run", e);
+}

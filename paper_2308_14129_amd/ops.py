@@ -1,7 +1,8 @@
 """Thin ctypes binding over the operators of a trained head in include/tig.h (tig_linear_*, tig_softmax_ce_*,
-tig_adamw_*).  Argument marshalling only; PyTorch supplies device memory and the stream handle.  Every call enqueues on
-the current stream of its tensors' device and does not synchronise.  No graph is recorded: linear() and softmax_ce() refuse
-tensors that require a gradient where torch.is_grad_enabled(); linear_backward() and softmax_ce() give the gradients."""
+tig_adamw_*) and of histories in a paged cache (tig_cache_*, tig_beam_select_*).  Argument marshalling only; PyTorch supplies device
+memory and the stream handle.  Every call enqueues on the current stream of its tensors' device and does not synchronise.  No graph is
+recorded: tensors that require a gradient are refused where torch.is_grad_enabled(); linear_backward() and softmax_ce() give the
+gradients, the cache and the selection have none."""
 from __future__ import annotations
 
 import ctypes
@@ -43,6 +44,39 @@ class tig_adamw_config(Structure):
                 ("eps", c_double), ("step", c_void_p)]
 
 
+class tig_cache(Structure):
+    _fields_ = [("struct_size", c_uint32), ("dtype", c_int32), ("pages", c_int64), ("page_size", c_int32), ("heads", c_int32),
+                ("head_dim", c_int32), ("max_pages", c_int32), ("k", c_void_p), ("v", c_void_p), ("page_stride", c_int64),
+                ("token_stride", c_int64), ("head_stride", c_int64)]
+
+
+class tig_cache_append(Structure):
+    _fields_ = [("struct_size", c_uint32), ("rotary", c_int32), ("interleaved", c_int32), ("position_type", c_int32), ("seqs", c_int64),
+                ("tokens", c_int64), ("table", c_void_p), ("ld_table", c_int64), ("lengths", c_void_p), ("starts", c_void_p),
+                ("positions", c_void_p), ("freq", c_void_p), ("k", c_void_p), ("v", c_void_p), ("q", c_void_p), ("q_out", c_void_p),
+                ("q_heads", c_int32), ("reserved", c_int32)] + [
+                    (n, c_int64) for n in ("k_token", "k_head", "v_token", "v_head", "q_token", "q_head", "qo_token", "qo_head")]
+
+
+class tig_cache_attend(Structure):
+    _fields_ = [("struct_size", c_uint32), ("window", c_int32), ("seqs", c_int64), ("q_heads", c_int32), ("scale", c_float),
+                ("table", c_void_p), ("ld_table", c_int64), ("lengths", c_void_p), ("q", c_void_p), ("out", c_void_p), ("lse", c_void_p),
+                ("q_seq", c_int64), ("q_head", c_int64), ("o_seq", c_int64), ("o_head", c_int64)]
+
+
+class tig_beam_select(Structure):
+    _fields_ = [("struct_size", c_uint32), ("dtype", c_int32), ("batch", c_int64), ("beams", c_int32), ("k", c_int32), ("vocab", c_int64),
+                ("logits", c_void_p), ("l_batch", c_int64), ("l_beam", c_int64), ("scores", c_void_p), ("finished", c_void_p),
+                ("end", c_int32), ("reserved", c_int32), ("scores_out", c_void_p), ("parents", c_void_p), ("tokens", c_void_p),
+                ("finished_out", c_void_p)]
+
+
+class tig_cache_fork(Structure):
+    _fields_ = [("struct_size", c_uint32), ("reserved", c_int32), ("rows_in", c_int64), ("rows_out", c_int64), ("table", c_void_p),
+                ("ld_table", c_int64), ("lengths", c_void_p), ("parents", c_void_p), ("spare", c_void_p), ("table_out", c_void_p),
+                ("ld_out", c_int64), ("lengths_out", c_void_p)]
+
+
 _ready = None
 
 
@@ -63,6 +97,16 @@ def _lib():
         lib.tig_adamw_step.argtypes = [c_void_p, c_double, c_double, c_double, c_void_p, c_void_p]
         lib.tig_adamw_destroy.argtypes = [c_void_p]
         lib.tig_adamw_destroy.restype = None
+        assert [ctypes.sizeof(c) for c in (tig_cache, tig_cache_append, tig_cache_attend, tig_beam_select, tig_cache_fork)] == [72, 184, 104, 112, 88]
+        lib.tig_cache_append_run.argtypes = [c_void_p, c_void_p, c_void_p]
+        lib.tig_cache_attend_workspace_bytes.argtypes = [c_void_p, c_void_p, POINTER(c_size_t)]
+        lib.tig_cache_attend_run.argtypes = [c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+        lib.tig_cache_fork_run.argtypes = [c_void_p, c_void_p, c_void_p]
+        lib.tig_beam_select_workspace_bytes.argtypes = [c_void_p, POINTER(c_size_t)]
+        lib.tig_beam_select_run.argtypes = [c_void_p, c_void_p, c_size_t, c_void_p]
+        for n in ("tig_cache_append_run", "tig_cache_attend_workspace_bytes", "tig_cache_attend_run", "tig_cache_fork_run",
+                  "tig_beam_select_workspace_bytes", "tig_beam_select_run"):
+            getattr(lib, n).restype = ctypes.c_int
         for n in ("tig_linear_workspace_bytes", "tig_linear_forward", "tig_linear_backward", "tig_softmax_ce_workspace_bytes",
                   "tig_softmax_ce_run", "tig_adamw_workspace_bytes", "tig_adamw_create", "tig_adamw_step"):
             getattr(lib, n).restype = ctypes.c_int
@@ -93,7 +137,7 @@ def _dtype_code(dtype):
 def _no_graph(name):
     if torch.is_grad_enabled():
         _refuse(f"{name} requires a gradient, but the operators record no graph: call them under torch.no_grad(), with linear_backward "
-                "and softmax_ce's gradients for the way back")
+                "and softmax_ce's gradients for the way back (the cache and the selection have none)")
 
 
 def _matrix(t, rows, cols, dtype, device, name):
@@ -340,3 +384,182 @@ class AdamW:
             self.close()
         except Exception:
             pass
+
+
+# --------------------------------------------------------------------------- histories in a paged cache
+
+_cache_bytes = struct.Struct("=Iiqiiii2Q3q").pack
+_append_bytes = struct.Struct("=Iiii2qQq8Qii8q").pack
+_attend_bytes = struct.Struct("=IiqifQq4Q4q").pack
+_select_bytes = struct.Struct("=IiqiiqQ2q2Qii4Q").pack
+_fork_bytes = struct.Struct("=Ii2qQq4QqQ").pack
+
+
+def _cache(k_cache, v_cache, table, lengths):
+    """tig_cache of keys' and values' pages, its device and dtype, (seqs, heads, head_dim), and the addresses of table and lengths."""
+    if k_cache.dim() != 4 or table.dim() != 2:
+        _refuse("k_cache and v_cache are [pages, page_size, heads, head_dim], table is [sequences, pages of one at most]")
+    dtype, dev = k_cache.dtype, k_cache.device
+    code = _dtype_code(dtype)
+    pages, size, heads, dim = k_cache.shape
+    strides = k_cache.stride()
+    if v_cache.shape != k_cache.shape or v_cache.dtype is not dtype or v_cache.device != dev or v_cache.stride() != strides:
+        _refuse("v_cache differs from k_cache in shape, dtype, device or strides")
+    if strides[3] != 1 and dim > 1:
+        _refuse("k_cache and v_cache: columns have to be adjacent")
+    if k_cache.requires_grad or v_cache.requires_grad:
+        _no_graph("k_cache or v_cache")
+    seqs, width = table.shape
+    if table.dtype is not torch.int32 or table.device != dev or (width > 1 and table.stride(1) != 1):
+        _refuse(f"table is not an int32 tensor of adjacent columns on {dev}")
+    ld = table.stride(0) if seqs > 1 else width
+    pn = _vector(lengths, seqs, torch.int32, dev, "lengths")
+    p = _cache_bytes(72, code, pages, size, heads, dim, width, k_cache.data_ptr(), v_cache.data_ptr(), strides[0] if pages > 1 else 0,
+                     strides[1] if size > 1 else 0, strides[2] if heads > 1 else 0)
+    return p, dtype, dev, (seqs, heads, dim), (table.data_ptr(), ld, pn)
+
+
+def _heads(t, n, heads, dim, dtype, device, name):
+    """Address and strides of a [n, heads, dim] tensor of adjacent columns."""
+    if t.shape != (n, heads, dim) or t.dtype is not dtype or t.device != device:
+        _refuse(f"{name} is not a [{n}, {heads}, {dim}] tensor of {dtype} on {device}")
+    a, b, c = t.stride()
+    if c != 1 and dim > 1:
+        _refuse(f"{name}: columns have to be adjacent")
+    if t.requires_grad:
+        _no_graph(name)
+    return t.data_ptr(), (a if n > 1 else 0), (b if heads > 1 else 0)
+
+
+def cache_append(k_cache, v_cache, table, lengths, k, v, starts=None, q=None, freq=None, positions=None, interleaved=False, q_out=None):
+    """New keys and values [tokens, heads, head_dim] into the pages k_cache and v_cache [pages, page_size, heads, head_dim] (any strides,
+    columns adjacent) of the sequences table [sequences, pages] and lengths [sequences] (int32); lengths count the new tokens
+    already.  starts [sequences + 1] (int32): tokens starts[i] .. starts[i + 1] - 1 are sequence i's, without it token i is.  With freq
+    (float64, [pairs]) keys, and the queries q [tokens, query heads, head_dim], are rotated on the way by position * freq: pairs of
+    columns (j, j + pairs), or (2 j, 2 j + 1) if interleaved; positions [tokens] (int64 or float64) are the rows' own numbers if not
+    given.  Returns the rotated queries (q_out, which may be q; None without q).  A token without a row in the table or a page is left
+    out, in q_out too."""
+    c, dtype, dev, (seqs, heads, dim), (pt, ld, pn) = _cache(k_cache, v_cache, table, lengths)
+    if k.dim() != 3:
+        _refuse("k and v are [tokens, heads, head_dim]")
+    tokens = k.shape[0]
+    if starts is None and tokens != seqs:
+        _refuse(f"{tokens} tokens for {seqs} sequences, and no starts")
+    pk, k0, k1 = _heads(k, tokens, heads, dim, dtype, dev, "k")
+    pv, v0, v1 = _heads(v, tokens, heads, dim, dtype, dev, "v")
+    ps = _vector(starts, seqs + 1, torch.int32, dev, "starts")
+    pairs = 0 if freq is None else freq.numel()
+    pf = _vector(freq, pairs, torch.float64, dev, "freq")
+    kind = 0
+    if positions is not None and pairs:
+        kind = {torch.int64: 1, torch.float64: 2}.get(positions.dtype, 0)
+        if not kind:
+            _refuse("positions are int64 or float64")
+    pp = _vector(positions, tokens, positions.dtype, dev, "positions") if kind else 0
+    pq = po = q0 = q1 = o0 = o1 = qh = 0
+    if q is not None:
+        if q.dim() != 3:
+            _refuse("q is [tokens, query heads, head_dim]")
+        qh = q.shape[1]
+        pq, q0, q1 = _heads(q, tokens, qh, dim, dtype, dev, "q")
+        if q_out is not None:
+            po, o0, o1 = _heads(q_out, tokens, qh, dim, dtype, dev, "q_out")
+    elif q_out is not None:
+        _refuse("q_out without q")
+    lib = _lib()
+    with _On(dev) as stream:
+        if q is not None and q_out is None:
+            q_out = torch.empty((tokens, qh, dim), dtype=dtype, device=dev)
+            po, o0, o1 = q_out.data_ptr(), qh * dim, dim
+        p = _append_bytes(184, 2 * pairs, int(bool(interleaved)), kind, seqs, tokens, pt, ld, pn, ps, pp, pf, pk, pv, pq, po, qh, 0, k0, k1, v0, v1,
+                          q0, q1, o0, o1)
+        _check(lib.tig_cache_append_run(c, p, stream))
+    return q_out
+
+
+def cache_attend(q, k_cache, v_cache, table, lengths, scale=None, window=0, out=None, lse=False):
+    """Attention of one query per sequence, q [sequences, query heads, head_dim], over the sequences' rows in the pages k_cache and
+    v_cache (as in cache_append; as many query heads as heads, or a multiple, which share them).  scale: 1 / sqrt(head_dim) if not given;
+    window: only a sequence's last rows.  Returns out like q (out may be q), with lse=True (out, lse [sequences, query heads] in
+    float32).  A sequence without rows gives zeros and -infinity."""
+    c, dtype, dev, (seqs, heads, dim), (pt, ld, pn) = _cache(k_cache, v_cache, table, lengths)
+    if q.dim() != 3:
+        _refuse("q is [sequences, query heads, head_dim]")
+    qh = q.shape[1]
+    pq, q0, q1 = _heads(q, seqs, qh, dim, dtype, dev, "q")
+    po = o0 = o1 = 0
+    if out is not None:
+        po, o0, o1 = _heads(out, seqs, qh, dim, dtype, dev, "out")
+    lib = _lib()
+    with _On(dev) as stream:
+        if out is None:
+            out = torch.empty((seqs, qh, dim), dtype=dtype, device=dev)
+            po, o0, o1 = out.data_ptr(), qh * dim, dim
+        sums = torch.empty((seqs, qh), dtype=torch.float32, device=dev) if lse else None
+        p = _attend_bytes(104, window, seqs, qh, dim**-0.5 if scale is None else scale, pt, ld, pn, pq, po, sums.data_ptr() if lse else 0, q0, q1, o0, o1)
+        need = c_size_t(0)
+        _check(lib.tig_cache_attend_workspace_bytes(c, p, byref(need)))
+        ws = _workspace(need.value, dev)
+        _check(lib.tig_cache_attend_run(c, p, ws.data_ptr() if ws is not None else None, need.value, stream))
+    return (out, sums) if lse else out
+
+
+BeamSelect = namedtuple("BeamSelect", "scores parents tokens finished")
+
+
+def beam_select(logits, k, scores=None, finished=None, end=-1):
+    """The k best continuations over beams and candidates: logits [batch, beams, vocab] (candidates adjacent), scores [batch, beams]
+    (float32) of the beams so far, finished [batch, beams] (bool) the beams that go on with nothing but `end`, their score
+    unchanged.  Returns BeamSelect(scores [batch, k] in descending order, parents [batch, k] (rows of logits: entry * beams + beam), tokens
+    [batch, k], finished [batch, k]): ties to the lowest beam, then token; -infinity, -1, -1 where no candidate is left."""
+    if logits.dim() != 3:
+        _refuse("logits is [batch, beams, vocab]")
+    batch, beams, vocab = logits.shape
+    if not 1 <= k <= 128:
+        _refuse(f"k = {k} is not in 1 .. 128")
+    dev = logits.device
+    code = _dtype_code(logits.dtype)
+    l0, l1, l2 = logits.stride()
+    if l2 != 1 and vocab > 1:
+        _refuse("logits: candidates have to be adjacent")
+    if logits.requires_grad:
+        _no_graph("logits")
+    if scores is not None and (scores.shape != (batch, beams) or scores.dtype is not torch.float32 or scores.device != dev or not scores.is_contiguous()):
+        _refuse(f"scores is not a contiguous [{batch}, {beams}] tensor of float32 on {dev}")
+    if scores is not None and scores.requires_grad:
+        _no_graph("scores")
+    if finished is not None and (finished.shape != (batch, beams) or finished.dtype not in (torch.bool, torch.uint8) or finished.device != dev
+                                 or not finished.is_contiguous()):
+        _refuse(f"finished is not a contiguous [{batch}, {beams}] tensor of bool on {dev}")
+    lib = _lib()
+    with _On(dev) as stream:
+        new, parents, tokens = torch.empty((3, batch, k), dtype=torch.int32, device=dev).unbind(0)
+        new = new.view(torch.float32)
+        done = torch.empty((batch, k), dtype=torch.bool, device=dev)
+        p = _select_bytes(112, code, batch, beams, k, vocab, logits.data_ptr(), l0 if batch > 1 else 0, l1 if beams > 1 else 0,
+                          0 if scores is None else scores.data_ptr(), 0 if finished is None else finished.data_ptr(), end, 0, new.data_ptr(),
+                          parents.data_ptr(), tokens.data_ptr(), done.data_ptr())
+        need = c_size_t(0)
+        _check(lib.tig_beam_select_workspace_bytes(p, byref(need)))
+        ws = _workspace(need.value, dev)
+        _check(lib.tig_beam_select_run(p, ws.data_ptr() if ws is not None else None, need.value, stream))
+    return BeamSelect(new, parents, tokens, done)
+
+
+def cache_fork(k_cache, v_cache, table, lengths, parents, spare):
+    """The sequences parents (int32, any shape; rows of table, as beam_select gives them) as sequences of their own: full pages are shared, the
+    rows of a last page that is not full are copied into the page spare[r] (int32, one for each).  Returns (table, lengths) of the new
+    sequences; spare[r] stands behind their full pages and takes what is appended next.  Without a page (-1) a sequence shares its
+    parent's last one."""
+    c, dtype, dev, (rows, _, _), (pt, ld, pn) = _cache(k_cache, v_cache, table, lengths)
+    n, width = parents.numel(), table.shape[1]
+    for t, name in ((parents, "parents"), (spare, "spare")):
+        if t.dtype is not torch.int32 or t.device != dev or not t.is_contiguous() or t.numel() != n:
+            _refuse(f"{name} is not a contiguous int32 tensor of {n} on {dev}")
+    lib = _lib()
+    with _On(dev) as stream:
+        new = torch.empty((n, width), dtype=torch.int32, device=dev)
+        sizes = torch.empty(n, dtype=torch.int32, device=dev)
+        p = _fork_bytes(88, 0, rows, n, pt, ld, pn, parents.data_ptr(), spare.data_ptr(), new.data_ptr(), width, sizes.data_ptr())
+        _check(lib.tig_cache_fork_run(c, p, stream))
+    return new, sizes

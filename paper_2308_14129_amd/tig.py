@@ -94,7 +94,9 @@ EXPORTS = ("tig_workspace_bytes", "tig_init", "tig_step", "tig_step_static", "ti
            "tig_modules_workspace_bytes", "tig_modules_attach",
            "tig_linear_workspace_bytes", "tig_linear_forward", "tig_linear_backward", "tig_softmax_ce_workspace_bytes",
            "tig_train_head_workspace_bytes", "tig_train_head_attach", "tig_train_head_get", "tig_train_adamw_workspace_bytes",
-           "tig_train_adamw_attach", "tig_softmax_ce_run", "tig_adamw_workspace_bytes", "tig_adamw_create", "tig_adamw_step", "tig_adamw_destroy")
+           "tig_train_adamw_attach", "tig_softmax_ce_run", "tig_adamw_workspace_bytes", "tig_adamw_create", "tig_adamw_step", "tig_adamw_destroy",
+           "tig_cache_append_run", "tig_cache_attend_workspace_bytes", "tig_cache_attend_run", "tig_cache_fork_run",
+           "tig_beam_select_workspace_bytes", "tig_beam_select_run")
 
 _lib = None
 

@@ -1,0 +1,232 @@
+"""The selection over beams and vocabulary (ops.beam_select) against its definition in 64 bits, and the whole of a search with the paged
+cache against every hypothesis recomputed from its beginning."""
+import math
+
+import pytest
+import torch
+
+from paper_2308_14129_amd import ops
+from tests.paged import DEV, F64, TYPES, U, gen_of
+
+pytestmark = [pytest.mark.gpu, pytest.mark.timeout(120)]
+
+
+def reference(logits, k, scores, finished, end):
+    """Lists of (score, parent, token, finished) per entry, and all candidates' scores."""
+    B, J, V = logits.shape
+    x = logits.to(F64)
+    total = torch.log_softmax(x, -1)
+    total = torch.where(torch.isnan(total) | (x == float("-inf")), float("-inf"), total)
+    total = total + (0 if scores is None else scores.to(F64).unsqueeze(-1))
+    total = torch.where(torch.isnan(total), float("-inf"), total)
+    if finished is not None:
+        done = torch.full_like(total, float("-inf"))
+        done[..., end] = scores.to(F64) if scores is not None else 0
+        total = torch.where(finished.bool().unsqueeze(-1), done, total)
+    flat = total.view(B, J * V)
+    value, at = flat.sort(dim=1, descending=True, stable=True)
+    value, at = value[:, :k], at[:, :k]
+    if value.shape[1] < k:
+        pad = k - value.shape[1]
+        value = torch.cat([value, value.new_full((B, pad), float("-inf"))], 1)
+        at = torch.cat([at, at.new_full((B, pad), 0)], 1)
+    left = value > float("-inf")
+    parents = torch.where(left, at // V + torch.arange(B, device=DEV).unsqueeze(1) * J, -1)
+    tokens = torch.where(left, at % V, -1)
+    was = torch.zeros_like(left) if finished is None else finished.bool().view(-1)[parents.clamp(min=0)]
+    return value, parents, tokens, left & (was | ((tokens == end) if end >= 0 else False))
+
+
+def check(logits, k, scores=None, finished=None, end=-1):
+    print(f"[select] {tuple(logits.shape)} {logits.dtype} k {k} end {end}", flush=True)
+    r = ops.beam_select(logits, k, scores, finished=finished, end=end)
+    torch.cuda.synchronize()
+    value, parents, tokens, done = reference(logits, k, scores, finished, end)
+    assert torch.equal(r.parents.long(), parents) and torch.equal(r.tokens.long(), tokens) and torch.equal(r.finished, done)
+    # a score is rounded once; the log-sum of fp32 exponentials (4 units each and their argument's rounding, sums of eight and of the lanes)
+    # is off by at most 64 units of its own
+    ok = value > float("-inf")
+    assert torch.equal(r.scores[~ok], torch.full_like(r.scores[~ok], float("-inf")))
+    assert ((r.scores.to(F64) - value)[ok].abs() <= (U * value.abs() + 64 * U)[ok]).all()
+    return r
+
+
+SHAPES = [(1, 1, 1, 1), (1, 1, 7, 3), (3, 2, 100, 5), (1, 4, 32000, 4), (5, 3, 511, 8), (2, 5, 513, 16), (4, 8, 5003, 8), (2, 1, 20011, 128), (1, 64, 1000, 64),
+          (7, 1, 1, 4), (2, 16, 40_000, 100), (1, 3, 300_001, 3), (300, 2, 260, 2), (1, 40, 9000, 128), (2, 1, 1_000_003, 50)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_select(shape, dtype):
+    B, J, V, k = shape
+    gen = gen_of(V)
+    logits = (torch.randn(B, J, V, device=DEV, generator=gen) * 3).to(TYPES[dtype])
+    scores = -10 * torch.rand(B, J, device=DEV, generator=gen)
+    check(logits, k, scores)
+    check(logits, k)
+    end = V // 2
+    check(logits, k, scores, torch.rand(B, J, device=DEV, generator=gen) < 0.4, end)
+    check(logits, k, scores, torch.ones(B, J, dtype=torch.uint8, device=DEV), end)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_ties_go_to_the_lowest(dtype):
+    t, gen = TYPES[dtype], gen_of(3)
+    for B, J, V, k in ((2, 4, 3000, 8), (1, 3, 100, 128), (3, 1, 70_000, 64), (1, 8, 33_333, 128)):
+        check(torch.zeros(B, J, V, device=DEV, dtype=t), k)  # all alike
+        few = torch.randint(0, 3, (B, 1, V), device=DEV, generator=gen).to(t).expand(B, J, V)  # beams alike, three values
+        check(few.contiguous(), k, torch.full((B, J), -1.5, device=DEV))
+        check(few, k)
+        check((torch.randint(0, 2, (B, J, V), device=DEV, generator=gen) * 5).to(t), k)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_orders_and_masks(dtype):
+    t, gen = TYPES[dtype], gen_of(4)
+    minus = float("-inf")
+    V = 30_000
+    rising = torch.linspace(-20, 20, V, device=DEV)
+    for x in (rising, rising.flip(0), torch.cat([rising[::2], rising[1::2].flip(0)])):
+        check(x.to(t).expand(2, 3, V).contiguous(), 100, torch.tensor([[-1.0, -2.0, -1.0]] * 2, device=DEV))
+    x = torch.randn(4, 3, V, device=DEV, generator=gen).to(t)
+    x[0] = minus  # nothing left
+    x[1, 1] = minus  # a beam with nothing left
+    x[2, :, 5:] = minus  # fewer than k left
+    x[3, 0, 77] = float("nan")  # a row that counts nothing
+    x[3, 1, V - 1] = float("inf")
+    r = check(x, 40, -torch.rand(4, 3, device=DEV, generator=gen))
+    assert (r.parents[0] == -1).all() and (r.tokens[0] == -1).all() and (r.scores[0] == minus).all() and not r.finished[0].any()
+    assert (r.parents[2] >= 0).sum() == 15
+    low = torch.finfo(t).min
+    y = torch.randn(1, 2, 2000, device=DEV, generator=gen).to(t)
+    y[..., 100:] = low  # masked by the lowest value there is
+    check(y, 128)
+    y[:] = low
+    check(y, 8)
+    # beams without a score
+    s = torch.tensor([[0.0, minus, minus]], device=DEV)
+    r = check(torch.randn(1, 3, 500, device=DEV, generator=gen).to(t), 8, s)
+    assert (r.parents == 0).all()
+    check(torch.randn(1, 3, 4, device=DEV, generator=gen).to(t), 8, s)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_strides_and_alignment(dtype):
+    t, gen = TYPES[dtype], gen_of(9)
+    base = torch.randn(3, 5, 4111, device=DEV, generator=gen).to(t)
+    check(base[:, 1:4, 3:4000], 10)
+    check(base[:, ::2, 1:], 10)
+    check(base.transpose(0, 1)[..., :4097], 10)
+    check(base[:1].expand(3, 5, 4111), 10)
+
+
+def test_more_candidates_above_the_bound_than_there_is_room_for():
+    """Thousands of equal candidates, or better and better ones, in the few segments that are read again."""
+    V = 120_000
+    for t in (torch.float32, torch.bfloat16):
+        x = torch.zeros(2, 1, V, device=DEV)
+        x[:, :, 40_000:60_000] = 4.0
+        x[1, :, 50_000] = 5.0
+        check(x.to(t), 128)
+        check(x.to(t), 1)
+        y = torch.zeros(1, 4, V, device=DEV)
+        y[..., 64_000:68_000] = 3 + torch.arange(4000, device=DEV) / 1000
+        check(y.to(t), 100)
+
+
+def test_results_do_not_change_and_replays():
+    gen = gen_of(31)
+    sets = [((torch.randn(6, 4, 9001, device=DEV, generator=gen) * 2).bfloat16(), -torch.rand(6, 4, device=DEV, generator=gen),
+             torch.rand(6, 4, device=DEV, generator=gen) < 0.3) for _ in range(3)]
+    want = [ops.beam_select(x, 4, s, finished=f, end=1) for x, s, f in sets]
+    held = [x.clone() for x in sets[0]]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        ops.beam_select(held[0], 4, held[1], finished=held[2], end=1)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = ops.beam_select(held[0], 4, held[1], finished=held[2], end=1)
+    for turn in range(6):
+        for a, b in zip(held, sets[turn % 3]):
+            a.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want[turn % 3])), turn
+        x, s, f = sets[(turn + 1) % 3]
+        assert all(torch.equal(a, b) for a, b in zip(ops.beam_select(x, 4, s, finished=f, end=1), want[(turn + 1) % 3]))
+    assert ops.beam_select(torch.zeros(0, 4, 10, device=DEV), 3).scores.shape == (0, 3)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_a_search(dtype):
+    """Beams over candidate nodes, their histories in a paged cache: append, attend, a dense layer, select, fork.  Every hypothesis that is
+    left, and its score, is that of a computation from its beginning without a cache."""
+    t, gen = TYPES[dtype], gen_of(12)
+    B, J, V, heads, group, dim, size, steps, end = 3, 4, 90, 2, 2, 32, 4, 11, 7
+    E, qh, rows = 48, heads * group, B * J
+    width = -(-(steps + 1) // size) + 1
+
+    def mat(*shape, std):
+        return (torch.randn(*shape, device=DEV, generator=gen) * std).to(t)
+
+    emb, w_in, w_out = mat(V, E, std=1.0), mat((qh + 2 * heads) * dim, E, std=E**-0.5), mat(V, qh * dim, std=3 * dim**-0.5)
+    freq = 100.0 ** (-torch.arange(dim // 2, device=DEV, dtype=F64) / (dim // 2))
+    i32 = dict(dtype=torch.int32, device=DEV)
+    pool = torch.arange(rows * 2 * (steps + 1), **i32)  # a page for every row and step, in two sets
+    pages = torch.randperm(pool.numel(), generator=gen, device=DEV).to(torch.int32).view(steps + 1, 2, rows)
+    k_cache = torch.full((pool.numel(), size, heads, dim), float("nan"), device=DEV, dtype=t)
+    v_cache = k_cache.clone()
+    table = torch.full((rows, width), -1, **i32)
+    table[:, 0] = pages[steps, 0]
+    lengths = torch.zeros(rows, **i32)
+    tokens = torch.randint(0, V, (B, 1), device=DEV, generator=gen).expand(B, J).contiguous()
+    start = tokens.clone()
+    scores = torch.full((B, J), float("-inf"), device=DEV)
+    scores[:, 0] = 0.0
+    finished = torch.zeros(B, J, dtype=torch.bool, device=DEV)
+    chosen = torch.zeros(rows, 0, dtype=torch.long, device=DEV)
+    for step in range(steps):
+        lengths += 1
+        x = ops.linear(emb[tokens.view(-1).clamp(min=0).long()], w_in).view(rows, qh + 2 * heads, dim)
+        q = ops.cache_append(k_cache, v_cache, table, lengths, x[:, qh : qh + heads], x[:, qh + heads :], q=x[:, :qh], freq=freq)
+        a = ops.cache_attend(q, k_cache, v_cache, table, lengths)
+        logits = ops.linear(a.view(rows, qh * dim), w_out).view(B, J, V)
+        r = ops.beam_select(logits, J, scores, finished=finished, end=end)
+        table, lengths = ops.cache_fork(k_cache, v_cache, table, lengths, r.parents, pages[step, 0])
+        scores, finished, tokens = r.scores, r.finished, r.tokens
+        assert (r.parents >= 0).all()
+        chosen = torch.cat([chosen[r.parents.view(-1).long()], tokens.view(-1, 1).long()], 1)
+    torch.cuda.synchronize()
+    # from the beginning, in 64 bits but for the values that are kept in the type (and so are the same numbers here up to their rounding)
+    def keep(y):
+        return y.to(t).to(F64)
+
+    worst = 0.0
+    for row in range(rows):
+        seq = [int(start.view(-1)[row])] + chosen[row].tolist()
+        total, over = 0.0, False
+        x = keep(emb[torch.tensor(seq, device=DEV)].to(F64) @ w_in.to(F64).t()).view(len(seq), qh + 2 * heads, dim)
+        angle = torch.outer(torch.arange(len(seq), device=DEV, dtype=F64), freq)[:, None, :]
+        c, s = angle.cos(), angle.sin()
+        u, v = x[:, : qh + heads, : dim // 2], x[:, : qh + heads, dim // 2 :]
+        z = keep(torch.cat([u * c - v * s, v * c + u * s], -1))
+        for n in range(steps):
+            if over:
+                assert seq[n + 1] == end
+                continue
+            out = []
+            for h in range(qh):
+                p = torch.softmax(z[n, h] @ z[: n + 1, qh + h // group].t() * dim**-0.5, -1)
+                out.append(p @ x[: n + 1, qh + heads + h // group])
+            logp = torch.log_softmax(keep(keep(torch.cat(out)) @ w_out.to(F64).t()), -1)
+            total += float(logp[seq[n + 1]])
+            over = seq[n + 1] == end
+        worst = max(worst, abs(total - float(scores.view(-1)[row])))
+        assert over == bool(finished.view(-1)[row])
+    # logits of a few units, each a rounding (and a chain of five kept values' roundings, which differ where fp32 sums fall on the other side) off:
+    # fp32 chains of 1e-6 a step; bf16 two steps of 2^-8 of a logit below 16 and of its row's log-sum, each step
+    limit = steps * (2e-5 if dtype == "fp32" else 4 * 16 * 2.0**-8)
+    assert worst <= limit, (worst, limit)
+    assert math.isfinite(worst)

@@ -1,0 +1,430 @@
+"""The paged cache (ops.cache_append, ops.cache_attend, ops.cache_fork) against its formulas in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from paper_2308_14129_amd import ops
+from tests.paged import DEV, F64, LAYOUTS, TYPES, U, attention, close, gather, gen_of, half, make_cache, make_table, tiny
+
+pytestmark = [pytest.mark.gpu, pytest.mark.timeout(120)]
+
+
+def bits(t):
+    return t.contiguous().view(torch.uint8).clone()
+
+
+def fill_rows(cache, table, lengths, gen, std=1.0):
+    """Random rows where sequences have them, NaN stays elsewhere."""
+    size = cache.shape[1]
+    for i, n in enumerate(lengths):
+        if n > 0:
+            p = torch.arange(n, device=DEV)
+            rows = torch.randn(n, *cache.shape[2:], device=DEV, generator=gen, dtype=F64) * std
+            cache[table[i].long()[p // size], p % size] = rows.to(cache.dtype)
+
+
+# --------------------------------------------------------------------------- append
+
+
+def rotated(x, pos, freq, interleaved):
+    r = 2 * freq.numel()
+    y, a = x.to(F64).clone(), torch.outer(pos.to(F64), freq)[:, None, :]
+    c, s = a.cos(), a.sin()
+    first, second = (slice(0, r, 2), slice(1, r, 2)) if interleaved else (slice(0, r // 2), slice(r // 2, r))
+    u, v = x[..., first].to(F64), x[..., second].to(F64)
+    y[..., first], y[..., second] = u * c - v * s, v * c + u * s
+    size = y.abs()  # of the terms
+    size[..., first], size[..., second] = u.abs() * c.abs() + v.abs() * s.abs(), v.abs() * c.abs() + u.abs() * s.abs()
+    return y, size
+
+
+APPEND = [
+    # heads, query heads, dim, page, rotary, interleaved, positions, layout, new tokens of each sequence (None: one each)
+    (1, 1, 8, 1, 8, False, "place", "rows", None), (2, 2, 50, 20, 50, True, "time", "rows", None), (8, 32, 128, 16, 128, False, "place", "heads", None),
+    (3, 0, 100, 7, 100, False, "int64", "kv", None), (2, 6, 64, 32, 32, False, "place", "pairs", [3, 0, 17, 1, 64, 0]),
+    (4, 4, 256, 16, 256, True, "int64", "outer", [40, 1, 5]), (1, 5, 33, 9, 20, True, "time", "padded", [2, 2, 90]), (2, 8, 72, 64, 0, False, "place", "rows", [7, 100]),
+    (2, 3, 19, 5, 18, False, "place", "padded", [11]), (1, 1, 17, 3, 2, False, "int64", "heads", None), (2, 2, 24, 65, 22, False, "time", "kv", [1, 1, 1, 200]),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", APPEND, ids=lambda c: "-".join(map(str, c[:8])))
+def test_append(case, dtype):
+    heads, qh, dim, size, rotary, interleaved, where, layout, new = case
+    t, gen = TYPES[dtype], gen_of(dim)
+    counts = [1] * 13 if new is None else new
+    old = torch.randint(0, 3 * size + 2, (len(counts),), device=DEV, generator=gen).tolist()
+    lengths = [o + c for o, c in zip(old, counts)]
+    width = -(-max(lengths) // size) + 2
+    table, pages, _ = make_table(lengths, size, width, 3, gen)
+    k_cache, v_cache = make_cache(pages, size, heads, dim, t, layout)
+    tokens = sum(counts)
+    first, behind = (2, 3) if new is not None else (0, 0)  # tokens that are nobody's
+    qkv = torch.randn(tokens + first + behind, qh + 2 * heads, dim, device=DEV, generator=gen).to(t)
+    q, k, v = (qkv[:, :qh] if qh else None), qkv[:, qh : qh + heads], qkv[:, qh + heads :]
+    freq = 10000.0 ** (-torch.arange(rotary // 2, device=DEV, dtype=F64) / max(1, rotary // 2)) if rotary else None
+    n = qkv.shape[0]
+    positions = None
+    if where == "int64":
+        positions = torch.randint(-(1 << 40), 1 << 40, (n,), device=DEV, generator=gen)
+    elif where == "time":
+        positions = torch.rand(n, device=DEV, generator=gen, dtype=F64) * 2.6e6
+    starts = None
+    if new is not None:
+        starts = torch.tensor([first] + [first + sum(counts[: i + 1]) for i in range(len(counts))], dtype=torch.int32, device=DEV)
+    L = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    want_k, want_v = k_cache.to(F64), v_cache.to(F64)
+    tol_k = torch.zeros_like(want_k)
+    place = torch.cat([torch.arange(o, o + c) for o, c in zip(old, counts)]).to(DEV)
+    seq = torch.cat([torch.full((c,), i) for i, c in enumerate(counts)]).to(DEV)
+    page, row = table.long()[seq, place // size], place % size
+    inner = slice(first, first + tokens)
+
+    def turned(x):
+        if not rotary:
+            return x.to(F64), torch.zeros((), dtype=F64, device=DEV)
+        y, mag = rotated(x, place if positions is None else positions[inner], freq, interleaved)
+        # products and their sum: 4 units; cosine and sine rounded, and 1e-11 off; the angle is the same product in both
+        tol = half(t) * y.abs() + 8 * U * mag + tiny(t)
+        tol[..., rotary:] = 0
+        return y, tol
+
+    yk, tk = turned(k[inner])
+    want_k[page, row], want_v[page, row] = yk, v[inner].to(F64)
+    tol_k[page, row] = tk + 0 * yk
+    out = torch.full((n, qh, dim), 7.0, dtype=t, device=DEV) if qh else None
+    before = bits(qkv)
+    print(f"[append] {case} {dtype}", flush=True)
+    got = ops.cache_append(k_cache, v_cache, table, L, k, v, starts=starts, q=q, freq=freq, positions=positions, interleaved=interleaved, q_out=out)
+    torch.cuda.synchronize()
+    assert torch.equal(bits(qkv), before)
+    close(k_cache, want_k, tol_k, "k")
+    close(v_cache, want_v, torch.zeros_like(want_v), "v")
+    if qh:
+        assert got is out
+        yq, tq = turned(q[inner])
+        close(out[inner], yq, tq + 0 * yq, "q")
+        assert (out[:first] == 7).all() and (out[first + tokens :] == 7).all()
+        # in place, and into memory of its own
+        again = ops.cache_append(k_cache, v_cache, table, L, k, v, starts=starts, q=q, freq=freq, positions=positions, interleaved=interleaved)
+        assert torch.equal(again[inner], out[inner])
+        ops.cache_append(k_cache, v_cache, table, L, k, v, starts=starts, q=q, freq=freq, positions=positions, interleaved=interleaved, q_out=q)
+        assert torch.equal(q[inner], out[inner])
+        left = torch.cat([q[:first], q[first + tokens :]])
+        assert torch.equal(left, torch.cat([qkv[:first, :qh], qkv[first + tokens :, :qh]])) and torch.equal(bits(qkv[:, qh:]), bits(before.view(t).view_as(qkv)[:, qh:]))
+    else:
+        assert got is None
+
+
+def test_append_leaves_out_what_has_no_row():
+    t, size = torch.float32, 4
+    k_cache, v_cache = make_cache(6, size, 2, 16, t, "rows", fill=0.0)
+    #                     no page        beyond     length 0 / -3      fine
+    table = torch.tensor([[0, -1], [1, 6], [2, 3], [2, 3], [2, 3], [4, 5]], dtype=torch.int32, device=DEV)
+    lengths = torch.tensor([5, 8, 9, 0, -3, 8], dtype=torch.int32, device=DEV)
+    k = torch.randn(6, 2, 16, device=DEV)
+    out = torch.full_like(k, 7.0)
+    ops.cache_append(k_cache, v_cache, table, lengths, k, k, q=k, q_out=out)
+    torch.cuda.synchronize()
+    assert (out[:5] == 7).all() and torch.equal(out[5], k[5])
+    assert torch.equal(k_cache[5, 3], k[5]) and torch.equal(v_cache[5, 3], k[5])
+    k_cache[5, 3] = 0
+    v_cache[5, 3] = 0
+    assert not k_cache.any() and not v_cache.any()
+    # more new tokens than the sequence is long: the first of them have no row
+    starts = torch.tensor([0, 6], dtype=torch.int32, device=DEV)
+    out.fill_(7.0)
+    ops.cache_append(k_cache, v_cache, table[5:], torch.tensor([2], dtype=torch.int32, device=DEV), k, k, starts=starts, q=k, q_out=out)
+    assert (out[:4] == 7).all() and torch.equal(out[4:], k[4:]) and torch.equal(k_cache[4, :2], k[4:]) and not k_cache[4, 2:].any()
+    # starts that are not in order reach nothing that is not there
+    starts = torch.tensor([5, -9, 1 << 30, 3, -(1 << 31), 2, 6], dtype=torch.int32, device=DEV)
+    ops.cache_append(k_cache, v_cache, table, lengths, k, k, starts=starts, q=k, q_out=out)
+    torch.cuda.synchronize()
+
+
+def test_append_far_pages():
+    """Pages that lie more than 2^32 bytes into the cache."""
+    t = torch.float16
+    pages, size, heads, dim = 36000, 64, 8, 128  # 4.7 GB each
+    k_cache = torch.zeros(pages, size, heads, dim, dtype=t, device=DEV)
+    v_cache = torch.zeros_like(k_cache)
+    table = torch.tensor([[pages - 1], [0]], dtype=torch.int32, device=DEV)
+    lengths = torch.tensor([64, 1], dtype=torch.int32, device=DEV)
+    gen = gen_of(3)
+    k_cache[-1].copy_(torch.randn(size, heads, dim, device=DEV, generator=gen))
+    v_cache[-1].copy_(torch.randn(size, heads, dim, device=DEV, generator=gen))
+    k = torch.randn(2, heads, dim, device=DEV, generator=gen).to(t)
+    ops.cache_append(k_cache, v_cache, table, lengths, k, k)
+    assert torch.equal(k_cache[-1, 63], k[0]) and torch.equal(v_cache[-1, 63], k[0]) and torch.equal(k_cache[0, 0], k[1])
+    q = torch.randn(2, 16, dim, device=DEV, generator=gen).to(t)
+    out, lse = ops.cache_attend(q, k_cache, v_cache, table, lengths, lse=True)
+    ref, rl, tol, tl = attention(q, k_cache, v_cache, table, lengths, dim**-0.5, 0)
+    close(out, ref, tol, "out")
+    close(lse, rl, tl, "lse")
+    table2, n2 = ops.cache_fork(k_cache, v_cache, table, torch.tensor([50, 1], dtype=torch.int32, device=DEV), torch.tensor([0], dtype=torch.int32, device=DEV),
+                                torch.tensor([pages - 2], dtype=torch.int32, device=DEV))
+    assert table2.tolist() == [[pages - 2]] and n2.tolist() == [50]
+    assert torch.equal(k_cache[-2, :50], k_cache[-1, :50]) and torch.equal(v_cache[-2, :50], v_cache[-1, :50]) and not k_cache[-2, 50:].any()
+
+
+# --------------------------------------------------------------------------- attend
+
+ATTEND = [
+    # heads, group, dim, page, lengths, window, layout
+    (1, 1, 8, 16, [1], 0, "rows"), (1, 1, 64, 16, [0, 1, 2, 15, 16, 17, 31, 32, 33], 0, "rows"), (2, 4, 128, 16, [1000], 0, "rows"),
+    (2, 1, 50, 20, [0, 3, 200, 21, 1], 0, "rows"), (8, 4, 128, 64, [700, 64, 65, 1, 0, 513], 0, "heads"), (1, 16, 100, 1, [77, 5], 0, "kv"),
+    (3, 5, 72, 7, [300, 7, 8], 0, "pairs"), (1, 17, 128, 32, [257, 90], 0, "outer"), (1, 40, 64, 48, [130, 1], 0, "rows"), (2, 3, 256, 16, [333, 48], 0, "heads"),
+    (1, 20, 200, 80, [90, 411], 0, "rows"), (2, 2, 130, 33, [100, 34], 0, "padded"), (1, 2, 9, 16, [40, 3], 0, "padded"), (4, 2, 63, 16, [95, 2], 0, "padded"),
+    (2, 2, 64, 16, [1000, 10, 0, 129], 100, "rows"), (1, 8, 128, 24, [500, 64], 1, "heads"), (2, 1, 96, 16, [640, 20], 33, "kv"), (1, 33, 65, 5, [66], 64, "rows"),
+    (1, 64, 128, 16, [40], 0, "rows"), (2, 2, 12, 256, [1, 2, 3, 600], 0, "outer"),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", ATTEND, ids=lambda c: "-".join(map(str, (*c[:4], max(c[4]), c[5], c[6]))))
+def test_attend(case, dtype):
+    heads, group, dim, size, lengths, window, layout = case
+    t, gen = TYPES[dtype], gen_of(dim + size)
+    table, pages, _ = make_table(lengths, size, -(-max(lengths) // size) + 1, 2, gen)
+    k_cache, v_cache = make_cache(pages, size, heads, dim, t, layout)
+    fill_rows(k_cache, table, lengths, gen)
+    fill_rows(v_cache, table, lengths, gen)
+    L = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    q = torch.randn(len(lengths), heads * group + 2, dim + 1, device=DEV, generator=gen).to(t)[:, 1:-1, 1:]
+    for scale in (dim**-0.5, -0.3, 0.0):
+        print(f"[attend] {case} {dtype} scale {scale}", flush=True)
+        out, lse = ops.cache_attend(q, k_cache, v_cache, table, L, scale=scale, window=window, lse=True)
+        torch.cuda.synchronize()
+        ref, rl, tol, tl = attention(q, k_cache, v_cache, table, L, scale, window)
+        close(out, ref, tol, "out")
+        close(lse, rl, tl, "lse")
+    # without lse, into a view, and in place: the same bits
+    out = ops.cache_attend(q, k_cache, v_cache, table, L, window=window)
+    view = torch.zeros(len(lengths), dim, heads * group + 3, device=DEV, dtype=t)
+    into = torch.zeros(heads * group, len(lengths), dim + 2, device=DEV, dtype=t).transpose(0, 1)[..., 1:-1]
+    assert ops.cache_attend(q, k_cache, v_cache, table, L, window=window, out=into) is into and torch.equal(into, out)
+    ops.cache_attend(q, k_cache, v_cache, table, L, window=window, out=q)
+    assert torch.equal(q, out) and not view.any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", [16, 12])
+def test_attend_many_lengths(size, dtype):
+    """Every way that a sequence can lie in the dealt-out line: hundreds of lengths, short and long ones side by side."""
+    t, gen = TYPES[dtype], gen_of(5)
+    lengths = [0, 1, 3000] + [int(x) for x in torch.randint(0, 200, (150,), generator=torch.Generator().manual_seed(1))] + [2500, 0, 0, 40, 5000, 17]
+    table, pages, _ = make_table(lengths, size, -(-5000 // size), 2, gen)
+    k_cache, v_cache = make_cache(pages, size, 2, 64, t, "rows")
+    fill_rows(k_cache, table, lengths, gen)
+    fill_rows(v_cache, table, lengths, gen)
+    L = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    q = torch.randn(len(lengths), 6, 64, device=DEV, generator=gen).to(t)
+    out, lse = ops.cache_attend(q, k_cache, v_cache, table, L, lse=True)
+    ref, rl, tol, tl = attention(q, k_cache, v_cache, table, L, 0.125, 0)
+    close(out, ref, tol, "out")
+    close(lse, rl, tl, "lse")
+    for _ in range(3):
+        again = ops.cache_attend(q, k_cache, v_cache, table, L, lse=True)
+        assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attend_a_long_sequence(dtype):
+    t, gen, n = TYPES[dtype], gen_of(6), 100_003
+    table, pages, _ = make_table([n, 5], 16, -(-n // 16), 0, gen)
+    k_cache, v_cache = make_cache(pages, 16, 1, 64, t, "rows")
+    for c in (k_cache, v_cache):
+        fill_rows(c, table, [n, 5], gen)
+    # one row weighs as much as all the others together: half of a value, whatever the small weights are rounded to
+    q = torch.randn(2, 3, 64, device=DEV, generator=gen).to(t)
+    far = table[0].long()[70_000 // 16]
+    k_cache[far, 0, 0] = q[0, 0] * (8 * (math.log(n) + 0.5) / float(q[0, 0].float().square().sum()))
+    L = torch.tensor([n, 5], dtype=torch.int32, device=DEV)
+    out, lse = ops.cache_attend(q, k_cache, v_cache, table, L, lse=True)
+    ref, rl, tol, tl = attention(q, k_cache, v_cache, table, L, 0.125, 0)
+    close(out, ref, tol, "out")
+    close(lse, rl, tl, "lse")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", [16, 10])
+def test_attend_pages_that_are_not_there(size, dtype):
+    t, gen = TYPES[dtype], gen_of(8)
+    lengths = [5 * size, 5 * size, 3 * size + 1, 2 * size, 5 * size + 9]
+    table, pages, _ = make_table([5 * size] * 5, size, 5, 0, gen)
+    k_cache, v_cache = make_cache(pages, size, 2, 40, t, "rows")
+    for c in (k_cache, v_cache):
+        fill_rows(c, table, [5 * size] * 5, gen)
+    table[0, 1], table[0, 3] = -1, pages  # rows between others
+    table[1] = torch.tensor([-1, pages, 1 << 30, -(1 << 31), (1 << 31) - 1], dtype=torch.int32)  # none at all
+    table[2, 3] = -7
+    L = torch.tensor(lengths, dtype=torch.int32, device=DEV)  # the last one is longer than its table
+    q = torch.randn(5, 4, 40, device=DEV, generator=gen).to(t)
+    for window in (0, size + 3):
+        out, lse = ops.cache_attend(q, k_cache, v_cache, table, L, window=window, lse=True)
+        ref, rl, tol, tl = attention(q, k_cache, v_cache, table, L, 40**-0.5, window)
+        close(out, ref, tol, "out")
+        close(lse, rl, tl, "lse")
+        assert not out[1].any() and (lse[1] == float("-inf")).all()
+
+
+def test_attend_values_at_the_edges():
+    """Infinite and NaN rows count where they are seen, and nowhere else."""
+    t, size = torch.float32, 16
+    table = torch.arange(8, dtype=torch.int32, device=DEV).view(2, 4)
+    k_cache, v_cache = torch.randn(8, size, 1, 32, device=DEV), torch.randn(8, size, 1, 32, device=DEV)
+    L = torch.tensor([50, 50], dtype=torch.int32, device=DEV)
+    q = torch.rand(2, 2, 32, device=DEV) + 0.5
+    clean = ops.cache_attend(q, k_cache, v_cache, table, L)
+    k_cache[3, 2:], v_cache[3, 2:] = float("nan"), float("inf")  # behind the end
+    assert torch.equal(ops.cache_attend(q, k_cache, v_cache, table, L), clean)
+    v_cache[1, 3] = float("nan")  # a row of the first sequence
+    out = ops.cache_attend(q, k_cache, v_cache, table, L)
+    assert torch.isnan(out[0]).all() and torch.equal(out[1], clean[1])
+    assert torch.equal(ops.cache_attend(q, k_cache, v_cache, table, L, window=20)[1], ops.cache_attend(q, k_cache, v_cache, table, L, window=20)[1])
+    assert not torch.isnan(ops.cache_attend(q, k_cache, v_cache, table, L, window=50 - 20)).any()
+    v_cache[1, 3] = 0.0
+    k_cache[1, 3] = float("-inf")  # a score of -infinity: no weight
+    k_cache[5, 3] = float("nan")
+    out, lse = ops.cache_attend(q, k_cache, v_cache, table, L, lse=True)
+    assert torch.isfinite(out[0]).all() and torch.isfinite(lse[0]).all() and torch.isnan(out[1]).all() and torch.isnan(lse[1]).all()
+    # scores far apart and far from zero
+    k_cache.fill_(0.0)
+    k_cache[0, 7] = 1e5
+    v_cache.copy_(torch.randn_like(v_cache))
+    out, lse = ops.cache_attend(q, k_cache, v_cache, table, L, lse=True)
+    assert torch.equal(out[0], v_cache[0, 7].expand(2, 32)) and torch.isfinite(lse).all()
+    assert t is out.dtype
+
+
+# --------------------------------------------------------------------------- fork
+
+FORK = [
+    # heads, dim, page, lengths, layout, parents
+    (2, 16, 4, [5, 0, 8, 3], "rows", [0, 0, 2, 3, 1, 2, 0]), (8, 128, 16, [100, 16, 31], "heads", [2, 2, 1, 0, 0]), (1, 9, 7, [20, 7], "padded", [1, 0, 1, -1, 5, 0]),
+    (3, 50, 20, [59, 1], "kv", [0, 1, 1]), (2, 33, 1, [4, 2], "pairs", [1, 0]), (4, 64, 64, [200, 63], "outer", [0, 0, 0, 1]),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", FORK, ids=lambda c: "-".join(map(str, (*c[:3], c[4]))))
+def test_fork(case, dtype):
+    heads, dim, size, lengths, layout, parents = case
+    t, gen = TYPES[dtype], gen_of(dim)
+    width = max(lengths) // size + 1
+    table, pages, free = make_table(lengths, size, width, len(parents) + 2, gen)
+    k_cache, v_cache = make_cache(pages, size, heads, dim, t, layout)
+    for c in (k_cache, v_cache):
+        fill_rows(c, table, lengths, gen)
+    spare = torch.tensor(free[: len(parents)], dtype=torch.int32, device=DEV)
+    own = torch.ones(len(parents), dtype=torch.bool)
+    if len(parents) > 2:
+        spare[1], own[1] = -1, False
+    want = [c.clone() for c in (k_cache, v_cache)]
+    L, P = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in (lengths, parents))
+    new, sizes = ops.cache_fork(k_cache, v_cache, table, L, P, spare)
+    torch.cuda.synchronize()
+    for r, p in enumerate(parents):
+        n = lengths[p] if 0 <= p < len(lengths) else 0
+        assert int(sizes[r]) == n
+        full, left = n // size, n % size
+        line = (table[p, :full].tolist() if n else []) + [(int(table[p, full]) if left else -1) if not own[r] else int(spare[r])]
+        assert new[r].tolist() == line + [-1] * (width - len(line))
+        if own[r] and left:
+            for c in want:
+                c[int(spare[r]), :left] = c[int(table[p, full]), :left]
+    for c, w in zip((k_cache, v_cache), want):
+        assert torch.equal(bits(c), bits(w))
+
+
+def test_fork_with_full_tables_and_missing_pages():
+    k_cache, v_cache = make_cache(9, 4, 1, 8, torch.float32, "rows", fill=1.0)
+    table = torch.tensor([[0, 1], [2, -1], [3, 4]], dtype=torch.int32, device=DEV)
+    lengths = torch.tensor([8, 6, 99], dtype=torch.int32, device=DEV)
+    spare = torch.tensor([5, 6, 7, 9], dtype=torch.int32, device=DEV)
+    k_cache[6] = 2.0
+    new, sizes = ops.cache_fork(k_cache, v_cache, table, lengths, torch.tensor([0, 1, 2, 3], dtype=torch.int32, device=DEV), spare)
+    # full: no place for the spare page; on no page: still none; longer than its table: cut; no parent and no page: nothing
+    assert new.tolist() == [[0, 1], [2, -1], [3, 4], [-1, -1]] and sizes.tolist() == [8, 6, 8, 0]
+    assert (k_cache[6] == 2).all() and (k_cache[7] == 1).all()
+
+
+# --------------------------------------------------------------------------- beside other work
+
+
+def test_captured_and_on_two_streams():
+    gen = gen_of(21)
+    t, size, n = torch.bfloat16, 16, 40
+
+    def setup(seed):
+        g = gen_of(seed)
+        lengths = [int(x) for x in torch.randint(1, 1500, (n,), generator=torch.Generator().manual_seed(seed))]
+        table, pages, _ = make_table(lengths, size, 100, 1, g)
+        k_cache, v_cache = make_cache(pages, size, 2, 64, t, "rows")
+        for c in (k_cache, v_cache):
+            fill_rows(c, table, lengths, g)
+        return k_cache, v_cache, table, torch.tensor(lengths, dtype=torch.int32, device=DEV), torch.randn(n, 12, 64, device=DEV, generator=g).to(t)
+
+    freq = 100.0 ** (-torch.arange(32, device=DEV, dtype=F64) / 32)
+
+    def call(k_cache, v_cache, table, lengths, qkv):
+        q = ops.cache_append(k_cache, v_cache, table, lengths, qkv[:, 8:10], qkv[:, 10:], q=qkv[:, :8], freq=freq)
+        return ops.cache_attend(q, k_cache, v_cache, table, lengths, lse=True)
+
+    sets = [setup(s) for s in (1, 2, 3)]
+    want = [[x.clone() for x in call(*s)] for s in sets]
+    pages = max(s[0].shape[0] for s in sets)
+    held = [torch.zeros(pages, size, 2, 64, dtype=t, device=DEV), torch.zeros(pages, size, 2, 64, dtype=t, device=DEV), *(x.clone() for x in sets[0][2:])]
+
+    def put(s):
+        for a, b in zip(held, s):
+            a[: b.shape[0]].copy_(b)
+
+    put(sets[0])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call(*held)
+    torch.cuda.current_stream().wait_stream(side)
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            got = call(*held)
+        graphs.append((g, got))
+    for turn in range(6):
+        put(sets[turn % 3])
+        g, got = graphs[turn % 2]
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want[turn % 3])), turn
+        torch.randn(300, 300, device=DEV, generator=gen).sum()
+        assert all(torch.equal(a, b) for a, b in zip(call(*sets[(turn + 1) % 3]), want[(turn + 1) % 3]))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for turn in range(4):
+        with torch.cuda.stream(streams[turn % 2]):
+            got.append(call(*sets[turn % 2]))
+    torch.cuda.synchronize()
+    for turn in range(4):
+        assert all(torch.equal(a, b) for a, b in zip(got[turn], want[turn % 2]))
+
+
+def test_empty_calls():
+    k_cache, v_cache = make_cache(2, 16, 2, 32, torch.float32, "rows", fill=0.0)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    none = torch.zeros(0, 3, **i32), torch.zeros(0, **i32)
+    x = torch.zeros(0, 2, 32, device=DEV)
+    assert ops.cache_append(k_cache, v_cache, *none, x, x, q=x).shape == (0, 2, 32)
+    out, lse = ops.cache_attend(x, k_cache, v_cache, *none, lse=True)
+    assert out.shape == (0, 2, 32) and lse.shape == (0, 2)
+    table, n = ops.cache_fork(k_cache, v_cache, *none, torch.zeros(0, **i32), torch.zeros(0, **i32))
+    assert table.shape == (0, 3) and n.shape == (0,)
+    table, n = ops.cache_fork(k_cache, v_cache, *none, torch.tensor([0], **i32), torch.tensor([1], **i32))
+    assert table.tolist() == [[1, -1, -1]] and n.tolist() == [0]
+    # tokens, but no sequence: nobody's
+    y = torch.ones(3, 2, 32, device=DEV)
+    ops.cache_append(k_cache, v_cache, *none, y, y, starts=torch.zeros(1, **i32))
+    assert not k_cache.any() and gather(k_cache, torch.zeros(1, 1, **i32), 0, 0, 3)[1].all()
