@@ -738,9 +738,9 @@ typedef struct tig_cache {
     int32_t page_size;      /* 1 .. 2^16 */
     int32_t heads;          /* 1 .. 2^10 */
     int32_t head_dim;       /* 8 .. 256 */
-    int32_t max_pages;      /* 1 .. 2^24, max_pages * page_size < 2^31 */
+    int32_t max_pages;      /* 1 .. 2^24, max_pages * page_size <= 2^31 - 2^16 */
     void *k, *v;            /* element (page, row, head, column) at page * page_stride + row * token_stride + head * head_stride + column */
-    int64_t page_stride, token_stride, head_stride; /* elements, 0 .. 2^40; page_size * token_stride bytes, and a page's own, < 2^31 */
+    int64_t page_stride, token_stride, head_stride; /* elements, 0 .. 2^40; page_size * token_stride bytes, and a page's own, <= 2^30 */
 } tig_cache;
 
 /* New tokens of many sequences enter the cache: values as they are, keys rotated by their position, and queries that come with them

@@ -2,8 +2,8 @@
 //
 //   score of candidate (j, v) = scores_j + l_jv - log sum_u exp l_ju, the k largest, ties to the lowest (j, v)
 //
-//   k_select_segments  reads the logits once: for every segment (a sixteenth of a wavefront's stretch) its largest logit and the sum of
-//                      exp(l - largest); bound by memory
+//   k_select_segments  reads the logits once: for every segment (a lane's `steps` times eight logits of a wavefront's stretch) its largest
+//                      logit, for every stretch the sum of exp(l - largest); bound by memory
 //   k_select_pick      a workgroup per batch entry: log-sums from the segments'; a bound that at least k candidates reach; the few
 //                      segments that reach it are read again, and the candidates at or above it are ranked
 // Which bound: the segments are dealt to 128 groups of threads, and the k-th largest of the groups' maxima is the score of a candidate
@@ -12,8 +12,7 @@
 // beams with log-sums whose error, fp32 exponentials' of random sign over a vocabulary, is about 1e-8.
 #include <cmath>
 
-#include "act.h"
-#include "gemm.h"
+#include "cache.h"
 
 namespace tig {
 
@@ -23,11 +22,15 @@ struct SelectArgs {
     const void *logits;
     int64_t l_batch, l_beam;  // elements
     int64_t batch;
-    int32_t beams, k, vocab, steps, chunks;  // steps of 512 logits per wavefront; wavefronts per row
+    int32_t beams, k, vocab;
+    // a row: `chunks` chunks of `steps` times 512 logits, 64 segments each; a wavefront's stretch is `per` chunks
+    int32_t steps, chunks, per, stretches;
+    PageDiv by_segments, by_steps;  // divisions by a row's segments, and by `steps`
     const float *scores;
     const uint8_t *finished;
     int32_t end;
-    float2 *seg;  // [batch x beams][chunks x 4]: largest logit, sum of exp(l - largest)
+    float *top;     // [batch x beams][chunks x 64]: largest logit of a segment
+    float2 *sums;   // [batch x beams][stretches]: largest logit, sum of exp(l - largest)
     float *scores_out;
     int32_t *parents, *tokens;
     uint8_t *finished_out;
@@ -56,46 +59,89 @@ __device__ inline void load_eight(const T *row, int at, int vocab, float (&x)[8]
 
 constexpr float kLog2e = 1.44269504f;
 
+// written out: the compiler would canonicalise every operand.  A NaN loses: the row's sum has it.
+__device__ inline float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(256) k_select_segments(SelectArgs a)
 {
+    constexpr int kDeep = 4;  // steps whose logits are on their way together
     const int lane = lane_id();
     const int64_t id = (int64_t)blockIdx.x * 4 + wave_id_uniform();
-    const int64_t r = id / a.chunks;
-    const int chunk = (int)(id - r * a.chunks);
+    const int64_t r = id / a.stretches;
+    const int stretch = (int)(id - r * a.stretches);
     if (r >= a.batch * a.beams)
         return;
+    const bool done = a.finished && a.finished[r];
     float m = -INFINITY, s = 0.0f;
-    if (!a.finished || !a.finished[r]) {
-        const T *const row = (const T *)a.logits + r / a.beams * a.l_batch + r % a.beams * a.l_beam;
-        for (int t = 0; t < a.steps; ++t) {
-            const int at = (chunk * a.steps + t) * 512 + lane * 8;
-            float x[8];
-            load_eight(row, at, a.vocab, x);
-            float top = m;
+    const T *const row = (const T *)a.logits + r / a.beams * a.l_batch + r % a.beams * a.l_beam;
+    const int c0 = stretch * a.per, c1 = std::min(a.chunks, c0 + a.per);
+    for (int c = c0; c < c1; ++c) {
+        float seg = -INFINITY;
+        for (int t0 = 0; t0 < a.steps && !done; t0 += kDeep) {
+            float x[kDeep][8];
+            const int base = (c * a.steps + t0) * 512;
+            if (t0 + kDeep <= a.steps && base + kDeep * 512 <= a.vocab) {
+                Eight<T> q[kDeep];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                top = x[e] > top || x[e] != x[e] ? x[e] : top;  // (a NaN stays)
+                for (int t = 0; t < kDeep; ++t)
+                    q[t] = *(const Eight<T> *)(row + base + t * 512 + lane * 8);
+#pragma unroll
+                for (int t = 0; t < kDeep; ++t)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        x[t][e] = to_float(q[t].v[e]);
+            } else {
+#pragma unroll
+                for (int t = 0; t < kDeep; ++t)
+                    if (t0 + t < a.steps) {
+                        load_eight(row, base + t * 512 + lane * 8, a.vocab, x[t]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            x[t][e] = -INFINITY;
+                    }
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < kDeep; ++t)
+#pragma unroll
+                for (int e = 0; e < 8; e += 2)
+                    top = max3(x[t][e], x[t][e + 1], top);
+            seg = fmaxf(seg, top);
+            top = fmaxf(m, top);
             const float from = top == -INFINITY ? 0.0f : top;
             s *= __builtin_amdgcn_exp2f((m - from) * kLog2e);
+            float add[kDeep];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                s += __builtin_amdgcn_exp2f((x[e] - from) * kLog2e);
+            for (int t = 0; t < kDeep; ++t) {
+                add[t] = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    add[t] += __builtin_amdgcn_exp2f((x[t][e] - from) * kLog2e);
+            }
+#pragma unroll
+            for (int t = 0; t < kDeep; ++t)
+                s += add[t];
             m = top;
         }
+        a.top[(r * a.chunks + c) * 64 + lane] = seg;
     }
     float top = m;
 #pragma unroll
-    for (int d = 1; d < 16; d *= 2) {
-        const float other = __shfl_xor(top, d);
-        top = other > top || other != other ? other : top;
-    }
+    for (int d = 1; d < 64; d *= 2)
+        top = fmaxf(top, __shfl_xor(top, d));
     s *= __builtin_amdgcn_exp2f((m - (top == -INFINITY ? 0.0f : top)) * kLog2e);
 #pragma unroll
-    for (int d = 1; d < 16; d *= 2)
+    for (int d = 1; d < 64; d *= 2)
         s += __shfl_xor(s, d);
-    if (lane % 16 == 0)
-        a.seg[(r * a.chunks + chunk) * 4 + lane / 16] = {top, s};
+    if (lane == 0)
+        a.sums[r * a.stretches + stretch] = {top, s};
 }
 
 constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64, kGroups = 128, kMaxBeams = 64, kMaxK = 128;
@@ -146,8 +192,14 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
     __shared__ PickShared sh;
     const int tid = threadIdx.x, lane = lane_id(), wave = wave_id_uniform();
     const int64_t b = blockIdx.x;
-    const int per_beam = a.chunks * 4, all = a.beams * per_beam;
-    const float2 *const seg = a.seg + b * all;
+    const int per_beam = a.chunks * 64, all = a.beams * per_beam, n_sums = a.stretches;
+    const float *const seg = a.top + b * all;
+    const float2 *const sums = a.sums + b * a.beams * n_sums;
+    constexpr int kMine = kMaxSegments / kPickThreads;
+    float mine[kMine];  // the thread's segments tid, tid + 1024, ..: asked for ahead of all else
+#pragma unroll
+    for (int i = 0; i < kMine; ++i)
+        mine[i] = seg[std::min(tid + i * kPickThreads, all - 1)];
     // log-sums: some wavefronts per beam
     const int per = kPickWaves >= a.beams ? kPickWaves / a.beams : 1;  // wavefronts of a beam
     for (int j0 = 0; j0 < a.beams; j0 += kPickWaves / per) {
@@ -155,20 +207,16 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
         const bool is = j < a.beams && wave / per < kPickWaves / per;
         float m = -INFINITY;
         if (is)
-            for (int i = part * 64 + lane; i < per_beam; i += per * 64) {
-                const float x = seg[j * per_beam + i].x;
-                m = x > m || x != x ? x : m;
-            }
+            for (int i = part * 64 + lane; i < n_sums; i += per * 64)
+                m = fmaxf(m, sums[j * n_sums + i].x);
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const float o = __shfl_xor(m, d);
-            m = o > m || o != o ? o : m;
-        }
+        for (int d = 1; d < 64; d *= 2)
+            m = fmaxf(m, __shfl_xor(m, d));
         double s = 0.0;
-        if (is && m != -INFINITY)
-            for (int i = part * 64 + lane; i < per_beam; i += per * 64) {
-                const float2 x = seg[j * per_beam + i];
-                s += (double)x.y * exp((double)x.x - (double)m);
+        if (is)
+            for (int i = part * 64 + lane; i < n_sums; i += per * 64) {
+                const float2 x = sums[j * n_sums + i];
+                s += x.x == -INFINITY ? (double)x.y : (double)x.y * exp((double)x.x - (double)m);
             }
 #pragma unroll
         for (int d = 1; d < 64; d *= 2)
@@ -178,14 +226,12 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
         __syncthreads();
         if (tid < kPickWaves / per && j0 + tid < a.beams) {
             float top = -INFINITY;
-            for (int i = 0; i < per; ++i) {
-                const float o = sh.part_max[tid * per + i];
-                top = o > top || o != o ? o : top;
-            }
+            for (int i = 0; i < per; ++i)
+                top = fmaxf(top, sh.part_max[tid * per + i]);
             double sum = 0.0;
             for (int i = 0; i < per; ++i) {
                 const float o = sh.part_max[tid * per + i];
-                sum += o == -INFINITY ? 0.0 : sh.part_sum[tid * per + i] * exp((double)o - (double)top);
+                sum += o == -INFINITY ? sh.part_sum[tid * per + i] : sh.part_sum[tid * per + i] * exp((double)o - (double)top);
             }
             const int64_t row = b * a.beams + j0 + tid;
             sh.top[j0 + tid] = (double)top, sh.log_sum[j0 + tid] = log(sum);
@@ -198,14 +244,18 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
         const double v = (((double)logit - sh.top[j]) - sh.log_sum[j]) + sh.score[j];
         return v > -INFINITY && logit > -INFINITY ? v : (double)-INFINITY;  // (NaN is none)
     };
-    auto segment = [&](int n) {
-        const int j = n / per_beam;
-        return sh.is_finished[j] ? (double)-INFINITY : value(seg[n].x, j);
-    };
     // the bound
-    double top = -INFINITY;
-    for (int n = tid; n < all; n += kPickThreads)
-        top = fmax(top, segment(n));
+    double here[kMine], top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        const int n = tid + i * kPickThreads;
+        here[i] = -INFINITY;
+        if (n < all) {
+            const int j = a.by_segments.quotient(n);
+            here[i] = sh.is_finished[j] ? (double)-INFINITY : value(mine[i], j);
+        }
+        top = fmax(top, here[i]);
+    }
 #pragma unroll
     for (int d = 1; d < kPickThreads / kGroups; d *= 2)
         top = fmax(top, __shfl_xor(top, d));
@@ -217,15 +267,16 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
     {
         constexpr int kParts = kPickThreads / kGroups;
         const int t = tid / kParts, part = tid % kParts;
-        const double mine = sh.group[t];
+        const double group_top = sh.group[t];
         int rank = 0;
-        for (int i = part; i < kGroups; i += kParts)
-            rank += before(sh.group[i], i, mine, t);
+#pragma unroll
+        for (int i = 0; i < kGroups; i += kParts)
+            rank += before(sh.group[i + part], i + part, group_top, t);
 #pragma unroll
         for (int d = 1; d < kParts; d *= 2)
             rank += __shfl_xor(rank, d);
         if (part == 0 && rank == a.k - 1)
-            sh.bound = mine;
+            sh.bound = group_top;
     }
     __syncthreads();
     double bound = sh.bound;
@@ -238,33 +289,45 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
         if (tid < a.beams && sh.is_finished[tid] && sh.score[tid] >= bound && sh.score[tid] > -INFINITY)
             push(sh.score[tid], tid * a.vocab + a.end);
     };
-    for (int n = tid; n < all; n += kPickThreads) {
-        const double v = segment(n);
-        if (v >= bound && v > -INFINITY)
-            sh.list[atomicAdd(&sh.listed, 1)] = n;
-    }
+#pragma unroll
+    for (int i = 0; i < kMine; ++i)
+        if (here[i] >= bound && here[i] > -INFINITY)
+            sh.list[atomicAdd(&sh.listed, 1)] = tid + i * kPickThreads;
     push_finished();
     __syncthreads();
     const int listed = sh.listed;
-    // a listed segment's row, its first logit there, and its beam
+    // the step-th eight logits of the i-th listed segment: their row, the first one's place there, the beam
     struct Place {
         const T *row;
         int at, j;
     };
-    auto place = [&](int n) {
-        const int j = n / per_beam, c = n % per_beam;
-        return Place{(const T *)a.logits + b * a.l_batch + j * a.l_beam, c / 4 * a.steps * 512 + c % 4 * 128 + lane % 16 * 8, j};
+    auto place = [&](int i) {
+        const int of = a.by_steps.quotient(i), n = sh.list[of], j = a.by_segments.quotient(n), c = (n - j * per_beam) / 64;
+        return Place{(const T *)a.logits + b * a.l_batch + j * a.l_beam, (c * a.steps + i - of * a.steps) * 512 + n % 64 * 8, j};
     };
-    for (int i = tid / 16; i < listed; i += kPickThreads / 16) {
-        const Place p = place(sh.list[i]);
-        for (int t = 0; t < a.steps; ++t) {
-            float x[8];
-            load_eight(p.row, p.at + t * 512, a.vocab, x);
+    const int eights = listed * a.steps;
+    constexpr int kDeep = 4;
+    for (int i0 = tid; i0 < eights; i0 += kDeep * kPickThreads) {
+        Place p[kDeep];
+        Eight<T> q[kDeep];
+#pragma unroll
+        for (int t = 0; t < kDeep; ++t) {
+            p[t] = place(std::min(i0 + t * kPickThreads, eights - 1));
+            if (a.vocab >= 8)  // (eight from the row's end where there are fewer left)
+                q[t] = *(const Eight<T> *)(p[t].row + std::min(p[t].at, a.vocab - 8));
+        }
+#pragma unroll
+        for (int t = 0; t < kDeep; ++t) {
+            if (i0 + t * kPickThreads >= eights || p[t].at >= a.vocab)
+                continue;
+            const int first = a.vocab >= 8 ? std::min(p[t].at, a.vocab - 8) : 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const double v = value(x[e], p.j);
+                if (first + e < p[t].at || first + e >= a.vocab)
+                    continue;
+                const double v = value(a.vocab >= 8 ? to_float(q[t].v[e]) : to_float(p[t].row[e]), p[t].j);
                 if (v >= bound && v > -INFINITY)
-                    push(v, p.j * a.vocab + p.at + t * 512 + e);
+                    push(v, p[t].j * a.vocab + first + e);
             }
         }
     }
@@ -276,30 +339,28 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
         __syncthreads();
         push_finished();
         __syncthreads();
-        for (int i0 = 0; i0 < listed; i0 += kPickThreads / 16)
-            for (int t = 0; t < a.steps; ++t)
-                for (int e = 0; e < 8; ++e) {
-                    if (sh.count > kRoom - kPickThreads) {
-                        const int n = sh.count;
-                        sort_candidates(sh, n);
-                        if (n >= a.k)
-                            bound = sh.value[a.k - 1];
-                        if (tid == 0)
-                            sh.count = n < a.k ? n : a.k;
-                    }
-                    __syncthreads();
-                    const int i = i0 + tid / 16;
-                    if (i < listed) {
-                        const Place p = place(sh.list[i]);
-                        const int at = p.at + t * 512 + e;
-                        if (at < a.vocab) {
-                            const double v = value(to_float(p.row[at]), p.j);
-                            if (v >= bound && v > -INFINITY)
-                                push(v, p.j * a.vocab + at);
-                        }
-                    }
-                    __syncthreads();
+        for (int i0 = 0; i0 < eights; i0 += kPickThreads)
+            for (int e = 0; e < 8; ++e) {
+                if (sh.count > kRoom - kPickThreads) {
+                    const int n = sh.count;
+                    sort_candidates(sh, n);
+                    if (n >= a.k)
+                        bound = sh.value[a.k - 1];
+                    if (tid == 0)
+                        sh.count = n < a.k ? n : a.k;
                 }
+                __syncthreads();
+                const int i = i0 + tid;
+                if (i < eights) {
+                    const Place p = place(i);
+                    if (p.at + e < a.vocab) {
+                        const double v = value(to_float(p.row[p.at + e]), p.j);
+                        if (v >= bound && v > -INFINITY)
+                            push(v, p.j * a.vocab + p.at + e);
+                    }
+                }
+                __syncthreads();
+            }
     }
     const int count = sh.count;
     auto write = [&](int rank, double v, int32_t id) {
@@ -317,9 +378,13 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
             parts /= 2;
         const int t = tid / parts, part = tid % parts;
         int rank = 0;
-        if (t < count)
+        if (t < count) {
+            const double v = sh.value[t];
+            const int32_t id = sh.id[t];
+#pragma unroll 8
             for (int i = part; i < count; i += parts)
-                rank += before(sh.value[i], sh.id[i], sh.value[t], sh.id[t]);
+                rank += before(sh.value[i], sh.id[i], v, id);
+        }
         for (int d = 1; d < parts; d *= 2)
             rank += __shfl_xor(rank, d);
         if (t < count && part == 0 && rank < a.k)
@@ -334,21 +399,25 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
 }
 
 struct SelectPlan {
-    int steps, chunks;
-    size_t bytes;
+    int steps, chunks, per, stretches;
+    size_t sums, bytes;
 };
-// More steps per wavefront where there are wavefronts enough, and so many that an entry's segments fit.
+// Segments of as few steps as an entry's segments fit; wavefronts of several chunks where there are enough of them.
 SelectPlan select_plan(const tig_beam_select &p)
 {
     SelectPlan L = {};
     const int64_t blocks = (p.vocab + 511) / 512, rows = p.batch * p.beams;
-    int64_t steps = std::min<int64_t>(8, std::max<int64_t>(1, rows * blocks / 8192));
-    while (p.beams * ((blocks + steps - 1) / steps) * 4 > kMaxSegments)
-        ++steps;
-    while (rows * ((blocks + steps - 1) / steps) > (1 << 25))  // (a launch's threads fit 32 bits)
-        steps *= 2;
-    L.steps = (int)steps, L.chunks = (int)((blocks + steps - 1) / steps);
-    L.bytes = ((size_t)rows * L.chunks * 4 * sizeof(float2) + 255) / 256 * 256;
+    int64_t steps = 1;
+    while (p.beams * ((blocks + steps - 1) / steps) * 64 > kMaxSegments)
+        steps += steps < 4 ? 1 : 4;
+    const int64_t chunks = (blocks + steps - 1) / steps;
+    int64_t per = std::max<int64_t>(1, rows * chunks / 8192);
+    per = std::min<int64_t>(per, std::max<int64_t>(1, 32 / steps));
+    while (rows * ((chunks + per - 1) / per) > (1 << 25))  // (a launch's threads fit 32 bits)
+        per *= 2;
+    L.steps = (int)steps, L.chunks = (int)chunks, L.per = (int)std::min(per, chunks), L.stretches = (int)((chunks + L.per - 1) / L.per);
+    L.sums = ((size_t)rows * chunks * 64 * sizeof(float) + 255) / 256 * 256;
+    L.bytes = (L.sums + (size_t)rows * L.stretches * sizeof(float2) + 255) / 256 * 256;
     return L;
 }
 
@@ -414,9 +483,9 @@ int tig_beam_select_run(const tig_beam_select *p, void *workspace, size_t worksp
     if ((rc = check_select_apart(*p)) != TIG_OK)
         return rc;
     const hipStream_t s = (hipStream_t)hip_stream;
-    SelectArgs a = {p->logits, p->l_batch, p->l_beam, p->batch, p->beams, p->k, (int32_t)p->vocab, L.steps, L.chunks, p->scores, p->finished, p->end,
-                    (float2 *)workspace, p->scores_out, p->parents, p->tokens, p->finished_out};
-    const int64_t waves = p->batch * p->beams * L.chunks;
+    SelectArgs a = {p->logits, p->l_batch, p->l_beam, p->batch, p->beams, p->k, (int32_t)p->vocab, L.steps, L.chunks, L.per, L.stretches, page_div(L.chunks * 64), page_div(L.steps), p->scores, p->finished, p->end,
+                    (float *)workspace, (float2 *)((char *)workspace + L.sums), p->scores_out, p->parents, p->tokens, p->finished_out};
+    const int64_t waves = p->batch * p->beams * L.stretches;
     const hipError_t e = with_dtype(p->dtype, [&](auto t) {
         using T = decltype(t);
         hipLaunchKernelGGL((k_select_segments<T>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, a);

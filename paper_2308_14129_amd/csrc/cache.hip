@@ -34,17 +34,17 @@ int check_cache(const tig_cache *c)
     if (!dtype_ok(c->dtype))
         return fail_text(TIG_EINVAL, "tig_cache: unknown dtype");
     if (c->pages < 1 || c->pages > 0x7fffffff || c->page_size < 1 || c->page_size > (1 << 16) || c->heads < 1 || c->heads > (1 << 10) || c->head_dim < 8 ||
-        c->head_dim > 256 || c->max_pages < 1 || c->max_pages > (1 << 24) || (int64_t)c->max_pages * c->page_size > 0x7fffffff)
+        c->head_dim > 256 || c->max_pages < 1 || c->max_pages > (1 << 24) || (int64_t)c->max_pages * c->page_size > 0x7fff0000)
         return fail_text(TIG_EINVAL, "tig_cache: pages, page_size, heads, head_dim or max_pages out of range");
     const int es = dtype_bytes(c->dtype);
     if (!c->k || !c->v || !element_aligned(c->k, es) || !element_aligned(c->v, es))
         return fail_text(TIG_EINVAL, "tig_cache: k or v is NULL or not aligned to its element");
     const int64_t most = (int64_t)1 << 40;
     if (c->page_stride < 0 || c->token_stride < 0 || c->head_stride < 0 || c->page_stride > most || c->token_stride > most || c->head_stride > most ||
-        c->token_stride > 0x7fffffff || c->page_size * c->token_stride * es > 0x7fffffff)
+        c->token_stride > 0x7fffffff || (c->page_size > 1 && c->page_size * c->token_stride * es > (1 << 30)))
         return fail_text(TIG_EINVAL, "tig_cache: a stride is out of range");
-    if ((int64_t)c->page_size * c->heads * c->head_dim * es > 0x7fffffff)
-        return fail_text(TIG_EINVAL, "tig_cache: a page is 2 GiB or larger");
+    if ((int64_t)c->page_size * c->heads * c->head_dim * es > (1 << 30))
+        return fail_text(TIG_EINVAL, "tig_cache: a page is larger than 1 GiB");
     Dim d[3] = {{c->pages, c->page_stride}, {c->page_size, c->token_stride}, {c->heads, c->head_stride}};
     std::sort(d, d + 3, [](const Dim &a, const Dim &b) { return a.stride < b.stride; });
     int64_t span = c->head_dim;
@@ -132,20 +132,34 @@ __device__ inline void rotate_pair(T &a, T &b, float c, float s)
     b = (T)fmaf(y, c, x * s);
 }
 
-// A wavefront (or, where a token has many rows, a workgroup) per token: cosines and sines of its pairs into LDS once, then all its rows in
-// pieces of 16 bytes, a rotated pair of pieces to a lane.
+// A workgroup takes `per` tokens: where each goes, the cosines and sines of its pairs (once for all its heads, in LDS), then the rows in
+// units of 16 bytes, a rotated pair of pieces to a lane.  A lane has the same unit of every token (or of every `groups`-th one, where a token
+// has few): what it has to divide it divides once, and the pieces of several tokens are on their way together.
+constexpr int kAppendTokens = 16;
+
+constexpr int kAppendDeep = 4;  // tokens whose pieces are on their way together
+
+// Units of a row (pairs of pieces, pieces behind them, pieces of v), of all rows (`turning`, `resting`, `all`); tokens at a time, tokens of
+// a workgroup.
+struct AppendUnits {
+    int32_t n_pair, n_rest, n_v, turning, resting, all, groups, per, in_place;
+};
+
 template <typename T>
-__global__ void __launch_bounds__(256) k_cache_append(AppendArgs a, int lanes)
+__global__ void __launch_bounds__(256) k_cache_append(AppendArgs a, AppendUnits n)
 {
     constexpr int VE = 16 / sizeof(T), ES = sizeof(T);
-    __shared__ float turn[4][2][128];  // by token of the workgroup: cosines, sines
-    const int group = threadIdx.x / lanes, tid = threadIdx.x % lanes;
-    const int64_t token = (int64_t)blockIdx.x * (256 / lanes) + group;
+    __shared__ float turn[kAppendTokens][2][128];  // cosines, sines
+    __shared__ int64_t at[kAppendTokens];          // the row's first byte, head 0; -1: none
+    __shared__ double position[kAppendTokens];
+    const int tid = threadIdx.x;
+    const int64_t token0 = (int64_t)blockIdx.x * n.per;
+    const int count = (int)std::min<int64_t>(n.per, a.tokens - token0);
     const CacheView &c = a.c;
     const int d = c.head_dim, pairs = a.rotary / 2;
-    int page = -1, row = 0;
-    if (token < a.tokens) {
-        int64_t seq = token;
+    if (tid < count) {
+        const int64_t token = token0 + tid;
+        int64_t seq = token, row = -1;
         int place = -1;
         if (a.starts) {  // the last sequence that starts at or before the token
             int64_t lo = 0, hi = a.seqs;
@@ -163,68 +177,111 @@ __global__ void __launch_bounds__(256) k_cache_append(AppendArgs a, int lanes)
             place = std::max(c.lengths[seq], 0) - 1;
         }
         if (place >= 0 && place < c.capacity()) {
-            const int n = c.div.quotient(place);
-            row = place - n * c.page_size;
-            page = c.table[seq * c.ld_table + n];
-            if (!c.page_ok(page))
-                page = -1;
+            const int in_table = c.div.quotient(place), page = c.table[seq * c.ld_table + in_table];
+            if (c.page_ok(page))
+                row = c.offset(page, place - in_table * c.page_size, 0);
         }
-        if (page >= 0)
-            for (int j = tid; j < pairs; j += lanes) {
-                const double pos = a.position_type == 0 ? (double)place : a.position_type == 1 ? (double)((const int64_t *)a.positions)[token]
-                                                                                               : ((const double *)a.positions)[token];
-                cos_sin(pos * a.freq[j], turn[group][0][j], turn[group][1][j]);
-            }
+        at[tid] = row;
+        position[tid] = a.position_type == 0 ? (double)place : a.position_type == 1 ? (double)((const int64_t *)a.positions)[token]
+                                                                                     : ((const double *)a.positions)[token];
     }
     __syncthreads();
-    if (page < 0)
+    for (int i = tid; i < count * pairs; i += 256) {
+        const int t = i / pairs, j = i - t * pairs;
+        cos_sin(position[t] * a.freq[j], turn[t][0][j], turn[t][1][j]);
+    }
+    __syncthreads();
+    const int group = n.groups > 1 ? tid / n.all : 0;
+    if (group >= n.groups)
         return;
-    const int n_pair = (pairs + VE - 1) / VE, rest = d - a.rotary, n_rest = (rest + VE - 1) / VE, per_row = n_pair + n_rest;
-    const int rotated = (a.q_heads + c.heads) * per_row, n_v = (d + VE - 1) / VE, all = rotated + c.heads * n_v;
-    const float *const cs = turn[group][0], *const sn = turn[group][1];
-    for (int u = tid; u < all; u += lanes) {
-        if (u >= rotated) {
-            const int h = (u - rotated) / n_v, at = piece_start((u - rotated) % n_v, d * ES);
-            *(Sixteen *)(c.v + c.offset(page, row, h) + at) = *(const Sixteen *)(a.v + token * a.v_token + h * a.v_head + at);
-            continue;
-        }
-        const int r = u / per_row, w = u % per_row;
-        const bool is_q = r < a.q_heads;
-        const int h = is_q ? r : r - a.q_heads;
-        const T *const from = (const T *)(is_q ? a.q + token * a.q_token + h * a.q_head : a.k + token * a.k_token + h * a.k_head);
-        T *const to = (T *)(is_q ? a.qo + token * a.qo_token + h * a.qo_head : c.k + c.offset(page, row, h));
-        if (w >= n_pair) {
-            const int at = a.rotary + (w - n_pair) * VE;
-            if (at + VE <= d)
-                *(Piece16<T> *)(to + at) = *(const Piece16<T> *)(from + at);
-            else
-                for (int e = at; e < d; ++e)
-                    to[e] = from[e];
-            continue;
-        }
-        const int j = w * VE;
-        const int at_a = a.interleaved ? 2 * j : j, at_b = a.interleaved ? 2 * j + VE : pairs + j;
-        if (j + VE <= pairs) {
-            Piece16<T> x = *(const Piece16<T> *)(from + at_a), y = *(const Piece16<T> *)(from + at_b);
-            if (a.interleaved) {
-#pragma unroll
-                for (int e = 0; e < VE / 2; ++e) {
-                    rotate_pair(x.v[2 * e], x.v[2 * e + 1], cs[j + e], sn[j + e]);
-                    rotate_pair(y.v[2 * e], y.v[2 * e + 1], cs[j + VE / 2 + e], sn[j + VE / 2 + e]);
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < VE; ++e)
-                    rotate_pair(x.v[e], y.v[e], cs[j + e], sn[j + e]);
-            }
-            *(Piece16<T> *)(to + at_a) = x;
-            *(Piece16<T> *)(to + at_b) = y;
+    for (int u = n.groups > 1 ? tid - group * n.all : tid; u < n.all; u += 256) {
+        // the unit: where its one or two pieces come from and go to in a token.  All pairs of pieces, then what is copied: a wavefront is
+        // mostly of one kind.
+        const char *from;
+        char *to;
+        int64_t from_token, to_token = -1;
+        const bool turns = u < n.turning;
+        const int r = turns ? u / n.n_pair : (u - n.turning) / n.n_rest, w = turns ? u - r * n.n_pair : (u - n.turning) - r * n.n_rest;
+        int at_a, at_b, j = 0, left = VE;  // bytes in the row; first pair; pairs or elements there
+        if (!turns && u >= n.turning + n.resting) {
+            const int h = (u - n.turning - n.resting) / n.n_v;
+            at_a = at_b = piece_start((u - n.turning - n.resting) - h * n.n_v, d * ES);
+            from = a.v + h * a.v_head, from_token = a.v_token;
+            to = c.v + h * c.head_stride;
         } else {
-            for (int e = j; e < pairs; ++e) {
-                const int p = a.interleaved ? 2 * e : e, o = a.interleaved ? 2 * e + 1 : pairs + e;
-                T x = from[p], y = from[o];
-                rotate_pair(x, y, cs[e], sn[e]);
-                to[p] = x, to[o] = y;
+            if (r < a.q_heads) {
+                from = a.q + r * a.q_head, from_token = a.q_token;
+                to = a.qo + r * a.qo_head, to_token = a.qo_token;
+            } else {
+                from = a.k + (r - a.q_heads) * a.k_head, from_token = a.k_token;
+                to = c.k + (r - a.q_heads) * c.head_stride;
+            }
+            if (turns) {
+                j = w * VE, left = pairs - j;
+                // fewer pairs than a piece has: the row's last ones (some are then turned twice, which a row in place does not bear)
+                if (left < VE && pairs >= VE && !(n.in_place && r < a.q_heads))
+                    j = pairs - VE, left = VE;
+                at_a = (a.interleaved ? 2 * j : j) * ES, at_b = a.interleaved ? at_a + 16 : (pairs + j) * ES;
+            } else {
+                const int e = a.rotary + w * VE;
+                left = d - e;
+                at_a = at_b = left < VE && d - VE >= a.rotary ? (d - VE) * ES : e * ES;
+                if (at_a != e * ES)
+                    left = VE;
+            }
+        }
+        auto target = [&](int t) { return to + (to_token < 0 ? at[t] : (token0 + t) * to_token); };
+        auto source = [&](int t) { return from + (token0 + t) * from_token; };
+        if (left >= VE) {
+            for (int t0 = group; t0 < count; t0 += kAppendDeep * n.groups) {
+                Piece16<T> x[kAppendDeep], y[kAppendDeep];
+#pragma unroll
+                for (int i = 0; i < kAppendDeep; ++i) {
+                    const char *const p = source(std::min(t0 + i * n.groups, count - 1));
+                    x[i] = *(const Piece16<T> *)(p + at_a);
+                    if (turns)
+                        y[i] = *(const Piece16<T> *)(p + at_b);
+                }
+#pragma unroll
+                for (int i = 0; i < kAppendDeep; ++i) {
+                    const int t = t0 + i * n.groups;
+                    if (t >= count || at[t] < 0)
+                        continue;
+                    if (turns) {
+                        const float *const cs = turn[t][0] + j, *const sn = turn[t][1] + j;
+                        if (a.interleaved) {
+#pragma unroll
+                            for (int e = 0; e < VE / 2; ++e) {
+                                rotate_pair(x[i].v[2 * e], x[i].v[2 * e + 1], cs[e], sn[e]);
+                                rotate_pair(y[i].v[2 * e], y[i].v[2 * e + 1], cs[VE / 2 + e], sn[VE / 2 + e]);
+                            }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < VE; ++e)
+                                rotate_pair(x[i].v[e], y[i].v[e], cs[e], sn[e]);
+                        }
+                        *(Piece16<T> *)(target(t) + at_b) = y[i];
+                    }
+                    *(Piece16<T> *)(target(t) + at_a) = x[i];
+                }
+            }
+        } else {  // element by element
+            for (int t = group; t < count; t += n.groups) {
+                if (at[t] < 0)
+                    continue;
+                const T *const f = (const T *)source(t);
+                T *const o = (T *)target(t);
+                if (!turns) {
+                    for (int e = d - left; e < d; ++e)
+                        o[e] = f[e];
+                } else {
+                    for (int e = j; e < pairs; ++e) {
+                        const int p = a.interleaved ? 2 * e : e, q = a.interleaved ? 2 * e + 1 : pairs + e;
+                        T x = f[p], y = f[q];
+                        rotate_pair(x, y, turn[t][0][e], turn[t][1][e]);
+                        o[p] = x, o[q] = y;
+                    }
+                }
             }
         }
     }
@@ -359,11 +416,21 @@ int tig_cache_append_run(const tig_cache *cache, const tig_cache_append *p, void
     a.k_token = p->k_token * es, a.k_head = p->k_head * es, a.v_token = p->v_token * es, a.v_head = p->v_head * es;
     a.q_token = p->q_token * es, a.q_head = p->q_head * es, a.qo_token = p->qo_token * es, a.qo_head = p->qo_head * es;
     a.q_heads = p->q_heads, a.rotary = p->rotary, a.interleaved = p->interleaved, a.position_type = p->position_type;
-    const int64_t pieces = (int64_t)(p->q_heads + 2 * cache->heads) * (cache->head_dim * es + 15) / 16;
-    const int lanes = pieces > 256 ? 256 : 64;
-    const dim3 grid((unsigned)((p->tokens + 256 / lanes - 1) / (256 / lanes)));
+    const int ve = (int)(16 / es), d = cache->head_dim;
+    AppendUnits n = {};
+    n.n_pair = (p->rotary / 2 + ve - 1) / ve;
+    n.n_rest = std::max(1, (d - p->rotary + ve - 1) / ve);  // (a divisor)
+    n.n_v = (d + ve - 1) / ve;
+    n.turning = (p->q_heads + cache->heads) * n.n_pair;
+    n.resting = p->rotary < d ? (p->q_heads + cache->heads) * n.n_rest : 0;
+    n.all = n.turning + n.resting + cache->heads * n.n_v;
+    n.in_place = p->q != nullptr && p->q == p->q_out;
+    n.groups = std::max(1, 256 / n.all);
+    // a workgroup's tokens: as many as leave about four workgroups for a compute unit
+    n.per = (int)std::min<int64_t>(kAppendTokens, std::max<int64_t>(1, p->tokens / 1024));
+    const dim3 grid((unsigned)((p->tokens + n.per - 1) / n.per));
     with_dtype(cache->dtype, [&](auto t) {
-        hipLaunchKernelGGL((k_cache_append<decltype(t)>), grid, dim3(256), 0, (hipStream_t)hip_stream, a, lanes);
+        hipLaunchKernelGGL((k_cache_append<decltype(t)>), grid, dim3(256), 0, (hipStream_t)hip_stream, a, n);
         return 0;
     });
     const hipError_t e = hipGetLastError();

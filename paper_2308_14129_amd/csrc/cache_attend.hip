@@ -34,11 +34,12 @@ struct AttendArgs {
     float *lse;
     int64_t q_seq, q_head, o_seq, o_head;  // bytes
     int32_t q_heads, group, blocks, rows;  // query heads of a cache head, blocks of 16 QT of them, rows of a record
+    int32_t together;                      // wavefronts of a workgroup that go through the same rows, each for another unit: 1, 2 or 4
     int32_t window;
     uint32_t flip;                         // sign bits of Q, to keep the factor positive
     float scale, factor;                   // scale; |scale| log2(e)
-    float *part;                           // [workgroups x 2] records: rows x (head_dim padded + 2)
-    struct Tail *tails;                    // [workgroups]
+    float *part;                           // [workgroups x together x 2] records: rows x (head_dim + 2)
+    struct Tail *tails;                    // [workgroups x together]
     int64_t rec;                           // floats of a record
 };
 // The unit that a workgroup's stretch ends in, if it goes on in the next one's.
@@ -80,19 +81,34 @@ __device__ inline int tiles_of(const Seen &s)
     return std::max(1, (s.end + KT - 1) / KT - s.first / KT);
 }
 
-__device__ inline int64_t wave_sum_i64(int64_t v)
+// (a division in 64 bits is a hundred instructions)
+__device__ inline int64_t quotient(int64_t a, int64_t b) { return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b; }
+
+// sums over the lanes up to and with each
+__device__ inline int64_t wave_scan_i64(int64_t v)
 {
 #pragma unroll
-    for (int m = 1; m < 64; m *= 2)
-        v += __shfl_xor(v, m);
+    for (int m = 1; m < 64; m *= 2) {
+        const int64_t up = __shfl_up(v, m);
+        if (lane_id() >= m)
+            v += up;
+    }
     return v;
+}
+
+__device__ inline int64_t uniform_i64(int64_t v)
+{
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(v & 0xffffffff)), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32));
+    return (int64_t)(((uint64_t)hi << 32) | lo);
 }
 
 // maximum / sum over the four lanes that share lane % 16
 __device__ inline float groups_max(float v)
 {
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 __device__ inline float groups_sum(float v)
 {
@@ -120,50 +136,52 @@ struct Attend {
 
     // per lane
     int lane, c16, g;
-    int k_at[NKB];                 // byte of the lane's piece of a key row (and of q), -1: none
-    int v_at[NG];
-    int dup;                       // elements of the last block's piece that the one before has as well
+    int k_off[NKB];                // byte of the lane's piece of a key (PAGED: of sixteen rows of keys; outside of them: none)
+    int v_off[PAGED ? 4 : 1][NG];  // ... of values
+    intx4 tail;                    // of the lane's piece of the last block: nothing behind the row, once what two pieces have
     // per unit
     intx4 qv[QT][NKB];
+    // per tile
+    intx4 kv[NS][NKB];
+    Vpiece vv[VK][NG];
+    int64_t from[NS];              // where each sixteen rows lie; not PAGED: where the lane's row of them does, -1: nowhere
+    int extent[NS];                // bytes there (PAGED)
     float m[QT], l[QT];
     floatx4 o[QT][NG * VE];
 
     __device__ inline void init(const AttendArgs &a)
     {
         lane = lane_id(), c16 = lane % 16, g = lane / 16;
-        const int d = a.c.head_dim;
-        dup = 0;
+        const int d = a.c.head_dim, stride = (int)a.c.token_stride;
+        constexpr int kNone = PAGED ? 0x40000000 : 0;  // (no sixteen rows are that long)
 #pragma unroll
         for (int b = 0; b < NKB; ++b) {
             const int e = (b * 4 + g) * PE;
-            k_at[b] = e >= d ? -1 : std::min(e, d - PE) * ES;
-            if (e < d && e + PE > d)
-                dup = e + PE - d;
+            k_off[b] = e >= d ? kNone : (PAGED ? c16 * stride : 0) + std::min(e, d - PE) * ES;
         }
+        const int e0 = ((d - 1) / (4 * PE) * 4 + g) * PE, dup = e0 + PE - d;  // elements of a last piece that the one before has as well
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (ES == 4)
+                tail[i] = i < dup ? 0 : -1;
+            else
+                tail[i] = 2 * i + 1 < dup ? 0 : 2 * i < dup ? (int)0xffff0000 : -1;
+        }
+        if (e0 >= d)
+            tail = intx4{0, 0, 0, 0};
 #pragma unroll
         for (int b = 0; b < NG; ++b) {
             const int e = (b * 16 + c16) * VE;
-            v_at[b] = e >= d ? -1 : std::min(e, d - VE) * ES;
+#pragma unroll
+            for (int i = 0; i < (PAGED ? 4 : 1); ++i)
+                v_off[i][b] = e >= d ? kNone : (PAGED ? (4 * g + i) * stride : 0) + std::min(e, d - VE) * ES;
         }
     }
-    // a piece's first `dup` elements are the piece before's: zero
-    __device__ inline intx4 without_dup(intx4 x, int b, int d) const
+    // what of the b-th blocks' pieces a row has: all, nothing, or in the last block that it reaches into what `tail` keeps
+    __device__ inline intx4 within(intx4 x, int b, int d) const
     {
-        if ((b * 4 + g) * PE + PE <= d)
-            return x;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (ES == 4) {
-                if (i < dup)
-                    x[i] = 0;
-            } else {
-                if (2 * i < dup)
-                    x[i] &= 0xffff0000;
-                if (2 * i + 1 < dup)
-                    x[i] = 0;
-            }
-        }
-        return x;
+        const int last = (d - 1) / (4 * PE);
+        return b < last ? x : b == last ? x & tail : intx4{0, 0, 0, 0};
     }
     __device__ inline void begin(const AttendArgs &a, int64_t seq, int head, int block)
     {
@@ -175,9 +193,10 @@ struct Attend {
             const char *const p = a.q + seq * a.q_seq + (int64_t)(head * a.group + (is ? row : 0)) * a.q_head;
 #pragma unroll
             for (int b = 0; b < NKB; ++b) {
-                intx4 x = ((const Sixteen *)(p + std::max(k_at[b], 0)))->v;
-                x = without_dup(x, b, a.c.head_dim);
-                const uint32_t keep = is && k_at[b] >= 0 ? 0xffffffffu : 0u;
+                const int e = (b * 4 + g) * PE;
+                intx4 x = ((const Sixteen *)(p + std::min(e, a.c.head_dim - PE) * ES))->v;
+                x = within(x, b, a.c.head_dim);
+                const uint32_t keep = is ? 0xffffffffu : 0u;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     qv[t][b][i] = (x[i] ^ a.flip) & keep;
@@ -189,94 +208,109 @@ struct Attend {
         }
     }
 
-    // rows base .. base + KT - 1 of the sequence
-    __device__ inline void tile(const AttendArgs &a, const int32_t *table, int head, int base, const Seen &s)
+    // Where rows base .. base + KT - 1 of the sequence lie: asked for two tiles ahead.  PAGED: the page of each sixteen rows, else the
+    // one of the lane's row of each sixteen; -1: none.
+    struct Pages {
+        int page[NS];
+    };
+    __device__ inline Pages pages(const CacheView &c, const int32_t *table, int base, const Seen &s) const
+    {
+        Pages x;
+#pragma unroll
+        for (int t = 0; t < NS; ++t) {
+            if constexpr (PAGED) {  // (a scalar load: nothing behind it waits for the rows that are on their way)
+                typedef const __attribute__((address_space(4))) int32_t Const;
+                const int at = base + 16 * t;
+                x.page[t] = at < s.end ? ((Const *)(uintptr_t)table)[c.div.quotient(at)] : -1;
+            } else {  // (no choice between the load and another value: it would become a branch; an empty sequence reads its table's first entry)
+                const int key = base + 16 * t + c16;
+                x.page[t] = table[c.div.quotient(std::max(0, std::min(std::max(key, s.first), s.end - 1)))] | (key >= s.first && key < s.end ? 0 : -1);
+            }
+        }
+        return x;
+    }
+    // ... and as offsets from the head's first row
+    __device__ inline void resolve(const CacheView &c, const Pages &where, int base, const Seen &s)
+    {
+#pragma unroll
+        for (int t = 0; t < NS; ++t) {
+            const int at = base + 16 * t + (PAGED ? 0 : c16), page = where.page[t];
+            const bool ok = c.page_ok(page);
+            from[t] = ok ? page * c.page_stride + (at - c.div.quotient(at) * c.page_size) * c.token_stride : PAGED ? 0 : -1;
+            if constexpr (PAGED)  // rows behind the end lie outside of the extent and read as zero, where there is no page all do
+                extent[t] = ok ? (std::min(16, s.end - at) - 1) * (int)c.token_stride + c.head_dim * ES : 0;
+        }
+    }
+
+    // The tile's keys: rows base .. base + KT - 1 of the sequence, as resolved.  PAGED: a descriptor for sixteen rows, the lane's
+    // offsets are the same for every tile.  Else each row by itself; one that is not there reads another one's memory and counts nothing.
+    __device__ inline void load_keys(const char *rows)
+    {
+#pragma unroll
+        for (int t = 0; t < NS; ++t) {
+            if constexpr (PAGED) {
+                const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(rows + from[t]), 0, extent[t], kBufferFlags);
+#pragma unroll
+                for (int b = 0; b < NKB; ++b)
+                    kv[t][b] = __builtin_bit_cast(intx4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, k_off[b], 0, 0));
+            } else {
+                const char *const p = rows + std::max<int64_t>(from[t], 0);
+#pragma unroll
+                for (int b = 0; b < NKB; ++b)
+                    kv[t][b] = ((const Sixteen *)(p + k_off[b]))->v;
+            }
+        }
+    }
+    // ... and its values
+    __device__ inline void load_values(const char *rows)
+    {
+#pragma unroll
+        for (int t = 0; t < NS; ++t) {
+            if constexpr (PAGED) {
+                const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(rows + from[t]), 0, extent[t], kBufferFlags);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int b = 0; b < NG; ++b) {
+                        if constexpr (VE * ES == 16)
+                            vv[4 * t + i][b] = __builtin_bit_cast(Vpiece, __builtin_amdgcn_raw_buffer_load_b128(rsrc, v_off[i][b], 0, 0));
+                        else
+                            vv[4 * t + i][b] = __builtin_bit_cast(Vpiece, __builtin_amdgcn_raw_buffer_load_b64(rsrc, v_off[i][b], 0, 0));
+                    }
+            } else {
+                struct __attribute__((packed, aligned(2))) Any {
+                    Vpiece v;
+                };
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const char *const p = rows + std::max<int64_t>(__shfl(from[t], 4 * g + i), 0);
+#pragma unroll
+                    for (int b = 0; b < NG; ++b)
+                        vv[4 * t + i][b] = ((const Any *)(p + v_off[0][b]))->v;
+                }
+            }
+        }
+    }
+
+    // A tile whose keys and values are on their way; those of the next one are asked for as soon as the registers are free.
+    __device__ inline void tile(const AttendArgs &a, const Pages &next, const char *keys, const char *values, int base, const Seen &s)
     {
         const CacheView &c = a.c;
-        intx4 kv[NS][NKB];
-        Vpiece vv[VK][NG];
-        bool valid[VK];
         const int d = c.head_dim;
-        if constexpr (PAGED) {  // sixteen rows lie in one page
-            bool ok[NS];
+        // (the load's value is used whatever the conditions: else it would move into a branch, and be waited for there)
+        if (PAGED ? d % PE != 0 : d < DP) {
 #pragma unroll
-            for (int t = 0; t < NS; ++t) {
-                const int at = base + 16 * t, n = c.div.quotient(at), r0 = at - n * c.page_size;
-                const int page = at < s.end ? table[n] : -1;
-                ok[t] = c.page_ok(page);
-                const int64_t from = c.offset(ok[t] ? page : 0, r0, head);
-                const int extent = ok[t] ? 15 * (int)c.token_stride + d * ES : 0;
-                const auto kr = __builtin_amdgcn_make_buffer_rsrc((void *)(c.k + from), 0, extent, kBufferFlags);
-                const auto vr = __builtin_amdgcn_make_buffer_rsrc((void *)(c.v + from), 0, extent, kBufferFlags);
-                const int key = at + c16;
-                const uint32_t row = key >= s.first && key < s.end ? (uint32_t)(c16 * (int)c.token_stride) : kBufferNone;
-#pragma unroll
-                for (int b = 0; b < NKB; ++b)
-                    kv[t][b] = __builtin_bit_cast(intx4, __builtin_amdgcn_raw_buffer_load_b128(kr, (int)(k_at[b] < 0 ? kBufferNone : row + k_at[b]), 0, 0));
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int vkey = at + 4 * g + i;
-                    const bool in = vkey >= s.first && vkey < s.end;
-                    valid[4 * t + i] = in && ok[t];
-                    const uint32_t vrow = in ? (uint32_t)((4 * g + i) * (int)c.token_stride) : kBufferNone;
-#pragma unroll
-                    for (int b = 0; b < NG; ++b) {
-                        const int off = (int)(v_at[b] < 0 ? kBufferNone : vrow + v_at[b]);
-                        if constexpr (VE * ES == 16)
-                            vv[4 * t + i][b] = __builtin_bit_cast(Vpiece, __builtin_amdgcn_raw_buffer_load_b128(vr, off, 0, 0));
-                        else
-                            vv[4 * t + i][b] = __builtin_bit_cast(Vpiece, __builtin_amdgcn_raw_buffer_load_b64(vr, off, 0, 0));
-                    }
-                }
-            }
-        } else {  // each row's page by itself; rows that are not there read another one's memory and count nothing
-            int64_t from[NS];
-#pragma unroll
-            for (int t = 0; t < NS; ++t) {
-                const int key = base + 16 * t + c16;
-                const bool in = key >= s.first && key < s.end;
-                const int n = c.div.quotient(in ? key : 0);
-                const int page = in ? table[n] : -1;
-                from[t] = c.page_ok(page) ? c.offset(page, key - n * c.page_size, head) : -1;
-                const char *const p = c.k + (from[t] < 0 ? head * c.head_stride : from[t]);
+            for (int t = 0; t < NS; ++t)
 #pragma unroll
                 for (int b = 0; b < NKB; ++b) {
-                    kv[t][b] = ((const Sixteen *)(p + std::max(k_at[b], 0)))->v;
-                    if (k_at[b] < 0)
-                        kv[t][b] = intx4{0, 0, 0, 0};
-                }
-            }
-#pragma unroll
-            for (int t = 0; t < NS; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int64_t f = __shfl(from[t], 4 * g + i);
-                    valid[4 * t + i] = f >= 0;
-                    const char *const p = c.v + (f < 0 ? head * c.head_stride : f);
-                    struct __attribute__((packed, aligned(2))) Any {
-                        Vpiece v;
-                    };
-#pragma unroll
-                    for (int b = 0; b < NG; ++b) {
-                        vv[4 * t + i][b] = ((const Any *)(p + std::max(v_at[b], 0)))->v;
-#pragma unroll
-                        for (int e = 0; e < VE * ES / 4; ++e)
-                            vv[4 * t + i][b].d[e] = f < 0 ? 0 : vv[4 * t + i][b].d[e];
-                    }
+                    if constexpr (!PAGED)
+                        asm volatile("" : "+v"(kv[t][b]));
+                    kv[t][b] = within(kv[t][b], b, d);
                 }
         }
-        if (d % PE != 0) {
-#pragma unroll
-            for (int t = 0; t < NS; ++t)
-#pragma unroll
-                for (int b = 0; b < NKB; ++b)
-                    kv[t][b] = without_dup(kv[t][b], b, d);
-        }
-        // scores and weights
         float p[QT][VK];
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            float top = -INFINITY;
+        for (int t = 0; t < QT; ++t)
 #pragma unroll
             for (int u = 0; u < NS; ++u) {
                 floatx4 sc = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -284,27 +318,72 @@ struct Attend {
                 for (int b = 0; b < NKB; ++b)
                     mma16(sc, kv[u][b], qv[t][b], T());
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    p[t][4 * u + i] = valid[4 * u + i] ? sc[i] : -INFINITY;
-                    top = fmaxf(top, p[t][4 * u + i]);
-                }
+                for (int i = 0; i < 4; ++i)
+                    p[t][4 * u + i] = sc[i];
             }
+        // which of the lane's four (eight) keys are there; whole: all keys of the tile
+        bool whole = base >= s.first && base + KT <= s.end;
+        unsigned long long there[NS];
+#pragma unroll
+        for (int u = 0; u < NS; ++u) {
+            there[u] = PAGED ? (extent[u] > 0 ? ~0ull : 0ull) : __ballot(from[u] >= 0);
+            whole = whole && there[u] == ~0ull;
+        }
+        auto valid = [&](int i) {
+            const int key = base + 16 * (i / 4) + 4 * g + i % 4;
+            return (PAGED ? there[i / 4] != 0 && key >= s.first && key < s.end : (there[i / 4] >> (4 * g + i % 4)) & 1);
+        };
+        resolve(c, next, base + KT, s);
+        load_keys(keys);
+        if (!whole) {
+#pragma unroll
+            for (int t = 0; t < QT; ++t)
+#pragma unroll
+                for (int i = 0; i < VK; ++i)
+                    p[t][i] = valid(i) ? p[t][i] : -INFINITY;
+        }
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            float top = p[t][0];
+#pragma unroll
+            for (int i = 1; i < VK; ++i)
+                top = fmaxf(top, p[t][i]);
             top = fmaxf(m[t], groups_max(top));
+            if (__any(top > m[t])) {  // (most tiles of a long sequence bring no new maximum)
+                const float keep = exp2_fast((m[t] - top) * a.factor);
+                l[t] *= keep;
+#pragma unroll
+                for (int i = 0; i < NG * VE; ++i)
+                    o[t][i] *= keep;
+                m[t] = top;
+            }
             const float from = top == -INFINITY ? 0.0f : top;
-            const float keep = exp2_fast((m[t] - from) * a.factor);
-            m[t] = top;
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < VK; ++i) {
                 p[t][i] = exp2_fast((p[t][i] - from) * a.factor);
                 sum += p[t][i];
             }
-            l[t] = l[t] * keep + sum;
-#pragma unroll
-            for (int i = 0; i < NG * VE; ++i)
-                o[t][i] *= keep;
+            l[t] += sum;
         }
-        // values
+        if constexpr (!PAGED) {
+#pragma unroll
+            for (int i = 0; i < VK; ++i)
+#pragma unroll
+                for (int b = 0; b < NG; ++b)
+#pragma unroll
+                    for (int e = 0; e < VE * ES / 4; ++e)
+                        asm volatile("" : "+v"(vv[i][b].d[e]));
+        }
+        if (PAGED ? base < s.first : !whole) {  // (zero times what no sequence has is not zero where that is infinite)
+#pragma unroll
+            for (int i = 0; i < VK; ++i)
+#pragma unroll
+                for (int b = 0; b < NG; ++b)
+#pragma unroll
+                    for (int e = 0; e < VE * ES / 4; ++e)
+                        vv[i][b].d[e] = valid(i) ? vv[i][b].d[e] : 0;
+        }
         if constexpr (ES == 4) {
 #pragma unroll
             for (int b = 0; b < NG; ++b)
@@ -344,6 +423,7 @@ struct Attend {
                     }
                 }
         }
+        load_values(values);
     }
 
     // the whole of a unit
@@ -424,12 +504,6 @@ __device__ inline void write_row(const AttendArgs &a, int64_t seq, int unit, int
         a.lse[seq * a.q_heads + q] = log_sum(a, x.top, x.total);
 }
 
-__device__ inline int64_t uniform_i64(int64_t v)
-{
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(v & 0xffffffff)), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32));
-    return (int64_t)(((uint64_t)hi << 32) | lo);
-}
-
 template <typename T, int DP, int QT, bool PAGED>
 __global__ void __launch_bounds__(64 * kAttendWaves) k_cache_attend(AttendArgs a)
 {
@@ -442,37 +516,79 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_cache_attend(AttendArgs a
     };
     __shared__ Part parts[WAVES][2];
     const int wave = wave_id_uniform(), lane = lane_id();
-    const int per_seq = a.c.heads * a.blocks;
-    // the line's length
-    int64_t sum = 0;
-    for (int64_t i = lane; i < a.seqs; i += 64)
-        sum += tiles_of<KT>(seen(a.c, a.window, i));
-    const int64_t all = uniform_i64(wave_sum_i64(sum)) * per_seq, waves = (int64_t)gridDim.x * WAVES;
-    const int64_t each = (all + waves - 1) / waves;
-    const int64_t wg_begin = std::min(all, (int64_t)blockIdx.x * WAVES * each), wg_end = std::min(all, wg_begin + WAVES * each);
-    const int64_t begin = std::min(all, wg_begin + wave * each), end = std::min(wg_end, begin + each);
-    // the sequence that the stretch begins in
-    int64_t seq = 0, at = 0;
-    for (int64_t i0 = 0; i0 < a.seqs; i0 += 64) {
-        int64_t n = i0 + lane < a.seqs ? (int64_t)tiles_of<KT>(seen(a.c, a.window, i0 + lane)) * per_seq : 0;
+    const int units = a.c.heads * a.blocks, together = a.together, strides = WAVES / together;  // stretches of a workgroup
+    const int mine = wave % together, stretch = wave / together;
+    const int per_seq = (units + together - 1) / together;
+    const int64_t waves = (int64_t)gridDim.x * strides;
+    int64_t all, at = 0, each, wg_begin, wg_end, begin, end;  // at: where sequence s32 begins
+    int s32 = 0;
+    auto deal = [&]() {
+        each = quotient(all + waves - 1, waves);
+        wg_begin = std::min(all, (int64_t)blockIdx.x * strides * each), wg_end = std::min(all, wg_begin + strides * each);
+        begin = std::min(all, wg_begin + stretch * each), end = std::min(wg_end, begin + each);
+    };
+    // among sequences s32 + lane, the one that the stretch begins in
+    auto find = [&](int n_here, int64_t scan) {  // scan: tiles up to and with the lane's sequence, from `at` on
+        const unsigned long long past = __ballot(lane < n_here && at + scan > begin);
+        const int j = past ? __ffsll(past) - 1 : 0;
+        if (j > 0)
+            at = uniform_i64(at + __shfl(scan, j - 1));
+        s32 = __builtin_amdgcn_readfirstlane(s32 + j);
+        return past != 0;
+    };
+    if (a.seqs <= 64) {
+        const int64_t scan = wave_scan_i64(lane < a.seqs ? (int64_t)tiles_of<KT>(seen(a.c, a.window, lane)) * per_seq : 0);
+        all = uniform_i64(__shfl(scan, 63));
+        deal();
+        find((int)a.seqs, scan);
+    } else {  // each thread adds a range of sequences up; then the range, then the sequence
+        constexpr int kRanges = 256;
+        __shared__ int64_t ranges[kRanges];
+        const int blocks = (int)((a.seqs + 63) / 64), span = (blocks + kRanges - 1) / kRanges;  // a range: `span` times 64 sequences
+        const int n_ranges = (blocks + span - 1) / span;
+        for (int r = wave; r < n_ranges; r += WAVES) {
+            int64_t sum = 0;
+            for (int i = r * span * 64 + lane, end = std::min<int64_t>(a.seqs, (r + 1) * (int64_t)span * 64); i < end; i += 64)
+                sum += tiles_of<KT>(seen(a.c, a.window, i));
 #pragma unroll
-        for (int m = 1; m < 64; m *= 2) {
-            const int64_t up = __shfl_up(n, m);
-            if (lane >= m)
-                n += up;
+            for (int m = 1; m < 64; m *= 2)
+                sum += __shfl_xor(sum, m);
+            if (lane == 0)
+                ranges[r] = sum * per_seq;
         }
-        const unsigned long long past = __ballot(at + n > begin);
-        if (past) {
-            const int j = __ffsll(past) - 1;
-            if (j > 0)
-                at += __shfl(n, j - 1);
-            seq = i0 + j;
-            break;
+        __syncthreads();
+        int64_t scan[kRanges / 64];
+        all = 0;
+#pragma unroll
+        for (int i = 0; i < kRanges / 64; ++i) {
+            scan[i] = 0;
+            if (64 * i < n_ranges) {
+                scan[i] = all + wave_scan_i64(64 * i + lane < n_ranges ? ranges[64 * i + lane] : 0);
+                all = uniform_i64(__shfl(scan[i], 63));
+            }
         }
-        at += __shfl(n, 63);
+        deal();
+        bool found = false;
+#pragma unroll
+        for (int i = 0; i < kRanges / 64; ++i) {
+            const unsigned long long past = __ballot(64 * i + lane < n_ranges && scan[i] > begin);
+            if (past && !found) {
+                found = true;
+                const int r = 64 * i + __ffsll(past) - 1;
+                at = r > 0 ? __shfl(r % 64 > 0 ? scan[i] : scan[std::max(i - 1, 0)], (r - 1) % 64) : 0;
+                s32 = r * span * 64;
+            }
+        }
+        at = uniform_i64(at), s32 = __builtin_amdgcn_readfirstlane(s32);
+        const int s_end = (int)std::min<int64_t>(a.seqs, s32 + span * 64);
+        while (begin < end && s32 < s_end) {
+            const int n = std::min(64, s_end - s32);
+            const int64_t within = wave_scan_i64(lane < n ? (int64_t)tiles_of<KT>(seen(a.c, a.window, s32 + lane)) * per_seq : 0);
+            if (find(n, within))
+                break;
+            at = uniform_i64(at + __shfl(within, 63)), s32 += n;
+        }
     }
-    at = uniform_i64(at);
-    int s32 = __builtin_amdgcn_readfirstlane((int)seq);
     if (lane < 2)
         parts[wave][lane].is = 0;
     A w;
@@ -485,14 +601,28 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_cache_attend(AttendArgs a
             ++s32;
             continue;
         }
-        const int unit = (int)((pos - at) / nt);  // head * blocks + block
-        const int64_t u0 = at + (int64_t)unit * nt, u1 = u0 + nt, stop = std::min(end, u1);
+        const int turn = (int)quotient(pos - at, nt), unit = turn * together + mine;  // head * blocks + block
+        const int64_t u0 = at + (int64_t)turn * nt, u1 = u0 + nt, stop = std::min(end, u1);
+        if (unit >= units) {
+            pos = stop;
+            continue;
+        }
         const int head = unit / a.blocks, block = unit % a.blocks;
-        w.begin(a, s32, head, block);
         const int32_t *const table = a.c.table + s32 * a.c.ld_table;
         const int first = s.first / KT * KT + (int)(pos - u0) * KT, n = (int)(stop - pos);
-        for (int t = 0; t < n; ++t)
-            w.tile(a, table, head, first + t * KT, s);
+        const Seen in = {s.first, std::min(s.end, first + n * KT)};  // (nothing is asked for behind the stretch)
+        const char *const keys = a.c.k + head * a.c.head_stride, *const values = a.c.v + head * a.c.head_stride;
+        typename A::Pages next = w.pages(a.c, table, first, in);
+        w.resolve(a.c, next, first, in);
+        next = w.pages(a.c, table, first + KT, in);
+        w.load_keys(keys);
+        w.load_values(values);
+        w.begin(a, s32, head, block);
+        for (int t = 0; t < n; ++t) {
+            const typename A::Pages then = w.pages(a.c, table, first + (t + 2) * KT, in);
+            w.tile(a, next, keys, values, first + t * KT, in);
+            next = then;
+        }
         if (pos == u0 && stop == u1) {
             w.finish(a, s32, head, block);
         } else {  // slot 0: it has begun before the stretch
@@ -506,26 +636,26 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_cache_attend(AttendArgs a
     __syncthreads();
     // chains of parts: one of slot 1, or the first wavefront's of slot 0, and the slots 0 that follow while the unit goes on
     const int d = a.c.head_dim, elems = a.rows * d;
-    bool goes_on = false;
+    int goes_on = 0;
     for (int p = 0; p < 2 * WAVES; ++p) {
         const int w0 = p / 2, slot = p % 2;
-        if (!parts[w0][slot].is || (slot == 0 && w0 > 0))
+        if (!parts[w0][slot].is || (slot == 0 && w0 >= together))
             continue;
         const Part unit = parts[w0][slot];
         int n = 1;
-        while (w0 + n < WAVES && wg_begin + (int64_t)(w0 + n) * each < std::min(unit.u1, wg_end))
+        while (w0 + n * together < WAVES && wg_begin + (int64_t)(w0 / together + n) * each < std::min(unit.u1, wg_end))
             ++n;
-        const bool whole = unit.u0 >= wg_begin && unit.u1 <= wg_end;
-        float *const to = a.part + ((int64_t)blockIdx.x * 2 + (unit.u0 >= wg_begin)) * a.rec;
-        goes_on |= unit.u0 >= wg_begin && unit.u1 > wg_end;
+        const bool whole = unit.u0 >= wg_begin && unit.u1 <= wg_end, first = unit.u0 >= wg_begin;
+        const int64_t line = (int64_t)blockIdx.x * together + w0 % together;
+        float *const to = a.part + (line * 2 + first) * a.rec;
         for (int i = threadIdx.x; i < elems; i += 64 * WAVES) {
             const int row = i / d, e = i % d;
             Joined x = {0.0f, -INFINITY, 0.0f};
             for (int k = 0; k < n; ++k)
-                x.top = fmaxf(x.top, records[((w0 + k) * 2 + (k == 0 ? slot : 0)) * a.rec + elems + row]);
+                x.top = fmaxf(x.top, records[((w0 + k * together) * 2 + (k == 0 ? slot : 0)) * a.rec + elems + row]);
             const float from = x.top == -INFINITY ? 0.0f : x.top;
             for (int k = 0; k < n; ++k) {
-                const float *const r = records + ((w0 + k) * 2 + (k == 0 ? slot : 0)) * a.rec;
+                const float *const r = records + ((w0 + k * together) * 2 + (k == 0 ? slot : 0)) * a.rec;
                 const float f = exp2_fast((r[elems + row] - from) * a.factor);
                 x.sum += r[i] * f;
                 x.total += r[elems + a.rows + row] * f;
@@ -538,53 +668,119 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_cache_attend(AttendArgs a
                     to[elems + row] = x.top, to[elems + a.rows + row] = x.total;
             }
         }
-        if (goes_on && threadIdx.x == 0)
-            a.tails[blockIdx.x] = {unit.seq, unit.unit, (int32_t)((unit.u1 - 1) / (WAVES * each))};
+        if (first && !whole) {
+            goes_on |= 1 << w0 % together;
+            if (threadIdx.x == 0)
+                a.tails[line] = {unit.seq, unit.unit, (int32_t)quotient(unit.u1 - 1, strides * each)};
+        }
     }
-    if (!goes_on && threadIdx.x == 0)
-        a.tails[blockIdx.x].last = -1;
+    if (threadIdx.x < together && !(goes_on >> threadIdx.x & 1))
+        a.tails[(int64_t)blockIdx.x * together + threadIdx.x].last = -1;
 }
 
-// Units that several workgroups have parts of: a workgroup for each that such a unit begins in, and for a share of its rows.
+// Units that several workgroups have parts of: those that begin in four workgroups' stretches, one row of them.  A unit of up to
+// four parts is one wavefront's, of the others' parts each of the four takes every fourth.  Sixty-four parts at a time: their maxima and sums
+// are a lane's each, while the first rows are on their way.
 template <typename T>
-__global__ void __launch_bounds__(256) k_cache_attend_join(AttendArgs a)
+__global__ void __launch_bounds__(256) k_cache_attend_join(AttendArgs a, int lines)
 {
-    __shared__ float sums[4][256];
-    const int b = blockIdx.x, d = a.c.head_dim, elems = a.rows * d, wave = wave_id_uniform(), lane = lane_id();
-    const Tail tail = a.tails[b];
-    if (tail.last < 0)
-        return;
-    const int n = tail.last - b + 1;
-    auto record = [&](int k) { return a.part + ((int64_t)(b + k) * 2 + (k == 0)) * a.rec; };
-    for (int row = blockIdx.y; row < a.rows; row += gridDim.y) {
+    constexpr int kDeep = 8;
+    __shared__ float sums[4][256], tops[4], totals[4];
+    const int d = a.c.head_dim, elems = a.rows * d, wave = wave_id_uniform(), lane = lane_id(), row = blockIdx.y;
+    auto join = [&](int b, const Tail &tail, int k0, int step, float (&acc)[4]) {
+        const int n = (tail.last - b / a.together + step - k0) / step;  // parts k0, k0 + step, ..
+        auto record = [&](int k) { return a.part + ((int64_t)(b + (k0 + k * step) * a.together) * 2 + (k0 + k * step == 0)) * a.rec; };
         Joined x = {0.0f, -INFINITY, 0.0f};
-        for (int k = lane; k < n; k += 64)
-            x.top = fmaxf(x.top, record(k)[elems + row]);
+        for (int first = 0; first < n; first += 64) {
+            const int left = std::min(64, n - first);
+            const float *const mine = record(first + std::min(lane, left - 1)) + elems + row;
+            float m = mine[0], l = mine[a.rows];
+            if (lane >= left)
+                m = -INFINITY, l = 0.0f;
+            float top = m;
 #pragma unroll
-        for (int m = 1; m < 64; m *= 2)
-            x.top = fmaxf(x.top, __shfl_xor(x.top, m));
-        const float from = x.top == -INFINITY ? 0.0f : x.top;
-        for (int k = lane; k < n; k += 64)
-            x.total += record(k)[elems + a.rows + row] * exp2_fast((record(k)[elems + row] - from) * a.factor);
+            for (int i = 1; i < 64; i *= 2)
+                top = fmaxf(top, __shfl_xor(top, i));
+            top = fmaxf(top, x.top);
+            const float from = top == -INFINITY ? 0.0f : top;
+            const float f = exp2_fast((m - from) * a.factor), keep = exp2_fast((x.top - from) * a.factor);
+            l *= f;
 #pragma unroll
-        for (int m = 1; m < 64; m *= 2)
-            x.total += __shfl_xor(x.total, m);
-        float acc[4] = {};
-        for (int k = wave; k < n; k += 4) {
-            const float *const r = record(k);
-            const float f = exp2_fast((r[elems + row] - from) * a.factor);
+            for (int i = 1; i < 64; i *= 2)
+                l += __shfl_xor(l, i);
+            x.total = x.total * keep + l;
+            x.top = top;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (lane + 64 * j < d)
-                    acc[j] += r[row * d + lane + 64 * j] * f;
+                acc[j] *= keep;
+            for (int k = 0; k < left; k += kDeep) {
+                float r[kDeep][4];
+#pragma unroll
+                for (int i = 0; i < kDeep; ++i) {
+                    const float *const p = record(first + std::min(k + i, left - 1)) + row * d;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (64 * j < d)
+                            r[i][j] = p[std::min(lane + 64 * j, d - 1)];
+                }
+#pragma unroll
+                for (int i = 0; i < kDeep; ++i) {
+                    if (k + i >= left)
+                        break;
+                    const float by = __shfl(f, k + i);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (64 * j < d)
+                            acc[j] += r[i][j] * by;
+                }
+            }
+        }
+        return x;
+    };
+    Tail tails[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int b = blockIdx.x * 4 + i;
+        tails[i] = a.tails[std::min(b, lines - 1)];
+        if (b >= lines)
+            tails[i].last = -1;
+    }
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) {
+        const int b = blockIdx.x * 4 + i;
+        const Tail tail = i == 0 ? tails[0] : i == 1 ? tails[1] : i == 2 ? tails[2] : tails[3];
+        if (tail.last < 0)
+            continue;
+        const bool alone = tail.last - b / a.together < 4;
+        if (alone && wave != i)
+            continue;
+        float acc[4] = {};
+        Joined x = join(b, tail, alone ? 0 : wave, alone ? 1 : 4, acc);
+        if (alone) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (lane + 64 * j < d) {
+                    x.sum = acc[j];
+                    write_row<T>(a, tail.seq, tail.unit, row, lane + 64 * j, x);
+                }
+            continue;
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             sums[wave][lane + 64 * j] = acc[j];
+        if (lane == 0)
+            tops[wave] = x.top, totals[wave] = x.total;
         __syncthreads();
         const int e = threadIdx.x;
         if (e < d) {
-            x.sum = (sums[0][e] + sums[1][e]) + (sums[2][e] + sums[3][e]);
+            x = {0.0f, fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), 0.0f};
+            const float from = x.top == -INFINITY ? 0.0f : x.top;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float f = exp2_fast((tops[w] - from) * a.factor);
+                x.sum += sums[w][e] * f;
+                x.total += totals[w] * f;
+            }
             write_row<T>(a, tail.seq, tail.unit, row, e, x);
         }
         __syncthreads();
@@ -594,7 +790,7 @@ __global__ void __launch_bounds__(256) k_cache_attend_join(AttendArgs a)
 struct AttendPlan {
     int qt, rows, blocks;
     int64_t rec;  // floats
-    int wgs;
+    int wgs, together;
     int64_t tails;  // offset in the workspace
     size_t bytes;
 };
@@ -607,10 +803,15 @@ AttendPlan attend_plan(const tig_cache &c, const tig_cache_attend &p)
     L.blocks = (group + 16 * L.qt - 1) / (16 * L.qt);
     L.rec = (int64_t)L.rows * (c.head_dim + 2);
     const int64_t cap = p.window > 0 ? std::min<int64_t>(p.window, (int64_t)c.max_pages * c.page_size) : (int64_t)c.max_pages * c.page_size;
-    const int64_t tiles = p.seqs * c.heads * L.blocks * (cap / kt + 2);
-    L.wgs = (int)std::min<int64_t>(1024, (tiles + kAttendWaves - 1) / kAttendWaves);
-    L.tails = ((int64_t)L.wgs * 2 * L.rec * 4 + 255) / 256 * 256;
-    L.bytes = (size_t)(L.tails + ((int64_t)L.wgs * sizeof(Tail) + 255) / 256 * 256);
+    const int units = c.heads * L.blocks;
+    // rows of several heads side by side that share lines of 128 bytes
+    const bool shared = c.heads > 1 && c.head_stride < c.token_stride && c.head_stride * es % 128 != 0;
+    L.together = shared ? (units >= 3 ? 4 : 2) : 1;
+    const int64_t tiles = p.seqs * ((units + L.together - 1) / L.together) * (cap / kt + 2);
+    const int per_cu = c.head_dim <= 64 ? (L.qt == 1 ? 3 : 2) : c.head_dim <= 128 && L.qt == 1 ? 2 : 1;  // workgroups on a compute unit: registers
+    L.wgs = (int)std::min<int64_t>(256 * per_cu, (tiles + kAttendWaves / L.together - 1) / (kAttendWaves / L.together));
+    L.tails = ((int64_t)L.wgs * L.together * 2 * L.rec * 4 + 255) / 256 * 256;
+    L.bytes = (size_t)(L.tails + ((int64_t)L.wgs * L.together * sizeof(Tail) + 255) / 256 * 256);
     return L;
 }
 
@@ -627,7 +828,7 @@ hipError_t launch_attend(const AttendArgs &a, const AttendPlan &L, hipStream_t s
     hipLaunchKernelGGL(kernel, dim3((unsigned)L.wgs), dim3(64 * kAttendWaves), (unsigned)lds, s, a);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && L.wgs > 1) {
-        hipLaunchKernelGGL((k_cache_attend_join<T>), dim3((unsigned)(L.wgs - 1), (unsigned)L.rows), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((k_cache_attend_join<T>), dim3((unsigned)((L.wgs * L.together + 3) / 4), (unsigned)L.rows), dim3(256), 0, s, a, L.wgs * L.together);
         e = hipGetLastError();
     }
     return e;
@@ -717,7 +918,7 @@ int tig_cache_attend_run(const tig_cache *cache, const tig_cache_attend *p, void
     a.c = cache_view(*cache, p->table, p->ld_table, p->lengths);
     a.seqs = p->seqs, a.q = (const char *)p->q, a.out = (char *)p->out, a.lse = p->lse;
     a.q_seq = p->q_seq * es, a.q_head = p->q_head * es, a.o_seq = p->o_seq * es, a.o_head = p->o_head * es;
-    a.q_heads = p->q_heads, a.group = p->q_heads / cache->heads, a.blocks = L.blocks, a.rows = L.rows, a.window = p->window;
+    a.q_heads = p->q_heads, a.group = p->q_heads / cache->heads, a.blocks = L.blocks, a.rows = L.rows, a.window = p->window, a.together = L.together;
     a.scale = p->scale;
     a.factor = std::max(std::fabs(p->scale) * 1.44269504f, FLT_MIN);  // (not zero: a masked score times it has to stay -infinity)
     a.flip = p->scale < 0.0f ? (es == 4 ? 0x80000000u : 0x80008000u) : 0u;

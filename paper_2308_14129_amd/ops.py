@@ -395,40 +395,74 @@ _select_bytes = struct.Struct("=IiqiiqQ2q2Qii4Q").pack
 _fork_bytes = struct.Struct("=Ii2qQq4QqQ").pack
 
 
+def _here(t, index, name):
+    """Refuses a tensor on another GPU than `index`, and one that wants a graph."""
+    if t.get_device() != index:
+        _refuse(f"{name} is on {t.device}, not with the others")
+    if t.requires_grad:
+        _no_graph(name)
+
+
 def _cache(k_cache, v_cache, table, lengths):
-    """tig_cache of keys' and values' pages, its device and dtype, (seqs, heads, head_dim), and the addresses of table and lengths."""
-    if k_cache.dim() != 4 or table.dim() != 2:
+    """tig_cache of keys' and values' pages, their dtype and GPU, sequences, heads and head_dim, and what a call is told of the sequences.
+    (A small call is as long as its way to the launch: what can be asked once is, devices as numbers.)"""
+    shape, strides, dtype, index = k_cache.shape, k_cache.stride(), k_cache.dtype, k_cache.get_device()
+    if len(shape) != 4 or table.dim() != 2:
         _refuse("k_cache and v_cache are [pages, page_size, heads, head_dim], table is [sequences, pages of one at most]")
-    dtype, dev = k_cache.dtype, k_cache.device
-    code = _dtype_code(dtype)
-    pages, size, heads, dim = k_cache.shape
-    strides = k_cache.stride()
-    if v_cache.shape != k_cache.shape or v_cache.dtype is not dtype or v_cache.device != dev or v_cache.stride() != strides:
-        _refuse("v_cache differs from k_cache in shape, dtype, device or strides")
+    code = _codes.get(dtype)
+    if code is None:
+        _dtype_code(dtype)
+    pages, size, heads, dim = shape
+    if v_cache.shape != shape or v_cache.dtype is not dtype or v_cache.stride() != strides:
+        _refuse("v_cache differs from k_cache in shape, dtype or strides")
     if strides[3] != 1 and dim > 1:
         _refuse("k_cache and v_cache: columns have to be adjacent")
+    seqs, width = table.shape
+    ld, step = table.stride()
+    if table.dtype is not torch.int32 or (step != 1 and width > 1):
+        _refuse("table is no int32 tensor of adjacent columns")
+    if lengths.dtype is not torch.int32 or lengths.shape != (seqs,) or not (lengths.is_contiguous() or seqs <= 1):
+        _refuse(f"lengths is not a contiguous [{seqs}] tensor of int32")
     if k_cache.requires_grad or v_cache.requires_grad:
         _no_graph("k_cache or v_cache")
-    seqs, width = table.shape
-    if table.dtype is not torch.int32 or table.device != dev or (width > 1 and table.stride(1) != 1):
-        _refuse(f"table is not an int32 tensor of adjacent columns on {dev}")
-    ld = table.stride(0) if seqs > 1 else width
-    pn = _vector(lengths, seqs, torch.int32, dev, "lengths")
+    if v_cache.get_device() != index or table.get_device() != index or lengths.get_device() != index:
+        _refuse("k_cache, v_cache, table and lengths are not on one device")
     p = _cache_bytes(72, code, pages, size, heads, dim, width, k_cache.data_ptr(), v_cache.data_ptr(), strides[0] if pages > 1 else 0,
                      strides[1] if size > 1 else 0, strides[2] if heads > 1 else 0)
-    return p, dtype, dev, (seqs, heads, dim), (table.data_ptr(), ld, pn)
+    return p, dtype, index, seqs, heads, dim, table.data_ptr(), ld if seqs > 1 else width, lengths.data_ptr()
 
 
-def _heads(t, n, heads, dim, dtype, device, name):
+def _heads(t, n, heads, dim, dtype, index, name):
     """Address and strides of a [n, heads, dim] tensor of adjacent columns."""
-    if t.shape != (n, heads, dim) or t.dtype is not dtype or t.device != device:
-        _refuse(f"{name} is not a [{n}, {heads}, {dim}] tensor of {dtype} on {device}")
+    if t.shape != (n, heads, dim) or t.dtype is not dtype:
+        _refuse(f"{name} is not a [{n}, {heads}, {dim}] tensor of {dtype}")
     a, b, c = t.stride()
     if c != 1 and dim > 1:
         _refuse(f"{name}: columns have to be adjacent")
-    if t.requires_grad:
-        _no_graph(name)
+    if t.get_device() != index or t.requires_grad:
+        _here(t, index, name)
     return t.data_ptr(), (a if n > 1 else 0), (b if heads > 1 else 0)
+
+
+def _flat(t, n, dtype, index, name):
+    """Address of a contiguous tensor of n elements of any shape."""
+    if t.numel() != n or t.dtype is not dtype or not t.is_contiguous():
+        _refuse(f"{name} is not a contiguous tensor of {n} {dtype}")
+    if t.get_device() != index or t.requires_grad:
+        _here(t, index, name)
+    return t.data_ptr()
+
+
+def _gpu(index, t):
+    """The current stream of a call's GPU, where that is the current device; else None, and the caller goes through _On."""
+    if index < 0:
+        _refuse(f"tensors are on {t.device}, not on a GPU")
+    return torch._C._cuda_getCurrentRawStream(index) if torch._C._cuda_getDevice() == index else None
+
+
+def _elsewhere(t, f, *args, **kw):
+    with _On(t.device):
+        return f(*args, **kw)
 
 
 def cache_append(k_cache, v_cache, table, lengths, k, v, starts=None, q=None, freq=None, positions=None, interleaved=False, q_out=None):
@@ -439,41 +473,41 @@ def cache_append(k_cache, v_cache, table, lengths, k, v, starts=None, q=None, fr
     columns (j, j + pairs), or (2 j, 2 j + 1) if interleaved; positions [tokens] (int64 or float64) are the rows' own numbers if not
     given.  Returns the rotated queries (q_out, which may be q; None without q).  A token without a row in the table or a page is left
     out, in q_out too."""
-    c, dtype, dev, (seqs, heads, dim), (pt, ld, pn) = _cache(k_cache, v_cache, table, lengths)
-    if k.dim() != 3:
-        _refuse("k and v are [tokens, heads, head_dim]")
-    tokens = k.shape[0]
+    c, dtype, index, seqs, heads, dim, pt, ld, pn = _cache(k_cache, v_cache, table, lengths)
+    tokens = len(k)
     if starts is None and tokens != seqs:
         _refuse(f"{tokens} tokens for {seqs} sequences, and no starts")
-    pk, k0, k1 = _heads(k, tokens, heads, dim, dtype, dev, "k")
-    pv, v0, v1 = _heads(v, tokens, heads, dim, dtype, dev, "v")
-    ps = _vector(starts, seqs + 1, torch.int32, dev, "starts")
-    pairs = 0 if freq is None else freq.numel()
-    pf = _vector(freq, pairs, torch.float64, dev, "freq")
-    kind = 0
-    if positions is not None and pairs:
-        kind = {torch.int64: 1, torch.float64: 2}.get(positions.dtype, 0)
-        if not kind:
-            _refuse("positions are int64 or float64")
-    pp = _vector(positions, tokens, positions.dtype, dev, "positions") if kind else 0
-    pq = po = q0 = q1 = o0 = o1 = qh = 0
+    pk, k0, k1 = _heads(k, tokens, heads, dim, dtype, index, "k")
+    pv, v0, v1 = _heads(v, tokens, heads, dim, dtype, index, "v")
+    ps = pf = pp = pq = po = q0 = q1 = o0 = o1 = qh = kind = pairs = 0
+    if starts is not None:
+        ps = _flat(starts, seqs + 1, torch.int32, index, "starts")
+    if freq is not None:
+        pairs = freq.numel()
+        pf = _flat(freq, pairs, torch.float64, index, "freq") if pairs else 0
+        if positions is not None and pairs:
+            kind = 1 if positions.dtype is torch.int64 else 2
+            pp = _flat(positions, tokens, torch.int64 if kind == 1 else torch.float64, index, "positions")
     if q is not None:
         if q.dim() != 3:
             _refuse("q is [tokens, query heads, head_dim]")
         qh = q.shape[1]
-        pq, q0, q1 = _heads(q, tokens, qh, dim, dtype, dev, "q")
+        pq, q0, q1 = _heads(q, tokens, qh, dim, dtype, index, "q")
         if q_out is not None:
-            po, o0, o1 = _heads(q_out, tokens, qh, dim, dtype, dev, "q_out")
+            po, o0, o1 = _heads(q_out, tokens, qh, dim, dtype, index, "q_out")
     elif q_out is not None:
         _refuse("q_out without q")
-    lib = _lib()
-    with _On(dev) as stream:
-        if q is not None and q_out is None:
-            q_out = torch.empty((tokens, qh, dim), dtype=dtype, device=dev)
-            po, o0, o1 = q_out.data_ptr(), qh * dim, dim
-        p = _append_bytes(184, 2 * pairs, int(bool(interleaved)), kind, seqs, tokens, pt, ld, pn, ps, pp, pf, pk, pv, pq, po, qh, 0, k0, k1, v0, v1,
-                          q0, q1, o0, o1)
-        _check(lib.tig_cache_append_run(c, p, stream))
+    stream = _gpu(index, k)
+    if stream is None:
+        return _elsewhere(k, cache_append, k_cache, v_cache, table, lengths, k, v, starts, q, freq, positions, interleaved, q_out)
+    if q is not None and q_out is None:
+        q_out = q.new_empty((tokens, qh, dim))
+        po, o0, o1 = q_out.data_ptr(), qh * dim, dim
+    p = _append_bytes(184, 2 * pairs, 1 if interleaved else 0, kind, seqs, tokens, pt, ld, pn, ps, pp, pf, pk, pv, pq, po, qh, 0, k0, k1, v0, v1,
+                      q0, q1, o0, o1)
+    rc = _lib().tig_cache_append_run(c, p, stream)
+    if rc:
+        _check(rc)
     return q_out
 
 
@@ -482,25 +516,33 @@ def cache_attend(q, k_cache, v_cache, table, lengths, scale=None, window=0, out=
     v_cache (as in cache_append; as many query heads as heads, or a multiple, which share them).  scale: 1 / sqrt(head_dim) if not given;
     window: only a sequence's last rows.  Returns out like q (out may be q), with lse=True (out, lse [sequences, query heads] in
     float32).  A sequence without rows gives zeros and -infinity."""
-    c, dtype, dev, (seqs, heads, dim), (pt, ld, pn) = _cache(k_cache, v_cache, table, lengths)
+    c, dtype, index, seqs, heads, dim, pt, ld, pn = _cache(k_cache, v_cache, table, lengths)
     if q.dim() != 3:
         _refuse("q is [sequences, query heads, head_dim]")
     qh = q.shape[1]
-    pq, q0, q1 = _heads(q, seqs, qh, dim, dtype, dev, "q")
-    po = o0 = o1 = 0
+    pq, q0, q1 = _heads(q, seqs, qh, dim, dtype, index, "q")
+    po = o0 = o1 = pl = 0
     if out is not None:
-        po, o0, o1 = _heads(out, seqs, qh, dim, dtype, dev, "out")
-    lib = _lib()
-    with _On(dev) as stream:
-        if out is None:
-            out = torch.empty((seqs, qh, dim), dtype=dtype, device=dev)
-            po, o0, o1 = out.data_ptr(), qh * dim, dim
-        sums = torch.empty((seqs, qh), dtype=torch.float32, device=dev) if lse else None
-        p = _attend_bytes(104, window, seqs, qh, dim**-0.5 if scale is None else scale, pt, ld, pn, pq, po, sums.data_ptr() if lse else 0, q0, q1, o0, o1)
-        need = c_size_t(0)
-        _check(lib.tig_cache_attend_workspace_bytes(c, p, byref(need)))
-        ws = _workspace(need.value, dev)
-        _check(lib.tig_cache_attend_run(c, p, ws.data_ptr() if ws is not None else None, need.value, stream))
+        po, o0, o1 = _heads(out, seqs, qh, dim, dtype, index, "out")
+    stream = _gpu(index, q)
+    if stream is None:
+        return _elsewhere(q, cache_attend, q, k_cache, v_cache, table, lengths, scale, window, out, lse)
+    if out is None:
+        out = q.new_empty((seqs, qh, dim))
+        po, o0, o1 = out.data_ptr(), qh * dim, dim
+    if lse:
+        sums = q.new_empty((seqs, qh), dtype=torch.float32)
+        pl = sums.data_ptr()
+    p = _attend_bytes(104, window, seqs, qh, dim**-0.5 if scale is None else scale, pt, ld, pn, pq, po, pl, q0, q1, o0, o1)
+    lib, need = _lib(), c_size_t(0)
+    rc = lib.tig_cache_attend_workspace_bytes(c, p, byref(need))
+    if rc:
+        _check(rc)
+    n = need.value
+    ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    rc = lib.tig_cache_attend_run(c, p, ws.data_ptr() if n else None, n, stream)
+    if rc:
+        _check(rc)
     return (out, sums) if lse else out
 
 
@@ -517,32 +559,38 @@ def beam_select(logits, k, scores=None, finished=None, end=-1):
     batch, beams, vocab = logits.shape
     if not 1 <= k <= 128:
         _refuse(f"k = {k} is not in 1 .. 128")
-    dev = logits.device
-    code = _dtype_code(logits.dtype)
+    code, index = _dtype_code(logits.dtype), logits.get_device()
     l0, l1, l2 = logits.stride()
     if l2 != 1 and vocab > 1:
         _refuse("logits: candidates have to be adjacent")
     if logits.requires_grad:
         _no_graph("logits")
-    if scores is not None and (scores.shape != (batch, beams) or scores.dtype is not torch.float32 or scores.device != dev or not scores.is_contiguous()):
-        _refuse(f"scores is not a contiguous [{batch}, {beams}] tensor of float32 on {dev}")
-    if scores is not None and scores.requires_grad:
-        _no_graph("scores")
-    if finished is not None and (finished.shape != (batch, beams) or finished.dtype not in (torch.bool, torch.uint8) or finished.device != dev
-                                 or not finished.is_contiguous()):
-        _refuse(f"finished is not a contiguous [{batch}, {beams}] tensor of bool on {dev}")
-    lib = _lib()
-    with _On(dev) as stream:
-        new, parents, tokens = torch.empty((3, batch, k), dtype=torch.int32, device=dev).unbind(0)
-        new = new.view(torch.float32)
-        done = torch.empty((batch, k), dtype=torch.bool, device=dev)
-        p = _select_bytes(112, code, batch, beams, k, vocab, logits.data_ptr(), l0 if batch > 1 else 0, l1 if beams > 1 else 0,
-                          0 if scores is None else scores.data_ptr(), 0 if finished is None else finished.data_ptr(), end, 0, new.data_ptr(),
-                          parents.data_ptr(), tokens.data_ptr(), done.data_ptr())
-        need = c_size_t(0)
-        _check(lib.tig_beam_select_workspace_bytes(p, byref(need)))
-        ws = _workspace(need.value, dev)
-        _check(lib.tig_beam_select_run(p, ws.data_ptr() if ws is not None else None, need.value, stream))
+    ps = pf = 0
+    if scores is not None:
+        if scores.shape != (batch, beams):
+            _refuse(f"scores is not [{batch}, {beams}]")
+        ps = _flat(scores, batch * beams, torch.float32, index, "scores")
+    if finished is not None:
+        if finished.shape != (batch, beams):
+            _refuse(f"finished is not [{batch}, {beams}]")
+        pf = _flat(finished, batch * beams, torch.uint8 if finished.dtype is torch.uint8 else torch.bool, index, "finished")
+    stream = _gpu(index, logits)
+    if stream is None:
+        return _elsewhere(logits, beam_select, logits, k, scores, finished, end)
+    shape = (batch, k)
+    new, parents = logits.new_empty(shape, dtype=torch.float32), logits.new_empty(shape, dtype=torch.int32)
+    tokens, done = torch.empty_like(parents), logits.new_empty(shape, dtype=torch.bool)
+    p = _select_bytes(112, code, batch, beams, k, vocab, logits.data_ptr(), l0 if batch > 1 else 0, l1 if beams > 1 else 0, ps, pf, end, 0,
+                      new.data_ptr(), parents.data_ptr(), tokens.data_ptr(), done.data_ptr())
+    lib, need = _lib(), c_size_t(0)
+    rc = lib.tig_beam_select_workspace_bytes(p, byref(need))
+    if rc:
+        _check(rc)
+    n = need.value
+    ws = torch.empty(n, dtype=torch.uint8, device=logits.device) if n else None
+    rc = lib.tig_beam_select_run(p, ws.data_ptr() if n else None, n, stream)
+    if rc:
+        _check(rc)
     return BeamSelect(new, parents, tokens, done)
 
 
@@ -551,15 +599,16 @@ def cache_fork(k_cache, v_cache, table, lengths, parents, spare):
     rows of a last page that is not full are copied into the page spare[r] (int32, one for each).  Returns (table, lengths) of the new
     sequences; spare[r] stands behind their full pages and takes what is appended next.  Without a page (-1) a sequence shares its
     parent's last one."""
-    c, dtype, dev, (rows, _, _), (pt, ld, pn) = _cache(k_cache, v_cache, table, lengths)
+    c, _, index, rows, _, _, pt, ld, pn = _cache(k_cache, v_cache, table, lengths)
     n, width = parents.numel(), table.shape[1]
-    for t, name in ((parents, "parents"), (spare, "spare")):
-        if t.dtype is not torch.int32 or t.device != dev or not t.is_contiguous() or t.numel() != n:
-            _refuse(f"{name} is not a contiguous int32 tensor of {n} on {dev}")
-    lib = _lib()
-    with _On(dev) as stream:
-        new = torch.empty((n, width), dtype=torch.int32, device=dev)
-        sizes = torch.empty(n, dtype=torch.int32, device=dev)
-        p = _fork_bytes(88, 0, rows, n, pt, ld, pn, parents.data_ptr(), spare.data_ptr(), new.data_ptr(), width, sizes.data_ptr())
-        _check(lib.tig_cache_fork_run(c, p, stream))
+    pp = _flat(parents, n, torch.int32, index, "parents")
+    ps = _flat(spare, n, torch.int32, index, "spare")
+    stream = _gpu(index, table)
+    if stream is None:
+        return _elsewhere(table, cache_fork, k_cache, v_cache, table, lengths, parents, spare)
+    new, sizes = table.new_empty((n, width)), table.new_empty((n,))
+    p = _fork_bytes(88, 0, rows, n, pt, ld, pn, pp, ps, new.data_ptr(), width, sizes.data_ptr())
+    rc = _lib().tig_cache_fork_run(c, p, stream)
+    if rc:
+        _check(rc)
     return new, sizes
