@@ -132,14 +132,8 @@ __global__ void __launch_bounds__(256) k_select_segments(SelectArgs a)
         }
         a.top[(r * a.chunks + c) * 64 + lane] = seg;
     }
-    float top = m;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2)
-        top = fmaxf(top, __shfl_xor(top, d));
-    s *= __builtin_amdgcn_exp2f((m - (top == -INFINITY ? 0.0f : top)) * kLog2e);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2)
-        s += __shfl_xor(s, d);
+    const float top = wave_max_all(m);
+    s = wave_sum_all(s * __builtin_amdgcn_exp2f((m - (top == -INFINITY ? 0.0f : top)) * kLog2e));
     if (lane == 0)
         a.sums[r * a.stretches + stretch] = {top, s};
 }
@@ -209,9 +203,7 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
         if (is)
             for (int i = part * 64 + lane; i < n_sums; i += per * 64)
                 m = fmaxf(m, sums[j * n_sums + i].x);
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2)
-            m = fmaxf(m, __shfl_xor(m, d));
+        m = wave_max_all(m);
         double s = 0.0;
         if (is)
             for (int i = part * 64 + lane; i < n_sums; i += per * 64) {

@@ -63,6 +63,25 @@ inline Placed placed_keys(const tig_cache &c, const void *p)
     return placed(p, {{c.pages, c.page_stride}, {c.page_size, c.token_stride}, {c.heads, c.head_stride}}, c.head_dim, dtype_bytes(c.dtype));
 }
 
+// maximum / sum over a wavefront's lanes, for every lane
+__device__ inline float wave_max_all(float v)
+{
+    v = row_max_all(v);
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+// ... of the four lanes that share lane % 16
+__device__ inline float groups_sum(float v)
+{
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+__device__ inline float wave_sum_all(float v) { return groups_sum(row_sum_all(v)); }
+
 inline bool element_aligned(const void *p, int elem) { return (uintptr_t)p % (uintptr_t)elem == 0; }
 
 // Bytes that are copied sixteen at a time wherever they start.

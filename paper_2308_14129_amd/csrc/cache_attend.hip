@@ -70,6 +70,12 @@ struct AttendType<_Float16> {
 struct Seen {
     int first, end;
 };
+typedef const __attribute__((address_space(4))) int32_t ConstInt;  // (scalar loads: nothing that waits for them waits for rows on their way)
+__device__ inline int seen_length(const CacheView &c, int seq)
+{
+    const int length = ((ConstInt *)(uintptr_t)c.lengths)[seq];
+    return std::min(std::max(length, 0), c.capacity());
+}
 __device__ inline Seen seen(const CacheView &c, int window, int64_t seq)
 {
     const int end = c.length(seq);
@@ -80,6 +86,8 @@ __device__ inline int tiles_of(const Seen &s)
 {
     return std::max(1, (s.end + KT - 1) / KT - s.first / KT);
 }
+// What a unit takes beside its tiles, in tiles: it stands that much longer in the line, ahead of them.
+constexpr int kUnitCost = 2;
 
 // (a division in 64 bits is a hundred instructions)
 __device__ inline int64_t quotient(int64_t a, int64_t b) { return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b; }
@@ -87,6 +95,16 @@ __device__ inline int64_t quotient(int64_t a, int64_t b) { return ((a | b) >> 32
 // sums over the lanes up to and with each
 __device__ inline int64_t wave_scan_i64(int64_t v)
 {
+    if (!__any((v >> 25) != 0)) {  // (within rows of sixteen lanes, then the rows' sums carried on)
+        int x = (int)v;
+        x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);
+        x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+        x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+        x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+        x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+        x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+        return x;
+    }
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) {
         const int64_t up = __shfl_up(v, m);
@@ -102,18 +120,13 @@ __device__ inline int64_t uniform_i64(int64_t v)
     return (int64_t)(((uint64_t)hi << 32) | lo);
 }
 
-// maximum / sum over the four lanes that share lane % 16
+// maximum over the four lanes that share lane % 16
 __device__ inline float groups_max(float v)
 {
     const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
     const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ inline float groups_sum(float v)
-{
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
 }
 
 // of a sum of weights; nothing was there: 0
@@ -183,23 +196,30 @@ struct Attend {
         const int last = (d - 1) / (4 * PE);
         return b < last ? x : b == last ? x & tail : intx4{0, 0, 0, 0};
     }
-    __device__ inline void begin(const AttendArgs &a, int64_t seq, int head, int block)
+    // A unit's queries: asked for here, taken at its first tile.
+    __device__ inline void load_queries(const AttendArgs &a, int seq, int head, int block)
     {
-        const int row0 = block * 16 * QT;
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            const int row = row0 + 16 * t + c16;
-            const bool is = row < a.group;
-            const char *const p = a.q + seq * a.q_seq + (int64_t)(head * a.group + (is ? row : 0)) * a.q_head;
+            const int row = block * 16 * QT + 16 * t + c16;
+            const char *const p = a.q + seq * a.q_seq + (int64_t)(head * a.group + std::min(row, a.group - 1)) * a.q_head;
+#pragma unroll
+            for (int b = 0; b < NKB; ++b)
+                qv[t][b] = ((const Sixteen *)(p + std::min((b * 4 + g) * PE, a.c.head_dim - PE) * ES))->v;
+        }
+    }
+    __device__ inline void start(const AttendArgs &a, int block)
+    {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            const uint32_t keep = block * 16 * QT + 16 * t + c16 < a.group ? 0xffffffffu : 0u;
 #pragma unroll
             for (int b = 0; b < NKB; ++b) {
-                const int e = (b * 4 + g) * PE;
-                intx4 x = ((const Sixteen *)(p + std::min(e, a.c.head_dim - PE) * ES))->v;
-                x = within(x, b, a.c.head_dim);
-                const uint32_t keep = is ? 0xffffffffu : 0u;
+                asm volatile("" : "+v"(qv[t][b]));
+                qv[t][b] = within(qv[t][b], b, a.c.head_dim);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    qv[t][b][i] = (x[i] ^ a.flip) & keep;
+                    qv[t][b][i] = (qv[t][b][i] ^ a.flip) & keep;
             }
             m[t] = -INFINITY, l[t] = 0.0f;
 #pragma unroll
@@ -213,15 +233,24 @@ struct Attend {
     struct Pages {
         int page[NS];
     };
+    __device__ inline Pages no_pages() const
+    {
+        Pages x;
+#pragma unroll
+        for (int t = 0; t < NS; ++t)
+            x.page[t] = -1;
+        return x;
+    }
     __device__ inline Pages pages(const CacheView &c, const int32_t *table, int base, const Seen &s) const
     {
         Pages x;
 #pragma unroll
         for (int t = 0; t < NS; ++t) {
-            if constexpr (PAGED) {  // (a scalar load: nothing behind it waits for the rows that are on their way)
-                typedef const __attribute__((address_space(4))) int32_t Const;
+            if constexpr (PAGED) {
                 const int at = base + 16 * t;
-                x.page[t] = at < s.end ? ((Const *)(uintptr_t)table)[c.div.quotient(at)] : -1;
+                x.page[t] = -1;
+                if (at < s.end)
+                    x.page[t] = ((ConstInt *)(uintptr_t)table)[c.div.quotient(at)];
             } else {  // (no choice between the load and another value: it would become a branch; an empty sequence reads its table's first entry)
                 const int key = base + 16 * t + c16;
                 x.page[t] = table[c.div.quotient(std::max(0, std::min(std::max(key, s.first), s.end - 1)))] | (key >= s.first && key < s.end ? 0 : -1);
@@ -292,8 +321,17 @@ struct Attend {
         }
     }
 
+    // A tile, of this unit or the next one's first.
+    struct Next {
+        Pages pages;
+        const char *keys, *values;  // the head's first row
+        int base;
+        Seen s;
+        int seq, head, block;       // seq >= 0: another unit, whose queries are wanted too
+    };
+
     // A tile whose keys and values are on their way; those of the next one are asked for as soon as the registers are free.
-    __device__ inline void tile(const AttendArgs &a, const Pages &next, const char *keys, const char *values, int base, const Seen &s)
+    __device__ inline void tile(const AttendArgs &a, int base, const Seen &s, const Next &next)
     {
         const CacheView &c = a.c;
         const int d = c.head_dim;
@@ -333,8 +371,10 @@ struct Attend {
             const int key = base + 16 * (i / 4) + 4 * g + i % 4;
             return (PAGED ? there[i / 4] != 0 && key >= s.first && key < s.end : (there[i / 4] >> (4 * g + i % 4)) & 1);
         };
-        resolve(c, next, base + KT, s);
-        load_keys(keys);
+        resolve(c, next.pages, next.base, next.s);
+        load_keys(next.keys);
+        if (next.seq >= 0)
+            load_queries(a, next.seq, next.head, next.block);
         if (!whole) {
 #pragma unroll
             for (int t = 0; t < QT; ++t)
@@ -423,7 +463,7 @@ struct Attend {
                     }
                 }
         }
-        load_values(values);
+        load_values(next.values);
     }
 
     // the whole of a unit
@@ -492,6 +532,14 @@ struct Joined {
     float sum, top, total;
 };
 
+// no tile of a unit
+__device__ inline void leave_nothing(const AttendArgs &a, float *rec)
+{
+    const int elems = a.rows * a.c.head_dim;
+    for (int i = lane_id(); i < elems + 2 * a.rows; i += 64)
+        rec[i] = i >= elems && i < elems + a.rows ? -INFINITY : 0.0f;
+}
+
 template <typename T>
 __device__ inline void write_row(const AttendArgs &a, int64_t seq, int unit, int row, int e, const Joined &x)
 {
@@ -504,11 +552,13 @@ __device__ inline void write_row(const AttendArgs &a, int64_t seq, int unit, int
         a.lse[seq * a.q_heads + q] = log_sum(a, x.top, x.total);
 }
 
-template <typename T, int DP, int QT, bool PAGED>
-__global__ void __launch_bounds__(64 * kAttendWaves) k_cache_attend(AttendArgs a)
+// SOLO: a workgroup for each unit, and no line.
+template <typename T, int DP, int QT, bool PAGED, int WAVES, bool SOLO>
+__global__ void __launch_bounds__(64 * WAVES) k_cache_attend(AttendArgs a)
 {
     using A = Attend<T, DP, QT, PAGED>;
-    constexpr int KT = A::KT, WAVES = kAttendWaves;
+    constexpr int KT = A::KT, kCost = SOLO ? 0 : kUnitCost;
+    auto place_of = [&](const Seen &s) { return tiles_of<KT>(s) + kCost; };
     extern __shared__ float records[];  // [waves][2]
     struct Part {
         int64_t u0, u1;  // the unit's tiles
@@ -516,7 +566,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_cache_attend(AttendArgs a
     };
     __shared__ Part parts[WAVES][2];
     const int wave = wave_id_uniform(), lane = lane_id();
-    const int units = a.c.heads * a.blocks, together = a.together, strides = WAVES / together;  // stretches of a workgroup
+    const int units = a.c.heads * a.blocks, together = SOLO ? 1 : a.together, strides = WAVES / together;  // stretches of a workgroup
     const int mine = wave % together, stretch = wave / together;
     const int per_seq = (units + together - 1) / together;
     const int64_t waves = (int64_t)gridDim.x * strides;
@@ -536,8 +586,14 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_cache_attend(AttendArgs a
         s32 = __builtin_amdgcn_readfirstlane(s32 + j);
         return past != 0;
     };
-    if (a.seqs <= 64) {
-        const int64_t scan = wave_scan_i64(lane < a.seqs ? (int64_t)tiles_of<KT>(seen(a.c, a.window, lane)) * per_seq : 0);
+    if constexpr (SOLO) {
+        s32 = blockIdx.x / units;
+        all = place_of(seen(a.c, a.window, s32));
+        at = -(int64_t)(blockIdx.x - s32 * units) * all;  // (the unit begins at 0)
+        each = (int)(all + WAVES - 1) / WAVES;
+        wg_begin = 0, wg_end = all, begin = std::min(all, wave * each), end = std::min(all, begin + each);
+    } else if (a.seqs <= 64) {
+        const int64_t scan = wave_scan_i64(lane < a.seqs ? (int64_t)place_of(seen(a.c, a.window, lane)) * per_seq : 0);
         all = uniform_i64(__shfl(scan, 63));
         deal();
         find((int)a.seqs, scan);
@@ -549,7 +605,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_cache_attend(AttendArgs a
         for (int r = wave; r < n_ranges; r += WAVES) {
             int64_t sum = 0;
             for (int i = r * span * 64 + lane, end = std::min<int64_t>(a.seqs, (r + 1) * (int64_t)span * 64); i < end; i += 64)
-                sum += tiles_of<KT>(seen(a.c, a.window, i));
+                sum += place_of(seen(a.c, a.window, i));
 #pragma unroll
             for (int m = 1; m < 64; m *= 2)
                 sum += __shfl_xor(sum, m);
@@ -583,7 +639,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_cache_attend(AttendArgs a
         const int s_end = (int)std::min<int64_t>(a.seqs, s32 + span * 64);
         while (begin < end && s32 < s_end) {
             const int n = std::min(64, s_end - s32);
-            const int64_t within = wave_scan_i64(lane < n ? (int64_t)tiles_of<KT>(seen(a.c, a.window, s32 + lane)) * per_seq : 0);
+            const int64_t within = wave_scan_i64(lane < n ? (int64_t)place_of(seen(a.c, a.window, s32 + lane)) * per_seq : 0);
             if (find(n, within))
                 break;
             at = uniform_i64(at + __shfl(within, 63)), s32 += n;
@@ -593,54 +649,92 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_cache_attend(AttendArgs a
         parts[wave][lane].is = 0;
     A w;
     w.init(a);
-    for (int64_t pos = begin; pos < end;) {
-        const Seen s = seen(a.c, a.window, s32);
-        const int nt = tiles_of<KT>(s);
-        if (pos >= at + (int64_t)per_seq * nt) {
-            at += (int64_t)per_seq * nt;
-            ++s32;
-            continue;
-        }
-        const int turn = (int)quotient(pos - at, nt), unit = turn * together + mine;  // head * blocks + block
-        const int64_t u0 = at + (int64_t)turn * nt, u1 = u0 + nt, stop = std::min(end, u1);
-        if (unit >= units) {
+    // The units of the stretch, one ahead of the one that is worked on.
+    struct Unit {
+        int64_t u0, u1;  // its place in the line
+        Seen s;          // what it sees
+        int seq, unit, head, block, base, n;  // first row and number of the tiles that are the stretch's; n < 0: there is no such unit
+        bool begins, ends;
+    };
+    int64_t pos = begin;
+    int length = seen_length(a.c, s32);
+    auto advance = [&]() {
+        Unit u;
+        u.n = -1;
+        while (pos < end) {
+            const Seen s = {a.window > 0 ? std::max(0, length - a.window) : 0, length};
+            const int place = place_of(s);
+            if (pos >= at + (int64_t)per_seq * place) {
+                at += (int64_t)per_seq * place;
+                length = seen_length(a.c, ++s32);
+                continue;
+            }
+            const int turn = (int)quotient(pos - at, place);
+            u.unit = turn * together + mine;  // head * blocks + block
+            u.u0 = at + (int64_t)turn * place, u.u1 = u.u0 + place;
+            const int64_t stop = std::min(end, u.u1);
+            const int from = std::max(0, (int)(pos - u.u0) - kCost), to = std::max(0, (int)(stop - u.u0) - kCost);
+            u.begins = pos == u.u0, u.ends = stop == u.u1;
             pos = stop;
-            continue;
+            if (u.unit >= units)
+                continue;
+            u.seq = s32, u.s = s, u.head = u.unit / a.blocks, u.block = u.unit - u.head * a.blocks;
+            if (to == from) {  // none of its tiles: a part all the same, so that the parts of a unit follow each other
+                leave_nothing(a, records + (wave * 2 + u.begins) * a.rec);
+                if (lane == 0)
+                    parts[wave][u.begins] = {u.u0, u.u1, u.seq, u.unit, 1, 0};
+                continue;
+            }
+            u.n = to - from, u.base = s.first / KT * KT + from * KT;
+            u.s.end = std::min(s.end, u.base + u.n * KT);  // (nothing is asked for behind the stretch)
+            break;
         }
-        const int head = unit / a.blocks, block = unit % a.blocks;
-        const int32_t *const table = a.c.table + s32 * a.c.ld_table;
-        const int first = s.first / KT * KT + (int)(pos - u0) * KT, n = (int)(stop - pos);
-        const Seen in = {s.first, std::min(s.end, first + n * KT)};  // (nothing is asked for behind the stretch)
-        const char *const keys = a.c.k + head * a.c.head_stride, *const values = a.c.v + head * a.c.head_stride;
-        typename A::Pages next = w.pages(a.c, table, first, in);
-        w.resolve(a.c, next, first, in);
-        next = w.pages(a.c, table, first + KT, in);
-        w.load_keys(keys);
-        w.load_values(values);
-        w.begin(a, s32, head, block);
-        for (int t = 0; t < n; ++t) {
-            const typename A::Pages then = w.pages(a.c, table, first + (t + 2) * KT, in);
-            w.tile(a, next, keys, values, first + t * KT, in);
-            next = then;
+        return u;
+    };
+    auto table_of = [&](const Unit &u) { return a.c.table + u.seq * a.c.ld_table; };
+    auto keys_of = [&](const Unit &u) { return a.c.k + u.head * a.c.head_stride; };
+    auto values_of = [&](const Unit &u) { return a.c.v + u.head * a.c.head_stride; };
+    Unit u = advance();
+    if (u.n > 0) {
+        w.resolve(a.c, w.pages(a.c, table_of(u), u.base, u.s), u.base, u.s);
+        w.load_keys(keys_of(u));
+        w.load_queries(a, u.seq, u.head, u.block);
+        w.load_values(values_of(u));
+    }
+    while (u.n > 0) {
+        typename A::Pages ahead = w.pages(a.c, table_of(u), u.base + KT, u.s);
+        const Unit v = advance();
+        typename A::Next other = {{}, keys_of(u), values_of(u), u.base, {0, 0}, -1, 0, 0};  // (nothing, where there is no other unit)
+        if (v.n > 0)
+            other = {w.pages(a.c, table_of(v), v.base, v.s), keys_of(v), values_of(v), v.base, v.s, v.seq, v.head, v.block};
+        else
+            other.pages = w.no_pages();
+        w.start(a, u.block);
+        const char *const keys = keys_of(u), *const values = values_of(u);
+        const int32_t *const table = table_of(u);
+        for (int t = 0; t < u.n - 1; ++t) {
+            const typename A::Pages then = w.pages(a.c, table, u.base + (t + 2) * KT, u.s);
+            w.tile(a, u.base + t * KT, u.s, {ahead, keys, values, u.base + (t + 1) * KT, u.s, -1, 0, 0});
+            ahead = then;
         }
-        if (pos == u0 && stop == u1) {
-            w.finish(a, s32, head, block);
+        w.tile(a, u.base + (u.n - 1) * KT, u.s, other);
+        if (u.begins && u.ends) {
+            w.finish(a, u.seq, u.head, u.block);
         } else {  // slot 0: it has begun before the stretch
-            const int slot = pos == u0;
-            w.leave(a, records + (wave * 2 + slot) * a.rec);
+            w.leave(a, records + (wave * 2 + u.begins) * a.rec);
             if (lane == 0)
-                parts[wave][slot] = {u0, u1, s32, unit, 1, 0};
+                parts[wave][u.begins] = {u.u0, u.u1, u.seq, u.unit, 1, 0};
         }
-        pos = stop;
+        u = v;
     }
     __syncthreads();
-    // chains of parts: one of slot 1, or the first wavefront's of slot 0, and the slots 0 that follow while the unit goes on
+    // chains of parts: one of slot 1, or a stretch's first one of slot 0, and the slots 0 that follow while the unit goes on
     const int d = a.c.head_dim, elems = a.rows * d;
     int goes_on = 0;
-    for (int p = 0; p < 2 * WAVES; ++p) {
-        const int w0 = p / 2, slot = p % 2;
-        if (!parts[w0][slot].is || (slot == 0 && w0 >= together))
-            continue;
+    unsigned long long starts = __ballot(lane < 2 * WAVES && parts[lane / 2 % WAVES][lane % 2].is && (lane % 2 == 1 || lane / 2 < together));
+    while (starts) {
+        const int p = __ffsll(starts) - 1, w0 = p / 2, slot = p % 2;
+        starts &= starts - 1;
         const Part unit = parts[w0][slot];
         int n = 1;
         while (w0 + n * together < WAVES && wg_begin + (int64_t)(w0 / together + n) * each < std::min(unit.u1, wg_end))
@@ -648,25 +742,35 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_cache_attend(AttendArgs a
         const bool whole = unit.u0 >= wg_begin && unit.u1 <= wg_end, first = unit.u0 >= wg_begin;
         const int64_t line = (int64_t)blockIdx.x * together + w0 % together;
         float *const to = a.part + (line * 2 + first) * a.rec;
-        for (int i = threadIdx.x; i < elems; i += 64 * WAVES) {
-            const int row = i / d, e = i % d;
+        auto record = [&](int k) { return records + ((w0 + k * together) * 2 + (k == 0 ? slot : 0)) * a.rec; };
+        for (int row = wave; row < a.rows; row += WAVES) {
+            float m[WAVES], l[WAVES];
             Joined x = {0.0f, -INFINITY, 0.0f};
-            for (int k = 0; k < n; ++k)
-                x.top = fmaxf(x.top, records[((w0 + k * together) * 2 + (k == 0 ? slot : 0)) * a.rec + elems + row]);
+#pragma unroll
+            for (int k = 0; k < WAVES; ++k) {
+                const float *const r = record(std::min(k, n - 1)) + elems + row;
+                m[k] = k < n ? r[0] : -INFINITY, l[k] = k < n ? r[a.rows] : 0.0f;
+                x.top = fmaxf(x.top, m[k]);
+            }
             const float from = x.top == -INFINITY ? 0.0f : x.top;
-            for (int k = 0; k < n; ++k) {
-                const float *const r = records + ((w0 + k * together) * 2 + (k == 0 ? slot : 0)) * a.rec;
-                const float f = exp2_fast((r[elems + row] - from) * a.factor);
-                x.sum += r[i] * f;
-                x.total += r[elems + a.rows + row] * f;
+#pragma unroll
+            for (int k = 0; k < WAVES; ++k) {
+                m[k] = exp2_fast((m[k] - from) * a.factor);
+                x.total += l[k] * m[k];
             }
-            if (whole) {
-                write_row<T>(a, unit.seq, unit.unit, row, e, x);
-            } else {
-                to[i] = x.sum;
-                if (e == 0)
-                    to[elems + row] = x.top, to[elems + a.rows + row] = x.total;
+            for (int e = lane; e < d; e += 64) {
+                x.sum = 0.0f;
+#pragma unroll
+                for (int k = 0; k < WAVES; ++k)
+                    if (k < n)
+                        x.sum += record(k)[row * d + e] * m[k];
+                if (whole)
+                    write_row<T>(a, unit.seq, unit.unit, row, e, x);
+                else
+                    to[row * d + e] = x.sum;
             }
+            if (!whole && lane == 0)
+                to[elems + row] = x.top, to[elems + a.rows + row] = x.total;
         }
         if (first && !whole) {
             goes_on |= 1 << w0 % together;
@@ -674,7 +778,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_cache_attend(AttendArgs a
                 a.tails[line] = {unit.seq, unit.unit, (int32_t)quotient(unit.u1 - 1, strides * each)};
         }
     }
-    if (threadIdx.x < together && !(goes_on >> threadIdx.x & 1))
+    if (!SOLO && (int)threadIdx.x < together && !(goes_on >> threadIdx.x & 1))
         a.tails[(int64_t)blockIdx.x * together + threadIdx.x].last = -1;
 }
 
@@ -697,18 +801,10 @@ __global__ void __launch_bounds__(256) k_cache_attend_join(AttendArgs a, int lin
             float m = mine[0], l = mine[a.rows];
             if (lane >= left)
                 m = -INFINITY, l = 0.0f;
-            float top = m;
-#pragma unroll
-            for (int i = 1; i < 64; i *= 2)
-                top = fmaxf(top, __shfl_xor(top, i));
-            top = fmaxf(top, x.top);
+            const float top = fmaxf(wave_max_all(m), x.top);
             const float from = top == -INFINITY ? 0.0f : top;
             const float f = exp2_fast((m - from) * a.factor), keep = exp2_fast((x.top - from) * a.factor);
-            l *= f;
-#pragma unroll
-            for (int i = 1; i < 64; i *= 2)
-                l += __shfl_xor(l, i);
-            x.total = x.total * keep + l;
+            x.total = x.total * keep + wave_sum_all(l * f);
             x.top = top;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -791,6 +887,7 @@ struct AttendPlan {
     int qt, rows, blocks;
     int64_t rec;  // floats
     int wgs, together;
+    bool solo;
     int64_t tails;  // offset in the workspace
     size_t bytes;
 };
@@ -803,32 +900,46 @@ AttendPlan attend_plan(const tig_cache &c, const tig_cache_attend &p)
     L.blocks = (group + 16 * L.qt - 1) / (16 * L.qt);
     L.rec = (int64_t)L.rows * (c.head_dim + 2);
     const int64_t cap = p.window > 0 ? std::min<int64_t>(p.window, (int64_t)c.max_pages * c.page_size) : (int64_t)c.max_pages * c.page_size;
-    const int units = c.heads * L.blocks;
-    // rows of several heads side by side that share lines of 128 bytes
-    const bool shared = c.heads > 1 && c.head_stride < c.token_stride && c.head_stride * es % 128 != 0;
-    L.together = shared ? (units >= 3 ? 4 : 2) : 1;
-    const int64_t tiles = p.seqs * ((units + L.together - 1) / L.together) * (cap / kt + 2);
-    const int per_cu = c.head_dim <= 64 ? (L.qt == 1 ? 3 : 2) : c.head_dim <= 128 && L.qt == 1 ? 2 : 1;  // workgroups on a compute unit: registers
-    L.wgs = (int)std::min<int64_t>(256 * per_cu, (tiles + kAttendWaves / L.together - 1) / (kAttendWaves / L.together));
+    const int64_t units = (int64_t)c.heads * L.blocks, tiles = cap / kt + 2, all = p.seqs * units * (tiles + kUnitCost);
+    // A workgroup for each unit and one launch where there are few tiles for its wavefronts.  8 heads of 128 columns in bf16: 300 rows 10.5 us
+    // this way, 15.7 the other one, 1000 rows 16.7 and 16.2, 4000 rows 42 and 18; 64 such units of 1000 rows 18.2 and 20.6, 256 of them 27 and 35.
+    L.solo = p.seqs * units <= 256 && tiles <= (p.seqs * units >= 64 ? 34 : 14);
+    if (L.solo) {
+        L.wgs = (int)(p.seqs * units), L.together = 1;
+        return L;
+    }
+    const bool side_by_side = c.heads > 1 && c.head_stride < c.token_stride;
+    L.together = !side_by_side || all < 16384 ? 1 : c.head_stride * es % 128 != 0 ? (units >= 3 ? 4 : 2) : p.seqs * units <= 128 ? 2 : 1;
+    const int64_t waves = (all + L.together - 1) / L.together;
+    const int wanted = p.seqs * units >= 2048 * L.together && c.head_dim <= 128 && L.qt == 1 ? 512 : 256;
+    L.wgs = (int)std::min<int64_t>(wanted, (waves + kAttendWaves / L.together - 1) / (kAttendWaves / L.together));
     L.tails = ((int64_t)L.wgs * L.together * 2 * L.rec * 4 + 255) / 256 * 256;
     L.bytes = (size_t)(L.tails + ((int64_t)L.wgs * L.together * sizeof(Tail) + 255) / 256 * 256);
     return L;
 }
 
-template <typename T, int DP, int QT, bool PAGED>
-hipError_t launch_attend(const AttendArgs &a, const AttendPlan &L, hipStream_t s)
+template <typename T, int DP, int QT, bool PAGED, int WAVES, bool SOLO>
+hipError_t launch_attend_main(const AttendArgs &a, const AttendPlan &L, hipStream_t s)
 {
-    const int lds = (int)(kAttendWaves * 2 * L.rec * 4);
-    auto *const kernel = k_cache_attend<T, DP, QT, PAGED>;
+    const int lds = (int)(WAVES * 2 * L.rec * 4);
+    auto *const kernel = k_cache_attend<T, DP, QT, PAGED, WAVES, SOLO>;
     if (lds > 48 * 1024) {
         const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess)
             return e;
     }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)L.wgs), dim3(64 * kAttendWaves), (unsigned)lds, s, a);
-    hipError_t e = hipGetLastError();
+    hipLaunchKernelGGL(kernel, dim3((unsigned)L.wgs), dim3(64 * WAVES), (unsigned)lds, s, a);
+    return hipGetLastError();
+}
+template <typename T, int DP, int QT, bool PAGED>
+hipError_t launch_attend(const AttendArgs &a, const AttendPlan &L, hipStream_t s)
+{
+    if (L.solo)
+        return launch_attend_main<T, DP, QT, PAGED, (DP <= 128 && QT == 1 ? 8 : 4), true>(a, L, s);
+    hipError_t e = launch_attend_main<T, DP, QT, PAGED, kAttendWaves, false>(a, L, s);
     if (e == hipSuccess && L.wgs > 1) {
-        hipLaunchKernelGGL((k_cache_attend_join<T>), dim3((unsigned)((L.wgs * L.together + 3) / 4), (unsigned)L.rows), dim3(256), 0, s, a, L.wgs * L.together);
+        const int lines = L.wgs * L.together;
+        hipLaunchKernelGGL((k_cache_attend_join<T>), dim3((unsigned)((lines + 3) / 4), (unsigned)L.rows), dim3(256), 0, s, a, lines);
         e = hipGetLastError();
     }
     return e;
@@ -907,7 +1018,7 @@ int tig_cache_attend_run(const tig_cache *cache, const tig_cache_attend *p, void
     if (rc != TIG_OK || p->seqs == 0)
         return rc;
     const AttendPlan L = attend_plan(*cache, *p);
-    if (!workspace || ((uintptr_t)workspace & 255))
+    if (L.bytes > 0 && (!workspace || ((uintptr_t)workspace & 255)))
         return fail_text(TIG_EINVAL, "tig_cache_attend_run: workspace is NULL or not 256-byte aligned");
     if (workspace_bytes < L.bytes)
         return fail_text(TIG_ENOSPACE, "tig_cache_attend_run: workspace too small");
