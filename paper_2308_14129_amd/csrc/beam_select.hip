@@ -2,8 +2,8 @@
 //
 //   score of candidate (j, v) = scores_j + l_jv - log sum_u exp l_ju, the k largest, ties to the lowest (j, v)
 //
-//   k_select_segments  reads the logits once: for every segment (a lane's `steps` times eight logits of a wavefront's stretch) its largest
-//                      logit, for every stretch the sum of exp(l - largest); bound by memory
+//   k_select_segments  reads the logits once: for every segment (`group` times 128 logits, 512 apart) its largest logit, for every
+//                      wavefront's stretch the sum of exp(l - largest); bound by memory
 //   k_select_pick      a workgroup per batch entry: log-sums from the segments'; a bound that at least k candidates reach; the few
 //                      segments that reach it are read again, and the candidates at or above it are ranked
 // Which bound: the segments are dealt to 128 groups of threads, and the k-th largest of the groups' maxima is the score of a candidate
@@ -23,13 +23,14 @@ struct SelectArgs {
     int64_t l_batch, l_beam;  // elements
     int64_t batch;
     int32_t beams, k, vocab;
-    // a row: `chunks` chunks of `steps` times 512 logits, 64 segments each; a wavefront's stretch is `per` chunks
-    int32_t steps, chunks, per, stretches;
-    PageDiv by_segments, by_steps;  // divisions by a row's segments, and by `steps`
+    // A row: `blocks` steps of 512 logits, each sixteen lanes' 128 of them; segments of `group` steps, 4 each; a wavefront's stretch is `per`
+    // steps (whole groups).
+    int32_t blocks, group, per, stretches, segments;
+    PageDiv by_segments, by_eights;  // divisions by a row's segments, and by the eights of a segment
     const float *scores;
     const uint8_t *finished;
     int32_t end;
-    float *top;     // [batch x beams][chunks x 64]: largest logit of a segment
+    float *top;     // [batch x beams][segments]: largest logit of segment 4 (step / group) + (lane / 16)
     float2 *sums;   // [batch x beams][stretches]: largest logit, sum of exp(l - largest)
     float *scores_out;
     int32_t *parents, *tokens;
@@ -67,6 +68,30 @@ __device__ inline float max3(float a, float b, float c)
     return r;
 }
 
+// the maxima of four values over each sixteen lanes (four at once: a read of a register just written would have to wait)
+__device__ inline void row_max_four(float (&v)[4])
+{
+    asm volatile("s_nop 1\n\t"
+                 "v_max_f32_dpp %0, %0, %0 row_ror:1 row_mask:0xf bank_mask:0xf\n\t"
+                 "v_max_f32_dpp %1, %1, %1 row_ror:1 row_mask:0xf bank_mask:0xf\n\t"
+                 "v_max_f32_dpp %2, %2, %2 row_ror:1 row_mask:0xf bank_mask:0xf\n\t"
+                 "v_max_f32_dpp %3, %3, %3 row_ror:1 row_mask:0xf bank_mask:0xf\n\t"
+                 "v_max_f32_dpp %0, %0, %0 row_ror:2 row_mask:0xf bank_mask:0xf\n\t"
+                 "v_max_f32_dpp %1, %1, %1 row_ror:2 row_mask:0xf bank_mask:0xf\n\t"
+                 "v_max_f32_dpp %2, %2, %2 row_ror:2 row_mask:0xf bank_mask:0xf\n\t"
+                 "v_max_f32_dpp %3, %3, %3 row_ror:2 row_mask:0xf bank_mask:0xf\n\t"
+                 "v_max_f32_dpp %0, %0, %0 row_ror:4 row_mask:0xf bank_mask:0xf\n\t"
+                 "v_max_f32_dpp %1, %1, %1 row_ror:4 row_mask:0xf bank_mask:0xf\n\t"
+                 "v_max_f32_dpp %2, %2, %2 row_ror:4 row_mask:0xf bank_mask:0xf\n\t"
+                 "v_max_f32_dpp %3, %3, %3 row_ror:4 row_mask:0xf bank_mask:0xf\n\t"
+                 "v_max_f32_dpp %0, %0, %0 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+                 "v_max_f32_dpp %1, %1, %1 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+                 "v_max_f32_dpp %2, %2, %2 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+                 "v_max_f32_dpp %3, %3, %3 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+                 "s_nop 1"
+                 : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]));
+}
+
 template <typename T>
 __global__ void __launch_bounds__(256) k_select_segments(SelectArgs a)
 {
@@ -78,60 +103,86 @@ __global__ void __launch_bounds__(256) k_select_segments(SelectArgs a)
     if (r >= a.batch * a.beams)
         return;
     const bool done = a.finished && a.finished[r];
-    float m = -INFINITY, s = 0.0f;
+    float m = -INFINITY, s = 0.0f, seg = -INFINITY;
     const T *const row = (const T *)a.logits + r / a.beams * a.l_batch + r % a.beams * a.l_beam;
-    const int c0 = stretch * a.per, c1 = std::min(a.chunks, c0 + a.per);
-    for (int c = c0; c < c1; ++c) {
-        float seg = -INFINITY;
-        for (int t0 = 0; t0 < a.steps && !done; t0 += kDeep) {
-            float x[kDeep][8];
-            const int base = (c * a.steps + t0) * 512;
-            if (t0 + kDeep <= a.steps && base + kDeep * 512 <= a.vocab) {
-                Eight<T> q[kDeep];
-#pragma unroll
-                for (int t = 0; t < kDeep; ++t)
-                    q[t] = *(const Eight<T> *)(row + base + t * 512 + lane * 8);
-#pragma unroll
-                for (int t = 0; t < kDeep; ++t)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        x[t][e] = to_float(q[t].v[e]);
-            } else {
-#pragma unroll
-                for (int t = 0; t < kDeep; ++t)
-                    if (t0 + t < a.steps) {
-                        load_eight(row, base + t * 512 + lane * 8, a.vocab, x[t]);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            x[t][e] = -INFINITY;
-                    }
-            }
-            float top = -INFINITY;
+    const int s0 = stretch * a.per, s1 = std::min(a.blocks, s0 + a.per);
+    int place = 0, within = 0;  // the segment of the sixteen that are collected, a lane each, and the step in it
+    int first = s0 / a.group;   // the first of them
+    auto flush = [&]() {
+        const int n = (first + lane % 16) * 4 + lane / 16;
+        if (lane % 16 < place && n < a.segments)
+            a.top[r * a.segments + n] = seg;
+        first += 16, place = 0, seg = -INFINITY;
+    };
+    for (int t0 = s0; t0 < s1; t0 += kDeep) {
+        float x[kDeep][8], top4[kDeep];
+        if (done) {
 #pragma unroll
             for (int t = 0; t < kDeep; ++t)
-#pragma unroll
-                for (int e = 0; e < 8; e += 2)
-                    top = max3(x[t][e], x[t][e + 1], top);
-            seg = fmaxf(seg, top);
-            top = fmaxf(m, top);
-            const float from = top == -INFINITY ? 0.0f : top;
-            s *= __builtin_amdgcn_exp2f((m - from) * kLog2e);
-            float add[kDeep];
-#pragma unroll
-            for (int t = 0; t < kDeep; ++t) {
-                add[t] = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    add[t] += __builtin_amdgcn_exp2f((x[t][e] - from) * kLog2e);
-            }
+                    x[t][e] = -INFINITY;
+        } else if (t0 + kDeep <= s1 && (t0 + kDeep) * 512 <= a.vocab) {
+            Eight<T> q[kDeep];
 #pragma unroll
             for (int t = 0; t < kDeep; ++t)
-                s += add[t];
-            m = top;
+                q[t] = *(const Eight<T> *)(row + (t0 + t) * 512 + lane * 8);
+#pragma unroll
+            for (int t = 0; t < kDeep; ++t)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    x[t][e] = to_float(q[t].v[e]);
+        } else {
+#pragma unroll
+            for (int t = 0; t < kDeep; ++t)
+                if (t0 + t < s1) {
+                    load_eight(row, (t0 + t) * 512 + lane * 8, a.vocab, x[t]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        x[t][e] = -INFINITY;
+                }
         }
-        a.top[(r * a.chunks + c) * 64 + lane] = seg;
+        float top = m;
+#pragma unroll
+        for (int t = 0; t < kDeep; ++t) {
+            top4[t] = max3(x[t][0], x[t][1], x[t][2]);
+            top4[t] = max3(x[t][3], x[t][4], top4[t]);
+            top4[t] = max3(x[t][5], x[t][6], top4[t]);
+            top4[t] = max3(x[t][7], top4[t], top4[t]);
+            top = fmaxf(top, top4[t]);
+        }
+        const float from = top == -INFINITY ? 0.0f : top;
+        s *= __builtin_amdgcn_exp2f((m - from) * kLog2e);
+        float add[kDeep];
+#pragma unroll
+        for (int t = 0; t < kDeep; ++t) {
+            add[t] = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                add[t] += __builtin_amdgcn_exp2f((x[t][e] - from) * kLog2e);
+        }
+#pragma unroll
+        for (int t = 0; t < kDeep; ++t)
+            s += add[t];
+        m = top;
+        row_max_four(top4);
+#pragma unroll
+        for (int t = 0; t < kDeep; ++t) {
+            if (t0 + t >= s1)
+                break;
+            seg = lane % 16 == place ? fmaxf(seg, top4[t]) : seg;
+            if (++within == a.group) {
+                within = 0;
+                if (++place == 16)
+                    flush();
+            }
+        }
     }
+    if (within > 0)
+        ++place;
+    if (place > 0)
+        flush();
     const float top = wave_max_all(m);
     s = wave_sum_all(s * __builtin_amdgcn_exp2f((m - (top == -INFINITY ? 0.0f : top)) * kLog2e));
     if (lane == 0)
@@ -150,7 +201,7 @@ struct PickShared {
     double bound;
     int count, listed;
     int is_finished[kMaxBeams];
-    double value[kRoom];
+    alignas(16) double value[kRoom];
     int32_t id[kRoom];
     int32_t list[kMaxSegments];
 };
@@ -186,7 +237,7 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
     __shared__ PickShared sh;
     const int tid = threadIdx.x, lane = lane_id(), wave = wave_id_uniform();
     const int64_t b = blockIdx.x;
-    const int per_beam = a.chunks * 64, all = a.beams * per_beam, n_sums = a.stretches;
+    const int per_beam = a.segments, all = a.beams * per_beam, n_sums = a.stretches;
     const float *const seg = a.top + b * all;
     const float2 *const sums = a.sums + b * a.beams * n_sums;
     constexpr int kMine = kMaxSegments / kPickThreads;
@@ -288,16 +339,17 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
     push_finished();
     __syncthreads();
     const int listed = sh.listed;
-    // the step-th eight logits of the i-th listed segment: their row, the first one's place there, the beam
+    // the i-th eight logits of the listed segments: their row, the first one's place there, the beam
     struct Place {
         const T *row;
         int at, j;
     };
+    const int per_segment = a.group * 16;
     auto place = [&](int i) {
-        const int of = a.by_steps.quotient(i), n = sh.list[of], j = a.by_segments.quotient(n), c = (n - j * per_beam) / 64;
-        return Place{(const T *)a.logits + b * a.l_batch + j * a.l_beam, (c * a.steps + i - of * a.steps) * 512 + n % 64 * 8, j};
+        const int of = a.by_eights.quotient(i), e = i - of * per_segment, n = sh.list[of], j = a.by_segments.quotient(n), c = n - j * per_beam;
+        return Place{(const T *)a.logits + b * a.l_batch + j * a.l_beam, (c / 4 * a.group + e / 16) * 512 + c % 4 * 128 + e % 16 * 8, j};
     };
-    const int eights = listed * a.steps;
+    const int eights = listed * per_segment;
     constexpr int kDeep = 4;
     for (int i0 = tid; i0 < eights; i0 += kDeep * kPickThreads) {
         Place p[kDeep];
@@ -312,14 +364,18 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
         for (int t = 0; t < kDeep; ++t) {
             if (i0 + t * kPickThreads >= eights || p[t].at >= a.vocab)
                 continue;
-            const int first = a.vocab >= 8 ? std::min(p[t].at, a.vocab - 8) : 0;
+            const int first = a.vocab >= 8 ? std::min(p[t].at, a.vocab - 8) : 0, j = p[t].j;
+            // the logit that reaches the bound, less a few roundings: whoever reaches that is looked at in fp64
+            const float near = (float)(((bound - sh.score[j]) + sh.log_sum[j]) + sh.top[j]);
+            const float least = near - (fabsf(near) * 1e-6f + 1e-30f);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (first + e < p[t].at || first + e >= a.vocab)
+                const float x = a.vocab >= 8 ? to_float(q[t].v[e]) : first + e < a.vocab ? to_float(p[t].row[e]) : -INFINITY;
+                if (x < least || first + e < p[t].at || first + e >= a.vocab)
                     continue;
-                const double v = value(a.vocab >= 8 ? to_float(q[t].v[e]) : to_float(p[t].row[e]), p[t].j);
+                const double v = value(x, j);
                 if (v >= bound && v > -INFINITY)
-                    push(v, p[t].j * a.vocab + first + e);
+                    push(v, j * a.vocab + first + e);
             }
         }
     }
@@ -370,12 +426,19 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
             parts /= 2;
         const int t = tid / parts, part = tid % parts;
         int rank = 0;
-        if (t < count) {
+        if (t < count) {  // (the ids only where values are equal)
             const double v = sh.value[t];
             const int32_t id = sh.id[t];
-#pragma unroll 8
-            for (int i = part; i < count; i += parts)
-                rank += before(sh.value[i], sh.id[i], v, id);
+            const int each = ((count + parts - 1) / parts + 1) / 2 * 2, end = std::min(count, (part + 1) * each);
+#pragma unroll 4
+            for (int i = part * each; i < end; i += 2) {
+                const double2 o = *(const double2 *)&sh.value[i];
+                rank += (o.x > v) + (i + 1 < end && o.y > v);
+                if (o.x == v && i != t)
+                    rank += sh.id[i] < id;
+                if (o.y == v && i + 1 < end && i + 1 != t)
+                    rank += sh.id[i + 1] < id;
+            }
         }
         for (int d = 1; d < parts; d *= 2)
             rank += __shfl_xor(rank, d);
@@ -391,24 +454,24 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
 }
 
 struct SelectPlan {
-    int steps, chunks, per, stretches;
+    int blocks, group, per, stretches, segments;
     size_t sums, bytes;
 };
-// Segments of as few steps as an entry's segments fit; wavefronts of several chunks where there are enough of them.
+// Segments as short as an entry's fit; stretches of up to 32 steps where there are wavefronts enough.
 SelectPlan select_plan(const tig_beam_select &p)
 {
     SelectPlan L = {};
     const int64_t blocks = (p.vocab + 511) / 512, rows = p.batch * p.beams;
-    int64_t steps = 1;
-    while (p.beams * ((blocks + steps - 1) / steps) * 64 > kMaxSegments)
-        steps += steps < 4 ? 1 : 4;
-    const int64_t chunks = (blocks + steps - 1) / steps;
-    int64_t per = std::max<int64_t>(1, rows * chunks / 8192);
-    per = std::min<int64_t>(per, std::max<int64_t>(1, 32 / steps));
-    while (rows * ((chunks + per - 1) / per) > (1 << 25))  // (a launch's threads fit 32 bits)
+    int64_t group = 1;
+    while (p.beams * ((blocks + group - 1) / group) * 4 > kMaxSegments)
+        ++group;
+    int64_t per = std::min<int64_t>(32, std::max<int64_t>(1, rows * blocks / 8192));
+    while (rows * ((blocks + per - 1) / per) > (1 << 25))  // (a launch's threads fit 32 bits)
         per *= 2;
-    L.steps = (int)steps, L.chunks = (int)chunks, L.per = (int)std::min(per, chunks), L.stretches = (int)((chunks + L.per - 1) / L.per);
-    L.sums = ((size_t)rows * chunks * 64 * sizeof(float) + 255) / 256 * 256;
+    per = (per + group - 1) / group * group;
+    L.blocks = (int)blocks, L.group = (int)group, L.per = (int)per, L.stretches = (int)((blocks + per - 1) / per);
+    L.segments = (int)((blocks + group - 1) / group * 4);
+    L.sums = ((size_t)rows * L.segments * sizeof(float) + 255) / 256 * 256;
     L.bytes = (L.sums + (size_t)rows * L.stretches * sizeof(float2) + 255) / 256 * 256;
     return L;
 }
@@ -475,7 +538,8 @@ int tig_beam_select_run(const tig_beam_select *p, void *workspace, size_t worksp
     if ((rc = check_select_apart(*p)) != TIG_OK)
         return rc;
     const hipStream_t s = (hipStream_t)hip_stream;
-    SelectArgs a = {p->logits, p->l_batch, p->l_beam, p->batch, p->beams, p->k, (int32_t)p->vocab, L.steps, L.chunks, L.per, L.stretches, page_div(L.chunks * 64), page_div(L.steps), p->scores, p->finished, p->end,
+    SelectArgs a = {p->logits, p->l_batch, p->l_beam, p->batch, p->beams, p->k, (int32_t)p->vocab, L.blocks, L.group, L.per, L.stretches, L.segments, page_div(L.segments), page_div(L.group * 16),
+                    p->scores, p->finished, p->end,
                     (float *)workspace, (float2 *)((char *)workspace + L.sums), p->scores_out, p->parents, p->tokens, p->finished_out};
     const int64_t waves = p->batch * p->beams * L.stretches;
     const hipError_t e = with_dtype(p->dtype, [&](auto t) {
