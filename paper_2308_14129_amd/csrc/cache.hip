@@ -192,10 +192,10 @@ __device__ inline void append_places(const AppendArgs &a, int64_t token0, int co
     __syncthreads();
 }
 
-// Rows of whole pieces, whose pairs are whole pieces too: a lane has one piece of a row and, for the pairs' other halves, reads the
-// piece that lies there as well (it is on its way for another lane of the wavefront), so that reads and writes are whole lines: a row in pairs
-// of pieces, 62500 tokens of 40 rows of 256 bytes, 192 of them turned, took 347 us, so it takes 279.  Rows do not cross wavefronts:
-// one may be turned in place.
+// Rows by pieces of 16 bytes: a lane has one piece of a row and, for the pairs' other halves, reads the piece that lies there as well (it
+// is on its way for another lane of the wavefront), so that reads and writes are whole lines: with a pair of pieces to a lane 62500 tokens of
+// 40 rows of 256 bytes, 192 of them turned, took 347 us, so they take 264 (a copy of as much 250).  Rows do not cross wavefronts: one
+// may be turned in place.
 template <typename T>
 __global__ void __launch_bounds__(256) k_cache_append_rows(AppendArgs a, AppendUnits n)
 {
@@ -207,10 +207,8 @@ __global__ void __launch_bounds__(256) k_cache_append_rows(AppendArgs a, AppendU
     const CacheView &c = a.c;
     const int pairs = a.rotary / 2;
     append_places(a, token0, count, sh);
-    for (int u = tid; u < n.all; u += 256) {
-        const int r = u >> n.shift, e = (u & ((1 << n.shift) - 1)) * VE;
-        if (e >= c.head_dim)
-            continue;
+    for (int u = blockIdx.y * 256 + tid; u < n.all; u += 256 * gridDim.y) {
+        const int r = u >> n.shift, w = u & ((1 << n.shift) - 1);
         const char *from;
         char *to;
         int64_t from_token, to_token = -1;
@@ -225,7 +223,14 @@ __global__ void __launch_bounds__(256) k_cache_append_rows(AppendArgs a, AppendU
             from = a.v + (r - a.q_heads - c.heads) * a.v_head, from_token = a.v_token;
             to = c.v + (r - a.q_heads - c.heads) * c.head_stride;
         }
-        const bool turns = (is_q || is_k) && e < a.rotary, first = e < pairs;
+        // the piece's first column: pieces of each part of the row (halves of the pairs, or the pairs; what is behind them), the last of a
+        // part from its end (some columns twice, from the same values: all lanes of the row have read before one writes)
+        const int parts = a.interleaved ? 1 : 2, turned = is_q || is_k ? parts * n.n_pair : 0;
+        const bool turns = w < turned, first = w < n.n_pair;
+        const int begin = !turns ? (turned > 0 ? a.rotary : 0) : first ? 0 : pairs, end = !turns ? c.head_dim : a.interleaved ? a.rotary : first ? pairs : a.rotary;
+        const int at = begin + (w - (!turns ? turned : first ? 0 : n.n_pair)) * VE, e = std::min(at, end - VE);
+        if (at >= end)
+            continue;
         const int other = !turns || a.interleaved ? e : first ? e + pairs : e - pairs;
         const int j = a.interleaved ? e / 2 : first ? e : e - pairs;
         from += token0 * from_token;
@@ -262,7 +267,7 @@ __global__ void __launch_bounds__(256) k_cache_append_rows(AppendArgs a, AppendU
     }
 }
 
-// Any rows.
+// Rows with a part that is shorter than a piece, or of more pieces than a wavefront has lanes: a pair of pieces to a lane, what is left element by element.
 template <typename T>
 __global__ void __launch_bounds__(256) k_cache_append(AppendArgs a, AppendUnits n)
 {
@@ -279,7 +284,7 @@ __global__ void __launch_bounds__(256) k_cache_append(AppendArgs a, AppendUnits 
     const int group = n.groups > 1 ? tid / n.all : 0;
     if (group >= n.groups)
         return;
-    for (int u = n.groups > 1 ? tid - group * n.all : tid; u < n.all; u += 256) {
+    for (int u = n.groups > 1 ? tid - group * n.all : blockIdx.y * 256 + tid; u < n.all; u += 256 * gridDim.y) {
         // the unit: where its one or two pieces come from and go to in a token.  All pairs of pieces, then what is copied: a wavefront is
         // mostly of one kind.
         const char *from;
@@ -503,9 +508,12 @@ int tig_cache_append_run(const tig_cache *cache, const tig_cache_append *p, void
     a.q_heads = p->q_heads, a.rotary = p->rotary, a.interleaved = p->interleaved, a.position_type = p->position_type;
     const int ve = (int)(16 / es), d = cache->head_dim;
     AppendUnits n = {};
-    const bool whole = d % ve == 0 && (p->interleaved ? p->rotary : p->rotary / 2) % ve == 0;
-    if (whole) {
-        while (ve << n.shift < d)
+    const int part = p->interleaved ? p->rotary : p->rotary / 2, rest = d - p->rotary;
+    const int in_part = (part + ve - 1) / ve, in_row = std::max((p->interleaved ? 1 : 2) * in_part + (rest + ve - 1) / ve, (d + ve - 1) / ve);
+    const bool pieces = (part == 0 || part >= ve) && (rest == 0 || rest >= ve) && in_row <= 64;  // parts of a piece at least, a row in a wavefront
+    if (pieces) {
+        n.n_pair = in_part;
+        while (1 << n.shift < in_row)
             ++n.shift;
         n.all = (p->q_heads + 2 * cache->heads) << n.shift;
     } else {
@@ -520,10 +528,12 @@ int tig_cache_append_run(const tig_cache *cache, const tig_cache_append *p, void
     }
     // a workgroup's tokens: as many as leave about four workgroups for a compute unit
     n.per = (int)std::min<int64_t>(kAppendTokens, std::max<int64_t>(1, p->tokens / 1024));
-    const dim3 grid((unsigned)((p->tokens + n.per - 1) / n.per));
+    // ... and a few tokens' rows by several workgroups (one token of 48 rows of 256 bytes: 5.0 us by one, 3.9 by three)
+    const int64_t groups = (p->tokens + n.per - 1) / n.per, shares = groups <= 256 ? (n.all + 255) / 256 : 1;
+    const dim3 grid((unsigned)groups, (unsigned)shares);
     with_dtype(cache->dtype, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL((whole ? k_cache_append_rows<T> : k_cache_append<T>), grid, dim3(256), 0, (hipStream_t)hip_stream, a, n);
+        hipLaunchKernelGGL((pieces ? k_cache_append_rows<T> : k_cache_append<T>), grid, dim3(256), 0, (hipStream_t)hip_stream, a, n);
         return 0;
     });
     const hipError_t e = hipGetLastError();

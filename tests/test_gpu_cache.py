@@ -45,6 +45,7 @@ APPEND = [
     (3, 0, 100, 7, 100, False, "int64", "kv", None), (2, 6, 64, 32, 32, False, "place", "pairs", [3, 0, 17, 1, 64, 0]),
     (4, 4, 256, 16, 256, True, "int64", "outer", [40, 1, 5]), (1, 5, 33, 9, 20, True, "time", "padded", [2, 2, 90]), (2, 8, 72, 64, 0, False, "place", "rows", [7, 100]),
     (2, 3, 19, 5, 18, False, "place", "padded", [11]), (1, 1, 17, 3, 2, False, "int64", "heads", None), (2, 2, 24, 65, 22, False, "time", "kv", [1, 1, 1, 200]),
+    (1, 2, 256, 16, 130, False, "int64", "rows", [30, 4]), (2, 3, 100, 16, 96, False, "place", "heads", [300, 1200]), (1, 2, 254, 16, 126, False, "place", "rows", None),
 ]
 
 
