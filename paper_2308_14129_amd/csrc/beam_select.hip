@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
     for (int i = 0; i < kMine; ++i)
         mine[i] = seg[std::min(tid + i * kPickThreads, all - 1)];
     // log-sums: some wavefronts per beam
-    const int per = kPickWaves >= a.beams ? kPickWaves / a.beams : 1;  // wavefronts of a beam
+    const int per = std::min(std::max(1, kPickWaves / a.beams), (n_sums + 63) / 64);  // wavefronts of a beam: a sum or two for each lane
     for (int j0 = 0; j0 < a.beams; j0 += kPickWaves / per) {
         const int j = j0 + wave / per, part = wave % per;
         const bool is = j < a.beams && wave / per < kPickWaves / per;

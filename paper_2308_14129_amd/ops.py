@@ -460,6 +460,20 @@ def _gpu(index, t):
     return torch._C._cuda_getCurrentRawStream(index) if torch._C._cuda_getDevice() == index else None
 
 
+_sizes = {}  # workspaces' bytes by the sizes of a call (which is all that they depend on)
+
+
+def _bytes_for(key, ask, *args):
+    n = _sizes.get(key)
+    if n is None:
+        need = c_size_t(0)
+        _check(ask(*args, byref(need)))
+        if len(_sizes) >= 4096:
+            _sizes.clear()
+        n = _sizes[key] = need.value
+    return n
+
+
 def _elsewhere(t, f, *args, **kw):
     with _On(t.device):
         return f(*args, **kw)
@@ -474,7 +488,9 @@ def cache_append(k_cache, v_cache, table, lengths, k, v, starts=None, q=None, fr
     given.  Returns the rotated queries (q_out, which may be q; None without q).  A token without a row in the table or a page is left
     out, in q_out too."""
     c, dtype, index, seqs, heads, dim, pt, ld, pn = _cache(k_cache, v_cache, table, lengths)
-    tokens = len(k)
+    if k.dim() != 3:
+        _refuse("k and v are [tokens, heads, head_dim]")
+    tokens = k.size(0)
     if starts is None and tokens != seqs:
         _refuse(f"{tokens} tokens for {seqs} sequences, and no starts")
     pk, k0, k1 = _heads(k, tokens, heads, dim, dtype, index, "k")
@@ -528,17 +544,14 @@ def cache_attend(q, k_cache, v_cache, table, lengths, scale=None, window=0, out=
     if stream is None:
         return _elsewhere(q, cache_attend, q, k_cache, v_cache, table, lengths, scale, window, out, lse)
     if out is None:
-        out = q.new_empty((seqs, qh, dim))
+        out = torch.empty_like(q) if q.is_contiguous() else q.new_empty((seqs, qh, dim))
         po, o0, o1 = out.data_ptr(), qh * dim, dim
     if lse:
         sums = q.new_empty((seqs, qh), dtype=torch.float32)
         pl = sums.data_ptr()
     p = _attend_bytes(104, window, seqs, qh, dim**-0.5 if scale is None else scale, pt, ld, pn, pq, po, pl, q0, q1, o0, o1)
-    lib, need = _lib(), c_size_t(0)
-    rc = lib.tig_cache_attend_workspace_bytes(c, p, byref(need))
-    if rc:
-        _check(rc)
-    n = need.value
+    lib = _lib()
+    n = _bytes_for((c[:32], c[48:], seqs, qh, window), lib.tig_cache_attend_workspace_bytes, c, p)
     ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
     rc = lib.tig_cache_attend_run(c, p, ws.data_ptr() if n else None, n, stream)
     if rc:
@@ -553,7 +566,8 @@ def beam_select(logits, k, scores=None, finished=None, end=-1):
     """The k best continuations over beams and candidates: logits [batch, beams, vocab] (candidates adjacent), scores [batch, beams]
     (float32) of the beams so far, finished [batch, beams] (bool) the beams that go on with nothing but `end`, their score
     unchanged.  Returns BeamSelect(scores [batch, k] in descending order, parents [batch, k] (rows of logits: entry * beams + beam), tokens
-    [batch, k], finished [batch, k]): ties to the lowest beam, then token; -infinity, -1, -1 where no candidate is left."""
+    [batch, k], finished [batch, k]; None without `end`): ties to the lowest beam, then token; -infinity, -1, -1 where no candidate is
+    left."""
     if logits.dim() != 3:
         _refuse("logits is [batch, beams, vocab]")
     batch, beams, vocab = logits.shape
@@ -578,15 +592,14 @@ def beam_select(logits, k, scores=None, finished=None, end=-1):
     if stream is None:
         return _elsewhere(logits, beam_select, logits, k, scores, finished, end)
     shape = (batch, k)
-    new, parents = logits.new_empty(shape, dtype=torch.float32), logits.new_empty(shape, dtype=torch.int32)
-    tokens, done = torch.empty_like(parents), logits.new_empty(shape, dtype=torch.bool)
+    new = logits.new_empty(shape, dtype=torch.float32) if scores is None or k != beams else torch.empty_like(scores)
+    parents = torch.empty_like(new, dtype=torch.int32)
+    tokens = torch.empty_like(parents)
+    done = torch.empty_like(new, dtype=torch.bool) if end >= 0 else None
     p = _select_bytes(112, code, batch, beams, k, vocab, logits.data_ptr(), l0 if batch > 1 else 0, l1 if beams > 1 else 0, ps, pf, end, 0,
-                      new.data_ptr(), parents.data_ptr(), tokens.data_ptr(), done.data_ptr())
-    lib, need = _lib(), c_size_t(0)
-    rc = lib.tig_beam_select_workspace_bytes(p, byref(need))
-    if rc:
-        _check(rc)
-    n = need.value
+                      new.data_ptr(), parents.data_ptr(), tokens.data_ptr(), 0 if done is None else done.data_ptr())
+    lib = _lib()
+    n = _bytes_for((code, batch, beams, vocab), lib.tig_beam_select_workspace_bytes, p)
     ws = torch.empty(n, dtype=torch.uint8, device=logits.device) if n else None
     rc = lib.tig_beam_select_run(p, ws.data_ptr() if n else None, n, stream)
     if rc:

@@ -42,7 +42,8 @@ def check(logits, k, scores=None, finished=None, end=-1):
     r = ops.beam_select(logits, k, scores, finished=finished, end=end)
     torch.cuda.synchronize()
     value, parents, tokens, done = reference(logits, k, scores, finished, end)
-    assert torch.equal(r.parents.long(), parents) and torch.equal(r.tokens.long(), tokens) and torch.equal(r.finished, done)
+    assert torch.equal(r.parents.long(), parents) and torch.equal(r.tokens.long(), tokens)
+    assert r.finished is None if end < 0 else torch.equal(r.finished, done)
     # a score is rounded once; the log-sum of fp32 exponentials (4 units each and their argument's rounding, sums of eight and of the lanes)
     # is off by at most 64 units of its own
     ok = value > float("-inf")
@@ -95,7 +96,7 @@ def test_orders_and_masks(dtype):
     x[3, 0, 77] = float("nan")  # a row that counts nothing
     x[3, 1, V - 1] = float("inf")
     r = check(x, 40, -torch.rand(4, 3, device=DEV, generator=gen))
-    assert (r.parents[0] == -1).all() and (r.tokens[0] == -1).all() and (r.scores[0] == minus).all() and not r.finished[0].any()
+    assert (r.parents[0] == -1).all() and (r.tokens[0] == -1).all() and (r.scores[0] == minus).all()
     assert (r.parents[2] >= 0).sum() == 15
     low = torch.finfo(t).min
     y = torch.randn(1, 2, 2000, device=DEV, generator=gen).to(t)
