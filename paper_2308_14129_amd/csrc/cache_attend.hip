@@ -135,6 +135,7 @@ __device__ inline float log_sum(const AttendArgs &a, float top, float total) { r
 
 template <typename T, int DP, int QT, bool PAGED>
 struct Attend {
+    using Type = T;
     static constexpr int ES = sizeof(T), PE = 16 / ES, KT = AttendType<T>::KT, NS = KT / 16;
     static constexpr int NKB = DP / (4 * PE);             // blocks of k of the scores' product
     static constexpr int VE = ES == 2 && DP == 64 ? 4 : PE;  // columns of V that a lane loads at once
@@ -321,6 +322,46 @@ struct Attend {
         }
     }
 
+    // The keys as they are multiplied.  (A load's value is used whatever the conditions: else it would move into a branch, and be waited
+    // for there.)
+    __device__ inline void take_keys(int d)
+    {
+        if (PAGED ? d % PE != 0 : d < DP) {
+#pragma unroll
+            for (int t = 0; t < NS; ++t)
+#pragma unroll
+                for (int b = 0; b < NKB; ++b) {
+                    if constexpr (!PAGED)
+                        asm volatile("" : "+v"(kv[t][b]));
+                    kv[t][b] = within(kv[t][b], b, d);
+                }
+        }
+    }
+    // ... and the values; cut: those of keys that do not count are zero (zero times what no sequence has is not zero where that is
+    // infinite)
+    template <class F>
+    __device__ inline void take_values(bool cut, F &&valid)
+    {
+        if constexpr (!PAGED) {
+#pragma unroll
+            for (int i = 0; i < VK; ++i)
+#pragma unroll
+                for (int b = 0; b < NG; ++b)
+#pragma unroll
+                    for (int e = 0; e < VE * ES / 4; ++e)
+                        asm volatile("" : "+v"(vv[i][b].d[e]));
+        }
+        if (cut) {
+#pragma unroll
+            for (int i = 0; i < VK; ++i)
+#pragma unroll
+                for (int b = 0; b < NG; ++b)
+#pragma unroll
+                    for (int e = 0; e < VE * ES / 4; ++e)
+                        vv[i][b].d[e] = valid(i) ? vv[i][b].d[e] : 0;
+        }
+    }
+
     // A tile, of this unit or the next one's first.
     struct Next {
         Pages pages;
@@ -335,17 +376,7 @@ struct Attend {
     {
         const CacheView &c = a.c;
         const int d = c.head_dim;
-        // (the load's value is used whatever the conditions: else it would move into a branch, and be waited for there)
-        if (PAGED ? d % PE != 0 : d < DP) {
-#pragma unroll
-            for (int t = 0; t < NS; ++t)
-#pragma unroll
-                for (int b = 0; b < NKB; ++b) {
-                    if constexpr (!PAGED)
-                        asm volatile("" : "+v"(kv[t][b]));
-                    kv[t][b] = within(kv[t][b], b, d);
-                }
-        }
+        take_keys(d);
         float p[QT][VK];
 #pragma unroll
         for (int t = 0; t < QT; ++t)
@@ -406,24 +437,7 @@ struct Attend {
             }
             l[t] += sum;
         }
-        if constexpr (!PAGED) {
-#pragma unroll
-            for (int i = 0; i < VK; ++i)
-#pragma unroll
-                for (int b = 0; b < NG; ++b)
-#pragma unroll
-                    for (int e = 0; e < VE * ES / 4; ++e)
-                        asm volatile("" : "+v"(vv[i][b].d[e]));
-        }
-        if (PAGED ? base < s.first : !whole) {  // (zero times what no sequence has is not zero where that is infinite)
-#pragma unroll
-            for (int i = 0; i < VK; ++i)
-#pragma unroll
-                for (int b = 0; b < NG; ++b)
-#pragma unroll
-                    for (int e = 0; e < VE * ES / 4; ++e)
-                        vv[i][b].d[e] = valid(i) ? vv[i][b].d[e] : 0;
-        }
+        take_values(PAGED ? base < s.first : !whole, valid);
         if constexpr (ES == 4) {
 #pragma unroll
             for (int b = 0; b < NG; ++b)
@@ -532,6 +546,159 @@ struct Joined {
     float sum, top, total;
 };
 
+// fp32 with one or two query heads to a head: sixteen queries' products of which one is wanted take the matrix units a thousand cycles a tile
+// of 16 keys and 64 columns, that one in vector instructions a tenth of it (4000 histories of two heads of 50 columns, 1.14 GB: 258 and 235 us).  The lanes have keys and values as
+// above; the scores' sums over a lane's columns are joined over the four lanes of a key, each lane then weighs its key, and the weights of
+// a lane's four keys of values are fetched from the lanes that have them.
+template <int DP, int G, bool PAGED>
+struct AttendFew : Attend<float, DP, 1, PAGED> {
+    using Base = Attend<float, DP, 1, PAGED>;
+    using Base::c16, Base::g, Base::kv, Base::vv, Base::from, Base::extent;
+    static constexpr int NKB = Base::NKB, NG = Base::NG, VE = Base::VE, KT = Base::KT, kColumns = NG * VE;
+    static_assert(KT == 16 && VE == 4, "");
+
+    floatx4 q[G][NKB];
+    float m[G], l[G], o[G][kColumns];  // m: all lanes alike; l: of the lane's key; o: of the lane's keys of values
+
+    __device__ inline void load_queries(const AttendArgs &a, int seq, int head, int)
+    {
+#pragma unroll
+        for (int t = 0; t < G; ++t) {
+            const char *const p = a.q + seq * a.q_seq + (int64_t)(head * a.group + std::min(t, a.group - 1)) * a.q_head;
+#pragma unroll
+            for (int b = 0; b < NKB; ++b)
+                q[t][b] = __builtin_bit_cast(floatx4, ((const Sixteen *)(p + std::min((b * 4 + g) * 4, a.c.head_dim - 4) * 4))->v);
+        }
+    }
+    __device__ inline void start(const AttendArgs &a, int)
+    {
+#pragma unroll
+        for (int t = 0; t < G; ++t) {
+#pragma unroll
+            for (int b = 0; b < NKB; ++b) {
+                intx4 x = __builtin_bit_cast(intx4, q[t][b]);
+                asm volatile("" : "+v"(x));
+                x = this->within(x, b, a.c.head_dim);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    x[i] ^= a.flip;
+                q[t][b] = __builtin_bit_cast(floatx4, x);
+            }
+            m[t] = -INFINITY, l[t] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kColumns; ++i)
+                o[t][i] = 0.0f;
+        }
+    }
+    __device__ inline void tile(const AttendArgs &a, int base, const Seen &s, const typename Base::Next &next)
+    {
+        const CacheView &c = a.c;
+        const int d = c.head_dim;
+        this->take_keys(d);
+        float sc[G];
+#pragma unroll
+        for (int t = 0; t < G; ++t) {
+            floatx4 part = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int b = 0; b < NKB; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    part[i] = fmaf(__int_as_float(kv[0][b][i]), q[t][b][i], part[i]);
+            sc[t] = groups_sum((part[0] + part[1]) + (part[2] + part[3]));
+        }
+        const int key = base + c16;
+        const bool here = PAGED ? extent[0] > 0 && key >= s.first && key < s.end : from[0] >= 0;
+        const unsigned long long there = __ballot(here);
+        const bool whole = there == ~0ull, cut = PAGED ? base < s.first : !whole;
+        this->resolve(c, next.pages, next.base, next.s);
+        this->load_keys(next.keys);
+        if (next.seq >= 0)
+            load_queries(a, next.seq, next.head, next.block);
+        float p[G][4];
+#pragma unroll
+        for (int t = 0; t < G; ++t) {
+            if (!whole)
+                sc[t] = here ? sc[t] : -INFINITY;
+            const float top = fmaxf(m[t], row_max_all(sc[t]));
+            if (__any(top > m[t])) {
+                const float keep = exp2_fast((m[t] - top) * a.factor);
+                l[t] *= keep;
+#pragma unroll
+                for (int i = 0; i < kColumns; ++i)
+                    o[t][i] *= keep;
+                m[t] = top;
+            }
+            const float w = exp2_fast((sc[t] - (top == -INFINITY ? 0.0f : top)) * a.factor);
+            l[t] += w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                p[t][i] = __shfl(w, 4 * g + i);
+        }
+        this->take_values(cut, [&](int i) { return (there >> (4 * g + i)) & 1; });
+#pragma unroll
+        for (int t = 0; t < G; ++t)
+#pragma unroll
+            for (int b = 0; b < NG; ++b)
+#pragma unroll
+                for (int e = 0; e < VE; ++e)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        o[t][b * VE + e] = fmaf(p[t][i], __int_as_float(vv[i][b].d[e]), o[t][b * VE + e]);
+        this->load_values(next.values);
+    }
+    // f(row, first column, the lane's four columns): each column of each row once
+    template <class F>
+    __device__ inline void columns(const AttendArgs &a, F &&f)
+    {
+#pragma unroll
+        for (int t = 0; t < G; ++t) {
+#pragma unroll
+            for (int b = 0; b < NG; ++b) {
+                floatx4 x;
+#pragma unroll
+                for (int e = 0; e < VE; ++e)
+                    x[e] = groups_sum(o[t][b * VE + e]);
+                const int e0 = (b * 16 + c16) * VE;
+                if (t < a.group && b % 4 == g && e0 < a.c.head_dim)
+                    f(t, std::min(e0, a.c.head_dim - VE), x);
+            }
+        }
+    }
+    __device__ inline void finish(const AttendArgs &a, int64_t seq, int head, int)
+    {
+        float by[G];
+#pragma unroll
+        for (int t = 0; t < G; ++t) {
+            const float total = row_sum_all(l[t]);
+            by[t] = inverse(total);
+            if (a.lse && t < a.group && this->lane == 0)
+                a.lse[seq * a.q_heads + head * a.group + t] = log_sum(a, m[t], total);
+        }
+        columns(a, [&](int t, int e, const floatx4 &x) {
+            float r = by[0];
+#pragma unroll
+            for (int i = 1; i < G; ++i)
+                r = t == i ? by[i] : r;
+            store_four((float *)(a.out + seq * a.o_seq + (int64_t)(head * a.group + t) * a.o_head) + e, x * r, 4);
+        });
+    }
+    __device__ inline void leave(const AttendArgs &a, float *rec)
+    {
+        const int elems = a.rows * a.c.head_dim;
+#pragma unroll
+        for (int t = 0; t < G; ++t) {
+            const float total = row_sum_all(l[t]);
+            if (t < a.group && this->lane == 0)
+                rec[elems + t] = m[t], rec[elems + a.rows + t] = total;
+        }
+        columns(a, [&](int t, int e, const floatx4 &x) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                rec[t * a.c.head_dim + e + i] = x[i];
+        });
+    }
+};
+
 // no tile of a unit
 __device__ inline void leave_nothing(const AttendArgs &a, float *rec)
 {
@@ -553,10 +720,10 @@ __device__ inline void write_row(const AttendArgs &a, int64_t seq, int unit, int
 }
 
 // SOLO: a workgroup for each unit, and no line.
-template <typename T, int DP, int QT, bool PAGED, int WAVES, bool SOLO>
+template <class A, int WAVES, bool SOLO>
 __global__ void __launch_bounds__(64 * WAVES) k_cache_attend(AttendArgs a)
 {
-    using A = Attend<T, DP, QT, PAGED>;
+    using T = typename A::Type;
     constexpr int KT = A::KT, kCost = SOLO ? 0 : kUnitCost;
     auto place_of = [&](const Seen &s) { return tiles_of<KT>(s) + kCost; };
     extern __shared__ float records[];  // [waves][2]
@@ -884,7 +1051,7 @@ __global__ void __launch_bounds__(256) k_cache_attend_join(AttendArgs a, int lin
 }
 
 struct AttendPlan {
-    int qt, rows, blocks;
+    int few, qt, rows, blocks;
     int64_t rec;  // floats
     int wgs, together;
     bool solo;
@@ -895,6 +1062,8 @@ AttendPlan attend_plan(const tig_cache &c, const tig_cache_attend &p)
 {
     AttendPlan L = {};
     const int group = p.q_heads / c.heads, es = dtype_bytes(c.dtype), kt = es == 4 ? 16 : 32;
+    // (four to a head: 300 us for 4000 histories, 280 on the matrix units; two of 256 columns: no registers)
+    L.few = es != 4 ? 0 : group == 1 ? 1 : group == 2 && c.head_dim <= 128 ? 2 : 0;
     L.qt = group > 16 && c.head_dim <= 128 ? 2 : 1;
     L.rows = std::min(group, 16 * L.qt);
     L.blocks = (group + 16 * L.qt - 1) / (16 * L.qt);
@@ -908,21 +1077,27 @@ AttendPlan attend_plan(const tig_cache &c, const tig_cache_attend &p)
         L.wgs = (int)(p.seqs * units), L.together = 1;
         return L;
     }
+    // Wavefronts that go through the same rows together where these lie side by side and share lines of 128 bytes (4000 histories of two heads of
+    // 200 bytes 318 us each by itself, 259 together), or where few long sequences are all there is (4 x 131071 rows of 8 x 256 bytes 404 and
+    // 390; 77 sequences of 16 x 128 bytes 135 and 138).
     const bool side_by_side = c.heads > 1 && c.head_stride < c.token_stride;
     L.together = !side_by_side || all < 16384 ? 1 : c.head_stride * es % 128 != 0 ? (units >= 3 ? 4 : 2) : p.seqs * units <= 128 ? 2 : 1;
     const int64_t waves = (all + L.together - 1) / L.together;
-    const int wanted = p.seqs * units >= 2048 * L.together && c.head_dim <= 128 && L.qt == 1 ? 512 : 256;
+    // A workgroup for each compute unit, one wavefront for each SIMD, fills the memory (4 x 131071 rows: 390 us, with two or four of them 399 and
+    // 418); two where there are many units of few tiles, whose ends nothing runs beside (4000 histories of up to 100 rows 51 and 45 us, of up to
+    // 3000 235 and 256; 600 sequences of up to 500 rows 146 and 140).
+    const int wanted = p.seqs * units >= 2048 * L.together && tiles <= 34 && c.head_dim <= 128 && L.qt == 1 ? 512 : 256;
     L.wgs = (int)std::min<int64_t>(wanted, (waves + kAttendWaves / L.together - 1) / (kAttendWaves / L.together));
     L.tails = ((int64_t)L.wgs * L.together * 2 * L.rec * 4 + 255) / 256 * 256;
     L.bytes = (size_t)(L.tails + ((int64_t)L.wgs * L.together * sizeof(Tail) + 255) / 256 * 256);
     return L;
 }
 
-template <typename T, int DP, int QT, bool PAGED, int WAVES, bool SOLO>
+template <class A, int WAVES, bool SOLO>
 hipError_t launch_attend_main(const AttendArgs &a, const AttendPlan &L, hipStream_t s)
 {
     const int lds = (int)(WAVES * 2 * L.rec * 4);
-    auto *const kernel = k_cache_attend<T, DP, QT, PAGED, WAVES, SOLO>;
+    auto *const kernel = k_cache_attend<A, WAVES, SOLO>;
     if (lds > 48 * 1024) {
         const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess)
@@ -931,27 +1106,34 @@ hipError_t launch_attend_main(const AttendArgs &a, const AttendPlan &L, hipStrea
     hipLaunchKernelGGL(kernel, dim3((unsigned)L.wgs), dim3(64 * WAVES), (unsigned)lds, s, a);
     return hipGetLastError();
 }
-template <typename T, int DP, int QT, bool PAGED>
+// solo_waves: wavefronts of a workgroup for each unit, as many as have the registers
+template <class A, int SOLO_WAVES>
 hipError_t launch_attend(const AttendArgs &a, const AttendPlan &L, hipStream_t s)
 {
     if (L.solo)
-        return launch_attend_main<T, DP, QT, PAGED, (DP <= 128 && QT == 1 ? 8 : 4), true>(a, L, s);
-    hipError_t e = launch_attend_main<T, DP, QT, PAGED, kAttendWaves, false>(a, L, s);
+        return launch_attend_main<A, SOLO_WAVES, true>(a, L, s);
+    hipError_t e = launch_attend_main<A, kAttendWaves, false>(a, L, s);
     if (e == hipSuccess && L.wgs > 1) {
         const int lines = L.wgs * L.together;
-        hipLaunchKernelGGL((k_cache_attend_join<T>), dim3((unsigned)((lines + 3) / 4), (unsigned)L.rows), dim3(256), 0, s, a, lines);
+        hipLaunchKernelGGL((k_cache_attend_join<typename A::Type>), dim3((unsigned)((lines + 3) / 4), (unsigned)L.rows), dim3(256), 0, s, a, lines);
         e = hipGetLastError();
     }
     return e;
 }
-template <typename T, int DP>
+template <typename T, int DP, bool PAGED>
 hipError_t launch_attend_dim(const AttendArgs &a, const AttendPlan &L, hipStream_t s)
 {
-    const bool paged = a.c.page_size % 16 == 0;
+    if constexpr (sizeof(T) == 4) {
+        if (L.few == 1)
+            return launch_attend<AttendFew<DP, 1, PAGED>, (DP <= 128 ? 8 : 4)>(a, L, s);
+        if constexpr (DP <= 128)
+            if (L.few == 2)
+                return launch_attend<AttendFew<DP, 2, PAGED>, 8>(a, L, s);
+    }
     if constexpr (DP <= 128)
         if (L.qt == 2)
-            return paged ? launch_attend<T, DP, 2, true>(a, L, s) : launch_attend<T, DP, 2, false>(a, L, s);
-    return paged ? launch_attend<T, DP, 1, true>(a, L, s) : launch_attend<T, DP, 1, false>(a, L, s);
+            return launch_attend<Attend<T, DP, 2, PAGED>, 4>(a, L, s);
+    return launch_attend<Attend<T, DP, 1, PAGED>, (DP <= 128 ? 8 : 4)>(a, L, s);
 }
 
 int check_attend(const tig_cache *c, const tig_cache_attend *p)
@@ -1034,13 +1216,13 @@ int tig_cache_attend_run(const tig_cache *cache, const tig_cache_attend *p, void
     a.factor = std::max(std::fabs(p->scale) * 1.44269504f, FLT_MIN);  // (not zero: a masked score times it has to stay -infinity)
     a.flip = p->scale < 0.0f ? (es == 4 ? 0x80000000u : 0x80008000u) : 0u;
     a.part = (float *)workspace, a.tails = (Tail *)((char *)workspace + L.tails), a.rec = L.rec;
+    const hipStream_t s = (hipStream_t)hip_stream;
     const hipError_t e = with_dtype(cache->dtype, [&](auto t) {
         using T = decltype(t);
-        if (cache->head_dim <= 64)
-            return launch_attend_dim<T, 64>(a, L, (hipStream_t)hip_stream);
-        if (cache->head_dim <= 128)
-            return launch_attend_dim<T, 128>(a, L, (hipStream_t)hip_stream);
-        return launch_attend_dim<T, 256>(a, L, (hipStream_t)hip_stream);
+        const int d = cache->head_dim;
+        if (cache->page_size % 16 == 0)
+            return d <= 64 ? launch_attend_dim<T, 64, true>(a, L, s) : d <= 128 ? launch_attend_dim<T, 128, true>(a, L, s) : launch_attend_dim<T, 256, true>(a, L, s);
+        return d <= 64 ? launch_attend_dim<T, 64, false>(a, L, s) : d <= 128 ? launch_attend_dim<T, 128, false>(a, L, s) : launch_attend_dim<T, 256, false>(a, L, s);
     });
     return e == hipSuccess ? TIG_OK : fail_global("tig_cache_attend_run", e);
 }
