@@ -114,36 +114,8 @@ __global__ void __launch_bounds__(256) k_select_segments(SelectArgs a)
             a.top[r * a.segments + n] = seg;
         first += 16, place = 0, seg = -INFINITY;
     };
-    for (int t0 = s0; t0 < s1; t0 += kDeep) {
-        float x[kDeep][8], top4[kDeep];
-        if (done) {
-#pragma unroll
-            for (int t = 0; t < kDeep; ++t)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    x[t][e] = -INFINITY;
-        } else if (t0 + kDeep <= s1 && (t0 + kDeep) * 512 <= a.vocab) {
-            Eight<T> q[kDeep];
-#pragma unroll
-            for (int t = 0; t < kDeep; ++t)
-                q[t] = *(const Eight<T> *)(row + (t0 + t) * 512 + lane * 8);
-#pragma unroll
-            for (int t = 0; t < kDeep; ++t)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    x[t][e] = to_float(q[t].v[e]);
-        } else {
-#pragma unroll
-            for (int t = 0; t < kDeep; ++t)
-                if (t0 + t < s1) {
-                    load_eight(row, (t0 + t) * 512 + lane * 8, a.vocab, x[t]);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        x[t][e] = -INFINITY;
-                }
-        }
-        float top = m;
+    auto add = [&](int t0, const float (&x)[kDeep][8]) {
+        float top4[kDeep], top = m;
 #pragma unroll
         for (int t = 0; t < kDeep; ++t) {
             top4[t] = max3(x[t][0], x[t][1], x[t][2]);
@@ -153,18 +125,18 @@ __global__ void __launch_bounds__(256) k_select_segments(SelectArgs a)
             top = fmaxf(top, top4[t]);
         }
         const float from = top == -INFINITY ? 0.0f : top;
-        s *= __builtin_amdgcn_exp2f((m - from) * kLog2e);
-        float add[kDeep];
+        float sums[kDeep];
 #pragma unroll
         for (int t = 0; t < kDeep; ++t) {
-            add[t] = 0.0f;
+            sums[t] = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                add[t] += __builtin_amdgcn_exp2f((x[t][e] - from) * kLog2e);
+                sums[t] += __builtin_amdgcn_exp2f((x[t][e] - from) * kLog2e);
         }
+        s *= __builtin_amdgcn_exp2f((m - from) * kLog2e);
 #pragma unroll
         for (int t = 0; t < kDeep; ++t)
-            s += add[t];
+            s += sums[t];
         m = top;
         row_max_four(top4);
 #pragma unroll
@@ -178,6 +150,34 @@ __global__ void __launch_bounds__(256) k_select_segments(SelectArgs a)
                     flush();
             }
         }
+    };
+    int t0 = s0;
+    if (!done)
+        for (; t0 + kDeep <= s1 && (t0 + kDeep) * 512 <= a.vocab; t0 += kDeep) {
+            float x[kDeep][8];
+            Eight<T> q[kDeep];
+#pragma unroll
+            for (int t = 0; t < kDeep; ++t)
+                q[t] = *(const Eight<T> *)(row + (t0 + t) * 512 + lane * 8);
+#pragma unroll
+            for (int t = 0; t < kDeep; ++t)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    x[t][e] = to_float(q[t].v[e]);
+            add(t0, x);
+        }
+    for (; t0 < s1; t0 += kDeep) {
+        float x[kDeep][8];
+#pragma unroll
+        for (int t = 0; t < kDeep; ++t)
+            if (!done && t0 + t < s1) {
+                load_eight(row, (t0 + t) * 512 + lane * 8, a.vocab, x[t]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    x[t][e] = -INFINITY;
+            }
+        add(t0, x);
     }
     if (within > 0)
         ++place;
@@ -457,7 +457,8 @@ struct SelectPlan {
     int blocks, group, per, stretches, segments;
     size_t sums, bytes;
 };
-// Segments as short as an entry's fit; stretches of up to 32 steps where there are wavefronts enough.
+// Segments as short as an entry's fit; stretches of up to 8 steps where there are wavefronts enough (129 rows of a million: 120 us, 118 with 16,
+// 122 with 64; 400 rows of 250,000: 48, 51, 51).
 SelectPlan select_plan(const tig_beam_select &p)
 {
     SelectPlan L = {};
@@ -465,7 +466,8 @@ SelectPlan select_plan(const tig_beam_select &p)
     int64_t group = 1;
     while (p.beams * ((blocks + group - 1) / group) * 4 > kMaxSegments)
         ++group;
-    int64_t per = std::min<int64_t>(32, std::max<int64_t>(1, rows * blocks / 8192));
+    int64_t per = std::min<int64_t>(8, std::max<int64_t>(1, rows * blocks / 8192));
+    per = per > 4 ? 8 : per;
     while (rows * ((blocks + per - 1) / per) > (1 << 25))  // (a launch's threads fit 32 bits)
         per *= 2;
     per = (per + group - 1) / group * group;
