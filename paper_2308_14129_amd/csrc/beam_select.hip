@@ -6,9 +6,10 @@
 //                      wavefront's stretch the sum of exp(l - largest); bound by memory
 //   k_select_pick      a workgroup per batch entry: log-sums from the segments'; a bound that at least k candidates reach; the few
 //                      segments that reach it are read again, and the candidates at or above it are ranked
-// Which bound: the segments are dealt to 128 groups of threads, and the k-th largest of the groups' maxima is the score of a candidate
-// that k - 1 others reach at least.  For values in no particular order a few more than k lie above it; whatever order they are
-// in, nothing above it is missed.  Scores are compared in fp64: candidates of one beam in the order of their logits, those of several
+// Which bound: the segments are dealt in turn to 128 groups, and the k-th largest of the groups' maxima is the score of a candidate that
+// k - 1 others reach at least.  For values in no particular order, also where one beam has all the best, a few more than k lie above it;
+// whatever order they are in, nothing above it is missed.  Where more than 512 candidates reach it, the candidates themselves are dealt to the
+// groups for a better one.  Scores are compared in fp64: candidates of one beam in the order of their logits, those of several
 // beams with log-sums whose error, fp32 exponentials' of random sign over a vocabulary, is about 1e-8.
 #include <cmath>
 
@@ -197,7 +198,7 @@ struct PickShared {
     double top[kMaxBeams], log_sum[kMaxBeams], score[kMaxBeams];  // a row's log-sum-exp is top + log_sum: beside a mask of -3e38 one number loses the sum
     double part_sum[kPickWaves];
     float part_max[kPickWaves];
-    double group[kGroups];
+    double tops[kPickThreads], group[kGroups];
     double bound;
     int count, listed;
     int is_finished[kMaxBeams];
@@ -229,6 +230,62 @@ __device__ inline void sort_candidates(PickShared &sh, int n)
             }
             __syncthreads();
         }
+}
+
+// the k-th largest of the groups' maxima, of every thread's `top`
+__device__ inline double group_bound(PickShared &sh, double top, int k)
+{
+    constexpr int kParts = kPickThreads / kGroups;
+    const int tid = threadIdx.x, t = tid / kParts, part = tid % kParts;
+    sh.tops[tid] = top;
+    __syncthreads();
+    if (tid < kGroups) {
+#pragma unroll
+        for (int i = 1; i < kParts; ++i)
+            top = fmax(top, sh.tops[tid + i * kGroups]);
+        sh.group[tid] = top;
+    }
+    __syncthreads();
+    const double mine = sh.group[t];
+    int rank = 0;
+#pragma unroll
+    for (int i = 0; i < kGroups; i += kParts)
+        rank += before(sh.group[i + part], i + part, mine, t);
+#pragma unroll
+    for (int d = 1; d < kParts; d *= 2)
+        rank += __shfl_xor(rank, d);
+    if (part == 0 && rank == k - 1)
+        sh.bound = mine;
+    __syncthreads();
+    return sh.bound;
+}
+
+// drops candidates below a better bound, if that is one
+__device__ inline double raise_bound(PickShared &sh, double bound, int k)
+{
+    static_assert(kRoom == 2 * kPickThreads, "");
+    const int tid = threadIdx.x, n = sh.count;
+    double v[2];
+    int32_t id[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int at = tid + i * kPickThreads;
+        v[i] = at < n ? sh.value[at] : -INFINITY, id[i] = at < n ? sh.id[at] : 0;
+    }
+    const double better = group_bound(sh, fmax(v[0], v[1]), k);
+    if (better <= bound)
+        return bound;
+    if (tid == 0)
+        sh.count = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (tid + i * kPickThreads < n && v[i] >= better) {
+            const int at = atomicAdd(&sh.count, 1);
+            sh.value[at] = v[i], sh.id[at] = id[i];
+        }
+    __syncthreads();
+    return better;
 }
 
 template <typename T>
@@ -299,30 +356,9 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
         }
         top = fmax(top, here[i]);
     }
-#pragma unroll
-    for (int d = 1; d < kPickThreads / kGroups; d *= 2)
-        top = fmax(top, __shfl_xor(top, d));
-    if (tid % (kPickThreads / kGroups) == 0)
-        sh.group[tid / (kPickThreads / kGroups)] = top;
     if (tid == 0)
         sh.count = sh.listed = 0;
-    __syncthreads();
-    {
-        constexpr int kParts = kPickThreads / kGroups;
-        const int t = tid / kParts, part = tid % kParts;
-        const double group_top = sh.group[t];
-        int rank = 0;
-#pragma unroll
-        for (int i = 0; i < kGroups; i += kParts)
-            rank += before(sh.group[i + part], i + part, group_top, t);
-#pragma unroll
-        for (int d = 1; d < kParts; d *= 2)
-            rank += __shfl_xor(rank, d);
-        if (part == 0 && rank == a.k - 1)
-            sh.bound = group_top;
-    }
-    __syncthreads();
-    double bound = sh.bound;
+    double bound = group_bound(sh, top, a.k);
     auto push = [&](double v, int32_t id) {
         const int at = atomicAdd(&sh.count, 1);
         if (at < kRoom)
@@ -389,6 +425,9 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
         __syncthreads();
         for (int i0 = 0; i0 < eights; i0 += kPickThreads)
             for (int e = 0; e < 8; ++e) {
+                if (sh.count > kRoom - kPickThreads)
+                    bound = raise_bound(sh, bound, a.k);
+                __syncthreads();
                 if (sh.count > kRoom - kPickThreads) {
                     const int n = sh.count;
                     sort_candidates(sh, n);
@@ -410,6 +449,8 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
                 __syncthreads();
             }
     }
+    if (sh.count > 512)
+        bound = raise_bound(sh, bound, a.k);
     const int count = sh.count;
     auto write = [&](int rank, double v, int32_t id) {
         const int64_t o = b * a.k + rank;
