@@ -92,12 +92,15 @@ constexpr double kQuarterHi = 1.57079632679489655800, kQuarterLo = 6.12323399573
 
 // Cosine and sine of an angle in fp64: quarter turns are taken off (exactly, by fused products with the two parts of pi / 2), the rest, at
 // most pi / 4, goes through the Taylor polynomials to the thirteenth and twelfth degree (their next terms are 2e-14 and 4e-13 there), and
-// each is rounded once.  About 25 operations at fp64's rate, which is fp32's on this card.
+// each is rounded once.  About 30 operations at fp64's rate, which is fp32's on this card.
 __device__ inline void cos_sin(double angle, float &c, float &s)
 {
-    const double n = rint(angle * kTurn8);
+    double n = rint(angle * kTurn8);
     double x = fma(n, -kQuarterHi, angle);
     x = fma(n, -kQuarterLo, x);
+    const double again = rint(x * kTurn8);  // (of a far angle the first count is off by one at most)
+    x = fma(again, -kQuarterHi, x);
+    n += again;
     const double y = x * x;
     double ps = 1.0 / 6227020800.0, pc = 1.0 / 479001600.0;
     ps = fma(y, ps, -1.0 / 39916800.0);

@@ -88,6 +88,7 @@ __device__ inline int tiles_of(const Seen &s)
 }
 // What a unit takes beside its tiles, in tiles: it stands that much longer in the line, ahead of them.
 constexpr int kUnitCost = 2;
+constexpr int kNeverShared = 2;  // tiles of a unit that one wavefront takes in any case
 
 // (a division in 64 bits is a hundred instructions)
 __device__ inline int64_t quotient(int64_t a, int64_t b) { return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b; }
@@ -823,11 +824,12 @@ __global__ void __launch_bounds__(64 * WAVES) k_cache_attend(AttendArgs a)
         int seq, unit, head, block, base, n;  // first row and number of the tiles that are the stretch's; n < 0: there is no such unit
         bool begins, ends;
     };
-    // Units that are short beside the stretches are not shared (2059 sequences of one row: 40 us shared, 17 not): the stretches differ by a
-    // sixteenth for it.
-    const int short_unit = (int)std::min<int64_t>(1 << 20, each / 16 + 1 + kCost);
+    // Units that are short beside the stretches are not shared, nor are units of two tiles (2059 sequences of one row: 40 us shared, 27 not): the
+    // stretches differ by a sixteenth for it.
+    const int short_unit = (int)std::min<int64_t>(1 << 20, std::max<int64_t>(each / 16 + 1, kNeverShared)) + kCost;
     int64_t pos = begin;
-    int length = seen_length(a.c, s32);
+    const int last_seq = (int)a.seqs - 1;
+    int length = seen_length(a.c, s32), next_length = seen_length(a.c, std::min(s32 + 1, last_seq));  // (asked for a unit ahead)
     auto advance = [&]() {
         Unit u;
         u.n = -1;
@@ -836,7 +838,7 @@ __global__ void __launch_bounds__(64 * WAVES) k_cache_attend(AttendArgs a)
             const int place = place_of(s);
             if (pos >= at + (int64_t)per_seq * place) {
                 at += (int64_t)per_seq * place;
-                length = seen_length(a.c, ++s32);
+                length = next_length, next_length = seen_length(a.c, std::min(++s32 + 1, last_seq));
                 continue;
             }
             const int turn = (int)quotient(pos - at, place);
@@ -1064,7 +1066,7 @@ struct AttendPlan {
     int few, qt, rows, blocks;
     int64_t rec;  // floats
     int wgs, together;
-    bool solo;
+    bool solo, joins;
     int64_t tails;  // offset in the workspace
     size_t bytes;
 };
@@ -1098,6 +1100,8 @@ AttendPlan attend_plan(const tig_cache &c, const tig_cache_attend &p)
     // 3000 235 and 256; 600 sequences of up to 500 rows 146 and 140).
     const int wanted = p.seqs * units >= 2048 * L.together && tiles <= 34 && c.head_dim <= 128 && L.qt == 1 ? 512 : 256;
     L.wgs = (int)std::min<int64_t>(wanted, (waves + kAttendWaves / L.together - 1) / (kAttendWaves / L.together));
+    const int64_t most = (cap + kt - 1) / kt + (p.window > 0 && cap == p.window ? 1 : 0);  // tiles of a unit
+    L.joins = L.wgs > 1 && most > kNeverShared;
     L.tails = ((int64_t)L.wgs * L.together * 2 * L.rec * 4 + 255) / 256 * 256;
     L.bytes = (size_t)(L.tails + ((int64_t)L.wgs * L.together * sizeof(Tail) + 255) / 256 * 256);
     return L;
@@ -1123,7 +1127,7 @@ hipError_t launch_attend(const AttendArgs &a, const AttendPlan &L, hipStream_t s
     if (L.solo)
         return launch_attend_main<A, SOLO_WAVES, true>(a, L, s);
     hipError_t e = launch_attend_main<A, kAttendWaves, false>(a, L, s);
-    if (e == hipSuccess && L.wgs > 1) {
+    if (e == hipSuccess && L.joins) {
         const int lines = L.wgs * L.together;
         hipLaunchKernelGGL((k_cache_attend_join<typename A::Type>), dim3((unsigned)((lines + 3) / 4), (unsigned)L.rows), dim3(256), 0, s, a, lines);
         e = hipGetLastError();

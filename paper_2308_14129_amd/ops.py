@@ -540,6 +540,8 @@ def cache_attend(q, k_cache, v_cache, table, lengths, scale=None, window=0, out=
     po = o0 = o1 = pl = 0
     if out is not None:
         po, o0, o1 = _heads(out, seqs, qh, dim, dtype, index, "out")
+    if window > 0x7FFFFFFF:  # (no sequence is that long)
+        window = 0
     stream = _gpu(index, q)
     if stream is None:
         return _elsewhere(q, cache_attend, q, k_cache, v_cache, table, lengths, scale, window, out, lse)
@@ -573,6 +575,8 @@ def beam_select(logits, k, scores=None, finished=None, end=-1):
     batch, beams, vocab = logits.shape
     if not 1 <= k <= 128:
         _refuse(f"k = {k} is not in 1 .. 128")
+    if not -1 <= end < vocab:
+        _refuse(f"end = {end} is no candidate")
     code, index = _dtype_code(logits.dtype), logits.get_device()
     l0, l1, l2 = logits.stride()
     if l2 != 1 and vocab > 1:

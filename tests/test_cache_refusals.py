@@ -255,7 +255,7 @@ CALLS = [(f, kw, n) for f in (append, attend, fork) for n, kw in SHARED.items()]
     (attend, dict(out=ROWS), "out of other heads"), (attend, dict(out=torch.zeros(3, 4, 32)[..., ::2]), "out's columns apart"),
     (fork, dict(parents=I32.long()), "int64 parents"), (fork, dict(spare=I32[:2]), "spare of others"), (fork, dict(parents=torch.zeros(6, dtype=torch.int32)[::2]), "parents apart"),
     (select, dict(logits=LOGITS[0]), "2-dimensional logits"), (select, dict(logits=LOGITS.double()), "float64 logits"), (select, dict(logits=torch.zeros(2, 3, 80)[..., ::2]), "candidates apart"),
-    (select, dict(k=0), "k 0"), (select, dict(k=129), "k 129"), (select, dict(scores=SCORES[0]), "scores of others"), (select, dict(scores=SCORES.double()), "float64 scores"),
+    (select, dict(k=0), "k 0"), (select, dict(end=40), "end behind the vocabulary"), (select, dict(end=2**40), "end far behind it"), (select, dict(end=-2), "end -2"), (select, dict(k=129), "k 129"), (select, dict(scores=SCORES[0]), "scores of others"), (select, dict(scores=SCORES.double()), "float64 scores"),
     (select, dict(finished=SCORES), "float32 finished"), (select, dict(finished=torch.zeros(2, 2, dtype=torch.bool)), "finished of others"),
     (select, dict(scores=torch.zeros(3, 2).t()), "scores in another order"),
 ]

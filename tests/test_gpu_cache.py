@@ -118,6 +118,22 @@ def test_append(case, dtype):
         assert got is None
 
 
+def test_append_far_positions():
+    """Angles up to 2^53 are reduced in 64 bits."""
+    n, d = 4000, 16
+    k_cache, v_cache = make_cache(n, 1, 1, d, torch.float32, "rows")
+    table = torch.arange(n, dtype=torch.int32, device=DEV)[:, None]
+    lengths = torch.ones(n, dtype=torch.int32, device=DEV)
+    gen = gen_of(17)
+    k = torch.randn(n, 1, d, device=DEV, generator=gen)
+    freq = torch.ones(d // 2, dtype=F64, device=DEV)
+    for top in (1 << 30, 1 << 45, 1 << 53):
+        pos = torch.randint(-top, top, (n,), device=DEV, generator=gen)
+        ops.cache_append(k_cache, v_cache, table, lengths, k, k, freq=freq, positions=pos)
+        want, mag = rotated(k.cpu(), pos.cpu(), freq.cpu(), False)  # (the host's cosine takes the angle as it is)
+        close(k_cache[:, 0].cpu(), want, 8 * U * mag + tiny(torch.float32), f"up to {top}")
+
+
 def test_append_leaves_out_what_has_no_row():
     t, size = torch.float32, 4
     k_cache, v_cache = make_cache(6, size, 2, 16, t, "rows", fill=0.0)
@@ -228,6 +244,37 @@ def test_attend_many_lengths(size, dtype):
     for _ in range(3):
         again = ops.cache_attend(q, k_cache, v_cache, table, L, lse=True)
         assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+
+
+@pytest.mark.parametrize("n, heads, qh", [(20_000, 1, 1), (20_000, 3, 6), (70_001, 2, 2), (65, 2, 4), (300, 5, 5)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attend_very_many_short_sequences(n, heads, qh, dtype):
+    """All of them at once in 64 bits: rows that are shared by many, none to five rows each."""
+    t, gen, size, d = TYPES[dtype], gen_of(n), 16, 24
+    k_cache, v_cache = (torch.randn(9, size, heads, d, device=DEV, generator=gen).to(t) for _ in range(2))
+    table = torch.randint(0, 9, (n, 3), device=DEV, generator=gen, dtype=torch.int32)
+    most = 5 if n > 1000 else 40
+    lengths = torch.randint(0, most + 1, (n,), device=DEV, generator=gen, dtype=torch.int32)
+    q = torch.randn(n, qh, d, device=DEV, generator=gen).to(t)
+    for window in (0, 3):
+        print(f"[attend] {n} sequences, window {window}", flush=True)
+        out, lse = ops.cache_attend(q, k_cache, v_cache, table, lengths, window=window, lse=True)
+        p = torch.arange(most, device=DEV)
+        page = table.long()[:, p // size]
+        seen = (p < lengths[:, None]) & ((p >= lengths[:, None] - window) if window else True)
+        K, V = k_cache[page, p % size].to(F64), v_cache[page, p % size].to(F64)  # [n, most, heads, d]
+        Q = q.to(F64).view(n, heads, qh // heads, d)
+        s = (Q[:, :, :, None, :] * K.permute(0, 2, 1, 3)[:, :, None]).sum(-1) * d**-0.5
+        size_s = (Q[:, :, :, None, :].abs() * K.permute(0, 2, 1, 3)[:, :, None].abs()).sum(-1) * d**-0.5
+        s = s.masked_fill(~seen[:, None, None, :], float("-inf"))
+        l = torch.logsumexp(s, -1)
+        w = torch.where(seen[:, None, None, :], torch.exp(s - l[..., None]), 0.0)
+        o = (w[..., None] * V.permute(0, 2, 1, 3)[:, :, None]).sum(-2)
+        size_o = (w[..., None] * V.permute(0, 2, 1, 3)[:, :, None].abs()).sum(-2)
+        off = 2 * (d + 3) * U * size_s.amax(-1) + 4 * U * 40 + (most + 32) * U + (0 if t is torch.float32 else 2.0**-17)  # (see attention())
+        close(out, o.reshape(n, qh, d), (half(t) * o.abs() + 2.02 * off[..., None] * size_o + tiny(t)).reshape(n, qh, d), "out")
+        close(lse, l.reshape(n, qh), (1.01 * off + 8 * U * (l.abs().nan_to_num(posinf=0.0) + 40)).reshape(n, qh), "lse")
+        assert not out[lengths == 0].any() and (lse[lengths == 0] == float("-inf")).all()
 
 
 @pytest.mark.parametrize("dtype", TYPES)
