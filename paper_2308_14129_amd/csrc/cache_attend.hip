@@ -14,8 +14,14 @@
 //   values       O[column][query] = V^T P^T: V's operand wants several keys of one column; a lane loads adjacent columns
 //                VE c .. (c = lane % 16) of the keys that it has the weights of, and one product takes the columns VE c + t of all c: packing the
 //                t-th columns of two keys is one instruction
-// Weights P are 16-bit operands in two parts, P = hi + lo: the matrix units have the time (a tile of 32 keys takes 16 KB through
-// memory and less than half a microsecond of them), and one rounding of P would cost as much as rounding the output does.
+// Weights P are 16-bit operands in two parts, P = hi + lo: the matrix units have the time (a tile of 32 keys of 128 columns takes a
+// wavefront two microseconds and more from memory and a quarter of one for both parts), and one rounding of P would cost as much as rounding
+// the output does.
+//
+// Bound by memory where there is much to read: 4 x 131071 rows of 8 heads of 128 columns in bf16, 64 query heads, 390 us (2.15 GB at 5.5 TB/s);
+// 77 sequences of up to 4096 rows of 16 heads of 64 columns in fp16 127 us (655 MB, 5.2 TB/s); 4000 histories of up to 3000 rows of two heads of 50
+// columns in fp32 235 us (1.14 GB, 4.9 TB/s).  Bound by its chain of reads (length, page, rows) and the two launches where there is
+// little: one sequence of 1000 rows 15 us.
 #include <cfloat>
 #include <cmath>
 #include <type_traits>
@@ -548,9 +554,9 @@ struct Joined {
 };
 
 // fp32 with one or two query heads to a head: sixteen queries' products of which one is wanted take the matrix units a thousand cycles a tile
-// of 16 keys and 64 columns, that one in vector instructions a tenth of it (4000 histories of two heads of 50 columns, 1.14 GB: 258 and 235 us).  The lanes have keys and values as
-// above; the scores' sums over a lane's columns are joined over the four lanes of a key, each lane then weighs its key, and the weights of
-// a lane's four keys of values are fetched from the lanes that have them.
+// of 16 keys and 64 columns, that one in vector instructions a tenth of it (4000 histories of two heads of 50 columns, 1.14 GB: 258 and
+// 235 us).  The lanes have keys and values as above; the scores' sums over a lane's columns are joined over the four lanes of a key, each
+// lane then weighs its key, and the weights of a lane's four keys of values are fetched from the lanes that have them.
 template <int DP, int G, bool PAGED>
 struct AttendFew : Attend<float, DP, 1, PAGED> {
     using Base = Attend<float, DP, 1, PAGED>;
@@ -738,7 +744,7 @@ __global__ void __launch_bounds__(64 * WAVES) k_cache_attend(AttendArgs a)
     const int mine = wave % together, stretch = wave / together;
     const int per_seq = (units + together - 1) / together;
     const int64_t waves = (int64_t)gridDim.x * strides;
-    int64_t all, at = 0, each, wg_begin, wg_end, begin, end;  // at: where sequence s32 begins
+    int64_t all, at = 0, each, wg_begin, wg_end, begin, end;  // the line and the stretch of it; at: where sequence s32 begins
     int s32 = 0;
     auto deal = [&]() {
         each = quotient(all + waves - 1, waves);
@@ -765,7 +771,7 @@ __global__ void __launch_bounds__(64 * WAVES) k_cache_attend(AttendArgs a)
         all = uniform_i64(__shfl(scan, 63));
         deal();
         find((int)a.seqs, scan);
-    } else {  // each thread adds a range of sequences up; then the range, then the sequence
+    } else {  // the wavefronts add ranges of sequences up; then the range, then the sequence
         constexpr int kRanges = 256;
         __shared__ int64_t ranges[kRanges];
         const int blocks = (int)((a.seqs + 63) / 64), span = (blocks + kRanges - 1) / kRanges;  // a range: `span` times 64 sequences
