@@ -404,9 +404,10 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
             if (i0 + t * kPickThreads >= eights || p[t].at >= a.vocab)
                 continue;
             const int first = a.vocab >= 8 ? std::min(p[t].at, a.vocab - 8) : 0, j = p[t].j;
-            // the logit that reaches the bound, less a few roundings: whoever reaches that is looked at in fp64
+            // the logit that reaches the bound, less a few roundings of it and of the score: whoever reaches that is looked at in fp64
             const float near = (float)(((bound - sh.score[j]) + sh.log_sum[j]) + sh.top[j]);
-            const float least = near - (fabsf(near) * 1e-6f + 1e-30f);
+            const float size = (float)(fabs(bound) + fabs(sh.score[j]) + fabs(sh.log_sum[j]) + fabs(sh.top[j]));
+            const float least = near - (fabsf(near) * 1e-6f + size * 1e-14f + 1e-30f);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float x = a.vocab >= 8 ? to_float(q[t].v[e]) : first + e < a.vocab ? to_float(p[t].row[e]) : -INFINITY;
@@ -426,16 +427,20 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
         __syncthreads();
         push_finished();
         __syncthreads();
+        int32_t bound_id = 0x7fffffff;  // of candidates at the bound, the last id that still counts
         for (int i0 = 0; i0 < eights; i0 += kPickThreads)
             for (int e = 0; e < 8; ++e) {
-                if (sh.count > kRoom - kPickThreads)
-                    bound = raise_bound(sh, bound, a.k);
+                if (sh.count > kRoom - kPickThreads) {
+                    const double better = raise_bound(sh, bound, a.k);
+                    if (better > bound)
+                        bound = better, bound_id = 0x7fffffff;
+                }
                 __syncthreads();
                 if (sh.count > kRoom - kPickThreads) {
                     const int n = sh.count;
                     sort_candidates(sh, n);
                     if (n >= a.k)
-                        bound = sh.value[a.k - 1];
+                        bound = sh.value[a.k - 1], bound_id = sh.id[a.k - 1];
                     if (tid == 0)
                         sh.count = n < a.k ? n : a.k;
                 }
@@ -445,8 +450,9 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
                     const Place p = place(i);
                     if (p.at + e < a.vocab) {
                         const double v = value(to_float(p.row[p.at + e]), p.j);
-                        if (v >= bound && v > -INFINITY)
-                            push(v, p.j * a.vocab + p.at + e);
+                        const int32_t id = p.j * a.vocab + p.at + e;
+                        if ((v > bound || (v == bound && id <= bound_id)) && v > -INFINITY)
+                            push(v, id);
                     }
                 }
                 __syncthreads();

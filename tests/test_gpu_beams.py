@@ -121,6 +121,18 @@ def test_strides_and_alignment(dtype):
     check(base[:1].expand(3, 5, 4111), 10)
 
 
+def test_scores_that_fp64_cannot_tell_apart_are_ties():
+    """Logits that differ by less than a score's last place: the lowest place wins, as among equal ones."""
+    x = torch.zeros(1, 2, 5000, device=DEV)
+    x[0, 0, 4000] = 1e-20
+    x[0, 1, 17] = -1e-25
+    x[0, :, 4500:] = 1e-30
+    check(x, 20, torch.tensor([[-7.0, -7.0]], device=DEV))
+    check(x, 128)
+    x[0, 0, 300:] = float("-inf")
+    check(x, 20, torch.tensor([[-3.0, -7.0]], device=DEV))
+
+
 def test_more_candidates_above_the_bound_than_there_is_room_for():
     """Thousands of equal candidates, or better and better ones, in the few segments that are read again."""
     V = 120_000
