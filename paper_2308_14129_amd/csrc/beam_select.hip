@@ -8,12 +8,12 @@
 //                      segments that reach it are read again, and the candidates at or above it are ranked
 // Which bound: the segments are dealt in turn to 128 groups, and the k-th largest of the groups' maxima is the score of a candidate that
 // k - 1 others reach at least.  For values in no particular order, also where one beam has all the best, a few more than k lie above it;
-// whatever order they are in, nothing above it is missed.  Where more than 512 candidates reach it, the candidates themselves are dealt to the
+// whatever order they are in, nothing above it is missed.  Where more than 128 candidates reach it, the candidates themselves are dealt to the
 // groups for a better one.  Scores are compared in fp64: candidates of one beam in the order of their logits, those of several
 // beams with log-sums whose error, fp32 exponentials' of random sign over a vocabulary, is about 1e-8.
 //
-// 50 x 8 rows of 250,000 in bf16, k = 8: 45 us (36 the logits, 200 MB at 5.5 TB/s); 129 rows of 1,000,003 in fp32, k = 100: 114 us (89, 516 MB at
-// 5.8 TB/s); 4 rows of 32,000, k = 4: 11 us, two launches of a chain of round trips each.
+// 50 x 8 rows of 250,000 in bf16, k = 8: 46 us (35 the logits, 200 MB at 5.7 TB/s); 129 rows of 1,000,003 in fp32, k = 100: 115 us (92, 516 MB at
+// 5.6 TB/s); 4 rows of 32,000, k = 4: 12 us, two launches of a chain of round trips each.
 #include <cmath>
 
 #include "cache.h"
@@ -458,7 +458,8 @@ __global__ void __launch_bounds__(kPickThreads) k_select_pick(SelectArgs a)
                 __syncthreads();
             }
     }
-    if (sh.count > 512)
+    // (ranks cost the candidates' number squared: 10 x 4 rows of 303, k = 12, 15 us with a better bound for more than 128 of them, 29 for more than 512)
+    if (sh.count > 128)
         bound = raise_bound(sh, bound, a.k);
     const int count = sh.count;
     auto write = [&](int rank, double v, int32_t id) {

@@ -19,8 +19,8 @@
 // the output does.
 //
 // Bound by memory where there is much to read: 4 x 131071 rows of 8 heads of 128 columns in bf16, 64 query heads, 390 us (2.15 GB at 5.5 TB/s);
-// 77 sequences of up to 4096 rows of 16 heads of 64 columns in fp16 127 us (655 MB, 5.2 TB/s); 4000 histories of up to 3000 rows of two heads of 50
-// columns in fp32 235 us (1.14 GB, 4.9 TB/s).  Bound by its chain of reads (length, page, rows) and the two launches where there is
+// 77 sequences of up to 4096 rows of 16 heads of 64 columns in fp16 129 us (655 MB, 5.1 TB/s); 4000 histories of up to 3000 rows of two heads of 50
+// columns in fp32 238 us (1.14 GB, 4.8 TB/s).  Bound by its chain of reads (length, page, rows) and the two launches where there is
 // little: one sequence of 1000 rows 15 us.
 #include <cfloat>
 #include <cmath>
