@@ -427,15 +427,15 @@ struct Attend {
             for (int i = 1; i < VK; ++i)
                 top = fmaxf(top, p[t][i]);
             top = fmaxf(m[t], groups_max(top));
+            const float from = top == -INFINITY ? 0.0f : top;
             if (__any(top > m[t])) {  // (most tiles of a long sequence bring no new maximum)
-                const float keep = exp2_fast((m[t] - top) * a.factor);
+                const float keep = exp2_fast((m[t] - from) * a.factor);  // (another lane's may be new where this one's is still -infinity)
                 l[t] *= keep;
 #pragma unroll
                 for (int i = 0; i < NG * VE; ++i)
                     o[t][i] *= keep;
                 m[t] = top;
             }
-            const float from = top == -INFINITY ? 0.0f : top;
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < VK; ++i) {
