@@ -748,7 +748,8 @@ typedef struct tig_cache {
  * row p = lengths[i] - (starts[i + 1] - t): lengths count the new tokens already.
  *   rotation: the first `rotary` columns are pairs (a, b) -- columns (j, j + rotary / 2), or (2 j, 2 j + 1) if interleaved --
  *   angle_j = position * freq[j], formed and reduced in fp64;  a' = a cos - b sin,  b' = b cos + a sin (fp32, rounded once)
- * The position is p, or positions[t] (any finite number of magnitude up to 2^53 as int64, or fp64: event times).  A token without a row
+ * The position is p, or positions[t] (int64 of magnitude up to 2^53, or fp64: event times).  Angles up to 2^64 are reduced as they
+ * are; a farther one, an infinite one and NaN give NaN.  A token without a row
  * (p < 0, beyond the table, or on no page) is left out: nothing is written for it, q_out neither.  Tokens before starts[0]
  * and from starts[seqs] on belong to nobody and are left out too.  No two tokens of a call may have the same row.
  * An output that overlaps another tensor of the call is refused; q_out may be q. */

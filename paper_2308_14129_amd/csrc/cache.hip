@@ -93,14 +93,19 @@ constexpr double kQuarterHi = 1.57079632679489655800, kQuarterLo = 6.12323399573
 // Cosine and sine of an angle in fp64: quarter turns are taken off (exactly, by fused products with the two parts of pi / 2), the rest, at
 // most pi / 4, goes through the Taylor polynomials to the thirteenth and twelfth degree (their next terms are 2e-14 and 4e-13 there), and
 // each is rounded once.  About 30 operations at fp64's rate, which is fp32's on this card.
+// Of a far angle the first count n is off by up to 2^-52 of itself, so that a second one is taken off what is left.  The two stay apart: only
+// their last two bits are wanted, and their sum would be rounded where n is beyond 2^53.  Up to 2^64 n is off by up to 2^12, what is
+// left is 2^13 at most, and rounding that (2^-40), and what pi / 2 is beyond its two parts (n times 1.5e-33), come to less than 1e-11.
+constexpr double kFarthest = 18446744073709551616.0;
 __device__ inline void cos_sin(double angle, float &c, float &s)
 {
-    double n = rint(angle * kTurn8);
+    const double n = rint(angle * kTurn8);
     double x = fma(n, -kQuarterHi, angle);
     x = fma(n, -kQuarterLo, x);
-    const double again = rint(x * kTurn8);  // (of a far angle the first count is off by one at most)
+    const double again = rint(x * kTurn8);
     x = fma(again, -kQuarterHi, x);
-    n += again;
+    if (!(fabs(angle) <= kFarthest))
+        x = NAN;
     const double y = x * x;
     double ps = 1.0 / 6227020800.0, pc = 1.0 / 479001600.0;
     ps = fma(y, ps, -1.0 / 39916800.0);
@@ -115,7 +120,7 @@ __device__ inline void cos_sin(double angle, float &c, float &s)
     pc = fma(y, pc, 1.0 / 24.0);
     pc = fma(y, pc, -0.5);
     pc = fma(y, pc, 1.0);
-    const int quarter = (int)(n - 4.0 * floor(n * 0.25));  // 0 .. 3
+    const int quarter = ((int)(n - 4.0 * floor(n * 0.25)) + (int)again) & 3;
     const double a = quarter & 1 ? ps : pc, b = quarter & 1 ? pc : ps;
     c = (float)((quarter + 1) & 2 ? -a : a);
     s = (float)(quarter & 2 ? -b : b);

@@ -485,7 +485,7 @@ def cache_append(k_cache, v_cache, table, lengths, k, v, starts=None, q=None, fr
     already.  starts [sequences + 1] (int32): tokens starts[i] .. starts[i + 1] - 1 are sequence i's, without it token i is.  With freq
     (float64, [pairs]) keys, and the queries q [tokens, query heads, head_dim], are rotated on the way by position * freq: pairs of
     columns (j, j + pairs), or (2 j, 2 j + 1) if interleaved; positions [tokens] (int64 or float64) are the rows' own numbers if not
-    given.  Returns the rotated queries (q_out, which may be q; None without q).  A token without a row in the table or a page is left
+    given; an angle beyond 2^64 gives NaN.  Returns the rotated queries (q_out, which may be q; None without q).  A token without a row in the table or a page is left
     out, in q_out too."""
     c, dtype, index, seqs, heads, dim, pt, ld, pn = _cache(k_cache, v_cache, table, lengths)
     if k.dim() != 3:
