@@ -63,6 +63,9 @@ inline Placed placed_keys(const tig_cache &c, const void *p)
     return placed(p, {{c.pages, c.page_stride}, {c.page_size, c.token_stride}, {c.heads, c.head_stride}}, c.head_dim, dtype_bytes(c.dtype));
 }
 
+// Whether two of the rows of `cols` elements at i * stride_a + j * stride_b, i < n_a and j < n_b, have an element in common.
+bool rows_meet(int64_t n_a, int64_t stride_a, int64_t n_b, int64_t stride_b, int64_t cols);
+
 // maximum / sum over a wavefront's lanes, for every lane
 __device__ inline float wave_max_all(float v)
 {

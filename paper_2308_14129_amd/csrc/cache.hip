@@ -27,6 +27,22 @@ Placed placed(const void *p, std::initializer_list<Dim> dims, int64_t cols, int 
     return {p, d[0].n, cols, d[0].stride, elem};
 }
 
+bool rows_meet(int64_t n_a, int64_t stride_a, int64_t n_b, int64_t stride_b, int64_t cols)
+{
+    if ((n_a > 1 && stride_a < cols) || (n_b > 1 && stride_b < cols))
+        return true;
+    if (n_a <= 1 || n_b <= 1 || stride_a >= (n_b - 1) * stride_b + cols || stride_b >= (n_a - 1) * stride_a + cols)
+        return false;
+    if (n_a < n_b)
+        std::swap(n_a, n_b), std::swap(stride_a, stride_b);
+    for (int64_t j = 1; j < n_b; ++j) {  // j steps of the one against the steps of the other on both sides of them (of heads there are 2^14 at most)
+        const int64_t i = j * stride_b / stride_a, past = j * stride_b - i * stride_a;
+        if ((i > 0 && i < n_a && past < cols) || (i + 1 < n_a && stride_a - past < cols))
+            return true;
+    }
+    return false;
+}
+
 int check_cache(const tig_cache *c)
 {
     if (!c || c->struct_size != sizeof(tig_cache))
@@ -411,7 +427,7 @@ int check_append(const tig_cache *c, const tig_cache_append *p)
     for (const int64_t s : {p->k_token, p->k_head, p->v_token, p->v_head, p->q_token, p->q_head, p->qo_token, p->qo_head})
         if (s < 0 || s > ((int64_t)1 << 32))
             return fail_text(TIG_EINVAL, "tig_cache_append: a stride is out of range");
-    if (p->q_out && ((p->tokens > 1 && p->qo_token < c->head_dim) || (p->q_heads > 1 && p->qo_head < c->head_dim)))
+    if (p->q_out && rows_meet(p->tokens, p->qo_token, p->q_heads, p->qo_head, c->head_dim))
         return fail_text(TIG_EINVAL, "tig_cache_append: rows of q_out overlap");
     return TIG_OK;
 }

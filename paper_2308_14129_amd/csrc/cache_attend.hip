@@ -1177,10 +1177,7 @@ int check_attend(const tig_cache *c, const tig_cache_attend *p)
     for (const int64_t s : {p->q_seq, p->q_head, p->o_seq, p->o_head})
         if (s < 0 || s > ((int64_t)1 << 32))
             return fail_text(TIG_EINVAL, "tig_cache_attend: a stride is out of range");
-    const int d = c->head_dim;
-    const int64_t seq_span = (p->q_heads - 1) * p->o_head + d, head_span = (p->seqs - 1) * p->o_seq + d;
-    if (p->seqs > 0 && ((p->seqs > 1 && p->o_seq < d) || (p->q_heads > 1 && p->o_head < d) ||
-                        (p->seqs > 1 && p->q_heads > 1 && p->o_seq < seq_span && p->o_head < head_span)))
+    if (p->seqs > 0 && rows_meet(p->seqs, p->o_seq, p->q_heads, p->o_head, c->head_dim))
         return fail_text(TIG_EINVAL, "tig_cache_attend: rows of out overlap");
     return TIG_OK;
 }

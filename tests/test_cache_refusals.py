@@ -278,3 +278,33 @@ def test_tensors_that_want_a_graph_are_refused(f, names):
         assert e.value.status == tig.TIG_EINVAL
         with torch.no_grad(), pytest.raises(tig.TigError, match="not on a GPU"):  # (the next thing that is refused here)
             f(**{n: given[n].clone().requires_grad_()})
+
+
+def rows_meet(n, a, m, b, d):
+    """Whether two of the rows of d columns at i a + j b, i < n, j < m, share one: row by row."""
+    starts = sorted(i * a + j * b for i in range(n) for j in range(m))
+    return any(y - x < d for x, y in zip(starts, starts[1:]))
+
+
+@pytest.mark.parametrize("token, head", [(32, 32), (64, 32), (32, 64), (64, 64), (96, 32), (224, 32), (255, 32), (240, 48), (33, 100), (100, 50), (250, 1000), (1000, 250)], ids=str)
+def test_rows_of_an_output_that_meet_are_refused(lib, token, head):
+    """... where each stride alone leaves room for a row: 5 tokens (sequences) of 8 heads of 32 columns."""
+    assert rows_meet(5, token, 8, head, 32)
+    assert lib.tig_cache_append_run(byref(make_cache()), byref(make_append(qo_token=token, qo_head=head)), None) == tig.TIG_EINVAL
+    assert b"rows of q_out overlap" in lib.tig_last_error(None)
+    assert lib.tig_cache_attend_run(byref(make_cache()), byref(make_attend(o_seq=token, o_head=head)), HOST, 1 << 40, None) == tig.TIG_EINVAL
+    assert b"rows of out overlap" in lib.tig_last_error(None)
+
+
+def test_rows_of_an_output_that_pass_each_other_are_taken(lib):
+    """Rows of one head between those of another are no overlap: what is refused next, a workspace that is missing, says so."""
+    c, taken = make_cache(max_pages=1000, heads=2, head_stride=64), 0
+    for seqs, q_heads in ((5, 8), (2, 2), (3, 4), (7, 2)):
+        for o_seq in range(32, 330, 7):
+            for o_head in range(32, 330, 9):
+                p = make_attend(seqs=seqs, q_heads=q_heads, o_seq=o_seq, o_head=o_head, ld_table=1000)
+                assert lib.tig_cache_attend_run(byref(c), byref(p), None, 1 << 40, None) == tig.TIG_EINVAL
+                said = lib.tig_last_error(None)
+                assert (b"rows of out overlap" if rows_meet(seqs, o_seq, q_heads, o_head, 32) else b"workspace is NULL") in said, (seqs, q_heads, o_seq, o_head)
+                taken += b"workspace" in said
+    assert taken > 100
