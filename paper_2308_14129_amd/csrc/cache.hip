@@ -266,6 +266,10 @@ __global__ void __launch_bounds__(256) k_cache_append_rows(AppendArgs a, AppendU
                 x[i] = *(const Piece16<T> *)(p + e * ES);
                 y[i] = *(const Piece16<T> *)(p + other * ES);
             }
+            // a row that is turned in place is read by all its lanes before one of them writes
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "global");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "global");
 #pragma unroll
             for (int i = 0; i < kAppendDeep; ++i) {
                 const int t = t0 + i;
