@@ -800,7 +800,10 @@ TIG_API int tig_cache_attend_run(const tig_cache *cache, const tig_cache_attend 
 /* The k best continuations over the beams of a batch entry and their candidates:
  *   candidate (j, v) of entry b has the score  scores[b, j] + l_bjv - log sum_u exp l_bju
  *   a finished beam has one candidate, (j, end), with its score unchanged
- * in descending order of the scores (formed and compared in fp64), ties to the lowest (j, v).  Candidates with a score of
+ * in descending order of the scores, ties to the lowest (j, v).  Scores are formed and compared in fp64, with a log-sum of fp32 exponentials for each
+ * row: candidates of one beam are in their order whatever lies between them; of several beams, or beside a finished one, those closer than
+ * a log-sum's error may stand in either order, the same from call to call (rows alike have log-sums alike).  It is about 1e-8 where many logits
+ * carry the sum, 1.4e-7 where the logits of one value do, and 4e-6 at most (beams * vocab up to 2^23).  Candidates with a score of
  * -infinity (masked logits) or none (NaN: a row that holds +infinity or NaN) are not taken; places that no candidate is left for get score -infinity, parent -1,
  * token -1.  `parents` are rows of logits, b * beams + j.  finished_out: the parent was finished, or the token is `end`.
  * beams = 1 is a plain selection of the k best of a vocabulary. */

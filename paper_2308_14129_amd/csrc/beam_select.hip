@@ -9,10 +9,13 @@
 // Which bound: the segments are dealt in turn to 128 groups, and the k-th largest of the groups' maxima is the score of a candidate that
 // k - 1 others reach at least.  For values in no particular order, also where one beam has all the best, a few more than k lie above it;
 // whatever order they are in, nothing above it is missed.  Where more than 128 candidates reach it, the candidates themselves are dealt to the
-// groups for a better one.  Scores are compared in fp64: candidates of one beam in the order of their logits, those of several
-// beams with log-sums whose error, fp32 exponentials' of random sign over a vocabulary, is about 1e-8.
+// groups for a better one.  Scores are compared in fp64: candidates of one beam in the order of their logits, those of several beams, and
+// finished ones beside them, with log-sums of fp32 exponentials.  These are off by 1e-8 where many logits carry the sum (a million of standard deviation 1:
+// 5e-9), by 1.4e-7 where one distance does (a peak over equal logits: an argument's rounding and the function's own are then all alike), by
+// 64 units of 2^-24 at most where beams * vocab is up to 2^23: 27 roundings on the way of a sum, two of an argument, which is ln vocab on average at
+// most, and the function's two.  (Rows beyond that have longer stretches: five more roundings for every four steps of 512 logits.)
 //
-// 50 x 8 rows of 250,000 in bf16, k = 8: 46 us (35 the logits, 200 MB at 5.7 TB/s); 129 rows of 1,000,003 in fp32, k = 100: 115 us (92, 516 MB at
+// 50 x 8 rows of 250,000 in bf16, k = 8: 47 us (36 the logits, 200 MB at 5.5 TB/s); 129 rows of 1,000,003 in fp32, k = 100: 115 us (92, 516 MB at
 // 5.6 TB/s); 4 rows of 32,000, k = 4: 12 us, two launches of a chain of round trips each.
 #include <cmath>
 
@@ -62,7 +65,11 @@ __device__ inline void load_eight(const T *row, int at, int vocab, float (&x)[8]
     }
 }
 
-constexpr float kLog2e = 1.44269504f;
+// exp(x), x <= 0.  log2 e in two parts: in fp32 alone it is 1.3e-8 of itself short, which makes every exponential that much of its argument too large,
+// always to one side, and a sum of however many keeps it (2.5e-8 of a million logits of standard deviation 1; 35.2 us for 200 MB of bf16 with one part,
+// 36.5 with both).
+constexpr float kLog2e = 1.44269504f, kLog2eRest = 1.92596299e-8f;
+__device__ inline float exp_below(float x) { return __builtin_amdgcn_exp2f(fmaf(x, kLog2e, x * kLog2eRest)); }
 
 // written out: the compiler would canonicalise every operand.  A NaN loses: the row's sum has it.
 __device__ inline float max3(float a, float b, float c)
@@ -135,9 +142,9 @@ __global__ void __launch_bounds__(256) k_select_segments(SelectArgs a)
             sums[t] = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                sums[t] += __builtin_amdgcn_exp2f((x[t][e] - from) * kLog2e);
+                sums[t] += exp_below(x[t][e] - from);
         }
-        s *= __builtin_amdgcn_exp2f((m - from) * kLog2e);
+        s *= exp_below(m - from);
 #pragma unroll
         for (int t = 0; t < kDeep; ++t)
             s += sums[t];
@@ -188,7 +195,7 @@ __global__ void __launch_bounds__(256) k_select_segments(SelectArgs a)
     if (place > 0)
         flush();
     const float top = wave_max_all(m);
-    s = wave_sum_all(s * __builtin_amdgcn_exp2f((m - (top == -INFINITY ? 0.0f : top)) * kLog2e));
+    s = wave_sum_all(s * exp_below(m - (top == -INFINITY ? 0.0f : top)));
     if (lane == 0)
         a.sums[r * a.stretches + stretch] = {top, s};
 }

@@ -568,7 +568,8 @@ def beam_select(logits, k, scores=None, finished=None, end=-1):
     """The k best continuations over beams and candidates: logits [batch, beams, vocab] (candidates adjacent), scores [batch, beams]
     (float32) of the beams so far, finished [batch, beams] (bool) the beams that go on with nothing but `end`, their score
     unchanged.  Returns BeamSelect(scores [batch, k] in descending order, parents [batch, k] (rows of logits: entry * beams + beam), tokens
-    [batch, k], finished [batch, k]; None without `end`): ties to the lowest beam, then token; -infinity, -1, -1 where no candidate is
+    [batch, k], finished [batch, k]; None without `end`): ties to the lowest beam, then token (between beams up to a
+    log-sum's error, 1e-8 where many logits carry it, 4e-6 at most); -infinity, -1, -1 where no candidate is
     left."""
     if logits.dim() != 3:
         _refuse("logits is [batch, beams, vocab]")
