@@ -218,9 +218,10 @@ __device__ inline void append_places(const AppendArgs &a, int64_t token0, int co
 
 // Rows by pieces of 16 bytes: a lane has one piece of a row and, for the pairs' other halves, reads the piece that lies there as well (it
 // is on its way for another lane of the wavefront), so that reads and writes are whole lines: with a pair of pieces to a lane 62500 tokens of
-// 40 rows of 256 bytes, 192 of them turned, took 347 us, so they take 264 (a copy of as much 250).  Rows do not cross wavefronts: one
-// may be turned in place.
-template <typename T>
+// 40 rows of 256 bytes, 192 of them turned, took 347 us, so they take 260 (a copy of as much 250).  Rows do not cross wavefronts: one
+// may be turned in place.  IN_PLACE: queries are; their lanes' reads then come before their lanes' writes for the compiler too, which else has some
+// tokens' loads behind others' stores (the same prompts: 260 us, with that order 264).
+template <typename T, bool IN_PLACE>
 __global__ void __launch_bounds__(256) k_cache_append_rows(AppendArgs a, AppendUnits n)
 {
     constexpr int VE = 16 / sizeof(T), ES = sizeof(T);
@@ -266,10 +267,11 @@ __global__ void __launch_bounds__(256) k_cache_append_rows(AppendArgs a, AppendU
                 x[i] = *(const Piece16<T> *)(p + e * ES);
                 y[i] = *(const Piece16<T> *)(p + other * ES);
             }
-            // a row that is turned in place is read by all its lanes before one of them writes
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "global");
-            __builtin_amdgcn_wave_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "global");
+            if constexpr (IN_PLACE) {
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "global");
+                __builtin_amdgcn_wave_barrier();
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "global");
+            }
 #pragma unroll
             for (int i = 0; i < kAppendDeep; ++i) {
                 const int t = t0 + i;
@@ -537,6 +539,7 @@ int tig_cache_append_run(const tig_cache *cache, const tig_cache_append *p, void
     a.q_heads = p->q_heads, a.rotary = p->rotary, a.interleaved = p->interleaved, a.position_type = p->position_type;
     const int ve = (int)(16 / es), d = cache->head_dim;
     AppendUnits n = {};
+    n.in_place = p->q != nullptr && p->q == p->q_out;
     const int part = p->interleaved ? p->rotary : p->rotary / 2, rest = d - p->rotary;
     const int in_part = (part + ve - 1) / ve, in_row = std::max((p->interleaved ? 1 : 2) * in_part + (rest + ve - 1) / ve, (d + ve - 1) / ve);
     const bool pieces = (part == 0 || part >= ve) && (rest == 0 || rest >= ve) && in_row <= 64;  // parts of a piece at least, a row in a wavefront
@@ -552,7 +555,6 @@ int tig_cache_append_run(const tig_cache *cache, const tig_cache_append *p, void
         n.turning = (p->q_heads + cache->heads) * n.n_pair;
         n.resting = p->rotary < d ? (p->q_heads + cache->heads) * n.n_rest : 0;
         n.all = n.turning + n.resting + cache->heads * n.n_v;
-        n.in_place = p->q != nullptr && p->q == p->q_out;
         n.groups = std::max(1, 256 / n.all);
     }
     // a workgroup's tokens: as many as leave about four workgroups for a compute unit
@@ -562,7 +564,8 @@ int tig_cache_append_run(const tig_cache *cache, const tig_cache_append *p, void
     const dim3 grid((unsigned)groups, (unsigned)shares);
     with_dtype(cache->dtype, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL((pieces ? k_cache_append_rows<T> : k_cache_append<T>), grid, dim3(256), 0, (hipStream_t)hip_stream, a, n);
+        auto *const rows = n.in_place ? k_cache_append_rows<T, true> : k_cache_append_rows<T, false>;
+        hipLaunchKernelGGL((pieces ? rows : k_cache_append<T>), grid, dim3(256), 0, (hipStream_t)hip_stream, a, n);
         return 0;
     });
     const hipError_t e = hipGetLastError();
