@@ -20,7 +20,7 @@
 //
 // Bound by memory where there is much to read: 4 x 131071 rows of 8 heads of 128 columns in bf16, 64 query heads, 390 us (2.15 GB at 5.5 TB/s);
 // 77 sequences of up to 4096 rows of 16 heads of 64 columns in fp16 129 us (655 MB, 5.1 TB/s); 4000 histories of up to 3000 rows of two heads of 50
-// columns in fp32 238 us (1.14 GB, 4.8 TB/s).  Bound by its chain of reads (length, page, rows) and the two launches where there is
+// columns in fp32 236 us (1.14 GB, 4.8 TB/s).  Bound by its chain of reads (length, page, rows) and the two launches where there is
 // little: one sequence of 1000 rows 15 us.
 #include <cfloat>
 #include <cmath>
@@ -554,8 +554,8 @@ struct Joined {
 };
 
 // fp32 with one or two query heads to a head: sixteen queries' products of which one is wanted take the matrix units a thousand cycles a tile
-// of 16 keys and 64 columns, that one in vector instructions a tenth of it (4000 histories of two heads of 50 columns, 1.14 GB: 258 and
-// 235 us).  The lanes have keys and values as above; the scores' sums over a lane's columns are joined over the four lanes of a key, each
+// of 16 keys and 64 columns, that one in vector instructions a tenth of it (4000 histories of two heads of 50 columns, 1.14 GB: 260 and
+// 236 us).  The lanes have keys and values as above; the scores' sums over a lane's columns are joined over the four lanes of a key, each
 // lane then weighs its key, and the weights of a lane's four keys of values are fetched from the lanes that have them.
 template <int DP, int G, bool PAGED>
 struct AttendFew : Attend<float, DP, 1, PAGED> {
@@ -1088,22 +1088,24 @@ AttendPlan attend_plan(const tig_cache &c, const tig_cache_attend &p)
     L.rec = (int64_t)L.rows * (c.head_dim + 2);
     const int64_t cap = p.window > 0 ? std::min<int64_t>(p.window, (int64_t)c.max_pages * c.page_size) : (int64_t)c.max_pages * c.page_size;
     const int64_t units = (int64_t)c.heads * L.blocks, tiles = cap / kt + 2, all = p.seqs * units * (tiles + kUnitCost);
-    // A workgroup for each unit and one launch where there are few tiles for its wavefronts.  8 heads of 128 columns in bf16: 300 rows 10.5 us
-    // this way, 15.7 the other one, 1000 rows 16.7 and 16.2, 4000 rows 42 and 18; 64 such units of 1000 rows 18.2 and 20.6, 256 of them 27 and 35.
+    // A workgroup for each unit and one launch where there are few tiles for its wavefronts.  8 heads of 128 columns in bf16: 300 rows 10.4 us
+    // this way, 14.5 the other one, 1000 rows 16.7 and 15.1, 4000 rows 42 and 17.5; 64 such units of 1000 rows 17.8 and 19.7, 256 of them 26 and 34.5.
+    // (The table's width stands for the lengths here and below, which only the device knows: a table as wide as the longest sequence there may
+    // be has short ones worked on the way of long ones.)
     L.solo = p.seqs * units <= 256 && tiles <= (p.seqs * units >= 64 ? 34 : 14);
     if (L.solo) {
         L.wgs = (int)(p.seqs * units), L.together = 1;
         return L;
     }
     // Wavefronts that go through the same rows together where these lie side by side and share lines of 128 bytes (4000 histories of two heads of
-    // 200 bytes 318 us each by itself, 259 together), or where few long sequences are all there is (4 x 131071 rows of 8 x 256 bytes 404 and
-    // 390; 77 sequences of 16 x 128 bytes 135 and 138).
+    // 200 bytes 319 us each by itself, 236 together), or where few long sequences are all there is (4 x 131071 rows of 8 x 256 bytes 404 and
+    // 390; 77 sequences of 16 x 128 bytes 130 and 133).
     const bool side_by_side = c.heads > 1 && c.head_stride < c.token_stride;
     L.together = !side_by_side || all < 16384 ? 1 : c.head_stride * es % 128 != 0 ? (units >= 3 ? 4 : 2) : p.seqs * units <= 128 ? 2 : 1;
     const int64_t waves = (all + L.together - 1) / L.together;
-    // A workgroup for each compute unit, one wavefront for each SIMD, fills the memory (4 x 131071 rows: 390 us, with two or four of them 399 and
-    // 418); two where there are many units of few tiles, whose ends nothing runs beside (4000 histories of up to 100 rows 51 and 45 us, of up to
-    // 3000 235 and 256; 600 sequences of up to 500 rows 146 and 140).
+    // A workgroup for each compute unit, one wavefront for each SIMD, fills the memory (4 x 131071 rows: 390 us, with two or four of them 402 and
+    // 421); two where there are many units of few tiles, whose ends nothing runs beside (4000 histories of up to 100 rows 51 and 44 us, of up to
+    // 3000 236 and 256; 600 sequences of up to 500 rows of 8 x 256 bytes 132 and 134).
     const int wanted = p.seqs * units >= 2048 * L.together && tiles <= 34 && c.head_dim <= 128 && L.qt == 1 ? 512 : 256;
     L.wgs = (int)std::min<int64_t>(wanted, (waves + kAttendWaves / L.together - 1) / (kAttendWaves / L.together));
     const int64_t most = (cap + kt - 1) / kt + (p.window > 0 && cap == p.window ? 1 : 0);  // tiles of a unit
