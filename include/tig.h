@@ -752,7 +752,7 @@ typedef struct tig_cache {
  * are; a farther one, an infinite one and NaN give NaN.  A token without a row
  * (p < 0, beyond the table, or on no page) is left out: nothing is written for it, q_out neither.  Tokens before starts[0]
  * and from starts[seqs] on belong to nobody and are left out too.  No two tokens of a call may have the same row.
- * An output that overlaps another tensor of the call is refused; q_out may be q. */
+ * An output that overlaps another tensor of the call, or rows of q_out that meet, are refused; q_out may be q. */
 typedef struct tig_cache_append {
     uint32_t struct_size;
     int32_t rotary;          /* even, 0 .. head_dim */
@@ -830,7 +830,7 @@ TIG_API int tig_beam_select_run(const tig_beam_select *p, void *workspace, size_
 /* Sequences taken over by their selected continuations: new sequence r is sequence parents[r], in its full pages as they are, and in
  * spare[r] a copy of the rows of a last page that is not full, so that each may be appended to.
  *   n = length / page_size;  table_out[r] = table[parents[r]][0 .. n - 1], spare[r], -1 ...;  lengths_out[r] = the length
- * (Where n == max_pages there is no place for spare[r], and nothing to copy.)  Without a page of its own (spare[r] outside of 0 .. pages - 1)
+ * (Where n == max_pages there is no place for spare[r], and nothing to copy; where the parent's last page is no page it stays the sequence's.)  Without a page of its own (spare[r] outside of 0 .. pages - 1)
  * a sequence shares its parent's last page: for one that is the only one to go on with it.  A parent outside of 0 ..
  * rows_in - 1 gives an empty sequence: length 0, its table spare[r], -1 ....  A spare page must be in no other sequence of the call and no
  * other spare.  Outputs that overlap another tensor of the call are refused. */

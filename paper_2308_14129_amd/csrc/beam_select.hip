@@ -15,7 +15,7 @@
 // 64 units of 2^-24 at most where beams * vocab is up to 2^23: 27 roundings on the way of a sum, two of an argument, which is ln vocab on average at
 // most, and the function's two.  (Rows beyond that have longer stretches: five more roundings for every four steps of 512 logits.)
 //
-// 50 x 8 rows of 250,000 in bf16, k = 8: 47 us (36 the logits, 200 MB at 5.5 TB/s); 129 rows of 1,000,003 in fp32, k = 100: 115 us (92, 516 MB at
+// 50 x 8 rows of 250,000 in bf16, k = 8: 46 us (37 the logits, 200 MB at 5.4 TB/s); 129 rows of 1,000,003 in fp32, k = 100: 113 us (93, 516 MB at
 // 5.6 TB/s); 4 rows of 32,000, k = 4: 12 us, two launches of a chain of round trips each.
 #include <cmath>
 
@@ -67,7 +67,7 @@ __device__ inline void load_eight(const T *row, int at, int vocab, float (&x)[8]
 
 // exp(x), x <= 0.  log2 e in two parts: in fp32 alone it is 1.3e-8 of itself short, which makes every exponential that much of its argument too large,
 // always to one side, and a sum of however many keeps it (2.5e-8 of a million logits of standard deviation 1; 35.2 us for 200 MB of bf16 with one part,
-// 36.5 with both).
+// 37 with both).
 constexpr float kLog2e = 1.44269504f, kLog2eRest = 1.92596299e-8f;
 __device__ inline float exp_below(float x) { return __builtin_amdgcn_exp2f(fmaf(x, kLog2e, x * kLog2eRest)); }
 
